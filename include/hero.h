@@ -24,8 +24,8 @@
  * (text via hero_last_error()).  A device-side wait that exceeded its bound (a pipeline bug, never
  * expected) sets a device error word; hero_check() synchronizes the stream and returns
  * HERO_ERR_DEVICE_TIMEOUT if it is set.  The same word reports an embedding id outside its table (the gather of
- * hero_layernorm_quant clamps such an id, so nothing is read out of bounds): hero_check() then returns
- * HERO_ERR_INVALID_ARG.
+ * hero_layernorm_quant clamps such an id, so nothing is read out of bounds), a page id or row range of a block cache or a
+ * position outside its bounds: hero_check() then returns HERO_ERR_INVALID_ARG.
  */
 #ifndef HERO_H_
 #define HERO_H_
@@ -476,10 +476,125 @@ hero_status hero_layer_forward_static(const hero_layer_desc* d, const hero_tenso
  * nothing (a symbol copy). */
 hero_status hero_static_check(void* stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * Serving over an 8-bit block cache (no counterpart in the paper, whose key / value scales are one static value per
+ * tensor: hero_int8_decode_attention above).  Keys and values live in pages of `page` tokens; every page has one FP32
+ * scale per key / value head, taken from the data as it is written, so that nothing needs calibration and a loud token
+ * costs the other heads and pages nothing.  A page table names the pages of each sequence.
+ *
+ *   value of (page p, head g, token t, feature c) = code(p, g, t, c) * scale[p * nkv + g]
+ *   code at k (or v) + p * page_stride + g * head_stride + t * ld + c, one byte: I8 in [-127, 127] or F8 (e4m3)
+ *   token t of sequence b is token t % page of page table[b * ld_table + t / page]
+ *
+ * Strides are in elements (= bytes), multiples of 16 and at least dh, so that [pages][nkv][page][dh] and
+ * [pages][page][nkv][dh] are both expressible; k and v are 16-byte aligned.  `len[b]` counts the tokens that sequence b
+ * holds, those of the call included (the caller raises it before the call); 0 <= len[b] <= max_len, a larger value is
+ * treated as max_len, a negative one as 0.
+ *
+ * Rows of a call: row_start (device int32 [B + 1]) gives sequence b the rows row_start[b] .. row_start[b + 1] - 1 of the
+ * call's matrices, n_b of them, n_b <= max_rows; they stand for the LAST n_b tokens of the sequence: row i of a sequence
+ * is its token len[b] - n_b + i.  NULL: one row per sequence, row b.  Rows that belong to no sequence are neither read nor
+ * written.  n_b may be 0 and may exceed len[b]: a row without a token stores nothing (append), reads as zero, attends to
+ * nothing and yields zeros.
+ *
+ * What the host cannot see is bounded on the device and reported by the next hero_check() as HERO_ERR_INVALID_ARG: a page id
+ * outside [0, n_pages) (clamped where it is read, skipped where it would be written), a row range that is decreasing,
+ * outside the matrices or longer than max_rows (cut to what is inside). */
+typedef struct {
+  void* k;
+  void* v;
+  float* k_scale;          /* device [n_pages][nkv] */
+  float* v_scale;          /* device [n_pages][nkv] */
+  int32_t dtype;           /* HERO_I8 or HERO_F8 */
+  int32_t page;            /* tokens per page: 16, 32, 64 or 128 */
+  int64_t n_pages;
+  int64_t page_stride, head_stride, ld;
+  const int32_t* table;    /* device [B][ld_table] */
+  int64_t ld_table;        /* at least max_len / page, rounded up */
+  const int32_t* len;      /* device [B] */
+  int32_t max_len;         /* host-side upper bound on len[b] */
+  int32_t B, nkv, dh;      /* dh is 64 or 128 */
+} hero_block_cache;
+
+/* hero_block_cache_append: stores new keys and values.  For every page and head that receives tokens, with
+ * top = 127 (I8) or 448 (F8):
+ *     s_new = max(s_old, max |x| / top) over the new tokens; s_old counts only if the page holds earlier tokens of the
+ *             sequence (a page that is begun takes its scale from the new tokens alone, whatever it held before)
+ *     code  = clip(Round(x / s_new)) (I8) or the saturating round-to-nearest-even e4m3 conversion of x / s_new (F8);
+ *             0 when s_new = 0
+ *     where s_new > s_old the page's earlier tokens are quantised again from their values code * s_old
+ *   All in FP32 with correctly rounded division.  A NaN is stored as 0 and an infinity as the largest code of its sign; the
+ *   scale is taken from the finite values.  k, v: F16 / BF16 [rows][nkv*dh].  A page must not be written for two sequences
+ *   in one call (its codes would be those of either); copying a shared page first is the caller's part.
+ * hero_block_cache_read: the inverse: code * scale, rounded to F16 / BF16, into k, v [rows][nkv*dh]; either may be absent. */
+typedef struct {
+  hero_tensor k;
+  hero_tensor v;
+  const int32_t* row_start;  /* device [B + 1] or NULL */
+  int32_t max_rows;          /* host-side upper bound on n_b */
+} hero_block_rows_args;
+hero_status hero_block_cache_append(hero_handle* h, const hero_block_cache* c, const hero_block_rows_args* a, void* stream);
+hero_status hero_block_cache_read(hero_handle* h, const hero_block_cache* c, const hero_block_rows_args* a, void* stream);
+
+/* hero_block_attention: o = softmax(scale q K^T) V over the cache for the last n_b tokens of each sequence; the row of token t
+ * attends to tokens 0 .. t (causal).  Query head j reads key / value head j / (nq / nkv).  The cache must already hold the
+ * rows' own tokens (append first, on the same stream).
+ *   q   : F16 / BF16 [rows][nq*dh]
+ *   out : [rows][nq*dh] F16 / BF16, or I8 / F8 with gran FWQ (scale[nq*dh]) or SQ (scale[1]): the quantised input of the
+ *         attention-output linear (clip(Round(o / s)); for F8 the saturating conversion of o / s)
+ *   scale : factor of the scores; 0 selects 1 / sqrt(dh)
+ *   workspace : device scratch of hero_block_attention_workspace_bytes(), 16-byte aligned, for the partial results of sequences
+ *         split over several CTAs; it needs no clearing and holds nothing between calls.  Calls that may overlap on the GPU (two
+ *         streams, two graphs) need a workspace each.
+ * Arithmetic: codes and queries enter the products exactly (a query row is scaled by a power of two into FP16), scores,
+ * maxima, sums and outputs are FP32, probabilities are FP16 relative to the running maximum. */
+typedef struct {
+  hero_tensor q;
+  hero_tensor out;
+  const int32_t* row_start;  /* device [B + 1] or NULL */
+  int32_t max_rows;          /* host-side upper bound on n_b */
+  int32_t nq;
+  float scale;
+  void* workspace;
+  size_t workspace_bytes;
+} hero_block_attn_args;
+hero_status hero_block_attention_workspace_bytes(hero_handle* h, const hero_block_cache* c, int32_t nq, int64_t rows,
+                                                 int32_t max_rows, size_t* bytes);
+hero_status hero_block_attention(hero_handle* h, const hero_block_cache* c, const hero_block_attn_args* a, void* stream);
+
+/* hero_qk_norm_rope: norm and rotation of query and key heads in one pass (what stands between a QKV projection and the
+ * cache in models with rotary positions).  Per row i and head, x its dh features, FP32 throughout, rounded once:
+ *     y = x / sqrt(mean(x^2) + eps) * gamma            (no norm where the head's gamma is NULL: y = x)
+ *     (y[a], y[b]) -> (y[a] cos - y[b] sin, y[b] cos + y[a] sin) for the rot / 2 pairs j, with cos[pos[i]][j], sin[pos[i]][j]
+ *       HERO_PAIR_HALVES: a = j, b = j + rot / 2;  HERO_PAIR_ADJACENT: a = 2 j, b = 2 j + 1;  features >= rot pass through
+ *   q, k         : F16 / BF16 of one type, [rows][nq*dh] and [rows][nkv*dh]; k may be absent (nkv = 0)
+ *   q_out, k_out : the same type, or I8 with gran SQ (clip(Round(y / scale[0])): the operands of hero_int8_attention).  An output
+ *                  of the input's type may be its input (same pointer and ld); other overlaps are not allowed.
+ *   pos          : device int32 [rows]; one outside [0, n_pos) is clamped and reported by the next hero_check() as
+ *                  HERO_ERR_INVALID_ARG.  cos, sin: device [n_pos][rot / 2], contiguous, 16-byte aligned.
+ *   rot          : 0 (no rotation: pos, cos, sin may be NULL) or a multiple of 16 up to dh; dh: a multiple of 16 up to 256 */
+typedef enum { HERO_PAIR_HALVES = 0, HERO_PAIR_ADJACENT = 1 } hero_pairing;
+typedef struct {
+  hero_tensor q;
+  hero_tensor k;
+  hero_tensor q_out;
+  hero_tensor k_out;
+  int32_t nq, nkv, dh, rot;
+  int32_t pairing;           /* hero_pairing */
+  float eps;
+  const float* q_gamma;      /* device [dh] or NULL */
+  const float* k_gamma;      /* device [dh] or NULL */
+  const int32_t* pos;
+  const float* cos;
+  const float* sin;
+  int64_t n_pos;
+} hero_qk_norm_rope_args;
+hero_status hero_qk_norm_rope(hero_handle* h, const hero_qk_norm_rope_args* a, void* stream);
+
 /* Per-launch device timing for benchmarks (no counterpart in the paper, which measured nothing): between
  * _begin and _end every kernel the handle launches is bracketed by a pair of CUDA events on its stream.
  * _end waits for them and returns, per launch in order, the elapsed milliseconds and the kernel family
- * (1 = LN^quant, 2 = GeMM^quant, 3 = attention core).  Arrays must hold max_launches entries. */
+ * (1 = LN^quant, 2 = GeMM^quant, 3 = attention core, 4 = block cache and rotation).  Arrays must hold max_launches entries. */
 hero_status hero_profile_begin(hero_handle* h, int32_t max_launches);
 hero_status hero_profile_end(hero_handle* h, float* ms_out, int32_t* tag_out, int32_t* n_out);
 

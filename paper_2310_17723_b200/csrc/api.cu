@@ -31,6 +31,13 @@ hero_status cuda_fail(cudaError_t e, const char* what) {
   return HERO_ERR_CUDA;
 }
 
+hero_status check_device(const hero_handle* h) {
+  int dev = -1;
+  HERO_CUDA(cudaGetDevice(&dev));
+  HERO_REQUIRE(dev == h->device, HERO_ERR_INVALID_ARG, "the handle belongs to device %d, device %d is current", h->device, dev);
+  return HERO_OK;
+}
+
 hero_status check_matrix(const hero_tensor& t, const char* name) {
   size_t es = dtype_size(t.dtype);
   HERO_REQUIRE(es != 0, HERO_ERR_INVALID_ARG, "%s: unknown dtype %d", name, t.dtype);
@@ -184,6 +191,12 @@ hero_status hero_check(hero_handle* h, void* stream) {
     cudaMemset(h->d_error, 0, sizeof(int));
     if (code == hero::ERR_BAD_ID) {
       hero::set_error("an embedding id was outside its table; it was clamped to the nearest valid row");
+      return HERO_ERR_INVALID_ARG;
+    }
+    if (code == hero::ERR_BAD_PAGE || code == hero::ERR_BAD_ROWS || code == hero::ERR_BAD_POS) {
+      hero::set_error(code == hero::ERR_BAD_PAGE ? "a page table named a page outside the cache; it was clamped (read) or skipped (written)"
+                      : code == hero::ERR_BAD_ROWS ? "a row range was decreasing, outside the matrices or longer than max_rows; it was cut"
+                                                   : "a position was outside the rotation tables; it was clamped");
       return HERO_ERR_INVALID_ARG;
     }
     hero::set_error("a bounded device-side wait gave up (code 0x%x)", code);

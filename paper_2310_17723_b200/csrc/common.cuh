@@ -74,15 +74,20 @@ __host__ __device__
 inline bool is_q8(int dt) { return dt == HERO_I8 || dt == HERO_F8; }   // 8-bit payload that carries a scale
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
+// the handle's device is the current one (tensors and streams of another device would be handed to the wrong one)
+hero_status check_device(const hero_handle* h);
+
 // data pointer 16-byte aligned, row pitch a multiple of 16 bytes, ld >= cols
 hero_status check_matrix(const hero_tensor& t, const char* name);
 
 // Codes a kernel may leave in the device error word besides "a bounded wait gave up" (those carry the place in
 // their low 16 bits and nothing above): an embedding id outside its table, clamped by LN^quant's gather.
 constexpr int ERR_BAD_ID = 0x1D000001;
+// ... a page id outside its pool, a row range outside its matrix, a position outside the rotation tables
+constexpr int ERR_BAD_PAGE = 0x1D000002, ERR_BAD_ROWS = 0x1D000003, ERR_BAD_POS = 0x1D000004;
 
 // Kernel families for the per-launch timing records.
-enum { KERNEL_LN = 1, KERNEL_GEMM = 2, KERNEL_ATTN = 3 };
+enum { KERNEL_LN = 1, KERNEL_GEMM = 2, KERNEL_ATTN = 3, KERNEL_CACHE = 4 };
 // Brackets one kernel launch with events when timing is on; counts the launch either way.
 struct LaunchScope {
   hero_handle* h; cudaStream_t s; int slot;

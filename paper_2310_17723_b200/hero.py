@@ -103,12 +103,35 @@ class KvCache(C.Structure):
                 ("len", C.c_void_p), ("max_len", C.c_int32)]
 
 
+class BlockCache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("dtype", C.c_int32),
+                ("page", C.c_int32), ("n_pages", C.c_int64), ("page_stride", C.c_int64), ("head_stride", C.c_int64),
+                ("ld", C.c_int64), ("table", C.c_void_p), ("ld_table", C.c_int64), ("len", C.c_void_p), ("max_len", C.c_int32),
+                ("B", C.c_int32), ("nkv", C.c_int32), ("dh", C.c_int32)]
+
+
+class BlockRowsArgs(C.Structure):
+    _fields_ = [("k", Tensor), ("v", Tensor), ("row_start", C.c_void_p), ("max_rows", C.c_int32)]
+
+
+class BlockAttnArgs(C.Structure):
+    _fields_ = [("q", Tensor), ("out", Tensor), ("row_start", C.c_void_p), ("max_rows", C.c_int32), ("nq", C.c_int32),
+                ("scale", C.c_float), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
+class QkNormRopeArgs(C.Structure):
+    _fields_ = [("q", Tensor), ("k", Tensor), ("q_out", Tensor), ("k_out", Tensor), ("nq", C.c_int32), ("nkv", C.c_int32),
+                ("dh", C.c_int32), ("rot", C.c_int32), ("pairing", C.c_int32), ("eps", C.c_float), ("q_gamma", C.c_void_p),
+                ("k_gamma", C.c_void_p), ("pos", C.c_void_p), ("cos", C.c_void_p), ("sin", C.c_void_p), ("n_pos", C.c_int64)]
+
+
 class LayerLayout(C.Structure):
     _fields_ = [(n, C.c_size_t) for n in ("qkv", "x_attn", "x_o", "x_mid", "x_mid_scale", "a", "x_2", "x_in", "x_in_scale",
                                           "h_in", "h_mid", "total")]
 
 
 P_MODE = {"static": 0, "rowmax": 1}
+PAIRING = {"halves": 0, "adjacent": 1}
 HIST_BINS = 2048
 
 EXPORTS = ("hero_create", "hero_destroy", "hero_last_error", "hero_check", "hero_launch_count",
@@ -116,7 +139,8 @@ EXPORTS = ("hero_create", "hero_destroy", "hero_last_error", "hero_check", "hero
            "hero_layer_workspace_bytes", "hero_layer_workspace_layout", "hero_layer_forward", "hero_layer_forward_host", "hero_layer_forward_host_async", "hero_profile_begin",
            "hero_profile_end", "hero_layer_forward_static", "hero_absmax_observe", "hero_quantize_weight", "hero_abs_histogram",
            "hero_int8_decode_attention", "hero_layer_decode", "hero_static_check", "hero_int8_attention_probe", "hero_stack_forward",
-           "hero_stack_forward_host_async", "hero_quantize_weight_f8")
+           "hero_stack_forward_host_async", "hero_quantize_weight_f8", "hero_block_cache_append", "hero_block_cache_read",
+           "hero_block_attention_workspace_bytes", "hero_block_attention", "hero_qk_norm_rope")
 
 _lib = None
 
@@ -169,6 +193,12 @@ def lib():
         L.hero_stack_forward.argtypes = [C.c_void_p, C.POINTER(StackDesc), C.c_void_p, C.c_size_t, C.c_void_p]
         L.hero_stack_forward_host_async.argtypes = [C.c_void_p, C.POINTER(StackDesc), C.POINTER(Tensor), C.POINTER(Tensor),
                                                     C.c_void_p, C.c_size_t, C.c_void_p]
+        L.hero_block_cache_append.argtypes = [C.c_void_p, C.POINTER(BlockCache), C.POINTER(BlockRowsArgs), C.c_void_p]
+        L.hero_block_cache_read.argtypes = L.hero_block_cache_append.argtypes
+        L.hero_block_attention_workspace_bytes.argtypes = [C.c_void_p, C.POINTER(BlockCache), C.c_int32, C.c_int64, C.c_int32,
+                                                           C.POINTER(C.c_size_t)]
+        L.hero_block_attention.argtypes = [C.c_void_p, C.POINTER(BlockCache), C.POINTER(BlockAttnArgs), C.c_void_p]
+        L.hero_qk_norm_rope.argtypes = [C.c_void_p, C.POINTER(QkNormRopeArgs), C.c_void_p]
         L.hero_profile_begin.argtypes = [C.c_void_p, C.c_int32]
         L.hero_profile_end.argtypes = [C.c_void_p, C.POINTER(C.c_float), C.POINTER(C.c_int32), C.POINTER(C.c_int32)]
         _lib = L
@@ -204,6 +234,40 @@ def tensor(t, gran="none", scale=None):
     return T
 
 
+def _vector(t, dtype, name):
+    """Address of a contiguous CUDA vector (or table) of the given type; None -> absent."""
+    if t is None:
+        return None
+    if not (t.is_cuda and t.dtype == dtype and t.is_contiguous()):
+        raise HeroError(ERR_INVALID_ARG, "%s: a contiguous CUDA tensor of %s is needed" % (name, dtype))
+    return t.data_ptr()
+
+
+def block_cache(k, v, k_scale, v_scale, table, lens, max_len):
+    """hero_block_cache over k, v: int8 / float8_e4m3fn [n_pages, nkv, page, dh] views of equal strides (feature stride 1;
+    a [n_pages, page, nkv, dh] buffer is passed as buffer.transpose(1, 2)); k_scale, v_scale: float32 [n_pages, nkv];
+    table: int32 [B, pages per sequence]; lens: int32 [B].  The struct keeps the tensors alive; it can be kept and used for
+    every call on the cache, `lens` and `table` being read on the device each time."""
+    need = lambda ok, what: None if ok else _refuse(what)      # noqa: E731
+    need(k.dim() == 4 and k.shape == v.shape and k.stride() == v.stride() and k.stride(3) == 1, "k, v: [n_pages, nkv, page, dh] views of equal strides")
+    need(k.dtype == v.dtype and k.dtype in (torch.int8, torch.float8_e4m3fn), "k, v: int8 or float8_e4m3fn")
+    need(k_scale.shape == v_scale.shape == k.shape[:2], "k_scale, v_scale: [n_pages, nkv]")
+    need(table.dim() == 2 and lens.shape == (table.shape[0],), "table: [B, pages], lens: [B]")
+    need(len({t.device for t in (k, v, k_scale, v_scale, table, lens)}) == 1 and k.is_cuda, "all tensors of a cache live on one CUDA device")
+    n, nkv, page, dh = k.shape
+    s = BlockCache(k.data_ptr(), v.data_ptr(), _vector(k_scale, torch.float32, "k_scale"), _vector(v_scale, torch.float32, "v_scale"),
+                   _DT[k.dtype], page, n, k.stride(0) if n > 1 else max(k.stride(0), dh), k.stride(1) if nkv > 1 else max(k.stride(1), dh),
+                   k.stride(2), _vector(table, torch.int32, "table"), table.shape[1], _vector(lens, torch.int32, "lens"), int(max_len),
+                   table.shape[0], nkv, dh)
+    s._keep = (k, v, k_scale, v_scale, table, lens)
+    s._device = k.get_device()
+    return s
+
+
+def _refuse(what):
+    raise HeroError(ERR_INVALID_ARG, what)
+
+
 class Handle:
     """Owns a hero_handle on the current CUDA device."""
 
@@ -212,6 +276,7 @@ class Handle:
             raise RuntimeError("hero needs a CUDA device (sm_100a); none is visible")
         self._h = C.c_void_p()
         _check(lib().hero_create(C.byref(self._h)))
+        self._device = torch.cuda.current_device()
 
     def close(self):
         if self._h:
@@ -302,6 +367,70 @@ class Handle:
         _check(fn(self._h, C.c_void_p(W.data_ptr()), W.stride(0), W.shape[0], W.shape[1],
                                           _ptr(in_scale), _ptr(out_scale), _ptr(bias), C.c_void_p(Wq.data_ptr()),
                                           Wq.stride(0), _ptr(w_scale), _ptr(bias_out), _stream(stream)))
+
+    # ---- serving over an 8-bit block cache
+    def _here(self, *tensors):
+        """Every tensor of a call lives on the handle's device."""
+        for t in tensors:
+            if t is not None and (t._keep[0] if isinstance(t, Tensor) else t).get_device() != self._device:
+                _refuse("a tensor is not on the handle's device %d" % self._device)
+
+    def _rows(self, cache, row_start, *tensors):
+        if cache._device != self._device:
+            _refuse("the cache is not on the handle's device %d" % self._device)
+        self._here(row_start, *tensors)
+        if row_start is None:
+            return None
+        if row_start.numel() != cache.B + 1:
+            _refuse("row_start has B + 1 = %d entries" % (cache.B + 1))
+        return _vector(row_start, torch.int32, "row_start")
+
+    def hero_block_cache_append(self, cache, k, v, row_start=None, max_rows=1, stream=None):
+        """cache: hero.block_cache; k, v: hero.Tensor (F16 / BF16 [rows, nkv*dh]) of the new tokens; row_start: int32 [B + 1]
+        (None: one row per sequence); max_rows: upper bound on a sequence's rows.  `lens` already counts the new tokens."""
+        a = BlockRowsArgs(k, v, self._rows(cache, row_start, k, v), max_rows)
+        _check(lib().hero_block_cache_append(self._h, C.byref(cache), C.byref(a), _stream(stream)))
+
+    def hero_block_cache_read(self, cache, k, v, row_start=None, max_rows=1, stream=None):
+        """k, v: hero.Tensor (F16 / BF16 [rows, nkv*dh]) to be written, either may be None: the values of the last tokens of each
+        sequence, as many as it has rows."""
+        a = BlockRowsArgs(k or tensor(None), v or tensor(None), self._rows(cache, row_start, k, v), max_rows)
+        _check(lib().hero_block_cache_read(self._h, C.byref(cache), C.byref(a), _stream(stream)))
+
+    def hero_block_attention_workspace_bytes(self, cache, nq, rows, max_rows=1):
+        n = C.c_size_t()
+        _check(lib().hero_block_attention_workspace_bytes(self._h, C.byref(cache), nq, rows, max_rows, C.byref(n)))
+        return int(n.value)
+
+    def hero_block_attention(self, cache, q, out, nq, row_start=None, max_rows=1, scale=0.0, workspace=None, stream=None):
+        """q: hero.Tensor (F16 / BF16 [rows, nq*dh]); out: hero.Tensor of the same shape (F16 / BF16, or I8 / F8 with a
+        feature-wise or static scale); workspace: 1-D uint8 CUDA tensor of hero_block_attention_workspace_bytes (may be empty or
+        None when that is 0); scale 0: 1 / sqrt(dh)."""
+        start = self._rows(cache, row_start, q, out)
+        ws, n = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
+        if n:
+            self._here(workspace)
+        a = BlockAttnArgs(q, out, start, max_rows, nq, scale, ws, n)
+        _check(lib().hero_block_attention(self._h, C.byref(cache), C.byref(a), _stream(stream)))
+
+    def hero_qk_norm_rope(self, q, k, q_out, k_out, nq, nkv, pos=None, cos=None, sin=None, q_gamma=None, k_gamma=None, eps=1e-6,
+                          pairing="halves", stream=None):
+        """q, k, q_out, k_out: hero.Tensor ([rows, nq*dh] / [rows, nkv*dh]; k and k_out None with nkv = 0; an output may be its
+        input); pos: int32 [rows]; cos, sin: float32 [n_pos, rot / 2] (None: no rotation); gammas: float32 [dh] (None: no norm)."""
+        self._here(q, k, q_out, k_out, pos, cos, sin, q_gamma, k_gamma)
+        dh, rot, n_pos = q.cols // nq, 0, 0
+        if cos is not None:
+            if cos.dim() != 2 or sin is None or cos.shape != sin.shape or pos is None or pos.numel() < q.rows:
+                _refuse("cos, sin: [n_pos, rot / 2], pos: [rows]")
+            n_pos, rot = cos.shape[0], 2 * cos.shape[1]
+        for g in (q_gamma, k_gamma):
+            if g is not None and g.numel() != dh:
+                _refuse("a gamma has dh = %d entries" % dh)
+        none = tensor(None)
+        a = QkNormRopeArgs(q, k or none, q_out, k_out or none, nq, nkv, dh, rot, PAIRING[pairing] if isinstance(pairing, str) else pairing,
+                           eps, _vector(q_gamma, torch.float32, "q_gamma"), _vector(k_gamma, torch.float32, "k_gamma"),
+                           _vector(pos, torch.int32, "pos"), _vector(cos, torch.float32, "cos"), _vector(sin, torch.float32, "sin"), n_pos)
+        _check(lib().hero_qk_norm_rope(self._h, C.byref(a), _stream(stream)))
 
     def hero_layer_workspace_bytes(self, desc, M):
         n = C.c_size_t()
