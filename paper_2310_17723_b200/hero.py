@@ -231,6 +231,7 @@ def tensor(t, gran="none", scale=None):
     ld = t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
     T = Tensor(t.data_ptr(), _DT[t.dtype], g, t.shape[0], t.shape[1], ld, None if scale is None else scale.data_ptr())
     T._keep = (t, scale)      # the struct holds raw pointers: keep the buffers alive as long as it lives
+    T._device = t.get_device()
     return T
 
 
@@ -268,6 +269,15 @@ def _refuse(what):
     raise HeroError(ERR_INVALID_ARG, what)
 
 
+def _current_raw_stream(device):
+    """Address of torch's current stream on `device` (what torch.cuda.current_stream(device).cuda_stream holds, without the
+    stream object)."""
+    return torch._C._cuda_getCurrentRawStream(device)
+
+
+_ABSENT = tensor(None)
+
+
 class Handle:
     """Owns a hero_handle on the current CUDA device."""
 
@@ -276,7 +286,7 @@ class Handle:
             raise RuntimeError("hero needs a CUDA device (sm_100a); none is visible")
         self._h = C.c_void_p()
         _check(lib().hero_create(C.byref(self._h)))
-        self._device = torch.cuda.current_device()
+        self._device, self._lib = torch.cuda.current_device(), lib()
 
     def close(self):
         if self._h:
@@ -368,69 +378,79 @@ class Handle:
                                           _ptr(in_scale), _ptr(out_scale), _ptr(bias), C.c_void_p(Wq.data_ptr()),
                                           Wq.stride(0), _ptr(w_scale), _ptr(bias_out), _stream(stream)))
 
-    # ---- serving over an 8-bit block cache
-    def _here(self, *tensors):
-        """Every tensor of a call lives on the handle's device."""
-        for t in tensors:
-            if t is not None and (t._keep[0] if isinstance(t, Tensor) else t).get_device() != self._device:
+    # ---- serving over an 8-bit block cache (a decode step is a few microseconds of GPU time: these methods are kept lean)
+    def _address(self, t, dtype, name):
+        """Address of a contiguous vector (or table) of the given type on the handle's device; None -> absent."""
+        if t is None:
+            return None
+        if t.dtype is not dtype or not t.is_contiguous() or t.get_device() != self._device:
+            _refuse("%s: a contiguous tensor of %s on CUDA device %d is needed" % (name, dtype, self._device))
+        return t.data_ptr()
+
+    def _here(self, *descs):
+        """Every hero.Tensor of a call lives on the handle's device."""
+        for d in descs:
+            if d is not None and getattr(d, "_device", self._device) != self._device:
                 _refuse("a tensor is not on the handle's device %d" % self._device)
 
-    def _rows(self, cache, row_start, *tensors):
+    def _raw_stream(self, stream):
+        return _current_raw_stream(self._device) if stream is None else stream.cuda_stream
+
+    def _rows(self, cache, row_start):
         if cache._device != self._device:
             _refuse("the cache is not on the handle's device %d" % self._device)
-        self._here(row_start, *tensors)
-        if row_start is None:
-            return None
-        if row_start.numel() != cache.B + 1:
+        if row_start is not None and row_start.numel() != cache.B + 1:
             _refuse("row_start has B + 1 = %d entries" % (cache.B + 1))
-        return _vector(row_start, torch.int32, "row_start")
+        return self._address(row_start, torch.int32, "row_start")
 
     def hero_block_cache_append(self, cache, k, v, row_start=None, max_rows=1, stream=None):
         """cache: hero.block_cache; k, v: hero.Tensor (F16 / BF16 [rows, nkv*dh]) of the new tokens; row_start: int32 [B + 1]
         (None: one row per sequence); max_rows: upper bound on a sequence's rows.  `lens` already counts the new tokens."""
-        a = BlockRowsArgs(k, v, self._rows(cache, row_start, k, v), max_rows)
-        _check(lib().hero_block_cache_append(self._h, C.byref(cache), C.byref(a), _stream(stream)))
+        self._here(k, v)
+        a = BlockRowsArgs(k, v, self._rows(cache, row_start), max_rows)
+        _check(self._lib.hero_block_cache_append(self._h, C.byref(cache), C.byref(a), self._raw_stream(stream)))
 
     def hero_block_cache_read(self, cache, k, v, row_start=None, max_rows=1, stream=None):
         """k, v: hero.Tensor (F16 / BF16 [rows, nkv*dh]) to be written, either may be None: the values of the last tokens of each
         sequence, as many as it has rows."""
-        a = BlockRowsArgs(k or tensor(None), v or tensor(None), self._rows(cache, row_start, k, v), max_rows)
-        _check(lib().hero_block_cache_read(self._h, C.byref(cache), C.byref(a), _stream(stream)))
+        self._here(k, v)
+        a = BlockRowsArgs(k or _ABSENT, v or _ABSENT, self._rows(cache, row_start), max_rows)
+        _check(self._lib.hero_block_cache_read(self._h, C.byref(cache), C.byref(a), self._raw_stream(stream)))
 
     def hero_block_attention_workspace_bytes(self, cache, nq, rows, max_rows=1):
         n = C.c_size_t()
-        _check(lib().hero_block_attention_workspace_bytes(self._h, C.byref(cache), nq, rows, max_rows, C.byref(n)))
+        _check(self._lib.hero_block_attention_workspace_bytes(self._h, C.byref(cache), nq, rows, max_rows, C.byref(n)))
         return int(n.value)
 
     def hero_block_attention(self, cache, q, out, nq, row_start=None, max_rows=1, scale=0.0, workspace=None, stream=None):
         """q: hero.Tensor (F16 / BF16 [rows, nq*dh]); out: hero.Tensor of the same shape (F16 / BF16, or I8 / F8 with a
         feature-wise or static scale); workspace: 1-D uint8 CUDA tensor of hero_block_attention_workspace_bytes (may be empty or
         None when that is 0); scale 0: 1 / sqrt(dh)."""
-        start = self._rows(cache, row_start, q, out)
-        ws, n = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
-        if n:
-            self._here(workspace)
-        a = BlockAttnArgs(q, out, start, max_rows, nq, scale, ws, n)
-        _check(lib().hero_block_attention(self._h, C.byref(cache), C.byref(a), _stream(stream)))
+        self._here(q, out)
+        ws, n = None, 0
+        if workspace is not None and workspace.numel():
+            ws, n = self._address(workspace, torch.uint8, "workspace"), workspace.numel()
+        a = BlockAttnArgs(q, out, self._rows(cache, row_start), max_rows, nq, scale, ws, n)
+        _check(self._lib.hero_block_attention(self._h, C.byref(cache), C.byref(a), self._raw_stream(stream)))
 
     def hero_qk_norm_rope(self, q, k, q_out, k_out, nq, nkv, pos=None, cos=None, sin=None, q_gamma=None, k_gamma=None, eps=1e-6,
                           pairing="halves", stream=None):
         """q, k, q_out, k_out: hero.Tensor ([rows, nq*dh] / [rows, nkv*dh]; k and k_out None with nkv = 0; an output may be its
         input); pos: int32 [rows]; cos, sin: float32 [n_pos, rot / 2] (None: no rotation); gammas: float32 [dh] (None: no norm)."""
-        self._here(q, k, q_out, k_out, pos, cos, sin, q_gamma, k_gamma)
+        self._here(q, k, q_out, k_out)
         dh, rot, n_pos = q.cols // nq, 0, 0
         if cos is not None:
-            if cos.dim() != 2 or sin is None or cos.shape != sin.shape or pos is None or pos.numel() < q.rows:
+            n_pos, half = cos.shape if cos.dim() == 2 else _refuse("cos, sin: [n_pos, rot / 2]")
+            rot = 2 * half
+            if sin is None or sin.numel() != n_pos * half or pos is None or pos.numel() < q.rows:
                 _refuse("cos, sin: [n_pos, rot / 2], pos: [rows]")
-            n_pos, rot = cos.shape[0], 2 * cos.shape[1]
-        for g in (q_gamma, k_gamma):
-            if g is not None and g.numel() != dh:
-                _refuse("a gamma has dh = %d entries" % dh)
-        none = tensor(None)
-        a = QkNormRopeArgs(q, k or none, q_out, k_out or none, nq, nkv, dh, rot, PAIRING[pairing] if isinstance(pairing, str) else pairing,
-                           eps, _vector(q_gamma, torch.float32, "q_gamma"), _vector(k_gamma, torch.float32, "k_gamma"),
-                           _vector(pos, torch.int32, "pos"), _vector(cos, torch.float32, "cos"), _vector(sin, torch.float32, "sin"), n_pos)
-        _check(lib().hero_qk_norm_rope(self._h, C.byref(a), _stream(stream)))
+        if (q_gamma is not None and q_gamma.numel() != dh) or (k_gamma is not None and k_gamma.numel() != dh):
+            _refuse("a gamma has dh = %d entries" % dh)
+        f32, at = torch.float32, self._address
+        a = QkNormRopeArgs(q, k or _ABSENT, q_out, k_out or _ABSENT, nq, nkv, dh, rot, PAIRING[pairing] if isinstance(pairing, str) else pairing,
+                           eps, at(q_gamma, f32, "q_gamma"), at(k_gamma, f32, "k_gamma"), at(pos, torch.int32, "pos"), at(cos, f32, "cos"),
+                           at(sin, f32, "sin"), n_pos)
+        _check(self._lib.hero_qk_norm_rope(self._h, C.byref(a), self._raw_stream(stream)))
 
     def hero_layer_workspace_bytes(self, desc, M):
         n = C.c_size_t()

@@ -7,6 +7,8 @@
     python -m paper_2310_17723_b200.microbench wquant --N 4096 --K 4096              # fold + Eq. 2 weight quantization GB/s
     python -m paper_2310_17723_b200.microbench decode --B 8 --S 2048 --nh 32 --dh 128 --graph   # decode attention GB/s
     python -m paper_2310_17723_b200.microbench layer-decode --workload c4 --B 8 --S 2048 --graph   # one decode step of a layer
+    python -m paper_2310_17723_b200.microbench block-attn --B 32 --S 4096 --nh 32 --nkv 8 --dh 128 --rows 1   # 8-bit block cache
+    python -m paper_2310_17723_b200.microbench block-append | block-read | rope ...   # same shape options
     python -m paper_2310_17723_b200.microbench layer --workload c3 [--f8 | --fp]   # one whole layer, us per forward
     ... --sweep runs the standalone-kernel sweep of the benchmark configurations instead of one shape.
 
@@ -237,6 +239,54 @@ def bench_layer_decode(h, workload, B, S, iters, p_mode="rowmax"):
           % (workload, B, S, p_mode, t * 1e6, B / t, byts / t / 1e9, byts / t / 1e9 / hbm, src), flush=True)
 
 
+def bench_block(h, op, B, S, rows, nh, nkv, dh, page, f8, iters):
+    """The operators of the 8-bit block cache: B sequences of S tokens, the last `rows` of them the call's (block-read: all S).
+    Algorithmic bytes: every cached byte of the call once, 16-bit rows once."""
+    q8 = torch.float8_e4m3fn if f8 else torch.int8
+    per = (S + page - 1) // page
+    fp = torch.bfloat16
+    total = B * S if op == "block-read" else B * rows
+    cached = 2 * B * S * nkv * dh
+    byts = {"block-attn": cached + 4 * total * nh * dh, "block-append": 6 * total * nkv * dh, "block-read": 6 * total * nkv * dh,
+            "rope": 4 * total * (nh + nkv) * dh + 4 * total * dh}[op]
+    flops = 4.0 * B * nh * dh * (rows * (S - rows) + rows * (rows + 1) / 2) if op == "block-attn" else 0.0
+    n = max(2, min(16, int(400e6 // byts) + 1))
+    sets = []
+    for _ in range(n):
+        c = [torch.randint(-127, 127, (B * per, nkv, page, dh), device="cuda", dtype=torch.int8).view(q8) for _ in range(2)]
+        if f8:                                    # no NaN codes
+            c = [(torch.randn(B * per, nkv, page, dh, device="cuda") * 100).clamp(-448, 448).to(q8) for _ in range(2)]
+        sc = [torch.rand(B * per, nkv, device="cuda") * 0.02 + 0.01 for _ in range(2)]
+        table = torch.randperm(B * per, device="cuda").to(torch.int32).reshape(B, per)
+        cache = hero.block_cache(*c, *sc, table, torch.full((B,), S, dtype=torch.int32, device="cuda"), S)
+        q, o = (torch.randn(total, nh * dh, device="cuda").to(fp) for _ in range(2))
+        k, v = (torch.randn(total, nkv * dh, device="cuda").to(fp) for _ in range(2))
+        sets.append((cache, *(hero.tensor(x) for x in (q, o, k, v))))
+    most = total // B
+    start = torch.arange(0, total + 1, most, dtype=torch.int32, device="cuda")
+    ws = torch.empty(h.hero_block_attention_workspace_bytes(sets[0][0], nh, total, most), dtype=torch.uint8, device="cuda")
+    pos = torch.arange(total, dtype=torch.int32, device="cuda")
+    cos = torch.rand(total, dh // 2, device="cuda")
+    gamma = torch.ones(dh, device="cuda")
+
+    def call(i):
+        cache, q, o, k, v = sets[i]
+        if op == "block-attn":
+            h.hero_block_attention(cache, q, o, nh, row_start=start, max_rows=most, workspace=ws)
+        elif op == "block-append":
+            h.hero_block_cache_append(cache, k, v, row_start=start, max_rows=most)
+        elif op == "block-read":
+            h.hero_block_cache_read(cache, k, v, row_start=start, max_rows=most)
+        else:
+            h.hero_qk_norm_rope(q, k, o, v, nh, nkv, pos, cos, cos, gamma, gamma)
+    t = _time(call, n, iters)
+    hbm, _, src = _peaks()
+    _say("%s B=%d S=%d rows=%d heads %d / %d of %d, pages of %d %s: %.1f us, %.0f GB/s, %.2f of %s copy bandwidth%s"
+         % (op, B, S, rows, nh, nkv, dh, page, "e4m3" if f8 else "i8", t * 1e6, byts / t / 1e9, byts / t / 1e9 / hbm, src,
+            ", %.0f TFLOP/s" % (flops / t / 1e12) if flops else ""))
+    return {"us": t * 1e6, "gbs": byts / t / 1e9}
+
+
 def bench_layer(h, workload, payload, fp, iters):
     """One forward of a single layer of a benchmark configuration (INT8, e4m3 or all-FP modules), L2 flushed between
     forwards by a 256 MB write (its time is measured alone and subtracted)."""
@@ -264,13 +314,14 @@ def bench_layer(h, workload, payload, fp, iters):
     h.profile_begin(64)
     st.forward()
     torch.cuda.synchronize()
-    fam = {1: "ln", 2: "gemm", 3: "attention"}
+    fam = {1: "ln", 2: "gemm", 3: "attention", 4: "block cache"}
     print("  launches: " + ", ".join("%s %.1f us" % (fam.get(k, "?"), ms * 1e3) for k, ms in h.profile_end()), flush=True)
 
 
 def main():
     ap = argparse.ArgumentParser()
-    ap.add_argument("kernel", choices=["ln", "gemm", "attn", "absmax", "wquant", "layer", "decode", "layer-decode"])
+    ap.add_argument("kernel", choices=["ln", "gemm", "attn", "absmax", "wquant", "layer", "decode", "layer-decode",
+                                       "block-attn", "block-append", "block-read", "rope"])
     ap.add_argument("--workload", default="c3", choices=["c1", "c3", "c4"])
     ap.add_argument("--M", type=int, default=65536)
     ap.add_argument("--H", type=int, default=1024)
@@ -280,6 +331,9 @@ def main():
     ap.add_argument("--S", type=int, default=384)
     ap.add_argument("--nh", type=int, default=16)
     ap.add_argument("--dh", type=int, default=64)
+    ap.add_argument("--nkv", type=int, default=8, help="key / value heads of the block cache")
+    ap.add_argument("--rows", type=int, default=1, help="new tokens per sequence (block cache)")
+    ap.add_argument("--page", type=int, default=64)
     ap.add_argument("--kind", default="i8", choices=["i8", "f16"])
     ap.add_argument("--act", default="none")
     ap.add_argument("--mask", default="none")
@@ -316,6 +370,8 @@ def main():
         bench_layer_decode(h, a.workload, a.B, a.S, a.iters, a.p_mode)
     elif a.kernel == "decode":
         bench_decode(h, a.B, a.S, a.nh, a.dh, a.iters, a.p_mode)
+    elif a.kernel.startswith("block-") or a.kernel == "rope":
+        bench_block(h, a.kernel, a.B, a.S, a.rows, a.nh, a.nkv, a.dh, a.page, a.f8, a.iters)
     elif a.kernel == "layer":
         bench_layer(h, a.workload, "f8" if a.f8 else "i8", a.fp, a.iters)
     else:
