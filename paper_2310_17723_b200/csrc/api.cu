@@ -58,18 +58,22 @@ typedef CUresult (*encode_tiled_fn)(CUtensorMap*, CUtensorMapDataType, cuuint32_
                                     const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
                                     CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
+static hero_tmap_slot& tmap_slot(hero_handle* h, const uint64_t (&key)[6]) {
+  uint64_t hsh = 0x9E3779B97F4A7C15ull;
+  for (int i = 0; i < 6; ++i) hsh = (hsh ^ key[i]) * 0xBF58476D1CE4E5B9ull + (hsh >> 29);
+  return h->tmap[(hsh >> 32) % HERO_TMAP_SLOTS];
+}
+
 hero_status make_tmap_2d(const hero_handle* h, CUtensorMap* out, const void* base, int elem_bytes, bool is_fp16,
                          bool is_bf16, uint64_t rows, uint64_t cols, uint64_t ld_bytes, uint32_t box_cols,
                          uint32_t box_rows, int swizzle_bytes) {
   HERO_REQUIRE(h && h->encode_tiled, HERO_ERR_CUDA, "tensor-map encoder unavailable");
   // cache look-up (see hero_tmap_slot)
-  const uint64_t key[5] = {reinterpret_cast<uint64_t>(base), rows, cols, ld_bytes,
+  const uint64_t key[6] = {reinterpret_cast<uint64_t>(base), rows, cols, ld_bytes,
                            (uint64_t)box_cols | ((uint64_t)box_rows << 16) | ((uint64_t)elem_bytes << 32) |
-                               ((uint64_t)(is_bf16 ? 1 : 0) << 40) | ((uint64_t)swizzle_bytes << 44)};
-  uint64_t hsh = 0x9E3779B97F4A7C15ull;
-  for (int i = 0; i < 5; ++i) hsh = (hsh ^ key[i]) * 0xBF58476D1CE4E5B9ull + (hsh >> 29);
+                               ((uint64_t)(is_bf16 ? 1 : 0) << 40) | ((uint64_t)swizzle_bytes << 44), 2};
   hero_handle* hm = const_cast<hero_handle*>(h);
-  hero_tmap_slot& slot = hm->tmap[(hsh >> 32) % HERO_TMAP_SLOTS];
+  hero_tmap_slot& slot = tmap_slot(hm, key);
   std::lock_guard<std::mutex> guard(hm->tmap_mu);
   if (slot.used && memcmp(slot.key, key, sizeof(key)) == 0) {
     *out = slot.map;
@@ -92,6 +96,32 @@ hero_status make_tmap_2d(const hero_handle* h, CUtensorMap* out, const void* bas
   HERO_REQUIRE(r == CUDA_SUCCESS, HERO_ERR_CUDA,
                "cuTensorMapEncodeTiled failed (%d): rows=%llu cols=%llu ld_bytes=%llu box=%ux%u", (int)r,
                (unsigned long long)rows, (unsigned long long)cols, (unsigned long long)ld_bytes, box_cols, box_rows);
+  memcpy(slot.key, key, sizeof(key));
+  slot.map = *out;
+  slot.used = true;
+  return HERO_OK;
+}
+
+hero_status make_tmap_pages(const hero_handle* h, CUtensorMap* out, const void* base, const hero_block_cache* c, uint32_t box_tokens) {
+  HERO_REQUIRE(h && h->encode_tiled, HERO_ERR_CUDA, "tensor-map encoder unavailable");
+  const uint64_t key[6] = {reinterpret_cast<uint64_t>(base), (uint64_t)c->page_stride, (uint64_t)c->head_stride, (uint64_t)c->ld,
+                           (uint64_t)c->n_pages | ((uint64_t)c->nkv << 32), 4 | ((uint64_t)c->page << 8) | ((uint64_t)c->dh << 16) | ((uint64_t)box_tokens << 32)};
+  hero_handle* hm = const_cast<hero_handle*>(h);
+  hero_tmap_slot& slot = tmap_slot(hm, key);
+  std::lock_guard<std::mutex> guard(hm->tmap_mu);
+  if (slot.used && memcmp(slot.key, key, sizeof(key)) == 0) {
+    *out = slot.map;
+    return HERO_OK;
+  }
+  cuuint64_t dims[4] = {(cuuint64_t)c->dh, (cuuint64_t)c->page, (cuuint64_t)c->nkv, (cuuint64_t)c->n_pages};
+  cuuint64_t strides[3] = {(cuuint64_t)c->ld, (cuuint64_t)c->head_stride, (cuuint64_t)c->page_stride};
+  cuuint32_t box[4] = {(cuuint32_t)c->dh, box_tokens, 1, 1};
+  cuuint32_t estr[4] = {1, 1, 1, 1};
+  CUresult r = reinterpret_cast<encode_tiled_fn>(h->encode_tiled)(
+      out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+      c->dh == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  HERO_REQUIRE(r == CUDA_SUCCESS, HERO_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d) for a block cache: strides %lld, %lld, %lld", (int)r,
+               (long long)c->ld, (long long)c->head_stride, (long long)c->page_stride);
   memcpy(slot.key, key, sizeof(key));
   slot.map = *out;
   slot.used = true;

@@ -1,8 +1,6 @@
 // Attention over the 8-bit block cache (hero_block_attention): o = softmax(scale q K^T) V, causal in a sequence's new rows.
 #include "block_cache.cuh"
 #include <cmath>
-#include <cstdlib>
-#include <cstdio>
 
 namespace hero {
 
@@ -29,25 +27,24 @@ __device__ __forceinline__ void store_out(const BlockAttnParams& p, long long ro
 
 // ------------------------------------------------------------------------------------------------------------------
 // Few rows per key / value head (decode steps, drafts).  Every cached byte is read once and meets at most 16 query rows, so
-// the kernel is bound by HBM and is built to keep loads in flight.  Each warp walks tiles of 16 tokens of its own through a ring of
-// asynchronous copies in which every lane fetches exactly the 16 bytes that it will hold in the matrix instruction's fragments: no
-// barrier in the loop, no bank conflicts, no transposition.  That works because the contraction's index may be permuted at will as
-// long as both operands agree:
-//   S^T [16 tokens x 8 rows] = K Q^T: lane (g, t) of mma.m16n8k16 loads features 64 c + 16 t .. + 15 of tokens g and g + 8; the four
-//       k slots it holds in step (c, j) stand for features 64 c + 16 t + 4 j .. + 3, for K and Q alike.
-//   O^T [features x 8 rows] = V^T P^T: lane (g, t) loads DH / 8 consecutive features of tokens 2t, 2t + 1, 2t + 8, 2t + 9; row g / g + 8
-//       of M tile j stands for feature (DH / 8) g + 2 j / + 1.
+// the kernel is bound by HBM and is built to keep loads in flight and the chains between them short.  Each warp walks steps of 32
+// tokens of its own (two halves of 16, each within a page) through a ring that bulk tensor copies fill: keys and values of a half are
+// one box each of a map over [pages][heads][tokens][features], swizzled so that the fragment loads below do not collide.
+// The operands need no transposition because a contraction's index may be permuted at will as long as both sides agree:
+//   S^T [16 tokens x 8 rows] = K Q^T: lane (g, t) of mma.m16n8k16 holds features 64 c + 16 t .. + 15 of tokens g and g + 8 (one 16-byte
+//       load each); the four k slots it has in step (c, j) stand for features 64 c + 16 t + 4 j .. + 3, for K and Q alike.
+//   O^T [features x 8 rows] = V^T P^T: lane (g, t) holds DH / 8 consecutive features of tokens 2t, 2t + 1, 2t + 8, 2t + 9; rows g and g + 8
+//       of M tile j stand for features (DH / 8) g + 2 j and + 1.  P^T is S^T's fragment, transposed by movmatrix.
 // Rows are the N dimension (8, the smallest there is), so a single query row does not pad a tile to 16.  Codes become FP16
 // exactly (INT8: byte permute into 1024 + u, subtract; e4m3: conversion instruction).  A query row is scaled by a power of two
 // into FP16 (exact for F16, for BF16 down to 2^-39 of the row's maximum).  The page's key scale multiplies the scores; the value
-// scale enters P relative to the largest one the warp has met (P <= 2^15: P is formed with a factor 2^11 so that pages whose scale
-// is 2^-25 of the largest still meet FP16's normal range).  The running maximum is moved only when a score exceeds it by more than
-// 4 in the exponent, so that most tiles need no reduction over tokens at all.
+// scale enters P relative to the largest one the warp has met (P is formed with a factor 2^11, so pages whose scale is 2^-25 of
+// the largest still meet FP16's normal range).  The running maximum moves only when a score exceeds it by more than 4 in
+// the exponent (P <= 2^15), so that most steps need no reduction over tokens.
 // Tokens are split over the warps of a CTA, the CTAs of a cluster (joined through distributed shared memory) and, where that does
 // not fill the GPU, over clusters (partial results in the workspace, joined by a second kernel).
 constexpr int ROWS_WARPS = 4;
 constexpr int ROWS_MAX_CLUSTER = 8;
-constexpr int ROWS_STAGES = 3;                  // ring depth in tiles of 16 tokens (keys and values: 32 DH bytes)
 constexpr float P_SHIFT = 11.0f, MAX_SLACK = 4.0f;
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -88,42 +85,61 @@ __device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
   return __uint_as_float(v);
 }
 
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory"); }
-__device__ __forceinline__ void copy8(uint32_t dst, const void* src) { asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory"); }
-__device__ __forceinline__ void copy4(uint32_t dst, const void* src) { asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory"); }
-__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+// one half (16 tokens) of a page: box {DH, 16, 1, 1} of the map over {features, tokens of a page, heads, pages}
+__device__ __forceinline__ void load_half(uint32_t dst, const CUtensorMap* m, int token, int head, int page, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(0), "r"(token), "r"(head), "r"(page), "r"(bar) : "memory");
+}
 
 template <int DH, int NT>
 struct RowsSmem {
-  static constexpr int STAGE = 32 * DH;                                     // bytes of a tile's keys and values
-  static constexpr int RING = ROWS_STAGES * STAGE;                          // per warp; afterwards its partial O [8 NT][DH]
-  static constexpr int PARTIAL = 8 * NT * DH * 4;
-  static constexpr int WARP = RING > PARTIAL ? RING : PARTIAL;
-  static constexpr int OFF_SCALES = ROWS_WARPS * WARP;                      // float [warps][stages][2]
-  static constexpr int OFF_ML = OFF_SCALES + ROWS_WARPS * ROWS_STAGES * 8;  // float [2][warps][8 NT], then the CTA's [2][8 NT]
-  static constexpr int BYTES = OFF_ML + (ROWS_WARPS + 1) * 8 * NT * 8;
+  static constexpr int STAGES = DH == 128 ? 2 : 4;                          // ring depth in steps of 32 tokens
+  static constexpr int HALF = 16 * DH;                                      // bytes of 16 keys (or values)
+  static constexpr int STAGE = 4 * HALF;                                    // keys of both halves, values of both halves
+  static constexpr int RING = STAGES * STAGE;                               // per warp; afterwards its partial O
+  static constexpr int OROW = DH + 8;                                       // floats between rows of a partial O (no bank conflicts)
+  static constexpr int PARTIAL = 8 * NT * OROW * 4;
+  static constexpr int WARP = ((RING > PARTIAL ? RING : PARTIAL) + 1023) / 1024 * 1024;
+  static constexpr int OFF_SCALES = ROWS_WARPS * WARP;                      // float2 [warps][stages][2]: key and value scale of a half
+  static constexpr int OFF_BARS = OFF_SCALES + ROWS_WARPS * STAGES * 16;    // uint64 [warps][stages]
+  static constexpr int OFF_ML = OFF_BARS + ROWS_WARPS * STAGES * 8;         // float [2][warps][8 NT], then the CTA's [2][8 NT]
+  static constexpr int BYTES = 1024 + OFF_ML + (ROWS_WARPS + 1) * 8 * NT * 8;
 };
+// place of a feature in a partial O: rows of O^T in the order of the lanes that hold them
+template <int DH>
+__device__ __forceinline__ int feature_at(int place) { return (DH / 8) * ((place & 15) >> 1) + 2 * (place >> 4) + (place & 1); }
 
 struct SplitPlan { int cluster, outer; };       // CTAs per cluster, clusters per (sequence, head, row tile)
 
 template <int DH, int NT, bool BF, bool F8>
-__global__ void __launch_bounds__(ROWS_WARPS * 32, NT == 1 ? 4 : 3) block_attn_rows_kernel(const BlockAttnParams p) {
+__global__ void __launch_bounds__(ROWS_WARPS * 32, 3) block_attn_rows_kernel(const __grid_constant__ CUtensorMap tm_k,
+                                                                             const __grid_constant__ CUtensorMap tm_v,
+                                                                             const __grid_constant__ BlockAttnParams p) {
+  using Smem = RowsSmem<DH, NT>;
+  constexpr int STAGES = Smem::STAGES;
   constexpr int R = 8 * NT;                      // rows of a tile: (row of the sequence, query head of the group) pairs
   constexpr int KC = DH / 64;                    // 64-feature pieces of a key
   constexpr int VW = DH / 32;                    // words of a lane's value slice
   constexpr int MT = DH / 16;                    // M tiles of O^T
-  using Smem = RowsSmem<DH, NT>;
-  extern __shared__ __align__(16) uint8_t smem[];
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   float* sm = reinterpret_cast<float*>(smem + Smem::OFF_ML);               // [warps][R] maxima
   float* sl = sm + ROWS_WARPS * R;                                         // [warps][R] sums
   float* cm = sl + ROWS_WARPS * R;                                         // [R] the CTA's
   float* cl = cm + R;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  uint64_t* full_bar = reinterpret_cast<uint64_t*>(smem + Smem::OFF_BARS) + warp * STAGES;
+  float2* scales = reinterpret_cast<float2*>(smem + Smem::OFF_SCALES) + warp * STAGES * 2;
+  if (lane == 0) {
+#pragma unroll
+    for (int i = 0; i < STAGES; ++i) ptx::mbar_init(&full_bar[i], 2);      // one arrival for each half
+    ptx::fence_mbar_init();
+  }
+  __syncwarp();
   ptx::pdl_launch_dependents();
   ptx::pdl_wait();
   const BlockView& c = p.c;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int b = blockIdx.z, hk = blockIdx.y % c.nkv, qt = blockIdx.y / c.nkv;
   const int splits = gridDim.x, cs = p.cluster;
   const SeqRows s = seq_rows(c, b);
@@ -131,51 +147,50 @@ __global__ void __launch_bounds__(ROWS_WARPS * 32, NT == 1 ? 4 : 3) block_attn_r
   if (rb >= total) return;                       // uniform over the cluster
   const int last = (min(rb + R, total) - 1) / p.group, base = s.len - s.n;
   const int L = max(base + last + 1, 0);         // keys of the tile's last row
-  const int full = base + rb / p.group + 1;      // keys of its first row: tiles below need no mask
-  const int per = ((L + splits - 1) / splits + 15) & ~15;
+  const int open = base + rb / p.group + 1;      // keys of its first row: steps below need no mask
+  const int per = ((L + splits - 1) / splits + 31) & ~31;
   const int k0 = min((int)blockIdx.x * per, L), k1 = min(k0 + per, L);
-  const int nt = (k1 - k0 + 15) >> 4;
+  const int steps = (k1 - k0 + 31) >> 5, mine = steps > warp ? (steps - warp + ROWS_WARPS - 1) / ROWS_WARPS : 0;
 
-  // page ids of the warp's next 32 tiles, one per lane
-  int my_id = 0;
-  auto load_pages = [&](int j0) {                // tiles j0, j0 + warps, ...
-    const int j = j0 + ROWS_WARPS * lane;
-    if (j < nt) my_id = page_for_read(c, b, (k0 + 16 * j) >> c.page_shift);
-  };
-  load_pages(warp);
-  const uint8_t* kbase = c.k + (long long)hk * c.head_stride + (long long)g * c.ld + 16 * t;
-  const uint8_t* vbase = c.v + (long long)hk * c.head_stride + (long long)(2 * t) * c.ld + (DH / 8) * g;
-  const uint8_t* ring = smem + warp * Smem::WARP;
-  const uint32_t ring_a = ptx::smem_u32(ring), scales_a = ptx::smem_u32(smem + Smem::OFF_SCALES) + warp * ROWS_STAGES * 8;
-  int jp = warp, slot = 0;                       // next tile to be requested, lane that holds its page
-  // requests tile jp into a stage: the lane's key pieces at [r * KC + q][lane], its value slices behind them, the two scales
-  auto request = [&](int stage) {
-    if (jp < nt) {
-      const int id = __shfl_sync(0xffffffffu, my_id, slot);
-      const long long at = (long long)id * c.page_stride + (long long)((k0 + 16 * jp) & (c.page - 1)) * c.ld;
-      const uint32_t dst = ring_a + stage * Smem::STAGE;
-#pragma unroll
-      for (int r = 0; r < 2; ++r)
-#pragma unroll
-        for (int q = 0; q < KC; ++q) copy16(dst + ((r * KC + q) * 32 + lane) * 16, kbase + at + (long long)(8 * r) * c.ld + 64 * q);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const uint8_t* src = vbase + at + (long long)((r & 1) + 8 * (r >> 1)) * c.ld;
-        if constexpr (VW == 4) copy16(dst + 16 * DH + (r * 32 + lane) * 16, src);
-        else copy8(dst + 16 * DH + (r * 32 + lane) * 8, src);
-      }
-      if (lane < 2) copy4(scales_a + stage * 8 + lane * 4, (lane ? c.vs : c.ks) + (long long)id * c.nkv + hk);
-      jp += ROWS_WARPS;
-      if (++slot == 32) { slot = 0; load_pages(jp); }
+  // lane i looks after half i % 2 of the warp's step i / 2 of every batch of 16: page id, scales, requests
+  int my_token = 0, my_id = -1;
+  float2 my_scales;
+  auto load_pages = [&](int n0) {                // steps n0 .. n0 + 15 of the warp
+    const int tok = k0 + 32 * (warp + ROWS_WARPS * (n0 + (lane >> 1))) + 16 * (lane & 1);
+    my_id = -1;
+    my_token = tok & (c.page - 1);
+    my_scales = make_float2(0.f, 0.f);
+    if (tok < k1) {
+      my_id = page_for_read(c, b, tok >> c.page_shift);
+      const long long at = (long long)my_id * c.nkv + hk;
+      my_scales = make_float2(__ldg(c.ks + at), __ldg(c.vs + at));
     }
-    copy_commit();                               // (an empty group keeps the count)
   };
+  const uint32_t ring_a = ptx::smem_u32(smem + warp * Smem::WARP);
+  auto request = [&](int n, int stage) {         // step n of the warp into a stage
+    if (n >= mine) return;
+    if (n && (n & 15) == 0) load_pages(n);
+    if ((lane >> 1) == (n & 15)) {
+      const int h = lane & 1;
+      scales[2 * stage + h] = my_scales;         // (before the arrival that releases it)
+      if (my_id >= 0) {
+        const uint32_t bar = ptx::smem_u32(&full_bar[stage]), dst = ring_a + stage * Smem::STAGE + h * Smem::HALF;
+        ptx::mbar_expect_tx(&full_bar[stage], 2 * Smem::HALF);
+        load_half(dst, &tm_k, my_token, hk, my_id, bar);
+        load_half(dst + 2 * Smem::HALF, &tm_v, my_token, hk, my_id, bar);
+      } else {
+        ptx::mbar_arrive(&full_bar[stage]);
+      }
+    }
+  };
+  load_pages(0);
 #pragma unroll
-  for (int i = 0; i < ROWS_STAGES - 1; ++i) request(i);
+  for (int i = 0; i < STAGES; ++i) request(i, i);
 
   // query fragments: lane (g, t) holds features 64 c + 16 t .. + 15 of row g of each N tile, scaled by a power of two
   uint32_t qf[NT][KC * 8];
-  float qs[NT];                                  // what undoes that scaling, for row g
+  float f[NT][2], u[NT][2], l[NT][2], acc[NT][MT][4];
+  int lim[NT][2];                                // per lane: rows 2 t and 2 t + 1 of each N tile (the columns of S^T and O^T it holds)
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
     const int rr = min(rb + 8 * n + g, total - 1);
@@ -195,158 +210,198 @@ __global__ void __launch_bounds__(ROWS_WARPS * 32, NT == 1 ? 4 : 3) block_attn_r
     const float amax = fp16ish_to_f32x2<BF>(top).x;
     // 2^(14 - exponent of the maximum); zero, infinite and NaN rows are left as they are
     const int e = (int)(__float_as_uint(amax) >> 23);
-    const bool odd = e == 0 || e == 255;
-    const float up = odd ? 1.0f : __uint_as_float((uint32_t)min(max(127 + 14 + 127 - e, 1), 254) << 23);
-    qs[n] = 1.0f / up;                           // a power of two within the normal range: exact
+    const float up = e == 0 || e == 255 ? 1.0f : __uint_as_float((uint32_t)min(127 + 14 + 127 - e, 253) << 23);
+    const float down = p.c2 / up;                // a power of two within the normal range: exact
 #pragma unroll
     for (int i = 0; i < KC * 8; ++i) {
-      const float2 f = fp16ish_to_f32x2<BF>(raw[i]);
-      qf[n][i] = pack_f16(f.x * up, f.y * up);
+      const float2 x = fp16ish_to_f32x2<BF>(raw[i]);
+      qf[n][i] = pack_f16(x.x * up, x.y * up);
     }
-  }
-  // per lane: rows 2 t and 2 t + 1 of each N tile (the columns of S^T and O^T it holds)
-  float f[NT][2], m[NT][2], l[NT][2], acc[NT][MT][4];
-  int lim[NT][2];
-#pragma unroll
-  for (int n = 0; n < NT; ++n)
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
-      f[n][r] = p.c2 * __shfl_sync(0xffffffffu, qs[n], 4 * (2 * t + r));
+      f[n][r] = __shfl_sync(0xffffffffu, down, 4 * (2 * t + r));
       lim[n][r] = base + min(rb + 8 * n + 2 * t + r, total - 1) / p.group + 1;
-      m[n][r] = -INFINITY; l[n][r] = 0.f;
+      u[n][r] = 0.f; l[n][r] = 0.f;              // u = P_SHIFT - running maximum
     }
-#pragma unroll
-  for (int n = 0; n < NT; ++n)
 #pragma unroll
     for (int j = 0; j < MT; ++j)
 #pragma unroll
       for (int i = 0; i < 4; ++i) acc[n][j][i] = 0.f;
-  float vref = 0.f;
+  }
+  float vref = 0.f, inv_vref = 0.f;
+  // byte offsets of the lane's pieces within a half, under the swizzle (128-byte rows: 16-byte piece ^ row % 8; 64-byte rows:
+  // piece ^ row / 2 % 4); rows g + 8 and 2 t + 8 lie 8 rows further with the same pattern
+  uint32_t k_off[KC], v_off[2];
+  if constexpr (DH == 128) {
+#pragma unroll
+    for (int q = 0; q < KC; ++q) k_off[q] = g * 128 + (((4 * q + t) ^ g) << 4);
+#pragma unroll
+    for (int r = 0; r < 2; ++r) v_off[r] = (2 * t + r) * 128 + ((g ^ (2 * t + r)) << 4);
+  } else {
+    k_off[0] = g * 64 + ((t ^ ((g >> 1) & 3)) << 4);
+#pragma unroll
+    for (int r = 0; r < 2; ++r) v_off[r] = (2 * t + r) * 64 + (((g >> 1) ^ t) << 4) + (g & 1) * 8;
+  }
 
+  bool ok = true;
   int stage = 0;
-  for (int j = warp; j < nt; j += ROWS_WARPS) {
-    copy_wait<ROWS_STAGES - 2>();
-    __syncwarp();                                // the scales come from other lanes' copies; and every lane is done with the stage requested next
-    request(stage == 0 ? ROWS_STAGES - 1 : stage - 1);
-    const uint8_t* tile = ring + stage * Smem::STAGE;
-    const float2 scales = *reinterpret_cast<const float2*>(smem + Smem::OFF_SCALES + (warp * ROWS_STAGES + stage) * 8);
-    const float ks = scales.x, vs = scales.y;
-    if (++stage == ROWS_STAGES) stage = 0;
-    const int tb = k0 + 16 * j;
-    // ---- scores
-    float sc[NT][4];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) sc[n][0] = sc[n][1] = sc[n][2] = sc[n][3] = 0.f;
-#pragma unroll
-    for (int q = 0; q < KC; ++q) {
-      const uint4 x = reinterpret_cast<const uint4*>(tile)[q * 32 + lane], y = reinterpret_cast<const uint4*>(tile)[(KC + q) * 32 + lane];
-      const uint32_t w0[4] = {x.x, x.y, x.z, x.w}, w1[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        uint32_t a0, a1, a2, a3;
-        codes4_to_f16<F8>(w0[i], a0, a2);
-        codes4_to_f16<F8>(w1[i], a1, a3);
-#pragma unroll
-        for (int n = 0; n < NT; ++n) mma_f16(sc[n], a0, a1, a2, a3, qf[n][8 * q + 2 * i], qf[n][8 * q + 2 * i + 1]);
+  uint32_t phase = 0;
+  for (int n = 0; n < mine; ++n) {
+    const int tb = k0 + 32 * (warp + ROWS_WARPS * n);
+    ok = ok && ptx::mbar_wait(&full_bar[stage], phase, c.err, 0x7000 | stage);
+    if (!__all_sync(0xffffffffu, ok)) {          // a copy never arrived (reported): wait, bounded, for the others before the ring is reused
+      for (int i = 1; i < STAGES && n + i < mine; ++i) {
+        if (++stage == STAGES) { stage = 0; phase ^= 1; }
+        ptx::mbar_wait(&full_bar[stage], phase, c.err, 0x7100 | stage);
       }
+      break;
+    }
+    const uint8_t* tile = smem + warp * Smem::WARP + stage * Smem::STAGE;
+    const float4 sv = *reinterpret_cast<const float4*>(&scales[2 * stage]);   // key and value scale of either half
+    // ---- scores, one chain of products per half and 64 features
+    float sc[2][NT][4];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float part[KC][NT][4];
+#pragma unroll
+      for (int q = 0; q < KC; ++q) {
+        const uint4 x = *reinterpret_cast<const uint4*>(tile + h * Smem::HALF + k_off[q]);
+        const uint4 y = *reinterpret_cast<const uint4*>(tile + h * Smem::HALF + k_off[q] + 8 * DH);
+        const uint32_t w0[4] = {x.x, x.y, x.z, x.w}, w1[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+        for (int r = 0; r < NT; ++r) part[q][r][0] = part[q][r][1] = part[q][r][2] = part[q][r][3] = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          uint32_t a0, a1, a2, a3;
+          codes4_to_f16<F8>(w0[i], a0, a2);
+          codes4_to_f16<F8>(w1[i], a1, a3);
+#pragma unroll
+          for (int r = 0; r < NT; ++r) mma_f16(part[q][r], a0, a1, a2, a3, qf[r][8 * q + 2 * i], qf[r][8 * q + 2 * i + 1]);
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < NT; ++r)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sc[h][r][i] = KC == 2 ? part[0][r][i] + part[KC - 1][r][i] : part[0][r][i];
     }
     // ---- probabilities
-    if (vs > vref) {                             // uniform over the warp
-      const float up = vref / vs;
+    if (fmaxf(sv.y, sv.w) > vref) {              // uniform over the warp
+      const float now = fmaxf(sv.y, sv.w), up = vref / now;
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
+      for (int r = 0; r < NT; ++r)
 #pragma unroll
         for (int k = 0; k < MT; ++k)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) acc[n][k][i] *= up;
-      vref = vs;
+          for (int i = 0; i < 4; ++i) acc[r][k][i] *= up;
+      vref = now;
+      inv_vref = 1.0f / now;
     }
-    const float rv = vref > 0.f ? vs / vref : 0.f;
-    uint32_t pb[NT][2];
+    const float rv[2] = {sv.y * inv_vref, sv.w * inv_vref};
+    uint32_t pb[2][NT][2];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      const float f0 = f[n][0] * ks, f1 = f[n][1] * ks;
-      float x0 = sc[n][0] * f0, x1 = sc[n][1] * f1, x2 = sc[n][2] * f0, x3 = sc[n][3] * f1;
-      if (tb + 16 > full) {
-        if (tb + g >= lim[n][0]) x0 = -INFINITY;
-        if (tb + g >= lim[n][1]) x1 = -INFINITY;
-        if (tb + g + 8 >= lim[n][0]) x2 = -INFINITY;
-        if (tb + g + 8 >= lim[n][1]) x3 = -INFINITY;
+    for (int r = 0; r < NT; ++r) {
+      float x[2][4];                             // score - maximum + P_SHIFT, base 2
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float f0 = f[r][0] * (h ? sv.z : sv.x), f1 = f[r][1] * (h ? sv.z : sv.x);
+        x[h][0] = fmaf(sc[h][r][0], f0, u[r][0]); x[h][1] = fmaf(sc[h][r][1], f1, u[r][1]);
+        x[h][2] = fmaf(sc[h][r][2], f0, u[r][0]); x[h][3] = fmaf(sc[h][r][3], f1, u[r][1]);
       }
-      float mx0 = fmaxf(x0, x2), mx1 = fmaxf(x1, x3);
-      if (__any_sync(0xffffffffu, mx0 > m[n][0] + MAX_SLACK || mx1 > m[n][1] + MAX_SLACK)) {
+      if (tb + 32 > open) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (tb + 16 * h + g + 8 * (i >> 1) >= lim[r][i & 1]) x[h][i] = -INFINITY;
+      }
+      float mx0 = fmaxf(fmaxf(x[0][0], x[0][2]), fmaxf(x[1][0], x[1][2])), mx1 = fmaxf(fmaxf(x[0][1], x[0][3]), fmaxf(x[1][1], x[1][3]));
+      if (n == 0 || __any_sync(0xffffffffu, fmaxf(mx0, mx1) > P_SHIFT + MAX_SLACK)) {
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) {
           mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, o));
           mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, o));
         }
-        mx0 = fmaxf(mx0, m[n][0]); mx1 = fmaxf(mx1, m[n][1]);
-        const float a0 = mx0 > -INFINITY ? ex2(m[n][0] - mx0) : 1.f, a1 = mx1 > -INFINITY ? ex2(m[n][1] - mx1) : 1.f;
-        m[n][0] = mx0; m[n][1] = mx1;
-        l[n][0] *= a0; l[n][1] *= a1;
+        // the maximum moves by mx - P_SHIFT: up, except in the first step (and not at all where every token is masked)
+        float d0 = mx0 - P_SHIFT, d1 = mx1 - P_SHIFT;
+        if (n != 0) { d0 = fmaxf(d0, 0.f); d1 = fmaxf(d1, 0.f); }
+        if (mx0 == -INFINITY) d0 = 0.f;
+        if (mx1 == -INFINITY) d1 = 0.f;
+        u[r][0] -= d0; u[r][1] -= d1;
+        if (n != 0) {
+          const float a0 = ex2(-d0), a1 = ex2(-d1);
+          l[r][0] *= a0; l[r][1] *= a1;
 #pragma unroll
-        for (int k = 0; k < MT; ++k) { acc[n][k][0] *= a0; acc[n][k][2] *= a0; acc[n][k][1] *= a1; acc[n][k][3] *= a1; }
+          for (int k = 0; k < MT; ++k) { acc[r][k][0] *= a0; acc[r][k][2] *= a0; acc[r][k][1] *= a1; acc[r][k][3] *= a1; }
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) { x[h][0] -= d0; x[h][2] -= d0; x[h][1] -= d1; x[h][3] -= d1; }
       }
-      const float u0 = m[n][0] > -INFINITY ? P_SHIFT - m[n][0] : 0.f, u1 = m[n][1] > -INFINITY ? P_SHIFT - m[n][1] : 0.f;
-      x0 = ex2(x0 + u0); x1 = ex2(x1 + u1); x2 = ex2(x2 + u0); x3 = ex2(x3 + u1);
-      l[n][0] += x0 + x2; l[n][1] += x1 + x3;
-      pb[n][0] = transpose8x8(pack_f16(x0 * rv, x1 * rv));
-      pb[n][1] = transpose8x8(pack_f16(x2 * rv, x3 * rv));
-    }
-    uint32_t vr[4][VW];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      if constexpr (VW == 4) {
-        const uint4 x = reinterpret_cast<const uint4*>(tile + 16 * DH)[r * 32 + lane];
-        vr[r][0] = x.x; vr[r][1] = x.y; vr[r][2] = x.z; vr[r][3] = x.w;
-      } else {
-        const uint2 x = reinterpret_cast<const uint2*>(tile + 16 * DH)[r * 32 + lane];
-        vr[r][0] = x.x; vr[r][1] = x.y;
+      for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[h][i] = ex2(x[h][i]);
+        l[r][0] += x[h][0] + x[h][2]; l[r][1] += x[h][1] + x[h][3];
+        pb[h][r][0] = transpose8x8(pack_f16(x[h][0] * rv[h], x[h][1] * rv[h]));
+        pb[h][r][1] = transpose8x8(pack_f16(x[h][2] * rv[h], x[h][3] * rv[h]));
       }
     }
     // ---- values; e4m3 slots behind the end may hold NaN, which a zero probability does not silence
-    if (F8 && tb + 16 > k1) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
-        if (tb + 2 * t + (r & 1) + 8 * (r >> 1) >= k1) {
+    for (int h = 0; h < 2; ++h) {
+      uint32_t vr[4][VW];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const uint8_t* at = tile + (2 + h) * Smem::HALF + v_off[r & 1] + (r >> 1) * 8 * DH;
+        if constexpr (VW == 4) {
+          const uint4 x = *reinterpret_cast<const uint4*>(at);
+          vr[r][0] = x.x; vr[r][1] = x.y; vr[r][2] = x.z; vr[r][3] = x.w;
+        } else {
+          const uint2 x = *reinterpret_cast<const uint2*>(at);
+          vr[r][0] = x.x; vr[r][1] = x.y;
+        }
+        if (F8 && tb + 32 > k1 && tb + 16 * h + 2 * t + (r & 1) + 8 * (r >> 1) >= k1) {
 #pragma unroll
           for (int w = 0; w < VW; ++w) vr[r][w] = 0;
         }
-    }
+      }
 #pragma unroll
-    for (int w = 0; w < VW; ++w) {
-      uint32_t ab[4], cd[4];                     // feature i of the word: tokens (2t, 2t + 1) and (2t + 8, 2t + 9)
-      codes4_to_f16<F8>(__byte_perm(vr[0][w], vr[1][w], 0x5140), ab[0], ab[1]);
-      codes4_to_f16<F8>(__byte_perm(vr[0][w], vr[1][w], 0x7362), ab[2], ab[3]);
-      codes4_to_f16<F8>(__byte_perm(vr[2][w], vr[3][w], 0x5140), cd[0], cd[1]);
-      codes4_to_f16<F8>(__byte_perm(vr[2][w], vr[3][w], 0x7362), cd[2], cd[3]);
+      for (int w = 0; w < VW; ++w) {
+        uint32_t ab[4], cd[4];                   // feature i of the word: tokens (2t, 2t + 1) and (2t + 8, 2t + 9)
+        codes4_to_f16<F8>(__byte_perm(vr[0][w], vr[1][w], 0x5140), ab[0], ab[1]);
+        codes4_to_f16<F8>(__byte_perm(vr[0][w], vr[1][w], 0x7362), ab[2], ab[3]);
+        codes4_to_f16<F8>(__byte_perm(vr[2][w], vr[3][w], 0x5140), cd[0], cd[1]);
+        codes4_to_f16<F8>(__byte_perm(vr[2][w], vr[3][w], 0x7362), cd[2], cd[3]);
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        mma_f16(acc[n][2 * w], ab[0], ab[1], cd[0], cd[1], pb[n][0], pb[n][1]);
-        mma_f16(acc[n][2 * w + 1], ab[2], ab[3], cd[2], cd[3], pb[n][0], pb[n][1]);
+        for (int r = 0; r < NT; ++r) {
+          mma_f16(acc[r][2 * w], ab[0], ab[1], cd[0], cd[1], pb[h][r][0], pb[h][r][1]);
+          mma_f16(acc[r][2 * w + 1], ab[2], ab[3], cd[2], cd[3], pb[h][r][0], pb[h][r][1]);
+        }
       }
     }
+    __syncwarp();                                // every lane has read the stage
+    request(n + STAGES, stage);
+    if (++stage == STAGES) { stage = 0; phase ^= 1; }
   }
 
-  // ---- join the warps of the CTA; a warp's partial O takes the place of its ring (all its copies have been waited for)
-  copy_wait<0>();
-  __syncwarp();
+  // ---- join the warps of the CTA; a warp's partial O takes the place of its ring (every copy it asked for has been waited for)
   float* my_o = reinterpret_cast<float*>(smem + warp * Smem::WARP);
+  __syncwarp();
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
 #pragma unroll
       for (int o = 4; o < 32; o <<= 1) l[n][r] += __shfl_xor_sync(0xffffffffu, l[n][r], o);
-      if (g == 0) { sm[warp * R + 8 * n + 2 * t + r] = m[n][r]; sl[warp * R + 8 * n + 2 * t + r] = l[n][r]; }
+      const int row = 8 * n + 2 * t + r;
+      if (g == 0) { sm[warp * R + row] = l[n][r] != 0.f ? P_SHIFT - u[n][r] : -INFINITY; sl[warp * R + row] = l[n][r]; }
 #pragma unroll
       for (int k = 0; k < MT; ++k)
-        *reinterpret_cast<float2*>(my_o + (8 * n + 2 * t + r) * DH + (DH / 8) * g + 2 * k) = make_float2(acc[n][k][r] * vref, acc[n][k][2 + r] * vref);
+        *reinterpret_cast<float2*>(my_o + row * Smem::OROW + 16 * k + 2 * g) = make_float2(acc[n][k][r] * vref, acc[n][k][2 + r] * vref);
     }
   }
   __syncthreads();
   for (int i = threadIdx.x; i < R * DH; i += ROWS_WARPS * 32) {
-    const int row = i / DH, d = i % DH;
+    const int row = i / DH, at = row * Smem::OROW + i % DH;
     float mt = sm[row];
 #pragma unroll
     for (int w = 1; w < ROWS_WARPS; ++w) mt = fmaxf(mt, sm[w * R + row]);
@@ -354,19 +409,19 @@ __global__ void __launch_bounds__(ROWS_WARPS * 32, NT == 1 ? 4 : 3) block_attn_r
 #pragma unroll
     for (int w = 0; w < ROWS_WARPS; ++w) {
       const float mw = sm[w * R + row], e = mw > -INFINITY ? ex2(mw - mt) : 0.f;
-      y = fmaf(e, reinterpret_cast<const float*>(smem + w * Smem::WARP)[i], y); lt = fmaf(e, sl[w * R + row], lt);
+      y = fmaf(e, reinterpret_cast<const float*>(smem + w * Smem::WARP)[at], y); lt = fmaf(e, sl[w * R + row], lt);
     }
-    reinterpret_cast<float*>(smem)[i] = y;
-    if (d == 0) { cm[row] = mt; cl[row] = lt; }
+    reinterpret_cast<float*>(smem)[at] = y;
+    if (i % DH == 0) { cm[row] = mt; cl[row] = lt; }
   }
   // ---- join the CTAs of the cluster: each finishes its share of the tile
   if (cs > 1) ptx::cluster_sync(); else __syncthreads();
   const int rank = cs > 1 ? (int)ptx::cluster_ctarank() : 0, share = R * DH / cs;
   const uint32_t am = ptx::smem_u32(cm), al = ptx::smem_u32(cl), ao = ptx::smem_u32(smem);
   for (int i = rank * share + threadIdx.x; i < (rank + 1) * share; i += ROWS_WARPS * 32) {
-    const int row = i / DH, d = i % DH, rr = rb + row;
+    const int row = i / DH, place = i % DH, rr = rb + row;
     if (rr >= total) continue;
-    float mt = cm[row], lt = cl[row], y = reinterpret_cast<const float*>(smem)[i];
+    float mt = cm[row], lt = cl[row], y = reinterpret_cast<const float*>(smem)[row * Smem::OROW + place];
     if (cs > 1) {
       float mq[ROWS_MAX_CLUSTER];
       mt = -INFINITY;
@@ -381,17 +436,17 @@ __global__ void __launch_bounds__(ROWS_WARPS * 32, NT == 1 ? 4 : 3) block_attn_r
         if (q < cs) {
           const float e = mq[q] > -INFINITY ? ex2(mq[q] - mt) : 0.f;
           lt = fmaf(e, ld_cluster_f32(ptx::mapa(al + 4 * row, q)), lt);
-          y = fmaf(e, ld_cluster_f32(ptx::mapa(ao + 4 * i, q)), y);
+          y = fmaf(e, ld_cluster_f32(ptx::mapa(ao + 4 * (row * Smem::OROW + place), q)), y);
         }
     }
     const long long row_g = s.r0 + rr / p.group;
     const int hq = hk * p.group + rr % p.group;
     if (p.outer == 1) {
-      store_out(p, row_g, hq * DH + d, lt > 0.f ? y / lt : 0.f);
+      store_out(p, row_g, hq * DH + feature_at<DH>(place), lt != 0.f ? y / lt : 0.f);
     } else {
       const long long at = (row_g * p.nq + hq) * p.outer + blockIdx.x / cs;
-      p.part_o[at * DH + d] = y;
-      if (d == 0) p.part_ml[at] = make_float2(mt, lt);
+      p.part_o[at * DH + place] = y;
+      if (place == 0) p.part_ml[at] = make_float2(mt, lt);
     }
   }
   if (cs > 1) ptx::cluster_sync();               // nobody leaves while a peer may still read its shared memory
@@ -424,19 +479,18 @@ __global__ void __launch_bounds__(128) block_attn_join_kernel(const BlockAttnPar
     for (int e = 0; e < E; ++e) y[e] = fmaf(f, p.part_o[(at + q) * DH + 32 * e + lane], y[e]);
   }
 #pragma unroll
-  for (int e = 0; e < E; ++e) store_out(p, s.r0 + i, hq * DH + 32 * e + lane, lt > 0.f ? y[e] / lt : 0.f);
+  for (int e = 0; e < E; ++e) store_out(p, s.r0 + i, hq * DH + feature_at<DH>(32 * e + lane), lt != 0.f ? y[e] / lt : 0.f);
 }
 
 // How the tokens of a (sequence, key / value head, row tile) are split: the host knows an upper bound of the lengths only.
 static SplitPlan plan_rows(const hero_handle* h, const hero_block_cache* cc, int nq, int max_rows, int nt) {
   const long long tiles = ((long long)max_rows * (nq / cc->nkv) + 8 * nt - 1) / (8 * nt);
   const long long groups = tiles * cc->nkv * cc->B;
-  const long long slots = (long long)h->sm_count * (nt == 1 ? 4 : 3);
+  const long long slots = (long long)h->sm_count * 3;
   long long want = (2 * slots + groups - 1) / groups;             // CTAs for two rounds of the GPU
   const long long most = (cc->max_len + 255) / 256;               // of at least 256 tokens each
   if (want > most) want = most;
   SplitPlan s = {1, 1};
-  if (getenv("DEV_SPLIT")) { sscanf(getenv("DEV_SPLIT"), "%d,%d", &s.cluster, &s.outer); return s; }
   while (s.cluster < ROWS_MAX_CLUSTER && s.cluster < want) s.cluster *= 2;
   if (want > ROWS_MAX_CLUSTER) s.outer = (int)((want + ROWS_MAX_CLUSTER - 1) / ROWS_MAX_CLUSTER);
   return s;
@@ -447,7 +501,7 @@ static size_t part_bytes(const SplitPlan& s, long long rows, int nq, int dh) {
 }
 
 template <int DH, int NT>
-static hero_status launch_rows(hero_handle* h, const BlockAttnParams& p, bool bf, int B, int tiles, cudaStream_t stream) {
+static hero_status launch_rows(hero_handle* h, const hero_block_cache* cc, const BlockAttnParams& p, bool bf, int B, int tiles, cudaStream_t stream) {
   auto kern = bf ? (p.c.f8 ? block_attn_rows_kernel<DH, NT, true, true> : block_attn_rows_kernel<DH, NT, true, false>)
                  : (p.c.f8 ? block_attn_rows_kernel<DH, NT, false, true> : block_attn_rows_kernel<DH, NT, false, false>);
   static PerDeviceOnce configured[4];            // per instantiation of the kernel
@@ -456,6 +510,9 @@ static hero_status launch_rows(hero_handle* h, const BlockAttnParams& p, bool bf
     HERO_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, RowsSmem<DH, NT>::BYTES));
     once.set(h->device);
   }
+  CUtensorMap tm_k, tm_v;
+  hero_status st;
+  if ((st = make_tmap_pages(h, &tm_k, cc->k, cc, 16)) != HERO_OK || (st = make_tmap_pages(h, &tm_v, cc->v, cc, 16)) != HERO_OK) return st;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(p.cluster * p.outer), (unsigned)(p.c.nkv * tiles), (unsigned)B);
   cfg.blockDim = dim3(ROWS_WARPS * 32);
@@ -476,7 +533,7 @@ static hero_status launch_rows(hero_handle* h, const BlockAttnParams& p, bool bf
   cfg.attrs = at; cfg.numAttrs = n;
   {
     LaunchScope scope(h, stream, KERNEL_ATTN);
-    HERO_CUDA(cudaLaunchKernelEx(&cfg, kern, p));
+    HERO_CUDA(cudaLaunchKernelEx(&cfg, kern, tm_k, tm_v, p));
   }
   if (p.outer > 1) {
     LaunchScope scope(h, stream, KERNEL_ATTN);
@@ -546,6 +603,6 @@ extern "C" hero_status hero_block_attention(hero_handle* h, const hero_block_cac
   HERO_REQUIRE(tiles * cc->nkv <= 65535, HERO_ERR_UNSUPPORTED, "max_rows=%d", a->max_rows);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (cc->dh == 64)
-    return nt == 1 ? launch_rows<64, 1>(h, p, bf, cc->B, (int)tiles, s) : launch_rows<64, 2>(h, p, bf, cc->B, (int)tiles, s);
-  return nt == 1 ? launch_rows<128, 1>(h, p, bf, cc->B, (int)tiles, s) : launch_rows<128, 2>(h, p, bf, cc->B, (int)tiles, s);
+    return nt == 1 ? launch_rows<64, 1>(h, cc, p, bf, cc->B, (int)tiles, s) : launch_rows<64, 2>(h, cc, p, bf, cc->B, (int)tiles, s);
+  return nt == 1 ? launch_rows<128, 1>(h, cc, p, bf, cc->B, (int)tiles, s) : launch_rows<128, 2>(h, cc, p, bf, cc->B, (int)tiles, s);
 }

@@ -18,7 +18,7 @@
 // host time, several per launch.  Layers launch the same shapes on the same buffers over and over: a small direct-mapped
 // cache in the handle spares the latency-bound workloads that host time.
 struct hero_tmap_slot {
-  uint64_t key[5];
+  uint64_t key[6];
   CUtensorMap map;
   bool used = false;
 };
@@ -179,5 +179,8 @@ __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;"
 hero_status make_tmap_2d(const hero_handle* h, CUtensorMap* out, const void* base, int elem_bytes, bool is_fp16,
                          bool is_bf16, uint64_t rows, uint64_t cols, uint64_t ld_bytes, uint32_t box_cols,
                          uint32_t box_rows, int swizzle_bytes);
+// 4-D TMA descriptor {features, tokens of a page, heads, pages} over the keys or values of a block cache; box = dh x box_tokens
+// bytes of one page and head, swizzled over rows of dh (64 or 128) bytes.
+hero_status make_tmap_pages(const hero_handle* h, CUtensorMap* out, const void* base, const hero_block_cache* c, uint32_t box_tokens);
 
 }  // namespace hero
