@@ -11,8 +11,9 @@ struct BlockAttnParams {
   const float* out_scale; int out_scale_stride;
   int nq, group;
   float c2;                      // scale * log2(e)
-  int cluster, outer;            // CTAs that share the tokens of a (sequence, head, row tile): of a cluster, clusters
-  float* part_o; float2* part_ml; // partial results [row][query head][cluster]: sum of P V [DH], (maximum, sum of P)
+  int B, tiles, direct;          // direct: CTA index = (sequence, row tile, head); else equal shares of all units
+  struct JoinRecord* records;    // [CTA]
+  float* part_o; float2* part_ml; // partial results [CTA][2]: sum of P V [rows][DH], (maximum, sum of P) [rows]
 };
 
 __device__ __forceinline__ void store_out(const BlockAttnParams& p, long long row, int col, float y) {
@@ -41,10 +42,15 @@ __device__ __forceinline__ void store_out(const BlockAttnParams& p, long long ro
 // scale enters P relative to the largest one the warp has met (P is formed with a factor 2^11, so pages whose scale is 2^-25 of
 // the largest still meet FP16's normal range).  The running maximum moves only when a score exceeds it by more than 4 in
 // the exponent (P <= 2^15), so that most steps need no reduction over tokens.
-// Tokens are split over the warps of a CTA, the CTAs of a cluster (joined through distributed shared memory) and, where that does
-// not fill the GPU, over clusters (partial results in the workspace, joined by a second kernel).
+// Work is dealt out in units of one step of one (sequence, row tile, key / value head).  The lengths are on the device, so each CTA of
+// one full GPU takes an equal, consecutive share of all units, whatever the lengths are: ragged batches, a long document
+// and many short ones end at the same time.  A group of units cut by a share's end leaves partial results in the workspace (at
+// most two per CTA), which a second kernel joins.  Short sequences take one CTA per group and no second kernel.
 constexpr int ROWS_WARPS = 4;
-constexpr int ROWS_MAX_CLUSTER = 8;
+constexpr int ROWS_CTAS = 3;                    // resident per SM
+constexpr int ROWS_GROUP_UNITS = 4;             // what a group costs beside its steps (queries in, partial results out), in steps
+constexpr int ROWS_MIN_UNITS = 12;              // units of a share, at least
+constexpr int ROWS_DIRECT_STEPS = 16;           // up to this many steps (512 tokens) a group is one CTA's
 constexpr float P_SHIFT = 11.0f, MAX_SLACK = 4.0f;
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -79,11 +85,6 @@ __device__ __forceinline__ void codes4_to_f16(uint32_t w, uint32_t& lo, uint32_t
     lo = *reinterpret_cast<const uint32_t*>(&x); hi = *reinterpret_cast<const uint32_t*>(&y);
   }
 }
-__device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
-  uint32_t v;
-  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
-  return __uint_as_float(v);
-}
 
 // one half (16 tokens) of a page: box {DH, 16, 1, 1} of the map over {features, tokens of a page, heads, pages}
 __device__ __forceinline__ void load_half(uint32_t dst, const CUtensorMap* m, int token, int head, int page, uint32_t bar) {
@@ -103,17 +104,47 @@ struct RowsSmem {
   static constexpr int WARP = ((RING > PARTIAL ? RING : PARTIAL) + 1023) / 1024 * 1024;
   static constexpr int OFF_SCALES = ROWS_WARPS * WARP;                      // float2 [warps][stages][2]: key and value scale of a half
   static constexpr int OFF_BARS = OFF_SCALES + ROWS_WARPS * STAGES * 16;    // uint64 [warps][stages]
-  static constexpr int OFF_ML = OFF_BARS + ROWS_WARPS * STAGES * 8;         // float [2][warps][8 NT], then the CTA's [2][8 NT]
-  static constexpr int BYTES = 1024 + OFF_ML + (ROWS_WARPS + 1) * 8 * NT * 8;
+  static constexpr int OFF_ML = OFF_BARS + ROWS_WARPS * STAGES * 8;         // float [2][warps][8 NT]
+  static constexpr int OFF_PLACE = OFF_ML + ROWS_WARPS * 8 * NT * 8;        // Place, long long [warps]
+  static constexpr int BYTES = 1024 + OFF_PLACE + 80 + ROWS_WARPS * 8;
 };
 // place of a feature in a partial O: rows of O^T in the order of the lanes that hold them
 template <int DH>
 __device__ __forceinline__ int feature_at(int place) { return (DH / 8) * ((place & 15) >> 1) + 2 * (place >> 4) + (place & 1); }
 
-struct SplitPlan { int cluster, outer; };       // CTAs per cluster, clusters per (sequence, head, row tile)
+// units of row tile qt of a sequence for one key / value head: its steps and a constant (so rows without a token are written too)
+template <int R>
+__device__ __forceinline__ int tile_units(const SeqRows& s, int group, int qt) {
+  const int total = s.n * group, last = (min((qt + 1) * R, total) - 1) / group;
+  return ((max(s.len - s.n + last + 1, 0) + 31) >> 5) + ROWS_GROUP_UNITS;
+}
+// A CTA's place in the work (in shared memory: nothing of it is held in registers through the loop over tokens).
+struct Place {
+  int b, qt, hk, len;            // the group; tokens of its sequence
+  int n, total, units;           // rows of its sequence, the same times the group size, the group's units
+  int ctas;                      // CTAs with a share
+  long long r0;                  // first row
+  long long first;               // units before the group
+  long long unit, end, all;      // next unit and end of this CTA's share, units of the call
+  template <int R>
+  __device__ __forceinline__ void enter(const SeqRows& s, int group) {
+    len = s.len; n = s.n; r0 = s.r0; total = s.n * group;
+    units = tile_units<R>(s, group, qt);
+  }
+};
+struct JoinRecord { int b, qt, hk, parts; };     // a group that starts in this CTA's share and ends in a later one's; parts 0: none
+
+template <int R>
+__device__ __forceinline__ long long seq_units(const BlockView& c, int group, int b) {
+  const SeqRows s = seq_rows(c, b);
+  const int tiles = (s.n * group + R - 1) / R;
+  long long u = 0;
+  for (int qt = 0; qt < tiles; ++qt) u += tile_units<R>(s, group, qt);
+  return u * c.nkv;
+}
 
 template <int DH, int NT, bool BF, bool F8>
-__global__ void __launch_bounds__(ROWS_WARPS * 32, 3) block_attn_rows_kernel(const __grid_constant__ CUtensorMap tm_k,
+__global__ void __launch_bounds__(ROWS_WARPS * 32, ROWS_CTAS) block_attn_rows_kernel(const __grid_constant__ CUtensorMap tm_k,
                                                                              const __grid_constant__ CUtensorMap tm_v,
                                                                              const __grid_constant__ BlockAttnParams p) {
   using Smem = RowsSmem<DH, NT>;
@@ -126,8 +157,6 @@ __global__ void __launch_bounds__(ROWS_WARPS * 32, 3) block_attn_rows_kernel(con
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   float* sm = reinterpret_cast<float*>(smem + Smem::OFF_ML);               // [warps][R] maxima
   float* sl = sm + ROWS_WARPS * R;                                         // [warps][R] sums
-  float* cm = sl + ROWS_WARPS * R;                                         // [R] the CTA's
-  float* cl = cm + R;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   uint64_t* full_bar = reinterpret_cast<uint64_t*>(smem + Smem::OFF_BARS) + warp * STAGES;
   float2* scales = reinterpret_cast<float2*>(smem + Smem::OFF_SCALES) + warp * STAGES * 2;
@@ -140,404 +169,468 @@ __global__ void __launch_bounds__(ROWS_WARPS * 32, 3) block_attn_rows_kernel(con
   ptx::pdl_launch_dependents();
   ptx::pdl_wait();
   const BlockView& c = p.c;
-  const int b = blockIdx.z, hk = blockIdx.y % c.nkv, qt = blockIdx.y / c.nkv;
-  const int splits = gridDim.x, cs = p.cluster;
-  const SeqRows s = seq_rows(c, b);
-  const int total = s.n * p.group, rb = qt * R;
-  if (rb >= total) return;                       // uniform over the cluster
-  const int last = (min(rb + R, total) - 1) / p.group, base = s.len - s.n;
-  const int L = max(base + last + 1, 0);         // keys of the tile's last row
-  const int open = base + rb / p.group + 1;      // keys of its first row: steps below need no mask
-  const int per = ((L + splits - 1) / splits + 31) & ~31;
-  const int k0 = min((int)blockIdx.x * per, L), k1 = min(k0 + per, L);
-  const int steps = (k1 - k0 + 31) >> 5, mine = steps > warp ? (steps - warp + ROWS_WARPS - 1) / ROWS_WARPS : 0;
 
-  // lane i looks after half i % 2 of the warp's step i / 2 of every batch of 16: page id, scales, requests
-  int my_token = 0, my_id = -1;
-  float2 my_scales;
-  auto load_pages = [&](int n0) {                // steps n0 .. n0 + 15 of the warp
-    const int tok = k0 + 32 * (warp + ROWS_WARPS * (n0 + (lane >> 1))) + 16 * (lane & 1);
-    my_id = -1;
-    my_token = tok & (c.page - 1);
-    my_scales = make_float2(0.f, 0.f);
-    if (tok < k1) {
-      my_id = page_for_read(c, b, tok >> c.page_shift);
-      const long long at = (long long)my_id * c.nkv + hk;
-      my_scales = make_float2(__ldg(c.ks + at), __ldg(c.vs + at));
+  // ---- this CTA's share of the units and the group it begins in
+  Place& at = *reinterpret_cast<Place*>(smem + Smem::OFF_PLACE);
+  static_assert(sizeof(Place) <= 80, "");
+  if (p.direct) {
+    const int b = blockIdx.x / c.nkv / p.tiles, qt = blockIdx.x / c.nkv % p.tiles;
+    const SeqRows s = seq_rows(c, b);
+    if (qt * R >= s.n * p.group) return;
+    if (threadIdx.x == 0) {
+      at.b = b; at.qt = qt; at.hk = blockIdx.x % c.nkv;
+      at.enter<R>(s, p.group);
+      at.first = at.unit = 0;
+      at.end = at.units;
     }
-  };
-  const uint32_t ring_a = ptx::smem_u32(smem + warp * Smem::WARP);
-  auto request = [&](int n, int stage) {         // step n of the warp into a stage
-    if (n >= mine) return;
-    if (n && (n & 15) == 0) load_pages(n);
-    if ((lane >> 1) == (n & 15)) {
-      const int h = lane & 1;
-      scales[2 * stage + h] = my_scales;         // (before the arrival that releases it)
-      if (my_id >= 0) {
-        const uint32_t bar = ptx::smem_u32(&full_bar[stage]), dst = ring_a + stage * Smem::STAGE + h * Smem::HALF;
-        ptx::mbar_expect_tx(&full_bar[stage], 2 * Smem::HALF);
-        load_half(dst, &tm_k, my_token, hk, my_id, bar);
-        load_half(dst + 2 * Smem::HALF, &tm_v, my_token, hk, my_id, bar);
-      } else {
-        ptx::mbar_arrive(&full_bar[stage]);
-      }
-    }
-  };
-  load_pages(0);
-#pragma unroll
-  for (int i = 0; i < STAGES; ++i) request(i, i);
-
-  // query fragments: lane (g, t) holds features 64 c + 16 t .. + 15 of row g of each N tile, scaled by a power of two
-  uint32_t qf[NT][KC * 8];
-  float f[NT][2], u[NT][2], l[NT][2], acc[NT][MT][4];
-  int lim[NT][2];                                // per lane: rows 2 t and 2 t + 1 of each N tile (the columns of S^T and O^T it holds)
-#pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    const int rr = min(rb + 8 * n + g, total - 1);
-    const uint16_t* q = p.q + (s.r0 + rr / p.group) * p.ld_q + ((long long)hk * p.group + rr % p.group) * DH + 16 * t;
-    uint32_t raw[KC * 8], top = 0;
-#pragma unroll
-    for (int k = 0; k < KC; ++k) {
-      const uint4 x = __ldg(reinterpret_cast<const uint4*>(q + 64 * k)), y = __ldg(reinterpret_cast<const uint4*>(q + 64 * k + 8));
-      raw[8 * k] = x.x; raw[8 * k + 1] = x.y; raw[8 * k + 2] = x.z; raw[8 * k + 3] = x.w;
-      raw[8 * k + 4] = y.x; raw[8 * k + 5] = y.y; raw[8 * k + 6] = y.z; raw[8 * k + 7] = y.w;
-    }
-#pragma unroll
-    for (int i = 0; i < KC * 8; ++i) top = __vmaxu2(top, raw[i] & 0x7fff7fffu);
-    top = max(top & 0xffffu, top >> 16);
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    const float amax = fp16ish_to_f32x2<BF>(top).x;
-    // 2^(14 - exponent of the maximum); zero, infinite and NaN rows are left as they are
-    const int e = (int)(__float_as_uint(amax) >> 23);
-    const float up = e == 0 || e == 255 ? 1.0f : __uint_as_float((uint32_t)min(127 + 14 + 127 - e, 253) << 23);
-    const float down = p.c2 / up;                // a power of two within the normal range: exact
-#pragma unroll
-    for (int i = 0; i < KC * 8; ++i) {
-      const float2 x = fp16ish_to_f32x2<BF>(raw[i]);
-      qf[n][i] = pack_f16(x.x * up, x.y * up);
-    }
-#pragma unroll
-    for (int r = 0; r < 2; ++r) {
-      f[n][r] = __shfl_sync(0xffffffffu, down, 4 * (2 * t + r));
-      lim[n][r] = base + min(rb + 8 * n + 2 * t + r, total - 1) / p.group + 1;
-      u[n][r] = 0.f; l[n][r] = 0.f;              // u = P_SHIFT - running maximum
-    }
-#pragma unroll
-    for (int j = 0; j < MT; ++j)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) acc[n][j][i] = 0.f;
-  }
-  float vref = 0.f, inv_vref = 0.f;
-  // byte offsets of the lane's pieces within a half, under the swizzle (128-byte rows: 16-byte piece ^ row % 8; 64-byte rows:
-  // piece ^ row / 2 % 4); rows g + 8 and 2 t + 8 lie 8 rows further with the same pattern
-  uint32_t k_off[KC], v_off[2];
-  if constexpr (DH == 128) {
-#pragma unroll
-    for (int q = 0; q < KC; ++q) k_off[q] = g * 128 + (((4 * q + t) ^ g) << 4);
-#pragma unroll
-    for (int r = 0; r < 2; ++r) v_off[r] = (2 * t + r) * 128 + ((g ^ (2 * t + r)) << 4);
   } else {
-    k_off[0] = g * 64 + ((t ^ ((g >> 1) & 3)) << 4);
+    long long* sums = reinterpret_cast<long long*>(smem + Smem::OFF_PLACE + 80);
+    const int chunk = (p.B + ROWS_WARPS * 32 - 1) / (ROWS_WARPS * 32), b0 = min((int)threadIdx.x * chunk, p.B), b1 = min(b0 + chunk, p.B);
+    long long own = 0, all = 0;
+    for (int b = b0; b < b1; ++b) own += seq_units<R>(c, p.group, b);
+    long long incl = own;
 #pragma unroll
-    for (int r = 0; r < 2; ++r) v_off[r] = (2 * t + r) * 64 + (((g >> 1) ^ t) << 4) + (g & 1) * 8;
-  }
-
-  bool ok = true;
-  int stage = 0;
-  uint32_t phase = 0;
-  for (int n = 0; n < mine; ++n) {
-    const int tb = k0 + 32 * (warp + ROWS_WARPS * n);
-    ok = ok && ptx::mbar_wait(&full_bar[stage], phase, c.err, 0x7000 | stage);
-    if (!__all_sync(0xffffffffu, ok)) {          // a copy never arrived (reported): wait, bounded, for the others before the ring is reused
-      for (int i = 1; i < STAGES && n + i < mine; ++i) {
-        if (++stage == STAGES) { stage = 0; phase ^= 1; }
-        ptx::mbar_wait(&full_bar[stage], phase, c.err, 0x7100 | stage);
-      }
-      break;
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long x = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += x;
     }
-    const uint8_t* tile = smem + warp * Smem::WARP + stage * Smem::STAGE;
-    const float4 sv = *reinterpret_cast<const float4*>(&scales[2 * stage]);   // key and value scale of either half
-    // ---- scores, one chain of products per half and 64 features
-    float sc[2][NT][4];
+    if (lane == 31) sums[warp] = incl;
+    __syncthreads();
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      float part[KC][NT][4];
-#pragma unroll
-      for (int q = 0; q < KC; ++q) {
-        const uint4 x = *reinterpret_cast<const uint4*>(tile + h * Smem::HALF + k_off[q]);
-        const uint4 y = *reinterpret_cast<const uint4*>(tile + h * Smem::HALF + k_off[q] + 8 * DH);
-        const uint32_t w0[4] = {x.x, x.y, x.z, x.w}, w1[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-        for (int r = 0; r < NT; ++r) part[q][r][0] = part[q][r][1] = part[q][r][2] = part[q][r][3] = 0.f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          uint32_t a0, a1, a2, a3;
-          codes4_to_f16<F8>(w0[i], a0, a2);
-          codes4_to_f16<F8>(w1[i], a1, a3);
-#pragma unroll
-          for (int r = 0; r < NT; ++r) mma_f16(part[q][r], a0, a1, a2, a3, qf[r][8 * q + 2 * i], qf[r][8 * q + 2 * i + 1]);
-        }
-      }
-#pragma unroll
-      for (int r = 0; r < NT; ++r)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) sc[h][r][i] = KC == 2 ? part[0][r][i] + part[KC - 1][r][i] : part[0][r][i];
+    for (int w = 0; w < ROWS_WARPS; ++w) { if (w < warp) incl += sums[w]; all += sums[w]; }
+    // (the lengths may be far below the host's bound: no share is empty and none is much below ROWS_MIN_UNITS)
+    const long long ctas = min((long long)gridDim.x, max(all / ROWS_MIN_UNITS, 1ll));
+    const long long unit = all * blockIdx.x / ctas, end = all * (blockIdx.x + 1) / ctas;
+    if (blockIdx.x >= ctas || all == 0) {
+      if (threadIdx.x == 0) p.records[blockIdx.x].parts = 0;
+      return;
     }
-    // ---- probabilities
-    if (fmaxf(sv.y, sv.w) > vref) {              // uniform over the warp
-      const float now = fmaxf(sv.y, sv.w), up = vref / now;
-#pragma unroll
-      for (int r = 0; r < NT; ++r)
-#pragma unroll
-        for (int k = 0; k < MT; ++k)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) acc[r][k][i] *= up;
-      vref = now;
-      inv_vref = 1.0f / now;
-    }
-    const float rv[2] = {sv.y * inv_vref, sv.w * inv_vref};
-    uint32_t pb[2][NT][2];
-#pragma unroll
-    for (int r = 0; r < NT; ++r) {
-      float x[2][4];                             // score - maximum + P_SHIFT, base 2
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const float f0 = f[r][0] * (h ? sv.z : sv.x), f1 = f[r][1] * (h ? sv.z : sv.x);
-        x[h][0] = fmaf(sc[h][r][0], f0, u[r][0]); x[h][1] = fmaf(sc[h][r][1], f1, u[r][1]);
-        x[h][2] = fmaf(sc[h][r][2], f0, u[r][0]); x[h][3] = fmaf(sc[h][r][3], f1, u[r][1]);
+    if (incl - own <= unit && unit < incl) {     // one thread: the sequence, then the row tile and head
+      long long first = incl - own;
+      int b = b0;
+      for (;; ++b) {
+        const long long n = seq_units<R>(c, p.group, b);
+        if (unit < first + n) break;
+        first += n;
       }
-      if (tb + 32 > open) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (tb + 16 * h + g + 8 * (i >> 1) >= lim[r][i & 1]) x[h][i] = -INFINITY;
+      const SeqRows s = seq_rows(c, b);
+      at.b = b; at.unit = unit; at.end = end; at.all = all; at.ctas = (int)ctas;
+      for (at.qt = 0;; ++at.qt) {
+        at.enter<R>(s, p.group);
+        if (unit < first + (long long)at.units * c.nkv) break;
+        first += (long long)at.units * c.nkv;
       }
-      float mx0 = fmaxf(fmaxf(x[0][0], x[0][2]), fmaxf(x[1][0], x[1][2])), mx1 = fmaxf(fmaxf(x[0][1], x[0][3]), fmaxf(x[1][1], x[1][3]));
-      if (n == 0 || __any_sync(0xffffffffu, fmaxf(mx0, mx1) > P_SHIFT + MAX_SLACK)) {
-#pragma unroll
-        for (int o = 4; o < 32; o <<= 1) {
-          mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, o));
-          mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, o));
-        }
-        // the maximum moves by mx - P_SHIFT: up, except in the first step (and not at all where every token is masked)
-        float d0 = mx0 - P_SHIFT, d1 = mx1 - P_SHIFT;
-        if (n != 0) { d0 = fmaxf(d0, 0.f); d1 = fmaxf(d1, 0.f); }
-        if (mx0 == -INFINITY) d0 = 0.f;
-        if (mx1 == -INFINITY) d1 = 0.f;
-        u[r][0] -= d0; u[r][1] -= d1;
-        if (n != 0) {
-          const float a0 = ex2(-d0), a1 = ex2(-d1);
-          l[r][0] *= a0; l[r][1] *= a1;
-#pragma unroll
-          for (int k = 0; k < MT; ++k) { acc[r][k][0] *= a0; acc[r][k][2] *= a0; acc[r][k][1] *= a1; acc[r][k][3] *= a1; }
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h) { x[h][0] -= d0; x[h][2] -= d0; x[h][1] -= d1; x[h][3] -= d1; }
-      }
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[h][i] = ex2(x[h][i]);
-        l[r][0] += x[h][0] + x[h][2]; l[r][1] += x[h][1] + x[h][3];
-        pb[h][r][0] = transpose8x8(pack_f16(x[h][0] * rv[h], x[h][1] * rv[h]));
-        pb[h][r][1] = transpose8x8(pack_f16(x[h][2] * rv[h], x[h][3] * rv[h]));
-      }
-    }
-    // ---- values; e4m3 slots behind the end may hold NaN, which a zero probability does not silence
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      uint32_t vr[4][VW];
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const uint8_t* at = tile + (2 + h) * Smem::HALF + v_off[r & 1] + (r >> 1) * 8 * DH;
-        if constexpr (VW == 4) {
-          const uint4 x = *reinterpret_cast<const uint4*>(at);
-          vr[r][0] = x.x; vr[r][1] = x.y; vr[r][2] = x.z; vr[r][3] = x.w;
-        } else {
-          const uint2 x = *reinterpret_cast<const uint2*>(at);
-          vr[r][0] = x.x; vr[r][1] = x.y;
-        }
-        if (F8 && tb + 32 > k1 && tb + 16 * h + 2 * t + (r & 1) + 8 * (r >> 1) >= k1) {
-#pragma unroll
-          for (int w = 0; w < VW; ++w) vr[r][w] = 0;
-        }
-      }
-#pragma unroll
-      for (int w = 0; w < VW; ++w) {
-        uint32_t ab[4], cd[4];                   // feature i of the word: tokens (2t, 2t + 1) and (2t + 8, 2t + 9)
-        codes4_to_f16<F8>(__byte_perm(vr[0][w], vr[1][w], 0x5140), ab[0], ab[1]);
-        codes4_to_f16<F8>(__byte_perm(vr[0][w], vr[1][w], 0x7362), ab[2], ab[3]);
-        codes4_to_f16<F8>(__byte_perm(vr[2][w], vr[3][w], 0x5140), cd[0], cd[1]);
-        codes4_to_f16<F8>(__byte_perm(vr[2][w], vr[3][w], 0x7362), cd[2], cd[3]);
-#pragma unroll
-        for (int r = 0; r < NT; ++r) {
-          mma_f16(acc[r][2 * w], ab[0], ab[1], cd[0], cd[1], pb[h][r][0], pb[h][r][1]);
-          mma_f16(acc[r][2 * w + 1], ab[2], ab[3], cd[2], cd[3], pb[h][r][0], pb[h][r][1]);
-        }
-      }
-    }
-    __syncwarp();                                // every lane has read the stage
-    request(n + STAGES, stage);
-    if (++stage == STAGES) { stage = 0; phase ^= 1; }
-  }
-
-  // ---- join the warps of the CTA; a warp's partial O takes the place of its ring (every copy it asked for has been waited for)
-  float* my_o = reinterpret_cast<float*>(smem + warp * Smem::WARP);
-  __syncwarp();
-#pragma unroll
-  for (int n = 0; n < NT; ++n) {
-#pragma unroll
-    for (int r = 0; r < 2; ++r) {
-#pragma unroll
-      for (int o = 4; o < 32; o <<= 1) l[n][r] += __shfl_xor_sync(0xffffffffu, l[n][r], o);
-      const int row = 8 * n + 2 * t + r;
-      if (g == 0) { sm[warp * R + row] = l[n][r] != 0.f ? P_SHIFT - u[n][r] : -INFINITY; sl[warp * R + row] = l[n][r]; }
-#pragma unroll
-      for (int k = 0; k < MT; ++k)
-        *reinterpret_cast<float2*>(my_o + row * Smem::OROW + 16 * k + 2 * g) = make_float2(acc[n][k][r] * vref, acc[n][k][2 + r] * vref);
+      at.hk = (int)((unit - first) / at.units);
+      at.first = first + (long long)at.hk * at.units;
     }
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < R * DH; i += ROWS_WARPS * 32) {
-    const int row = i / DH, at = row * Smem::OROW + i % DH;
-    float mt = sm[row];
-#pragma unroll
-    for (int w = 1; w < ROWS_WARPS; ++w) mt = fmaxf(mt, sm[w * R + row]);
-    float y = 0.f, lt = 0.f;
-#pragma unroll
-    for (int w = 0; w < ROWS_WARPS; ++w) {
-      const float mw = sm[w * R + row], e = mw > -INFINITY ? ex2(mw - mt) : 0.f;
-      y = fmaf(e, reinterpret_cast<const float*>(smem + w * Smem::WARP)[at], y); lt = fmaf(e, sl[w * R + row], lt);
-    }
-    reinterpret_cast<float*>(smem)[at] = y;
-    if (i % DH == 0) { cm[row] = mt; cl[row] = lt; }
-  }
-  // ---- join the CTAs of the cluster: each finishes its share of the tile
-  if (cs > 1) ptx::cluster_sync(); else __syncthreads();
-  const int rank = cs > 1 ? (int)ptx::cluster_ctarank() : 0, share = R * DH / cs;
-  const uint32_t am = ptx::smem_u32(cm), al = ptx::smem_u32(cl), ao = ptx::smem_u32(smem);
-  for (int i = rank * share + threadIdx.x; i < (rank + 1) * share; i += ROWS_WARPS * 32) {
-    const int row = i / DH, place = i % DH, rr = rb + row;
-    if (rr >= total) continue;
-    float mt = cm[row], lt = cl[row], y = reinterpret_cast<const float*>(smem)[row * Smem::OROW + place];
-    if (cs > 1) {
-      float mq[ROWS_MAX_CLUSTER];
-      mt = -INFINITY;
-#pragma unroll
-      for (int q = 0; q < ROWS_MAX_CLUSTER; ++q) {
-        mq[q] = q < cs ? ld_cluster_f32(ptx::mapa(am + 4 * row, q)) : -INFINITY;
-        mt = fmaxf(mt, mq[q]);
+
+  int stage = 0;                                 // ring position and parity go on from group to group
+  uint32_t phase = 0;
+  bool ok = true;
+  for (;;) {
+    const int b = at.b, hk = at.hk, total = at.total, rb = at.qt * R;
+    const int last = (min(rb + R, total) - 1) / p.group, base = at.len - at.n;
+    const int L = max(base + last + 1, 0);       // keys of the tile's last row
+    const int open = base + rb / p.group + 1;    // keys of its first row: steps below need no mask
+    const int k0 = (int)min((long long)L, 32 * (at.unit - at.first)), k1 = (int)min((long long)L, 32 * (at.end - at.first));
+    const int steps = (k1 - k0 + 31) >> 5, mine = steps > warp ? (steps - warp + ROWS_WARPS - 1) / ROWS_WARPS : 0;
+
+    // lane i looks after half i % 2 of the warp's step i / 2 of every batch of 16: page id, scales, requests
+    int my_token = 0, my_id = -1;
+    float2 my_scales;
+    auto load_pages = [&](int n0) {                // steps n0 .. n0 + 15 of the warp
+      const int tok = k0 + 32 * (warp + ROWS_WARPS * (n0 + (lane >> 1))) + 16 * (lane & 1);
+      my_id = -1;
+      my_token = tok & (c.page - 1);
+      my_scales = make_float2(0.f, 0.f);
+      if (tok < k1) {
+        my_id = page_for_read(c, b, tok >> c.page_shift);
+        const long long sc = (long long)my_id * c.nkv + hk;
+        my_scales = make_float2(__ldg(c.ks + sc), __ldg(c.vs + sc));
       }
-      lt = 0.f; y = 0.f;
-#pragma unroll
-      for (int q = 0; q < ROWS_MAX_CLUSTER; ++q)
-        if (q < cs) {
-          const float e = mq[q] > -INFINITY ? ex2(mq[q] - mt) : 0.f;
-          lt = fmaf(e, ld_cluster_f32(ptx::mapa(al + 4 * row, q)), lt);
-          y = fmaf(e, ld_cluster_f32(ptx::mapa(ao + 4 * (row * Smem::OROW + place), q)), y);
+    };
+    const uint32_t ring_a = ptx::smem_u32(smem + warp * Smem::WARP);
+    auto request = [&](int n, int stage) {         // step n of the warp into a stage
+      if (n >= mine) return;
+      if (n && (n & 15) == 0) load_pages(n);
+      if ((lane >> 1) == (n & 15)) {
+        const int h = lane & 1;
+        scales[2 * stage + h] = my_scales;         // (before the arrival that releases it)
+        if (my_id >= 0) {
+          const uint32_t bar = ptx::smem_u32(&full_bar[stage]), dst = ring_a + stage * Smem::STAGE + h * Smem::HALF;
+          ptx::mbar_expect_tx(&full_bar[stage], 2 * Smem::HALF);
+          load_half(dst, &tm_k, my_token, hk, my_id, bar);
+          load_half(dst + 2 * Smem::HALF, &tm_v, my_token, hk, my_id, bar);
+        } else {
+          ptx::mbar_arrive(&full_bar[stage]);
         }
+      }
+    };
+    load_pages(0);
+#pragma unroll
+    for (int i = 0; i < STAGES; ++i) request(i, (stage + i) % STAGES);
+
+    // query fragments: lane (g, t) holds features 64 c + 16 t .. + 15 of row g of each N tile, scaled by a power of two
+    uint32_t qf[NT][KC * 8];
+    float f[NT][2], u[NT][2], l[NT][2], acc[NT][MT][4];
+    int lim[NT][2];                                // per lane: rows 2 t and 2 t + 1 of each N tile (the columns of S^T and O^T it holds)
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const int rr = min(rb + 8 * n + g, total - 1);
+      const uint16_t* q = p.q + (at.r0 + rr / p.group) * p.ld_q + ((long long)hk * p.group + rr % p.group) * DH + 16 * t;
+      uint32_t raw[KC * 8], top = 0;
+#pragma unroll
+      for (int k = 0; k < KC; ++k) {
+        const uint4 x = __ldg(reinterpret_cast<const uint4*>(q + 64 * k)), y = __ldg(reinterpret_cast<const uint4*>(q + 64 * k + 8));
+        raw[8 * k] = x.x; raw[8 * k + 1] = x.y; raw[8 * k + 2] = x.z; raw[8 * k + 3] = x.w;
+        raw[8 * k + 4] = y.x; raw[8 * k + 5] = y.y; raw[8 * k + 6] = y.z; raw[8 * k + 7] = y.w;
+      }
+#pragma unroll
+      for (int i = 0; i < KC * 8; ++i) top = __vmaxu2(top, raw[i] & 0x7fff7fffu);
+      top = max(top & 0xffffu, top >> 16);
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      const float amax = fp16ish_to_f32x2<BF>(top).x;
+      // 2^(14 - exponent of the maximum); zero, infinite and NaN rows are left as they are
+      const int e = (int)(__float_as_uint(amax) >> 23);
+      const float up = e == 0 || e == 255 ? 1.0f : __uint_as_float((uint32_t)min(127 + 14 + 127 - e, 253) << 23);
+      const float down = p.c2 / up;                // a power of two within the normal range: exact
+#pragma unroll
+      for (int i = 0; i < KC * 8; ++i) {
+        const float2 x = fp16ish_to_f32x2<BF>(raw[i]);
+        qf[n][i] = pack_f16(x.x * up, x.y * up);
+      }
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        f[n][r] = __shfl_sync(0xffffffffu, down, 4 * (2 * t + r));
+        lim[n][r] = base + min(rb + 8 * n + 2 * t + r, total - 1) / p.group + 1;
+        u[n][r] = 0.f; l[n][r] = 0.f;              // u = P_SHIFT - running maximum
+      }
+#pragma unroll
+      for (int j = 0; j < MT; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[n][j][i] = 0.f;
     }
-    const long long row_g = s.r0 + rr / p.group;
-    const int hq = hk * p.group + rr % p.group;
-    if (p.outer == 1) {
-      store_out(p, row_g, hq * DH + feature_at<DH>(place), lt != 0.f ? y / lt : 0.f);
+    float vref = 0.f, inv_vref = 0.f;
+    // byte offsets of the lane's pieces within a half, under the swizzle (128-byte rows: 16-byte piece ^ row % 8; 64-byte rows:
+    // piece ^ row / 2 % 4); rows g + 8 and 2 t + 8 lie 8 rows further with the same pattern
+    uint32_t k_off[KC], v_off[2];
+    if constexpr (DH == 128) {
+#pragma unroll
+      for (int q = 0; q < KC; ++q) k_off[q] = g * 128 + (((4 * q + t) ^ g) << 4);
+#pragma unroll
+      for (int r = 0; r < 2; ++r) v_off[r] = (2 * t + r) * 128 + ((g ^ (2 * t + r)) << 4);
     } else {
-      const long long at = (row_g * p.nq + hq) * p.outer + blockIdx.x / cs;
-      p.part_o[at * DH + place] = y;
-      if (place == 0) p.part_ml[at] = make_float2(mt, lt);
+      k_off[0] = g * 64 + ((t ^ ((g >> 1) & 3)) << 4);
+#pragma unroll
+      for (int r = 0; r < 2; ++r) v_off[r] = (2 * t + r) * 64 + (((g >> 1) ^ t) << 4) + (g & 1) * 8;
     }
+
+    for (int n = 0; n < mine; ++n) {
+      const int tb = k0 + 32 * (warp + ROWS_WARPS * n);
+      ok = ok && ptx::mbar_wait(&full_bar[stage], phase, c.err, 0x7000 | stage);
+      if (!__all_sync(0xffffffffu, ok)) {          // a copy never arrived (reported): wait, bounded, for the others before the ring is reused
+        for (int i = 1; i < STAGES && n + i < mine; ++i) {
+          if (++stage == STAGES) { stage = 0; phase ^= 1; }
+          ptx::mbar_wait(&full_bar[stage], phase, c.err, 0x7100 | stage);
+        }
+        break;
+      }
+      const uint8_t* tile = smem + warp * Smem::WARP + stage * Smem::STAGE;
+      const float4 sv = *reinterpret_cast<const float4*>(&scales[2 * stage]);   // key and value scale of either half
+      // ---- scores, one chain of products per half and 64 features
+      float sc[2][NT][4];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float part[KC][NT][4];
+#pragma unroll
+        for (int q = 0; q < KC; ++q) {
+          const uint4 x = *reinterpret_cast<const uint4*>(tile + h * Smem::HALF + k_off[q]);
+          const uint4 y = *reinterpret_cast<const uint4*>(tile + h * Smem::HALF + k_off[q] + 8 * DH);
+          const uint32_t w0[4] = {x.x, x.y, x.z, x.w}, w1[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+          for (int r = 0; r < NT; ++r) part[q][r][0] = part[q][r][1] = part[q][r][2] = part[q][r][3] = 0.f;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            uint32_t a0, a1, a2, a3;
+            codes4_to_f16<F8>(w0[i], a0, a2);
+            codes4_to_f16<F8>(w1[i], a1, a3);
+#pragma unroll
+            for (int r = 0; r < NT; ++r) mma_f16(part[q][r], a0, a1, a2, a3, qf[r][8 * q + 2 * i], qf[r][8 * q + 2 * i + 1]);
+          }
+        }
+#pragma unroll
+        for (int r = 0; r < NT; ++r)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sc[h][r][i] = KC == 2 ? part[0][r][i] + part[KC - 1][r][i] : part[0][r][i];
+      }
+      // ---- probabilities
+      if (fmaxf(sv.y, sv.w) > vref) {              // uniform over the warp
+        const float now = fmaxf(sv.y, sv.w), up = vref / now;
+#pragma unroll
+        for (int r = 0; r < NT; ++r)
+#pragma unroll
+          for (int k = 0; k < MT; ++k)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[r][k][i] *= up;
+        vref = now;
+        inv_vref = 1.0f / now;
+      }
+      const float rv[2] = {sv.y * inv_vref, sv.w * inv_vref};
+      uint32_t pb[2][NT][2];
+#pragma unroll
+      for (int r = 0; r < NT; ++r) {
+        float x[2][4];                             // score - maximum + P_SHIFT, base 2
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float f0 = f[r][0] * (h ? sv.z : sv.x), f1 = f[r][1] * (h ? sv.z : sv.x);
+          x[h][0] = fmaf(sc[h][r][0], f0, u[r][0]); x[h][1] = fmaf(sc[h][r][1], f1, u[r][1]);
+          x[h][2] = fmaf(sc[h][r][2], f0, u[r][0]); x[h][3] = fmaf(sc[h][r][3], f1, u[r][1]);
+        }
+        if (tb + 32 > open) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (tb + 16 * h + g + 8 * (i >> 1) >= lim[r][i & 1]) x[h][i] = -INFINITY;
+        }
+        float mx0 = fmaxf(fmaxf(x[0][0], x[0][2]), fmaxf(x[1][0], x[1][2])), mx1 = fmaxf(fmaxf(x[0][1], x[0][3]), fmaxf(x[1][1], x[1][3]));
+        if (n == 0 || __any_sync(0xffffffffu, fmaxf(mx0, mx1) > P_SHIFT + MAX_SLACK)) {
+#pragma unroll
+          for (int o = 4; o < 32; o <<= 1) {
+            mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, o));
+            mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, o));
+          }
+          // the maximum moves by mx - P_SHIFT: up, except in the first step (and not at all where every token is masked)
+          float d0 = mx0 - P_SHIFT, d1 = mx1 - P_SHIFT;
+          if (n != 0) { d0 = fmaxf(d0, 0.f); d1 = fmaxf(d1, 0.f); }
+          if (mx0 == -INFINITY) d0 = 0.f;
+          if (mx1 == -INFINITY) d1 = 0.f;
+          u[r][0] -= d0; u[r][1] -= d1;
+          if (n != 0) {
+            const float a0 = ex2(-d0), a1 = ex2(-d1);
+            l[r][0] *= a0; l[r][1] *= a1;
+#pragma unroll
+            for (int k = 0; k < MT; ++k) { acc[r][k][0] *= a0; acc[r][k][2] *= a0; acc[r][k][1] *= a1; acc[r][k][3] *= a1; }
+          }
+#pragma unroll
+          for (int h = 0; h < 2; ++h) { x[h][0] -= d0; x[h][2] -= d0; x[h][1] -= d1; x[h][3] -= d1; }
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[h][i] = ex2(x[h][i]);
+          l[r][0] += x[h][0] + x[h][2]; l[r][1] += x[h][1] + x[h][3];
+          pb[h][r][0] = transpose8x8(pack_f16(x[h][0] * rv[h], x[h][1] * rv[h]));
+          pb[h][r][1] = transpose8x8(pack_f16(x[h][2] * rv[h], x[h][3] * rv[h]));
+        }
+      }
+      // ---- values; e4m3 slots behind the end may hold NaN, which a zero probability does not silence
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        uint32_t vr[4][VW];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const uint8_t* at = tile + (2 + h) * Smem::HALF + v_off[r & 1] + (r >> 1) * 8 * DH;
+          if constexpr (VW == 4) {
+            const uint4 x = *reinterpret_cast<const uint4*>(at);
+            vr[r][0] = x.x; vr[r][1] = x.y; vr[r][2] = x.z; vr[r][3] = x.w;
+          } else {
+            const uint2 x = *reinterpret_cast<const uint2*>(at);
+            vr[r][0] = x.x; vr[r][1] = x.y;
+          }
+          if (F8 && tb + 32 > k1 && tb + 16 * h + 2 * t + (r & 1) + 8 * (r >> 1) >= k1) {
+#pragma unroll
+            for (int w = 0; w < VW; ++w) vr[r][w] = 0;
+          }
+        }
+#pragma unroll
+        for (int w = 0; w < VW; ++w) {
+          uint32_t ab[4], cd[4];                   // feature i of the word: tokens (2t, 2t + 1) and (2t + 8, 2t + 9)
+          codes4_to_f16<F8>(__byte_perm(vr[0][w], vr[1][w], 0x5140), ab[0], ab[1]);
+          codes4_to_f16<F8>(__byte_perm(vr[0][w], vr[1][w], 0x7362), ab[2], ab[3]);
+          codes4_to_f16<F8>(__byte_perm(vr[2][w], vr[3][w], 0x5140), cd[0], cd[1]);
+          codes4_to_f16<F8>(__byte_perm(vr[2][w], vr[3][w], 0x7362), cd[2], cd[3]);
+#pragma unroll
+          for (int r = 0; r < NT; ++r) {
+            mma_f16(acc[r][2 * w], ab[0], ab[1], cd[0], cd[1], pb[h][r][0], pb[h][r][1]);
+            mma_f16(acc[r][2 * w + 1], ab[2], ab[3], cd[2], cd[3], pb[h][r][0], pb[h][r][1]);
+          }
+        }
+      }
+      __syncwarp();                                // every lane has read the stage
+      request(n + STAGES, stage);
+      if (++stage == STAGES) { stage = 0; phase ^= 1; }
+    }
+
+    // ---- join the warps of the CTA; a warp's partial O takes the place of its ring (every copy it asked for has been waited for)
+    float* my_o = reinterpret_cast<float*>(smem + warp * Smem::WARP);
+    __syncwarp();
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) l[n][r] += __shfl_xor_sync(0xffffffffu, l[n][r], o);
+        const int row = 8 * n + 2 * t + r;
+        if (g == 0) { sm[warp * R + row] = l[n][r] != 0.f ? P_SHIFT - u[n][r] : -INFINITY; sl[warp * R + row] = l[n][r]; }
+#pragma unroll
+        for (int k = 0; k < MT; ++k)
+          *reinterpret_cast<float2*>(my_o + row * Smem::OROW + 16 * k + 2 * g) = make_float2(acc[n][k][r] * vref, acc[n][k][2 + r] * vref);
+      }
+    }
+    __syncthreads();
+    const long long group_end = at.first + at.units;
+    const bool head = at.unit == at.first, tail = group_end <= at.end, whole = head && tail;   // the group begins / ends in this share
+    const long long slot = 2ll * blockIdx.x + (head ? 1 : 0);            // of a partial result: the group goes on / came in
+    for (int i = threadIdx.x; i < R * DH; i += ROWS_WARPS * 32) {
+      const int row = i / DH, place = i % DH, rr = at.qt * R + row;
+      if (rr >= at.total) continue;
+      float mt = sm[row];
+#pragma unroll
+      for (int w = 1; w < ROWS_WARPS; ++w) mt = fmaxf(mt, sm[w * R + row]);
+      float y = 0.f, lt = 0.f;
+#pragma unroll
+      for (int w = 0; w < ROWS_WARPS; ++w) {
+        const float mw = sm[w * R + row], e = mw > -INFINITY ? ex2(mw - mt) : 0.f;
+        y = fmaf(e, reinterpret_cast<const float*>(smem + w * Smem::WARP)[row * Smem::OROW + place], y); lt = fmaf(e, sl[w * R + row], lt);
+      }
+      if (whole) {
+        store_out(p, at.r0 + rr / p.group, (at.hk * p.group + rr % p.group) * DH + feature_at<DH>(place), lt != 0.f ? y / lt : 0.f);
+      } else {
+        p.part_o[slot * (R * DH) + i] = y;
+        if (place == 0) p.part_ml[slot * R + row] = make_float2(mt, lt);
+      }
+    }
+    const bool done = group_end >= at.end;
+    __syncthreads();                             // everybody has read the partial O and the place
+    if (threadIdx.x == 0) {
+      if (done) {
+        // the CTA that the group's last unit belongs to: shares are [all c / ctas, all (c + 1) / ctas)
+        if (!p.direct)
+          p.records[blockIdx.x] = JoinRecord{at.b, at.qt, at.hk, head && !tail ? (int)((group_end * at.ctas - 1) / at.all) - (int)blockIdx.x + 1 : 0};
+      } else {
+        at.unit = at.first = group_end;          // the next group: head, row tile, sequence
+        if (++at.hk == c.nkv) {
+          at.hk = 0;
+          SeqRows s = SeqRows{at.len, at.n, at.r0};
+          if (++at.qt * R >= at.total) {
+            at.qt = 0;
+            do s = seq_rows(c, ++at.b); while (s.n == 0);   // (a unit is left, so a sequence with rows is)
+          }
+          at.enter<R>(s, p.group);
+        }
+      }
+    }
+    if (done) break;
+    ptx::fence_proxy_async_smem();               // the partial O was written where copies will be
+    __syncthreads();
   }
-  if (cs > 1) ptx::cluster_sync();               // nobody leaves while a peer may still read its shared memory
 }
 
-// joins the partial results of the clusters of one (row, query head): a warp each
-template <int DH>
-__global__ void __launch_bounds__(128) block_attn_join_kernel(const BlockAttnParams p) {
+// joins the partial results of a group that was cut: CTA (c, row) takes one row of the tile of the group that began in share c.
+// The parts are dealt out to the warps, a lane holds DH / 32 places: the loads of all parts are in flight together.
+constexpr int JOIN_WARPS = 4, JOIN_MAX_PARTS = 1024;
+template <int DH, int NT>
+__global__ void __launch_bounds__(JOIN_WARPS * 32) block_attn_join_kernel(const __grid_constant__ BlockAttnParams p) {
+  constexpr int R = 8 * NT, E = DH / 32;
+  __shared__ float weight[JOIN_MAX_PARTS], red[JOIN_WARPS], sum[JOIN_WARPS], part[JOIN_WARPS][DH];
   ptx::pdl_launch_dependents();
   ptx::pdl_wait();
-  const SeqRows s = seq_rows(p.c, blockIdx.y);
-  const long long w = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
-  const int i = (int)(w / p.nq), hq = (int)(w % p.nq), lane = threadIdx.x & 31;
-  if (i >= s.n) return;
-  const long long at = ((s.r0 + i) * p.nq + hq) * p.outer;
+  const JoinRecord rec = p.records[blockIdx.x];
+  if (rec.parts == 0) return;
+  const SeqRows s = seq_rows(p.c, rec.b);
+  const int row = blockIdx.y, rr = rec.qt * R + row, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (rr >= s.n * p.group) return;
+  // the first part lies in the second slot of its CTA, the others in the first slots of the CTAs behind it
+  auto slot = [&](int q) { return (2ll * (blockIdx.x + q) + (q == 0 ? 1 : 0)) * R + row; };
   float mt = -INFINITY;
-  for (int q = lane; q < p.outer; q += 32) mt = fmaxf(mt, p.part_ml[at + q].x);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) mt = fmaxf(mt, __shfl_xor_sync(0xffffffffu, mt, o));
-  constexpr int E = DH / 32;
-  float lt = 0.f, y[E];
-#pragma unroll
-  for (int e = 0; e < E; ++e) y[e] = 0.f;
-#pragma unroll 4
-  for (int q = 0; q < p.outer; ++q) {
-    const float2 ml = p.part_ml[at + q];
-    const float f = ml.x > -INFINITY ? ex2(ml.x - mt) : 0.f;
-    lt = fmaf(f, ml.y, lt);
-#pragma unroll
-    for (int e = 0; e < E; ++e) y[e] = fmaf(f, p.part_o[(at + q) * DH + 32 * e + lane], y[e]);
+  for (int q = threadIdx.x; q < rec.parts; q += JOIN_WARPS * 32) {
+    weight[q] = p.part_ml[slot(q)].x;
+    mt = fmaxf(mt, weight[q]);
   }
 #pragma unroll
-  for (int e = 0; e < E; ++e) store_out(p, s.r0 + i, hq * DH + feature_at<DH>(32 * e + lane), lt != 0.f ? y[e] / lt : 0.f);
+  for (int o = 16; o > 0; o >>= 1) mt = fmaxf(mt, __shfl_xor_sync(0xffffffffu, mt, o));
+  if (lane == 0) red[warp] = mt;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < JOIN_WARPS; ++w) mt = fmaxf(mt, red[w]);
+  float lt = 0.f;
+  for (int q = threadIdx.x; q < rec.parts; q += JOIN_WARPS * 32) {
+    const float f = weight[q] > -INFINITY ? ex2(weight[q] - mt) : 0.f;
+    weight[q] = f;
+    lt = fmaf(f, p.part_ml[slot(q)].y, lt);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) lt += __shfl_xor_sync(0xffffffffu, lt, o);
+  if (lane == 0) sum[warp] = lt;
+  __syncthreads();
+  float y[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) y[e] = 0.f;
+#pragma unroll 8
+  for (int q = warp; q < rec.parts; q += JOIN_WARPS) {
+    const float f = weight[q];
+    const float* src = p.part_o + slot(q) * DH + lane * E;
+    if constexpr (E == 4) {
+      const float4 x = *reinterpret_cast<const float4*>(src);
+      y[0] = fmaf(f, x.x, y[0]); y[1] = fmaf(f, x.y, y[1]); y[2] = fmaf(f, x.z, y[2]); y[3] = fmaf(f, x.w, y[3]);
+    } else {
+      const float2 x = *reinterpret_cast<const float2*>(src);
+      y[0] = fmaf(f, x.x, y[0]); y[1] = fmaf(f, x.y, y[1]);
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < E; ++e) part[warp][lane * E + e] = y[e];
+  __syncthreads();
+  if (threadIdx.x < DH) {
+    float o = 0.f, l = 0.f;
+#pragma unroll
+    for (int w = 0; w < JOIN_WARPS; ++w) { o += part[w][threadIdx.x]; l += sum[w]; }
+    store_out(p, s.r0 + rr / p.group, (rec.hk * p.group + rr % p.group) * DH + feature_at<DH>(threadIdx.x), l != 0.f ? o / l : 0.f);
+  }
 }
 
-// How the tokens of a (sequence, key / value head, row tile) are split: the host knows an upper bound of the lengths only.
-static SplitPlan plan_rows(const hero_handle* h, const hero_block_cache* cc, int nq, int max_rows, int nt) {
-  const long long tiles = ((long long)max_rows * (nq / cc->nkv) + 8 * nt - 1) / (8 * nt);
-  const long long groups = tiles * cc->nkv * cc->B;
-  const long long slots = (long long)h->sm_count * 3;
-  long long want = (2 * slots + groups - 1) / groups;             // CTAs for two rounds of the GPU
-  const long long most = (cc->max_len + 255) / 256;               // of at least 256 tokens each
-  if (want > most) want = most;
-  SplitPlan s = {1, 1};
-  while (s.cluster < ROWS_MAX_CLUSTER && s.cluster < want) s.cluster *= 2;
-  if (want > ROWS_MAX_CLUSTER) s.outer = (int)((want + ROWS_MAX_CLUSTER - 1) / ROWS_MAX_CLUSTER);
-  return s;
-}
-static int rows_nt(const hero_block_cache* cc, int nq, int max_rows) { return (long long)max_rows * (nq / cc->nkv) <= 8 ? 1 : 2; }
-static size_t part_bytes(const SplitPlan& s, long long rows, int nq, int dh) {
-  return s.outer == 1 ? 0 : (size_t)rows * nq * s.outer * (dh * 4 + 8);
+// How a call is dealt out; the host knows upper bounds of lengths and rows only.
+struct RowsPlan { int nt, tiles, ctas; bool direct; size_t bytes; };
+static hero_status plan_rows(const hero_handle* h, const hero_block_cache* cc, int nq, int max_rows, RowsPlan* out) {
+  const long long rows = (long long)max_rows * (nq / cc->nkv);
+  RowsPlan r;
+  r.nt = rows <= 8 ? 1 : 2;
+  const long long tiles = (rows + 8 * r.nt - 1) / (8 * r.nt), groups = tiles * cc->nkv * cc->B, steps = ((long long)cc->max_len + 31) / 32;
+  HERO_REQUIRE(groups <= (1ll << 30), HERO_ERR_UNSUPPORTED, "B=%d nkv=%d max_rows=%d: too many", cc->B, cc->nkv, max_rows);
+  r.tiles = (int)tiles;
+  r.direct = steps <= ROWS_DIRECT_STEPS;
+  const long long full = (long long)h->sm_count * ROWS_CTAS < JOIN_MAX_PARTS ? (long long)h->sm_count * ROWS_CTAS : JOIN_MAX_PARTS, useful = (groups * (steps + ROWS_GROUP_UNITS) + ROWS_MIN_UNITS - 1) / ROWS_MIN_UNITS;
+  r.ctas = (int)(r.direct ? groups : (full < useful ? full : useful));
+  r.bytes = r.direct ? 0 : (size_t)r.ctas * (2 * 8 * r.nt * (cc->dh * 4 + 8) + sizeof(JoinRecord));
+  *out = r;
+  return HERO_OK;
 }
 
 template <int DH, int NT>
-static hero_status launch_rows(hero_handle* h, const hero_block_cache* cc, const BlockAttnParams& p, bool bf, int B, int tiles, cudaStream_t stream) {
+static hero_status launch_rows(hero_handle* h, const hero_block_cache* cc, const BlockAttnParams& p, bool bf, int ctas, cudaStream_t stream) {
   auto kern = bf ? (p.c.f8 ? block_attn_rows_kernel<DH, NT, true, true> : block_attn_rows_kernel<DH, NT, true, false>)
                  : (p.c.f8 ? block_attn_rows_kernel<DH, NT, false, true> : block_attn_rows_kernel<DH, NT, false, false>);
+  constexpr int BYTES = RowsSmem<DH, NT>::BYTES;
   static PerDeviceOnce configured[4];            // per instantiation of the kernel
   PerDeviceOnce& once = configured[(bf ? 2 : 0) + (p.c.f8 ? 1 : 0)];
-  if (RowsSmem<DH, NT>::BYTES > 48 * 1024 && !once.done(h->device)) {
-    HERO_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, RowsSmem<DH, NT>::BYTES));
+  if (!once.done(h->device)) {
+    HERO_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, BYTES));
     once.set(h->device);
   }
   CUtensorMap tm_k, tm_v;
   hero_status st;
   if ((st = make_tmap_pages(h, &tm_k, cc->k, cc, 16)) != HERO_OK || (st = make_tmap_pages(h, &tm_v, cc->v, cc, 16)) != HERO_OK) return st;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(p.cluster * p.outer), (unsigned)(p.c.nkv * tiles), (unsigned)B);
-  cfg.blockDim = dim3(ROWS_WARPS * 32);
-  cfg.dynamicSmemBytes = RowsSmem<DH, NT>::BYTES;
-  cfg.stream = stream;
-  cudaLaunchAttribute at[2];
-  int n = 0;
-  if (p.cluster > 1) {
-    at[n].id = cudaLaunchAttributeClusterDimension;
-    at[n].val.clusterDim.x = (unsigned)p.cluster; at[n].val.clusterDim.y = 1; at[n].val.clusterDim.z = 1;
-    ++n;
-  }
-  if (!pdl_take_fence(stream)) {                 // a fenced stream: ordinary serialisation
-    at[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[n].val.programmaticStreamSerializationAllowed = 1;
-    ++n;
-  }
-  cfg.attrs = at; cfg.numAttrs = n;
   {
     LaunchScope scope(h, stream, KERNEL_ATTN);
-    HERO_CUDA(cudaLaunchKernelEx(&cfg, kern, tm_k, tm_v, p));
+    HERO_CUDA(launch_dependent(kern, dim3((unsigned)ctas), dim3(ROWS_WARPS * 32), BYTES, stream, tm_k, tm_v, p));
   }
-  if (p.outer > 1) {
+  if (!p.direct) {
     LaunchScope scope(h, stream, KERNEL_ATTN);
-    HERO_CUDA(launch_dependent(block_attn_join_kernel<DH>, dim3((unsigned)(((long long)p.c.max_rows * p.nq + 3) / 4), (unsigned)B), dim3(128), 0, stream, p));
+    HERO_CUDA(launch_dependent(block_attn_join_kernel<DH, NT>, dim3((unsigned)ctas, 8 * NT), dim3(JOIN_WARPS * 32), 0, stream, p));
   }
   return HERO_OK;
 }
@@ -560,8 +653,9 @@ extern "C" hero_status hero_block_attention_workspace_bytes(hero_handle* h, cons
   if (st != HERO_OK) return st;
   HERO_REQUIRE(cc->B >= 0 && cc->max_len >= 1 && (cc->dh == 64 || cc->dh == 128), HERO_ERR_UNSUPPORTED, "B=%d max_len=%d dh=%d", cc->B, cc->max_len, cc->dh);
   if (cc->B == 0) return HERO_OK;
-  *bytes = part_bytes(plan_rows(h, cc, nq, max_rows, rows_nt(cc, nq, max_rows)), rows, nq, cc->dh);
-  return HERO_OK;
+  RowsPlan plan;
+  if ((st = plan_rows(h, cc, nq, max_rows, &plan)) == HERO_OK) *bytes = plan.bytes;
+  return st;
 }
 
 extern "C" hero_status hero_block_attention(hero_handle* h, const hero_block_cache* cc, const hero_block_attn_args* a, void* stream) {
@@ -591,18 +685,17 @@ extern "C" hero_status hero_block_attention(hero_handle* h, const hero_block_cac
   p.c2 = (float)((a->scale != 0.f ? (double)a->scale : 1.0 / std::sqrt((double)cc->dh)) * 1.4426950408889634);
   p.nq = a->nq;
   const bool bf = a->q.dtype == HERO_BF16;
-  const int nt = rows_nt(cc, a->nq, a->max_rows);
-  const SplitPlan plan = plan_rows(h, cc, a->nq, a->max_rows, nt);
-  const size_t need = part_bytes(plan, a->q.rows, a->nq, cc->dh);
-  HERO_REQUIRE(need == 0 || (a->workspace && a->workspace_bytes >= need), HERO_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", a->workspace_bytes, need);
-  HERO_REQUIRE(need == 0 || aligned16(a->workspace), HERO_ERR_ALIGNMENT, "the workspace must be 16-byte aligned");
-  p.cluster = plan.cluster; p.outer = plan.outer;
+  RowsPlan plan;
+  if ((st = plan_rows(h, cc, a->nq, a->max_rows, &plan)) != HERO_OK) return st;
+  HERO_REQUIRE(plan.bytes == 0 || (a->workspace && a->workspace_bytes >= plan.bytes), HERO_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed",
+               a->workspace_bytes, plan.bytes);
+  HERO_REQUIRE(plan.bytes == 0 || aligned16(a->workspace), HERO_ERR_ALIGNMENT, "the workspace must be 16-byte aligned");
+  p.B = cc->B; p.tiles = plan.tiles; p.direct = plan.direct;
   p.part_o = static_cast<float*>(a->workspace);
-  p.part_ml = reinterpret_cast<float2*>(p.part_o + (size_t)a->q.rows * a->nq * plan.outer * cc->dh);
-  const long long tiles = ((long long)a->max_rows * p.group + 8 * nt - 1) / (8 * nt);
-  HERO_REQUIRE(tiles * cc->nkv <= 65535, HERO_ERR_UNSUPPORTED, "max_rows=%d", a->max_rows);
+  p.part_ml = reinterpret_cast<float2*>(p.part_o + (size_t)plan.ctas * 2 * 8 * plan.nt * cc->dh);
+  p.records = reinterpret_cast<JoinRecord*>(p.part_ml + (size_t)plan.ctas * 2 * 8 * plan.nt);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (cc->dh == 64)
-    return nt == 1 ? launch_rows<64, 1>(h, cc, p, bf, cc->B, (int)tiles, s) : launch_rows<64, 2>(h, cc, p, bf, cc->B, (int)tiles, s);
-  return nt == 1 ? launch_rows<128, 1>(h, cc, p, bf, cc->B, (int)tiles, s) : launch_rows<128, 2>(h, cc, p, bf, cc->B, (int)tiles, s);
+    return plan.nt == 1 ? launch_rows<64, 1>(h, cc, p, bf, plan.ctas, s) : launch_rows<64, 2>(h, cc, p, bf, plan.ctas, s);
+  return plan.nt == 1 ? launch_rows<128, 1>(h, cc, p, bf, plan.ctas, s) : launch_rows<128, 2>(h, cc, p, bf, plan.ctas, s);
 }
