@@ -1,30 +1,8 @@
 // Attention over the 8-bit block cache (hero_block_attention): o = softmax(scale q K^T) V, causal in a sequence's new rows.
-#include "block_cache.cuh"
+#include "block_attention.cuh"
 #include <cmath>
 
 namespace hero {
-
-struct BlockAttnParams {
-  BlockView c;
-  const uint16_t* q; long long ld_q;
-  void* out; long long ld_out; int out_dt;
-  const float* out_scale; int out_scale_stride;
-  int nq, group;
-  float c2;                      // scale * log2(e)
-  int B, tiles, direct;          // direct: CTA index = (sequence, row tile, head); else equal shares of all units
-  struct JoinRecord* records;    // [CTA]
-  float* part_o; float2* part_ml; // partial results [CTA][2]: sum of P V [rows][DH], (maximum, sum of P) [rows]
-};
-
-__device__ __forceinline__ void store_out(const BlockAttnParams& p, long long row, int col, float y) {
-  const long long at = row * p.ld_out + col;
-  if (p.out_dt == HERO_F16) static_cast<__half*>(p.out)[at] = __float2half_rn(y);
-  else if (p.out_dt == HERO_BF16) static_cast<__nv_bfloat16*>(p.out)[at] = __float2bfloat16_rn(y);
-  else {
-    const float z = y / __ldg(p.out_scale + (long long)col * p.out_scale_stride);
-    static_cast<uint8_t*>(p.out)[at] = (uint8_t)(p.out_dt == HERO_F8 ? f32_to_codes4<true>(z, 0.f, 0.f, 0.f) : f32_to_codes4<false>(z, 0.f, 0.f, 0.f));
-  }
-}
 
 // ------------------------------------------------------------------------------------------------------------------
 // Few rows per key / value head (decode steps, drafts).  Every cached byte is read once and meets at most 16 query rows, so
@@ -51,7 +29,6 @@ constexpr int ROWS_CTAS = 3;                    // resident per SM
 constexpr int ROWS_GROUP_UNITS = 4;             // what a group costs beside its steps (queries in, partial results out), in steps
 constexpr int ROWS_MIN_UNITS = 12;              // units of a share, at least
 constexpr int ROWS_DIRECT_STEPS = 16;           // up to this many steps (512 tokens) a group is one CTA's
-constexpr float P_SHIFT = 11.0f, MAX_SLACK = 4.0f;
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -62,30 +39,6 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
-  const __half2 h = __floats2half2_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
-// four codes of one word -> f16x2 of codes (0, 1) and (2, 3)
-template <bool F8>
-__device__ __forceinline__ void codes4_to_f16(uint32_t w, uint32_t& lo, uint32_t& hi) {
-  if constexpr (F8) {
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(lo) : "h"((uint16_t)(w & 0xffffu)));
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(hi) : "h"((uint16_t)(w >> 16)));
-  } else {
-    const uint32_t u = w ^ 0x80808080u;
-    const __half2 off = __floats2half2_rn(1152.f, 1152.f);               // 1024 + 128
-    uint32_t a = __byte_perm(u, 0x64646464u, 0x4140), b = __byte_perm(u, 0x64646464u, 0x4342);
-    const __half2 x = __hsub2(*reinterpret_cast<__half2*>(&a), off), y = __hsub2(*reinterpret_cast<__half2*>(&b), off);
-    lo = *reinterpret_cast<const uint32_t*>(&x); hi = *reinterpret_cast<const uint32_t*>(&y);
-  }
-}
-
 // one half (16 tokens) of a page: box {DH, 16, 1, 1} of the map over {features, tokens of a page, heads, pages}
 __device__ __forceinline__ void load_half(uint32_t dst, const CUtensorMap* m, int token, int head, int page, uint32_t bar) {
   asm volatile(
@@ -594,10 +547,16 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) block_attn_join_kernel(const 
 }
 
 // How a call is dealt out; the host knows upper bounds of lengths and rows only.
-struct RowsPlan { int nt, tiles, ctas; bool direct; size_t bytes; };
+struct RowsPlan { int nt, tiles, ctas; bool direct, prompt; size_t bytes; };
 static hero_status plan_rows(const hero_handle* h, const hero_block_cache* cc, int nq, int max_rows, RowsPlan* out) {
   const long long rows = (long long)max_rows * (nq / cc->nkv);
   RowsPlan r;
+  r.prompt = rows > 32;
+  if (r.prompt) {
+    r.bytes = 0;
+    *out = r;
+    return HERO_OK;
+  }
   r.nt = rows <= 8 ? 1 : 2;
   const long long tiles = (rows + 8 * r.nt - 1) / (8 * r.nt), groups = tiles * cc->nkv * cc->B, steps = ((long long)cc->max_len + 31) / 32;
   HERO_REQUIRE(groups <= (1ll << 30), HERO_ERR_UNSUPPORTED, "B=%d nkv=%d max_rows=%d: too many", cc->B, cc->nkv, max_rows);
@@ -690,6 +649,7 @@ extern "C" hero_status hero_block_attention(hero_handle* h, const hero_block_cac
   HERO_REQUIRE(plan.bytes == 0 || (a->workspace && a->workspace_bytes >= plan.bytes), HERO_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed",
                a->workspace_bytes, plan.bytes);
   HERO_REQUIRE(plan.bytes == 0 || aligned16(a->workspace), HERO_ERR_ALIGNMENT, "the workspace must be 16-byte aligned");
+  if (plan.prompt) return launch_prompt(h, cc, p, bf, static_cast<cudaStream_t>(stream));
   p.B = cc->B; p.tiles = plan.tiles; p.direct = plan.direct;
   p.part_o = static_cast<float*>(a->workspace);
   p.part_ml = reinterpret_cast<float2*>(p.part_o + (size_t)plan.ctas * 2 * 8 * plan.nt * cc->dh);

@@ -1,0 +1,449 @@
+// hero_block_attention for many rows per key / value head (pieces of a prompt, long drafts): tensor-core bound, so the products run
+// on tcgen05 (kind::f16, FP32 accumulators in tensor memory) and everything else is arranged around keeping them fed.
+//
+// One CTA takes 256 rows ((row of the sequence, query head of the group) pairs, two tiles of 128) of one (sequence, key / value head)
+// and walks its keys in tiles of 128.  Keys and values have to become FP16 operands in shared memory on the way: done once per CTA,
+// for both row tiles.  Roles:
+//   warps 0-3, 4-7   softmax of row tile 0 / 1, one row per thread: no reduction across threads.  Scores are read from tensor memory
+//                    twice (maximum, then exponentials); P goes back as FP16 into the columns of the scores and is the A operand of
+//                    P V from there.  While one tile is in its softmax the tensor cores work for the other.
+//   warps 8-11       codes -> FP16: 16-byte loads one tile ahead in registers, exact conversion, stores in the 128-byte swizzled
+//                    operand layout.  Warp 8 also publishes what the softmax needs of each 16 tokens: key scale, value scale
+//                    relative to the largest so far.
+//   warps 12, 13     issue the products of row tile 0 / 1
+// The value scale of a page is folded into the exponent, e' = 2^(x + log2 rv), so that it costs nothing per element; the row sum
+// undoes it per 16 tokens (rv is kept above 2^-40, where P is zero anyway).  As in the kernel for few rows, queries are scaled into
+// FP16 by a power of two, P carries a factor 2^11 and the running maximum moves only beyond 2^4: the accumulator in
+// tensor memory is rescaled rarely.
+#include "block_attention.cuh"
+#include <cmath>
+
+namespace hero {
+
+constexpr int PR_SM_WARPS = 8, PR_CV_WARPS = 4;
+constexpr int PR_MMA_WARP = PR_SM_WARPS + PR_CV_WARPS;         // and the next one
+constexpr int PR_THREADS = (PR_MMA_WARP + 2) * 32;
+constexpr int PR_ROWS = 256, PR_KEYS = 128;
+constexpr int PR_INFO = 4;                                     // ring of scale records
+constexpr float PR_MIN_RV = 9.094947e-13f;                     // 2^-40
+
+struct KeyInfo { float ks, lrv, inv_rv, pad; };                // of 16 tokens: key scale, log2 and reciprocal of the relative value scale
+
+template <int DH>
+struct PromptCfg {
+  static constexpr int SUB = 128 * 128;                        // one [128 rows x 64 features] FP16 sub-tile, 128-byte rows
+  static constexpr int TILE = SUB * (DH / 64);
+  static constexpr int OFF_K = 2 * TILE, OFF_V = OFF_K + 2 * TILE;
+  static constexpr int OFF_INFO = OFF_V + 2 * TILE;            // KeyInfo [PR_INFO][8]
+  static constexpr int OFF_REF = OFF_INFO + PR_INFO * 8 * 16;  // float2 [PR_INFO]: largest value scale so far, its old / new ratio
+  static constexpr int OFF_BARS = OFF_REF + PR_INFO * 8;
+  static constexpr int NBARS = 2 + 4 + 4 + 2 * PR_INFO + 6;
+  static constexpr int BYTES = 1024 + OFF_BARS + NBARS * 8 + 16;
+  static constexpr int S_COL = 0, O_COL = 256;                 // scores (then P) 2 x 128 columns, O 2 x DH columns
+};
+
+template <int DH, bool BF, bool F8>
+__global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const __grid_constant__ BlockAttnParams p, const uint32_t idesc_qk,
+                                                                          const uint32_t idesc_pv) {
+  using Cfg = PromptCfg<DH>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + Cfg::OFF_BARS);
+  uint64_t* q_full = bars;                       // [2] softmax warps of a tile -> its issuer
+  uint64_t* k_full = q_full + 2;                 // [2] converters -> issuers
+  uint64_t* k_empty = k_full + 2;                // [2] issuers -> converters
+  uint64_t* v_full = k_empty + 2;                // [2]
+  uint64_t* v_empty = v_full + 2;                // [2]
+  uint64_t* i_full = v_empty + 2;                // [PR_INFO] warp 8 -> softmax
+  uint64_t* i_empty = i_full + PR_INFO;          // [PR_INFO] softmax -> warp 8
+  uint64_t* s_full = i_empty + PR_INFO;          // [2] scores of a tile are complete
+  uint64_t* p_full = s_full + 2;                 // [2] its P is in place (and O rescaled)
+  uint64_t* o_full = p_full + 2;                 // [2] its P V is complete
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(o_full + 2);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < 2; ++i) {
+      ptx::mbar_init(&q_full[i], 4);
+      ptx::mbar_init(&k_full[i], PR_CV_WARPS); ptx::mbar_init(&k_empty[i], 2);
+      ptx::mbar_init(&v_full[i], PR_CV_WARPS); ptx::mbar_init(&v_empty[i], 2);
+      ptx::mbar_init(&s_full[i], 1); ptx::mbar_init(&p_full[i], 4); ptx::mbar_init(&o_full[i], 1);
+    }
+    for (int i = 0; i < PR_INFO; ++i) { ptx::mbar_init(&i_full[i], 1); ptx::mbar_init(&i_empty[i], PR_SM_WARPS); }
+    ptx::fence_mbar_init();
+  }
+  if (warp == PR_MMA_WARP) { ptx::tmem_alloc(tmem_slot, 512); ptx::tmem_relinquish(); }
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  ptx::pdl_launch_dependents();
+  ptx::pdl_wait();
+
+  const BlockView& c = p.c;
+  const int b = blockIdx.y, hk = blockIdx.x % c.nkv, qt = p.tiles - 1 - blockIdx.x / c.nkv;   // late rows (many keys) first
+  const SeqRows s = seq_rows(c, b);
+  const int total = s.n * p.group, rb = qt * PR_ROWS, base = s.len - s.n;
+  // keys of a row tile's last row, and its tiles of keys
+  auto keys_of = [&](int t) {
+    const int first = rb + 128 * t;
+    return first >= total ? 0 : max(base + (min(first + 128, total) - 1) / p.group + 1, 0);
+  };
+  const int L = max(keys_of(0), keys_of(1));
+  const int n_all = (L + PR_KEYS - 1) / PR_KEYS;
+
+  if (rb >= total) {
+    // nothing of this sequence here
+  } else if (warp < PR_SM_WARPS) {
+    // ------------------------------------------------------------------ softmax of one row tile
+    const int t = warp >> 2, quarter = warp & 3, r = quarter * 32 + lane;
+    const int n = (keys_of(t) + PR_KEYS - 1) / PR_KEYS;
+    const int rr = rb + 128 * t + r;
+    const bool row_ok = rr < total;
+    const int lim = row_ok ? base + rr / p.group + 1 : 0;
+    const long long row_g = s.r0 + (row_ok ? rr / p.group : 0);
+    const int hq = hk * p.group + (row_ok ? rr % p.group : 0);
+    float f = 0.f;
+    if (n > 0) {
+      // the row as FP16, scaled by a power of two (and by the sign of the score factor), in the swizzled operand layout
+      uint32_t w[DH / 2], top = 0;
+      const uint4* q = reinterpret_cast<const uint4*>(p.q + row_g * p.ld_q + (long long)hq * DH);
+#pragma unroll
+      for (int i = 0; i < DH / 8; ++i) {
+        const uint4 x = row_ok ? __ldg(q + i) : make_uint4(0, 0, 0, 0);
+        w[4 * i] = x.x; w[4 * i + 1] = x.y; w[4 * i + 2] = x.z; w[4 * i + 3] = x.w;
+      }
+#pragma unroll
+      for (int i = 0; i < DH / 2; ++i) top = __vmaxu2(top, w[i] & 0x7fff7fffu);
+      const float amax = fp16ish_to_f32x2<BF>(max(top & 0xffffu, top >> 16)).x;
+      const int e = (int)(__float_as_uint(amax) >> 23);
+      const float up = e == 0 || e == 255 ? 1.0f : __uint_as_float((uint32_t)min(127 + 14 + 127 - e, 253) << 23);
+      f = fabsf(p.c2) / up;
+      const float up_s = p.c2 < 0.f ? -up : up;
+      uint8_t* row = smem + t * Cfg::TILE + (r >> 3) * 1024 + (r & 7) * 128;
+#pragma unroll
+      for (int i = 0; i < DH / 8; ++i) {
+        uint32_t h[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float2 x = fp16ish_to_f32x2<BF>(w[4 * i + j]);
+          h[j] = pack_f16(x.x * up_s, x.y * up_s);
+        }
+        *reinterpret_cast<uint4*>(row + (i >> 3) * Cfg::SUB + (((i & 7) ^ (r & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+      }
+      ptx::fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(&q_full[t]);
+    }
+    const uint32_t t_lane = tmem_base + ((uint32_t)(quarter * 32) << 16);
+    const uint32_t s_col = t_lane + Cfg::S_COL + t * 128, o_col = t_lane + Cfg::O_COL + t * DH;
+    float u = 0.f, l = 0.f, vref = 0.f;            // u = P_SHIFT - running maximum
+    bool ok = true;
+    for (int j = 0; j < n_all; ++j) {
+      const int slot = j % PR_INFO;
+      ok = __all_sync(0xffffffffu, ok && ptx::mbar_wait(&i_full[slot], (j / PR_INFO) & 1, c.err, 0x8000 | slot));
+      if (j < n) ok = __all_sync(0xffffffffu, ok && ptx::mbar_wait(&s_full[t], j & 1, c.err, 0x8100 | t));
+      if (j >= n || !ok) {                         // the other row tile's keys: only hand the record back
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(&i_empty[slot]);
+        continue;
+      }
+      ptx::tc_fence_after();
+      const KeyInfo* info = reinterpret_cast<const KeyInfo*>(smem + Cfg::OFF_INFO) + slot * 8;
+      const float2 ref = reinterpret_cast<const float2*>(smem + Cfg::OFF_REF)[slot];
+      vref = ref.x;
+      const int valid = lim - j * PR_KEYS;         // keys of this tile that the row sees
+      const bool whole = __all_sync(0xffffffffu, valid >= PR_KEYS);
+      // ---- pass 1: largest exponent
+      float mx = -INFINITY;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        uint32_t x[32];
+        ptx::tmem_ld32(s_col + 32 * k, x);
+        ptx::tmem_ld_wait();
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float m = -INFINITY;
+          if (whole) {
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) m = ptx::max3(m, __uint_as_float(x[16 * h + i]), __uint_as_float(x[16 * h + i + 1]));
+          } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) m = fmaxf(m, 32 * k + 16 * h + i < valid ? __uint_as_float(x[16 * h + i]) : -INFINITY);
+          }
+          if (m > -INFINITY) mx = fmaxf(mx, fmaf(m, f * info[2 * k + h].ks, u));
+        }
+      }
+      // ---- the maximum moves (always in the first tile), the value reference moves: O and the sum follow
+      const bool moves = j == 0 || mx > P_SHIFT + MAX_SLACK;
+      if (__any_sync(0xffffffffu, moves) || ref.y != 1.0f) {
+        float d = mx - P_SHIFT;
+        if (j > 0) d = fmaxf(d, 0.f);
+        if (mx == -INFINITY) d = 0.f;
+        u -= d;
+        if (j > 0) {
+          const float a = ex2(-d);
+          l *= a;
+          const float ao = a * ref.y;
+#pragma unroll
+          for (int k = 0; k < DH / 32; ++k) {
+            uint32_t x[32];
+            ptx::tmem_ld32(o_col + 32 * k, x);
+            ptx::tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 32; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * ao);
+            ptx::tmem_st32(o_col + 32 * k, x);
+          }
+        }
+      }
+      // ---- pass 2: e' = 2^(score - maximum + 11 + log2 rv); P over the scores' columns (those behind are read already)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        uint32_t x[32], w[16];
+        ptx::tmem_ld32(s_col + 32 * k, x);
+        ptx::tmem_ld_wait();
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float4 gi = *reinterpret_cast<const float4*>(&info[2 * k + h]);
+          const float fk = f * gi.x, ug = u + gi.y;
+          float2 sum = make_float2(0.f, 0.f);
+          if (whole) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const float2 a = __ffma2_rn(make_float2(__uint_as_float(x[16 * h + 2 * i]), __uint_as_float(x[16 * h + 2 * i + 1])), make_float2(fk, fk),
+                                          make_float2(ug, ug));
+              const float2 e = make_float2(ex2(a.x), ex2(a.y));
+              sum = __fadd2_rn(sum, e);
+              w[8 * h + i] = pack_f16(e.x, e.y);
+            }
+          } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const int key = 32 * k + 16 * h + 2 * i;
+              const float e0 = key < valid ? ex2(fmaf(__uint_as_float(x[16 * h + 2 * i]), fk, ug)) : 0.f;
+              const float e1 = key + 1 < valid ? ex2(fmaf(__uint_as_float(x[16 * h + 2 * i + 1]), fk, ug)) : 0.f;
+              sum.x += e0; sum.y += e1;
+              w[8 * h + i] = pack_f16(e0, e1);
+            }
+          }
+          l = fmaf(sum.x + sum.y, gi.z, l);
+        }
+        ptx::tmem_st16(s_col + 16 * k, w);
+      }
+      ptx::tmem_st_wait();
+      ptx::tc_fence_before();
+      __syncwarp();
+      if (lane == 0) { ptx::mbar_arrive(&p_full[t]); ptx::mbar_arrive(&i_empty[slot]); }
+    }
+    // ---- output
+    float scale_o = 0.f;
+    if (n > 0) {
+      ok = __all_sync(0xffffffffu, ok && ptx::mbar_wait(&o_full[t], (n - 1) & 1, c.err, 0x8200 | t));
+      ptx::tc_fence_after();
+      scale_o = l != 0.f ? vref / l : 0.f;
+    }
+#pragma unroll
+    for (int k = 0; k < DH / 32; ++k) {
+      uint32_t x[32];
+      if (n > 0) {
+        ptx::tmem_ld32(o_col + 32 * k, x);
+        ptx::tmem_ld_wait();
+      }
+      float y[32];
+#pragma unroll
+      for (int i = 0; i < 32; ++i) y[i] = n > 0 && l != 0.f ? __uint_as_float(x[i]) * scale_o : 0.f;
+      if (row_ok && ok) {
+        const int col = hq * DH + 32 * k;
+        const long long at = row_g * p.ld_out + col;
+        if (p.out_dt == HERO_F16 || p.out_dt == HERO_BF16) {
+          uint4* dst = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + at);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            uint32_t o[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              o[e] = p.out_dt == HERO_F16 ? f32x2_to_fp16ish<false>(y[8 * i + 2 * e], y[8 * i + 2 * e + 1]) : f32x2_to_fp16ish<true>(y[8 * i + 2 * e], y[8 * i + 2 * e + 1]);
+            dst[i] = make_uint4(o[0], o[1], o[2], o[3]);
+          }
+        } else {
+          uint4* dst = reinterpret_cast<uint4*>(static_cast<uint8_t*>(p.out) + at);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) y[i] /= __ldg(p.out_scale + (long long)(col + i) * p.out_scale_stride);
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            uint32_t o[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float* z = y + 16 * i + 4 * e;
+              o[e] = p.out_dt == HERO_F8 ? f32_to_codes4<true>(z[0], z[1], z[2], z[3]) : f32_to_codes4<false>(z[0], z[1], z[2], z[3]);
+            }
+            dst[i] = make_uint4(o[0], o[1], o[2], o[3]);
+          }
+        }
+      }
+    }
+  } else if (warp < PR_MMA_WARP) {
+    // ------------------------------------------------------------------ codes -> FP16 operands
+    constexpr int PPR = DH / 16;                   // 16-code pieces of a row = pieces of a tile per thread
+    constexpr int RPI = 128 / PPR;                 // rows between a thread's pieces
+    const int ct = threadIdx.x - PR_SM_WARPS * 32, piece = ct % PPR, r0 = ct / PPR;
+    const bool scribe = warp == PR_SM_WARPS;       // publishes the scale records
+    const uint8_t* kb = c.k + (long long)hk * c.head_stride + piece * 16;
+    const uint8_t* vb = c.v + (long long)hk * c.head_stride + piece * 16;
+    auto page_of = [&](int j) {                    // lane g < 8: page of tokens 128 j + 16 g ..
+      const int tok = j * PR_KEYS + 16 * lane;
+      return lane < 8 && tok < L ? page_for_read(c, b, tok >> c.page_shift) : -1;
+    };
+    auto load = [&](const uint8_t* from, int j, int ids, uint4 (&raw)[PPR]) {
+#pragma unroll
+      for (int i = 0; i < PPR; ++i) {
+        const int row = r0 + RPI * i, tok = j * PR_KEYS + row;
+        const int id = __shfl_sync(0xffffffffu, ids, DH == 128 ? i : 2 * i + (ct >> 6));
+        raw[i] = make_uint4(0, 0, 0, 0);           // slots behind the end may hold anything (e4m3: NaN)
+        if (tok < L) raw[i] = __ldg(reinterpret_cast<const uint4*>(from + (long long)id * c.page_stride + (long long)(tok & (c.page - 1)) * c.ld));
+      }
+    };
+    auto store = [&](uint8_t* tile, const uint4 (&raw)[PPR]) {
+#pragma unroll
+      for (int i = 0; i < PPR; ++i) {
+        const int row = r0 + RPI * i;
+        uint32_t h[8];
+        codes4_to_f16<F8>(raw[i].x, h[0], h[1]);
+        codes4_to_f16<F8>(raw[i].y, h[2], h[3]);
+        codes4_to_f16<F8>(raw[i].z, h[4], h[5]);
+        codes4_to_f16<F8>(raw[i].w, h[6], h[7]);
+        // 16-byte chunks 2 piece and 2 piece + 1 of the row; half of the lanes store them in the other order (no bank conflicts)
+        uint8_t* at = tile + (piece >> 2) * Cfg::SUB + (row >> 3) * 1024 + (row & 7) * 128;
+        const int first = (2 * piece) & 7, swap = DH == 128 ? piece >> 2 : 0;
+        *reinterpret_cast<uint4*>(at + (((first + swap) ^ (row & 7)) << 4)) = swap ? make_uint4(h[4], h[5], h[6], h[7]) : make_uint4(h[0], h[1], h[2], h[3]);
+        *reinterpret_cast<uint4*>(at + (((first + 1 - swap) ^ (row & 7)) << 4)) = swap ? make_uint4(h[0], h[1], h[2], h[3]) : make_uint4(h[4], h[5], h[6], h[7]);
+      }
+      ptx::fence_proxy_async_smem();
+      __syncwarp();
+    };
+    uint4 kr[PPR], vr[PPR];
+    bool ok = true;
+    int ids = page_of(0), ids_next = page_of(1);
+    float2 sc = make_float2(0.f, 0.f);             // scribe's lane g: scales of tokens 128 j + 16 g ..
+    auto scales = [&](int i) { return i >= 0 ? make_float2(__ldg(c.ks + (long long)i * c.nkv + hk), __ldg(c.vs + (long long)i * c.nkv + hk)) : make_float2(0.f, 0.f); };
+    if (n_all > 0) { load(kb, 0, ids, kr); load(vb, 0, ids, vr); }
+    if (scribe) sc = scales(ids);
+    float vref = 0.f;
+    for (int j = 0; j < n_all; ++j) {
+      const int st = j & 1;
+      const uint32_t par = ((j >> 1) & 1) ^ 1;
+      if (scribe) {
+        const int slot = j % PR_INFO;
+        ok = ok && ptx::mbar_wait(&i_empty[slot], ((j / PR_INFO) & 1) ^ 1, c.err, 0x8300 | slot);
+        float top = lane < 8 ? sc.y : 0.f;
+#pragma unroll
+        for (int o = 4; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const float now = fmaxf(vref, __shfl_sync(0xffffffffu, top, 0));
+        const float rv = fmaxf(now > 0.f ? sc.y / now : 1.f, PR_MIN_RV);
+        if (lane < 8) *reinterpret_cast<float4*>(smem + Cfg::OFF_INFO + (slot * 8 + lane) * 16) = make_float4(sc.x, __log2f(rv), 1.0f / rv, 0.f);
+        if (lane == 0) reinterpret_cast<float2*>(smem + Cfg::OFF_REF)[slot] = make_float2(now, now > vref ? vref / now : 1.0f);
+        vref = now;
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(&i_full[slot]);
+        sc = scales(ids_next);
+      }
+      const int ids_after = page_of(j + 2);
+      ok = ok && ptx::mbar_wait(&k_empty[st], par, c.err, 0x8400 | st);
+      store(smem + Cfg::OFF_K + st * Cfg::TILE, kr);
+      if (lane == 0) ptx::mbar_arrive(&k_full[st]);
+      if (j + 1 < n_all) load(kb, j + 1, ids_next, kr);
+      ok = ok && ptx::mbar_wait(&v_empty[st], par, c.err, 0x8500 | st);
+      store(smem + Cfg::OFF_V + st * Cfg::TILE, vr);
+      if (lane == 0) ptx::mbar_arrive(&v_full[st]);
+      if (j + 1 < n_all) load(vb, j + 1, ids_next, vr);
+      ids_next = ids_after;
+      if (!__all_sync(0xffffffffu, ok)) break;
+    }
+  } else {
+    // ------------------------------------------------------------------ issuer of one row tile
+    const int t = warp - PR_MMA_WARP, n = (keys_of(t) + PR_KEYS - 1) / PR_KEYS;
+    const bool issue = ptx::elect_one();
+    constexpr uint64_t kmaj = ptx::smem_desc_base(16, 1024, ptx::SWZ_128B);            // Q, K: K-major, 128-byte rows
+    constexpr uint64_t vmaj = ptx::smem_desc_base(Cfg::SUB, 1024, ptx::SWZ_128B);      // V: MN-major; 64-feature chunks SUB apart
+    const uint64_t qd = ptx::smem_desc(kmaj, ptx::smem_u32(smem + t * Cfg::TILE));
+    const uint64_t kd0 = ptx::smem_desc(kmaj, ptx::smem_u32(smem + Cfg::OFF_K)), vd0 = ptx::smem_desc(vmaj, ptx::smem_u32(smem + Cfg::OFF_V));
+    const uint32_t s_tmem = tmem_base + Cfg::S_COL + t * 128, o_tmem = tmem_base + Cfg::O_COL + t * DH;
+    auto scores = [&](int j) -> bool {
+      const int st = j & 1;
+      if (!ptx::mbar_wait(&k_full[st], (j >> 1) & 1, c.err, 0x8600 | st)) return false;
+      ptx::tc_fence_after();
+      if (issue) {
+        const uint64_t kd = kd0 + (uint32_t)((st * Cfg::TILE) >> 4);
+#pragma unroll
+        for (int k = 0; k < DH / 16; ++k) {
+          const uint32_t o = (uint32_t)(((k >> 2) * Cfg::SUB + (k & 3) * 32) >> 4);
+          ptx::umma_f16(s_tmem, qd + o, kd + o, idesc_qk, k != 0);
+        }
+        ptx::umma_commit(&k_empty[st]);
+        ptx::umma_commit(&s_full[t]);
+      }
+      return true;
+    };
+    bool ok = true;
+    if (n > 0) ok = ptx::mbar_wait(&q_full[t], 0, c.err, 0x8700 | t) && scores(0);
+    for (int j = 0; j < n && ok; ++j) {
+      const int st = j & 1;
+      ok = ptx::mbar_wait(&v_full[st], (j >> 1) & 1, c.err, 0x8800 | st) && ptx::mbar_wait(&p_full[t], j & 1, c.err, 0x8900 | t);
+      if (!ok) break;
+      ptx::tc_fence_after();
+      if (issue) {
+        const uint64_t vd = vd0 + (uint32_t)((st * Cfg::TILE) >> 4);
+#pragma unroll
+        for (int k = 0; k < PR_KEYS / 16; ++k)     // 16 keys: 8 columns of P, 2 eight-key groups of V
+          ptx::umma_f16_ta(o_tmem, s_tmem + 8 * k, vd + (uint32_t)((k * 2048) >> 4), idesc_pv, (j | k) != 0);
+        ptx::umma_commit(&v_empty[st]);
+        ptx::umma_commit(&o_full[t]);
+      }
+      if (j + 1 < n) {
+        // the next scores take the place of P: P V has to be complete
+        ok = ptx::mbar_wait(&o_full[t], j & 1, c.err, 0x8A00 | t) && scores(j + 1);
+      }
+    }
+    // keys that only the other row tile needs
+    for (int j = n; j < n_all && ok; ++j) {
+      const int st = j & 1;
+      ok = ptx::mbar_wait(&k_full[st], (j >> 1) & 1, c.err, 0x8B00 | st);
+      if (ok && lane == 0) ptx::mbar_arrive(&k_empty[st]);
+      ok = ok && ptx::mbar_wait(&v_full[st], (j >> 1) & 1, c.err, 0x8C00 | st);
+      if (ok && lane == 0) ptx::mbar_arrive(&v_empty[st]);
+    }
+    __syncwarp();
+  }
+  ptx::tc_fence_before();
+  __syncthreads();
+  if (warp == PR_MMA_WARP) ptx::tmem_dealloc(tmem_base, 512);
+}
+
+template <int DH>
+static hero_status launch(hero_handle* h, const hero_block_cache* cc, const BlockAttnParams& p, bool bf, cudaStream_t stream) {
+  auto kern = bf ? (p.c.f8 ? block_attn_prompt_kernel<DH, true, true> : block_attn_prompt_kernel<DH, true, false>)
+                 : (p.c.f8 ? block_attn_prompt_kernel<DH, false, true> : block_attn_prompt_kernel<DH, false, false>);
+  constexpr int BYTES = PromptCfg<DH>::BYTES;
+  static PerDeviceOnce configured[4];              // per instantiation of the kernel
+  PerDeviceOnce& once = configured[(bf ? 2 : 0) + (p.c.f8 ? 1 : 0)];
+  if (!once.done(h->device)) {
+    HERO_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, BYTES));
+    once.set(h->device);
+  }
+  const uint32_t idesc_qk = ptx::make_idesc(1, 0, 0, 0, 0, 128, PR_KEYS), idesc_pv = ptx::make_idesc(1, 0, 0, 0, 1, 128, DH);
+  {
+    LaunchScope scope(h, stream, KERNEL_ATTN);
+    HERO_CUDA(launch_dependent(kern, dim3((unsigned)(p.tiles * p.c.nkv), (unsigned)cc->B), dim3(PR_THREADS), BYTES, stream, p, idesc_qk, idesc_pv));
+  }
+  return HERO_OK;
+}
+
+hero_status launch_prompt(hero_handle* h, const hero_block_cache* cc, const BlockAttnParams& p_, bool bf, cudaStream_t stream) {
+  BlockAttnParams p = p_;
+  const long long tiles = ((long long)p.c.max_rows * p.group + PR_ROWS - 1) / PR_ROWS;
+  HERO_REQUIRE(tiles * p.c.nkv < (1ll << 31), HERO_ERR_UNSUPPORTED, "max_rows=%d nkv=%d: too many", p.c.max_rows, p.c.nkv);
+  p.tiles = (int)tiles;
+  return cc->dh == 64 ? launch<64>(h, cc, p, bf, stream) : launch<128>(h, cc, p, bf, stream);
+}
+
+}  // namespace hero
