@@ -5,7 +5,7 @@
 // and walks its keys in tiles of 128.  Keys and values have to become FP16 operands in shared memory on the way: done once per CTA,
 // for both row tiles.  Roles:
 //   warps 0-3, 4-7   softmax of row tile 0 / 1, one row per thread: no reduction across threads.  Scores are read from tensor memory
-//                    twice (maximum, then exponentials); P goes back as FP16 into the columns of the scores and is the A operand of
+//                    once (again only when the maximum moves); P goes back as FP16 into the columns of the scores and is the A operand of
 //                    P V from there.  While one tile is in its softmax the tensor cores work for the other.
 //   warps 8-11       codes -> FP16: 16-byte loads one tile ahead in registers, exact conversion, stores in the 128-byte swizzled
 //                    operand layout.  Warp 8 also publishes what the softmax needs of each 16 tokens: key scale, value scale
@@ -154,82 +154,76 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
       vref = ref.x;
       const int valid = lim - j * PR_KEYS;         // keys of this tile that the row sees
       const bool whole = __all_sync(0xffffffffu, valid >= PR_KEYS);
-      // ---- pass 1: largest exponent
-      float mx = -INFINITY;
+      // ---- e' = 2^(score - maximum + 11 + log2 rv), the row sum and the largest exponent in one reading; P waits in registers until
+      // it is known that the maximum may stay (else it moves and the tile is read again; always so for the first tile)
+      uint32_t w[64];
+      float l_new, mx;
+      auto read = [&]() {
+        l_new = l;
+        mx = -INFINITY;
+        uint32_t x[2][16];
+        ptx::tmem_ld16(s_col, x[0]);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        uint32_t x[32];
-        ptx::tmem_ld32(s_col + 32 * k, x);
-        ptx::tmem_ld_wait();
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int g = 0; g < 8; ++g) {
+          ptx::tmem_ld_wait();
+          if (g < 7) ptx::tmem_ld16(s_col + 16 * (g + 1), x[(g + 1) & 1]);
+          const uint32_t (&y)[16] = x[g & 1];
+          const float4 gi = *reinterpret_cast<const float4*>(&info[g]);
+          const float fk = f * gi.x, ug = u + gi.y;
+          float2 sum = make_float2(0.f, 0.f);
           float m = -INFINITY;
           if (whole) {
 #pragma unroll
-            for (int i = 0; i < 16; i += 2) m = ptx::max3(m, __uint_as_float(x[16 * h + i]), __uint_as_float(x[16 * h + i + 1]));
+            for (int i = 0; i < 8; ++i) {
+              const float2 a = __ffma2_rn(make_float2(__uint_as_float(y[2 * i]), __uint_as_float(y[2 * i + 1])), make_float2(fk, fk), make_float2(ug, ug));
+              m = ptx::max3(m, a.x, a.y);
+              const float2 e = make_float2(ex2(a.x), ex2(a.y));
+              sum = __fadd2_rn(sum, e);
+              w[8 * g + i] = pack_f16(e.x, e.y);
+            }
           } else {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) m = fmaxf(m, 32 * k + 16 * h + i < valid ? __uint_as_float(x[16 * h + i]) : -INFINITY);
+            for (int i = 0; i < 8; ++i) {
+              const int key = 16 * g + 2 * i;
+              const float a0 = key < valid ? fmaf(__uint_as_float(y[2 * i]), fk, ug) : -INFINITY;
+              const float a1 = key + 1 < valid ? fmaf(__uint_as_float(y[2 * i + 1]), fk, ug) : -INFINITY;
+              m = ptx::max3(m, a0, a1);
+              const float e0 = ex2(a0), e1 = ex2(a1);
+              sum.x += e0; sum.y += e1;
+              w[8 * g + i] = pack_f16(e0, e1);
+            }
           }
-          if (m > -INFINITY) mx = fmaxf(mx, fmaf(m, f * info[2 * k + h].ks, u));
+          l_new = fmaf(sum.x + sum.y, gi.z, l_new);
+          mx = fmaxf(mx, m - gi.y);
         }
-      }
-      // ---- the maximum moves (always in the first tile), the value reference moves: O and the sum follow
-      const bool moves = j == 0 || mx > P_SHIFT + MAX_SLACK;
-      if (__any_sync(0xffffffffu, moves) || ref.y != 1.0f) {
+      };
+      for (bool settled = false;; settled = true) {
+        read();
+        if (settled || !(__any_sync(0xffffffffu, j == 0 || mx > P_SHIFT + MAX_SLACK) || ref.y != 1.0f)) break;
         float d = mx - P_SHIFT;
         if (j > 0) d = fmaxf(d, 0.f);
         if (mx == -INFINITY) d = 0.f;
         u -= d;
         if (j > 0) {
+          // O and the sum follow the maximum, O the value reference
           const float a = ex2(-d);
           l *= a;
           const float ao = a * ref.y;
 #pragma unroll
-          for (int k = 0; k < DH / 32; ++k) {
-            uint32_t x[32];
-            ptx::tmem_ld32(o_col + 32 * k, x);
+          for (int k = 0; k < DH / 16; ++k) {
+            uint32_t x[16];
+            ptx::tmem_ld16(o_col + 16 * k, x);
             ptx::tmem_ld_wait();
 #pragma unroll
-            for (int i = 0; i < 32; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * ao);
-            ptx::tmem_st32(o_col + 32 * k, x);
+            for (int i = 0; i < 16; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * ao);
+            ptx::tmem_st16(o_col + 16 * k, x);
           }
         }
       }
-      // ---- pass 2: e' = 2^(score - maximum + 11 + log2 rv); P over the scores' columns (those behind are read already)
+      l = l_new;
+      // P over the scores' columns
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        uint32_t x[32], w[16];
-        ptx::tmem_ld32(s_col + 32 * k, x);
-        ptx::tmem_ld_wait();
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const float4 gi = *reinterpret_cast<const float4*>(&info[2 * k + h]);
-          const float fk = f * gi.x, ug = u + gi.y;
-          float2 sum = make_float2(0.f, 0.f);
-          if (whole) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const float2 a = __ffma2_rn(make_float2(__uint_as_float(x[16 * h + 2 * i]), __uint_as_float(x[16 * h + 2 * i + 1])), make_float2(fk, fk),
-                                          make_float2(ug, ug));
-              const float2 e = make_float2(ex2(a.x), ex2(a.y));
-              sum = __fadd2_rn(sum, e);
-              w[8 * h + i] = pack_f16(e.x, e.y);
-            }
-          } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const int key = 32 * k + 16 * h + 2 * i;
-              const float e0 = key < valid ? ex2(fmaf(__uint_as_float(x[16 * h + 2 * i]), fk, ug)) : 0.f;
-              const float e1 = key + 1 < valid ? ex2(fmaf(__uint_as_float(x[16 * h + 2 * i + 1]), fk, ug)) : 0.f;
-              sum.x += e0; sum.y += e1;
-              w[8 * h + i] = pack_f16(e0, e1);
-            }
-          }
-          l = fmaf(sum.x + sum.y, gi.z, l);
-        }
-        ptx::tmem_st16(s_col + 16 * k, w);
-      }
+      for (int k = 0; k < 4; ++k) ptx::tmem_st16(s_col + 16 * k, *reinterpret_cast<const uint32_t(*)[16]>(&w[16 * k]));
       ptx::tmem_st_wait();
       ptx::tc_fence_before();
       __syncwarp();
@@ -284,49 +278,56 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
     }
   } else if (warp < PR_MMA_WARP) {
     // ------------------------------------------------------------------ codes -> FP16 operands
-    constexpr int PPR = DH / 16;                   // 16-code pieces of a row = pieces of a tile per thread
-    constexpr int RPI = 128 / PPR;                 // rows between a thread's pieces
-    const int ct = threadIdx.x - PR_SM_WARPS * 32, piece = ct % PPR, r0 = ct / PPR;
+    constexpr int NP = DH / 16;                    // 16-code pieces of a tile per thread
+    constexpr int NSUB = DH / 64;
+    // four lanes take 64 features of a row, eight lanes two rows: whole sectors from memory, no bank conflicts in the operand tile
+    const int ct = threadIdx.x - PR_SM_WARPS * 32, piece = ct & 3, r0 = ct >> 2;       // rows r0 + 32 i
     const bool scribe = warp == PR_SM_WARPS;       // publishes the scale records
-    const uint8_t* kb = c.k + (long long)hk * c.head_stride + piece * 16;
-    const uint8_t* vb = c.v + (long long)hk * c.head_stride + piece * 16;
+    const long long mine = (long long)hk * c.head_stride + (long long)(r0 & 15) * c.ld + piece * 16;
+    uint8_t* const to = smem + (r0 >> 3) * 1024 + (r0 & 7) * 128;
+    const uint32_t swz0 = ((2 * piece) ^ (r0 & 7)) << 4, swz1 = ((2 * piece + 1) ^ (r0 & 7)) << 4;
     auto page_of = [&](int j) {                    // lane g < 8: page of tokens 128 j + 16 g ..
       const int tok = j * PR_KEYS + 16 * lane;
       return lane < 8 && tok < L ? page_for_read(c, b, tok >> c.page_shift) : -1;
     };
-    auto load = [&](const uint8_t* from, int j, int ids, uint4 (&raw)[PPR]) {
+    auto offset_of = [&](int j, int id) {          // and where they begin in the pool
+      return (long long)id * c.page_stride + (long long)((j * PR_KEYS + 16 * lane) & (c.page - 1)) * c.ld;
+    };
+    auto load = [&](const uint8_t* pool, int j, long long off, uint4 (&raw)[NP]) {
 #pragma unroll
-      for (int i = 0; i < PPR; ++i) {
-        const int row = r0 + RPI * i, tok = j * PR_KEYS + row;
-        const int id = __shfl_sync(0xffffffffu, ids, DH == 128 ? i : 2 * i + (ct >> 6));
-        raw[i] = make_uint4(0, 0, 0, 0);           // slots behind the end may hold anything (e4m3: NaN)
-        if (tok < L) raw[i] = __ldg(reinterpret_cast<const uint4*>(from + (long long)id * c.page_stride + (long long)(tok & (c.page - 1)) * c.ld));
+      for (int i = 0; i < 4; ++i) {
+        const long long at = mine + __shfl_sync(0xffffffffu, off, 2 * i + (r0 >> 4));
+#pragma unroll
+        for (int h = 0; h < NSUB; ++h) {
+          raw[i * NSUB + h] = make_uint4(0, 0, 0, 0);          // slots behind the end may hold anything (e4m3: NaN)
+          if (j * PR_KEYS + r0 + 32 * i < L) raw[i * NSUB + h] = __ldg(reinterpret_cast<const uint4*>(pool + at + 64 * h));
+        }
       }
     };
-    auto store = [&](uint8_t* tile, const uint4 (&raw)[PPR]) {
+    auto store = [&](uint32_t tile, const uint4 (&raw)[NP]) {
 #pragma unroll
-      for (int i = 0; i < PPR; ++i) {
-        const int row = r0 + RPI * i;
-        uint32_t h[8];
-        codes4_to_f16<F8>(raw[i].x, h[0], h[1]);
-        codes4_to_f16<F8>(raw[i].y, h[2], h[3]);
-        codes4_to_f16<F8>(raw[i].z, h[4], h[5]);
-        codes4_to_f16<F8>(raw[i].w, h[6], h[7]);
-        // 16-byte chunks 2 piece and 2 piece + 1 of the row; half of the lanes store them in the other order (no bank conflicts)
-        uint8_t* at = tile + (piece >> 2) * Cfg::SUB + (row >> 3) * 1024 + (row & 7) * 128;
-        const int first = (2 * piece) & 7, swap = DH == 128 ? piece >> 2 : 0;
-        *reinterpret_cast<uint4*>(at + (((first + swap) ^ (row & 7)) << 4)) = swap ? make_uint4(h[4], h[5], h[6], h[7]) : make_uint4(h[0], h[1], h[2], h[3]);
-        *reinterpret_cast<uint4*>(at + (((first + 1 - swap) ^ (row & 7)) << 4)) = swap ? make_uint4(h[0], h[1], h[2], h[3]) : make_uint4(h[4], h[5], h[6], h[7]);
-      }
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int h = 0; h < NSUB; ++h) {
+          const uint4 x = raw[i * NSUB + h];
+          uint32_t y[8];
+          codes4_to_f16<F8>(x.x, y[0], y[1]);
+          codes4_to_f16<F8>(x.y, y[2], y[3]);
+          codes4_to_f16<F8>(x.z, y[4], y[5]);
+          codes4_to_f16<F8>(x.w, y[6], y[7]);
+          uint8_t* at = to + tile + h * Cfg::SUB + i * 4096;
+          *reinterpret_cast<uint4*>(at + swz0) = make_uint4(y[0], y[1], y[2], y[3]);
+          *reinterpret_cast<uint4*>(at + swz1) = make_uint4(y[4], y[5], y[6], y[7]);
+        }
       ptx::fence_proxy_async_smem();
       __syncwarp();
     };
-    uint4 kr[PPR], vr[PPR];
+    uint4 kr[NP], vr[NP];
     bool ok = true;
     int ids = page_of(0), ids_next = page_of(1);
     float2 sc = make_float2(0.f, 0.f);             // scribe's lane g: scales of tokens 128 j + 16 g ..
     auto scales = [&](int i) { return i >= 0 ? make_float2(__ldg(c.ks + (long long)i * c.nkv + hk), __ldg(c.vs + (long long)i * c.nkv + hk)) : make_float2(0.f, 0.f); };
-    if (n_all > 0) { load(kb, 0, ids, kr); load(vb, 0, ids, vr); }
+    if (n_all > 0) { load(c.k, 0, offset_of(0, ids), kr); load(c.v, 0, offset_of(0, ids), vr); }
     if (scribe) sc = scales(ids);
     float vref = 0.f;
     for (int j = 0; j < n_all; ++j) {
@@ -348,14 +349,15 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
         sc = scales(ids_next);
       }
       const int ids_after = page_of(j + 2);
+      const long long off = offset_of(j + 1, ids_next);
       ok = ok && ptx::mbar_wait(&k_empty[st], par, c.err, 0x8400 | st);
-      store(smem + Cfg::OFF_K + st * Cfg::TILE, kr);
+      store(Cfg::OFF_K + st * Cfg::TILE, kr);
       if (lane == 0) ptx::mbar_arrive(&k_full[st]);
-      if (j + 1 < n_all) load(kb, j + 1, ids_next, kr);
+      if (j + 1 < n_all) load(c.k, j + 1, off, kr);
       ok = ok && ptx::mbar_wait(&v_empty[st], par, c.err, 0x8500 | st);
-      store(smem + Cfg::OFF_V + st * Cfg::TILE, vr);
+      store(Cfg::OFF_V + st * Cfg::TILE, vr);
       if (lane == 0) ptx::mbar_arrive(&v_full[st]);
-      if (j + 1 < n_all) load(vb, j + 1, ids_next, vr);
+      if (j + 1 < n_all) load(c.v, j + 1, off, vr);
       ids_next = ids_after;
       if (!__all_sync(0xffffffffu, ok)) break;
     }
