@@ -4,13 +4,14 @@
 // One CTA takes 256 rows ((row of the sequence, query head of the group) pairs, two tiles of 128) of one (sequence, key / value head)
 // and walks its keys in tiles of 128.  Keys and values have to become FP16 operands in shared memory on the way: done once per CTA,
 // for both row tiles.  Roles:
-//   warps 0-3, 4-7   softmax of row tile 0 / 1, one row per thread: no reduction across threads.  Scores are read from tensor memory
-//                    once (again only when the maximum moves); P goes back as FP16 into the columns of the scores and is the A operand of
-//                    P V from there.  While one tile is in its softmax the tensor cores work for the other.
-//   warps 8-11       codes -> FP16: 16-byte loads one tile ahead in registers, exact conversion, stores in the 128-byte swizzled
+//   warps 0-3, 4-7   softmax of row tile 0 / 1, one row per thread: no reduction across threads.  A tile of keys is two halves of 64
+//                    with a score buffer each, so the softmax of one half runs beside the products of the other.  Scores are read
+//                    from tensor memory once (again only when the maximum moves); P goes back as FP16 into the columns of
+//                    the scores and is the A operand of P V from there.
+//   warps 8-15       codes -> FP16: 16-byte loads one tile ahead in registers, exact conversion, stores in the 128-byte swizzled
 //                    operand layout.  Warp 8 also publishes what the softmax needs of each 16 tokens: key scale, value scale
 //                    relative to the largest so far.
-//   warps 12, 13     issue the products of row tile 0 / 1
+//   warps 16, 17     issue the products of row tile 0 / 1
 // The value scale of a page is folded into the exponent, e' = 2^(x + log2 rv), so that it costs nothing per element; the row sum
 // undoes it per 16 tokens (rv is kept above 2^-40, where P is zero anyway).  As in the kernel for few rows, queries are scaled into
 // FP16 by a power of two, P carries a factor 2^11 and the running maximum moves only beyond 2^4: the accumulator in
@@ -20,24 +21,23 @@
 
 namespace hero {
 
-constexpr int PR_SM_WARPS = 8, PR_CV_WARPS = 4;
+constexpr int PR_SM_WARPS = 8, PR_CV_WARPS = 8;
 constexpr int PR_MMA_WARP = PR_SM_WARPS + PR_CV_WARPS;         // and the next one
 constexpr int PR_THREADS = (PR_MMA_WARP + 2) * 32;
 constexpr int PR_ROWS = 256, PR_KEYS = 128;
 constexpr int PR_INFO = 4;                                     // ring of scale records
 constexpr float PR_MIN_RV = 9.094947e-13f;                     // 2^-40
 
-struct KeyInfo { float ks, lrv, inv_rv, pad; };                // of 16 tokens: key scale, log2 and reciprocal of the relative value scale
 
 template <int DH>
 struct PromptCfg {
   static constexpr int SUB = 128 * 128;                        // one [128 rows x 64 features] FP16 sub-tile, 128-byte rows
   static constexpr int TILE = SUB * (DH / 64);
   static constexpr int OFF_K = 2 * TILE, OFF_V = OFF_K + 2 * TILE;
-  static constexpr int OFF_INFO = OFF_V + 2 * TILE;            // KeyInfo [PR_INFO][8]
+  static constexpr int OFF_INFO = OFF_V + 2 * TILE;            // float4 [PR_INFO][8], of 16 tokens each: key scale, log2 and reciprocal of the relative value scale
   static constexpr int OFF_REF = OFF_INFO + PR_INFO * 8 * 16;  // float2 [PR_INFO]: largest value scale so far, its old / new ratio
   static constexpr int OFF_BARS = OFF_REF + PR_INFO * 8;
-  static constexpr int NBARS = 2 + 4 + 4 + 2 * PR_INFO + 6;
+  static constexpr int NBARS = 2 + 4 + 4 + 2 * PR_INFO + 12;
   static constexpr int BYTES = 1024 + OFF_BARS + NBARS * 8 + 16;
   static constexpr int S_COL = 0, O_COL = 256;                 // scores (then P) 2 x 128 columns, O 2 x DH columns
 };
@@ -56,10 +56,11 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
   uint64_t* v_empty = v_full + 2;                // [2]
   uint64_t* i_full = v_empty + 2;                // [PR_INFO] warp 8 -> softmax
   uint64_t* i_empty = i_full + PR_INFO;          // [PR_INFO] softmax -> warp 8
-  uint64_t* s_full = i_empty + PR_INFO;          // [2] scores of a tile are complete
-  uint64_t* p_full = s_full + 2;                 // [2] its P is in place (and O rescaled)
-  uint64_t* o_full = p_full + 2;                 // [2] its P V is complete
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(o_full + 2);
+  uint64_t* s_full = i_empty + PR_INFO;          // [tile][half] scores are complete
+  uint64_t* p_full = s_full + 4;                 // [tile][half] P is in place (and O rescaled)
+  uint64_t* o_full = p_full + 4;                 // [tile] P V of a half is complete
+  uint64_t* o_last = o_full + 2;                 // [tile] the last one is
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(o_last + 2);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
@@ -67,8 +68,9 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
       ptx::mbar_init(&q_full[i], 4);
       ptx::mbar_init(&k_full[i], PR_CV_WARPS); ptx::mbar_init(&k_empty[i], 2);
       ptx::mbar_init(&v_full[i], PR_CV_WARPS); ptx::mbar_init(&v_empty[i], 2);
-      ptx::mbar_init(&s_full[i], 1); ptx::mbar_init(&p_full[i], 4); ptx::mbar_init(&o_full[i], 1);
+      ptx::mbar_init(&o_full[i], 1); ptx::mbar_init(&o_last[i], 1);
     }
+    for (int i = 0; i < 4; ++i) { ptx::mbar_init(&s_full[i], 1); ptx::mbar_init(&p_full[i], 4); }
     for (int i = 0; i < PR_INFO; ++i) { ptx::mbar_init(&i_full[i], 1); ptx::mbar_init(&i_empty[i], PR_SM_WARPS); }
     ptx::fence_mbar_init();
   }
@@ -142,97 +144,101 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
     for (int j = 0; j < n_all; ++j) {
       const int slot = j % PR_INFO;
       ok = __all_sync(0xffffffffu, ok && ptx::mbar_wait(&i_full[slot], (j / PR_INFO) & 1, c.err, 0x8000 | slot));
-      if (j < n) ok = __all_sync(0xffffffffu, ok && ptx::mbar_wait(&s_full[t], j & 1, c.err, 0x8100 | t));
       if (j >= n || !ok) {                         // the other row tile's keys: only hand the record back
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(&i_empty[slot]);
         continue;
       }
-      ptx::tc_fence_after();
-      const KeyInfo* info = reinterpret_cast<const KeyInfo*>(smem + Cfg::OFF_INFO) + slot * 8;
       const float2 ref = reinterpret_cast<const float2*>(smem + Cfg::OFF_REF)[slot];
       vref = ref.x;
-      const int valid = lim - j * PR_KEYS;         // keys of this tile that the row sees
-      const bool whole = __all_sync(0xffffffffu, valid >= PR_KEYS);
-      // ---- e' = 2^(score - maximum + 11 + log2 rv), the row sum and the largest exponent in one reading; P waits in registers until
-      // it is known that the maximum may stay (else it moves and the tile is read again; always so for the first tile)
-      uint32_t w[64];
-      float l_new, mx;
-      auto read = [&]() {
-        l_new = l;
-        mx = -INFINITY;
-        uint32_t x[2][16];
-        ptx::tmem_ld16(s_col, x[0]);
+#pragma unroll 1
+      for (int h = 0; h < 2; ++h) {
+        ok = __all_sync(0xffffffffu, ok && ptx::mbar_wait(&s_full[2 * t + h], j & 1, c.err, 0x8100 | t));
+        if (!ok) break;
+        ptx::tc_fence_after();
+        const uint32_t s_half = s_col + 64 * h;
+        const float4* info = reinterpret_cast<const float4*>(smem + Cfg::OFF_INFO) + slot * 8 + 4 * h;
+        const int valid = lim - j * PR_KEYS - 64 * h;                      // keys of this half that the row sees
+        const bool whole = __all_sync(0xffffffffu, valid >= 64), first = (j | h) == 0, turn = h == 0 && ref.y != 1.0f;
+        // ---- e' = 2^(score - maximum + 11 + log2 rv), the row sum and the largest exponent in one reading; P waits in registers
+        // until it is known that the maximum may stay (else it moves and the half is read again; always so for the first one)
+        uint32_t w[32];
+        float l_new, mx;
+        for (bool settled = false;; settled = true) {
+          l_new = l;
+          mx = -INFINITY;
+          uint32_t x[2][16];
+          ptx::tmem_ld16(s_half, x[0]);
 #pragma unroll
-        for (int g = 0; g < 8; ++g) {
-          ptx::tmem_ld_wait();
-          if (g < 7) ptx::tmem_ld16(s_col + 16 * (g + 1), x[(g + 1) & 1]);
-          const uint32_t (&y)[16] = x[g & 1];
-          const float4 gi = *reinterpret_cast<const float4*>(&info[g]);
-          const float fk = f * gi.x, ug = u + gi.y;
-          float2 sum = make_float2(0.f, 0.f);
-          float m = -INFINITY;
-          if (whole) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const float2 a = __ffma2_rn(make_float2(__uint_as_float(y[2 * i]), __uint_as_float(y[2 * i + 1])), make_float2(fk, fk), make_float2(ug, ug));
-              m = ptx::max3(m, a.x, a.y);
-              const float2 e = make_float2(ex2(a.x), ex2(a.y));
-              sum = __fadd2_rn(sum, e);
-              w[8 * g + i] = pack_f16(e.x, e.y);
-            }
-          } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const int key = 16 * g + 2 * i;
-              const float a0 = key < valid ? fmaf(__uint_as_float(y[2 * i]), fk, ug) : -INFINITY;
-              const float a1 = key + 1 < valid ? fmaf(__uint_as_float(y[2 * i + 1]), fk, ug) : -INFINITY;
-              m = ptx::max3(m, a0, a1);
-              const float e0 = ex2(a0), e1 = ex2(a1);
-              sum.x += e0; sum.y += e1;
-              w[8 * g + i] = pack_f16(e0, e1);
-            }
-          }
-          l_new = fmaf(sum.x + sum.y, gi.z, l_new);
-          mx = fmaxf(mx, m - gi.y);
-        }
-      };
-      for (bool settled = false;; settled = true) {
-        read();
-        if (settled || !(__any_sync(0xffffffffu, j == 0 || mx > P_SHIFT + MAX_SLACK) || ref.y != 1.0f)) break;
-        float d = mx - P_SHIFT;
-        if (j > 0) d = fmaxf(d, 0.f);
-        if (mx == -INFINITY) d = 0.f;
-        u -= d;
-        if (j > 0) {
-          // O and the sum follow the maximum, O the value reference
-          const float a = ex2(-d);
-          l *= a;
-          const float ao = a * ref.y;
-#pragma unroll
-          for (int k = 0; k < DH / 16; ++k) {
-            uint32_t x[16];
-            ptx::tmem_ld16(o_col + 16 * k, x);
+          for (int g = 0; g < 4; ++g) {
             ptx::tmem_ld_wait();
+            if (g < 3) ptx::tmem_ld16(s_half + 16 * (g + 1), x[(g + 1) & 1]);
+            const uint32_t (&y)[16] = x[g & 1];
+            const float4 gi = info[g];
+            const float fk = f * gi.x, ug = u + gi.y;
+            float2 sum = make_float2(0.f, 0.f);
+            float m = -INFINITY;
+            if (whole) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * ao);
-            ptx::tmem_st16(o_col + 16 * k, x);
+              for (int i = 0; i < 8; ++i) {
+                const float2 a = __ffma2_rn(make_float2(__uint_as_float(y[2 * i]), __uint_as_float(y[2 * i + 1])), make_float2(fk, fk), make_float2(ug, ug));
+                m = ptx::max3(m, a.x, a.y);
+                const float2 e = make_float2(ex2(a.x), ex2(a.y));
+                sum = __fadd2_rn(sum, e);
+                w[8 * g + i] = pack_f16(e.x, e.y);
+              }
+            } else {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                const int key = 16 * g + 2 * i;
+                const float a0 = key < valid ? fmaf(__uint_as_float(y[2 * i]), fk, ug) : -INFINITY;
+                const float a1 = key + 1 < valid ? fmaf(__uint_as_float(y[2 * i + 1]), fk, ug) : -INFINITY;
+                m = ptx::max3(m, a0, a1);
+                const float e0 = ex2(a0), e1 = ex2(a1);
+                sum.x += e0; sum.y += e1;
+                w[8 * g + i] = pack_f16(e0, e1);
+              }
+            }
+            l_new = fmaf(sum.x + sum.y, gi.z, l_new);
+            mx = fmaxf(mx, m - gi.y);
+          }
+          if (settled || !(__any_sync(0xffffffffu, first || mx > P_SHIFT + MAX_SLACK) || turn)) break;
+          float d = mx - P_SHIFT;
+          if (!first) d = fmaxf(d, 0.f);
+          if (mx == -INFINITY) d = 0.f;
+          u -= d;
+          if (!first) {
+            // O and the sum follow the maximum, O the value reference; the previous half's P V has to be complete
+            ok = __all_sync(0xffffffffu, ok && ptx::mbar_wait(&o_full[t], (h + 1) & 1, c.err, 0x8180 | t));
+            ptx::tc_fence_after();
+            const float a = ex2(-d);
+            l *= a;
+            const float ao = turn ? a * ref.y : a;
+#pragma unroll
+            for (int k = 0; k < DH / 16; ++k) {
+              ptx::tmem_ld16(o_col + 16 * k, x[0]);
+              ptx::tmem_ld_wait();
+#pragma unroll
+              for (int i = 0; i < 16; ++i) x[0][i] = __float_as_uint(__uint_as_float(x[0][i]) * ao);
+              ptx::tmem_st16(o_col + 16 * k, x[0]);
+            }
           }
         }
-      }
-      l = l_new;
-      // P over the scores' columns
+        l = l_new;
+        // P over the scores' columns
 #pragma unroll
-      for (int k = 0; k < 4; ++k) ptx::tmem_st16(s_col + 16 * k, *reinterpret_cast<const uint32_t(*)[16]>(&w[16 * k]));
-      ptx::tmem_st_wait();
-      ptx::tc_fence_before();
-      __syncwarp();
-      if (lane == 0) { ptx::mbar_arrive(&p_full[t]); ptx::mbar_arrive(&i_empty[slot]); }
+        for (int k = 0; k < 2; ++k) ptx::tmem_st16(s_half + 16 * k, *reinterpret_cast<const uint32_t(*)[16]>(&w[16 * k]));
+        ptx::tmem_st_wait();
+        ptx::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(&p_full[2 * t + h]);
+      }
+      if (lane == 0) ptx::mbar_arrive(&i_empty[slot]);
     }
     // ---- output
     float scale_o = 0.f;
     if (n > 0) {
-      ok = __all_sync(0xffffffffu, ok && ptx::mbar_wait(&o_full[t], (n - 1) & 1, c.err, 0x8200 | t));
+      ok = __all_sync(0xffffffffu, ok && ptx::mbar_wait(&o_last[t], 0, c.err, 0x8200 | t));
       ptx::tc_fence_after();
       scale_o = l != 0.f ? vref / l : 0.f;
     }
@@ -278,10 +284,10 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
     }
   } else if (warp < PR_MMA_WARP) {
     // ------------------------------------------------------------------ codes -> FP16 operands
-    constexpr int NP = DH / 16;                    // 16-code pieces of a tile per thread
+    constexpr int NP = DH / 32;                    // 16-code pieces of a tile per thread
     constexpr int NSUB = DH / 64;
     // four lanes take 64 features of a row, eight lanes two rows: whole sectors from memory, no bank conflicts in the operand tile
-    const int ct = threadIdx.x - PR_SM_WARPS * 32, piece = ct & 3, r0 = ct >> 2;       // rows r0 + 32 i
+    const int ct = threadIdx.x - PR_SM_WARPS * 32, piece = ct & 3, r0 = ct >> 2;       // rows r0 + 64 i
     const bool scribe = warp == PR_SM_WARPS;       // publishes the scale records
     const long long mine = (long long)hk * c.head_stride + (long long)(r0 & 15) * c.ld + piece * 16;
     uint8_t* const to = smem + (r0 >> 3) * 1024 + (r0 & 7) * 128;
@@ -295,18 +301,18 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
     };
     auto load = [&](const uint8_t* pool, int j, long long off, uint4 (&raw)[NP]) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const long long at = mine + __shfl_sync(0xffffffffu, off, 2 * i + (r0 >> 4));
+      for (int i = 0; i < 2; ++i) {
+        const long long at = mine + __shfl_sync(0xffffffffu, off, 4 * i + (r0 >> 4));
 #pragma unroll
         for (int h = 0; h < NSUB; ++h) {
           raw[i * NSUB + h] = make_uint4(0, 0, 0, 0);          // slots behind the end may hold anything (e4m3: NaN)
-          if (j * PR_KEYS + r0 + 32 * i < L) raw[i * NSUB + h] = __ldg(reinterpret_cast<const uint4*>(pool + at + 64 * h));
+          if (j * PR_KEYS + r0 + 64 * i < L) raw[i * NSUB + h] = __ldg(reinterpret_cast<const uint4*>(pool + at + 64 * h));
         }
       }
     };
     auto store = [&](uint32_t tile, const uint4 (&raw)[NP]) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int h = 0; h < NSUB; ++h) {
           const uint4 x = raw[i * NSUB + h];
@@ -315,7 +321,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
           codes4_to_f16<F8>(x.y, y[2], y[3]);
           codes4_to_f16<F8>(x.z, y[4], y[5]);
           codes4_to_f16<F8>(x.w, y[6], y[7]);
-          uint8_t* at = to + tile + h * Cfg::SUB + i * 4096;
+          uint8_t* at = to + tile + h * Cfg::SUB + i * 8192;
           *reinterpret_cast<uint4*>(at + swz0) = make_uint4(y[0], y[1], y[2], y[3]);
           *reinterpret_cast<uint4*>(at + swz1) = make_uint4(y[4], y[5], y[6], y[7]);
         }
@@ -370,40 +376,50 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
     const uint64_t qd = ptx::smem_desc(kmaj, ptx::smem_u32(smem + t * Cfg::TILE));
     const uint64_t kd0 = ptx::smem_desc(kmaj, ptx::smem_u32(smem + Cfg::OFF_K)), vd0 = ptx::smem_desc(vmaj, ptx::smem_u32(smem + Cfg::OFF_V));
     const uint32_t s_tmem = tmem_base + Cfg::S_COL + t * 128, o_tmem = tmem_base + Cfg::O_COL + t * DH;
-    auto scores = [&](int j) -> bool {
-      const int st = j & 1;
-      if (!ptx::mbar_wait(&k_full[st], (j >> 1) & 1, c.err, 0x8600 | st)) return false;
-      ptx::tc_fence_after();
+    auto scores = [&](int j, int h) {              // of 64 keys, into buffer h
       if (issue) {
-        const uint64_t kd = kd0 + (uint32_t)((st * Cfg::TILE) >> 4);
+        const uint64_t kd = kd0 + (uint32_t)(((j & 1) * Cfg::TILE + h * 8192) >> 4);
 #pragma unroll
         for (int k = 0; k < DH / 16; ++k) {
           const uint32_t o = (uint32_t)(((k >> 2) * Cfg::SUB + (k & 3) * 32) >> 4);
-          ptx::umma_f16(s_tmem, qd + o, kd + o, idesc_qk, k != 0);
+          ptx::umma_f16(s_tmem + 64 * h, qd + o, kd + o, idesc_qk, k != 0);
         }
-        ptx::umma_commit(&k_empty[st]);
-        ptx::umma_commit(&s_full[t]);
+        ptx::umma_commit(&s_full[2 * t + h]);
+        if (h == 1) ptx::umma_commit(&k_empty[j & 1]);
       }
-      return true;
+    };
+    auto keys_ready = [&](int j) {
+      const bool r = ptx::mbar_wait(&k_full[j & 1], (j >> 1) & 1, c.err, 0x8600 | (j & 1));
+      ptx::tc_fence_after();
+      return r;
     };
     bool ok = true;
-    if (n > 0) ok = ptx::mbar_wait(&q_full[t], 0, c.err, 0x8700 | t) && scores(0);
+    if (n > 0) {
+      ok = ptx::mbar_wait(&q_full[t], 0, c.err, 0x8700 | t) && keys_ready(0);
+      if (ok) { scores(0, 0); scores(0, 1); }
+    }
     for (int j = 0; j < n && ok; ++j) {
       const int st = j & 1;
-      ok = ptx::mbar_wait(&v_full[st], (j >> 1) & 1, c.err, 0x8800 | st) && ptx::mbar_wait(&p_full[t], j & 1, c.err, 0x8900 | t);
-      if (!ok) break;
-      ptx::tc_fence_after();
-      if (issue) {
-        const uint64_t vd = vd0 + (uint32_t)((st * Cfg::TILE) >> 4);
+      ok = ptx::mbar_wait(&v_full[st], (j >> 1) & 1, c.err, 0x8800 | st);
+#pragma unroll 1
+      for (int h = 0; h < 2 && ok; ++h) {
+        ok = ptx::mbar_wait(&p_full[2 * t + h], j & 1, c.err, 0x8900 | t);
+        if (!ok) break;
+        ptx::tc_fence_after();
+        if (issue) {
+          const uint64_t vd = vd0 + (uint32_t)((st * Cfg::TILE + h * 8192) >> 4);
 #pragma unroll
-        for (int k = 0; k < PR_KEYS / 16; ++k)     // 16 keys: 8 columns of P, 2 eight-key groups of V
-          ptx::umma_f16_ta(o_tmem, s_tmem + 8 * k, vd + (uint32_t)((k * 2048) >> 4), idesc_pv, (j | k) != 0);
-        ptx::umma_commit(&v_empty[st]);
-        ptx::umma_commit(&o_full[t]);
-      }
-      if (j + 1 < n) {
-        // the next scores take the place of P: P V has to be complete
-        ok = ptx::mbar_wait(&o_full[t], j & 1, c.err, 0x8A00 | t) && scores(j + 1);
+          for (int k = 0; k < 4; ++k)              // 16 keys: 8 columns of P, 2 eight-key groups of V
+            ptx::umma_f16_ta(o_tmem, s_tmem + 64 * h + 8 * k, vd + (uint32_t)((k * 2048) >> 4), idesc_pv, (j | h | k) != 0);
+          if (h == 1) ptx::umma_commit(&v_empty[st]);
+          ptx::umma_commit(&o_full[t]);
+          if (h == 1 && j + 1 == n) ptx::umma_commit(&o_last[t]);
+        }
+        if (j + 1 < n) {
+          // the next tile's scores of this half take the place of its P: P V has to be complete
+          ok = (h == 1 || keys_ready(j + 1)) && ptx::mbar_wait(&o_full[t], h, c.err, 0x8A00 | t);
+          if (ok) scores(j + 1, h);
+        }
       }
     }
     // keys that only the other row tile needs
@@ -432,7 +448,7 @@ static hero_status launch(hero_handle* h, const hero_block_cache* cc, const Bloc
     HERO_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, BYTES));
     once.set(h->device);
   }
-  const uint32_t idesc_qk = ptx::make_idesc(1, 0, 0, 0, 0, 128, PR_KEYS), idesc_pv = ptx::make_idesc(1, 0, 0, 0, 1, 128, DH);
+  const uint32_t idesc_qk = ptx::make_idesc(1, 0, 0, 0, 0, 128, 64), idesc_pv = ptx::make_idesc(1, 0, 0, 0, 1, 128, DH);
   {
     LaunchScope scope(h, stream, KERNEL_ATTN);
     HERO_CUDA(launch_dependent(kern, dim3((unsigned)(p.tiles * p.c.nkv), (unsigned)cc->B), dim3(PR_THREADS), BYTES, stream, p, idesc_qk, idesc_pv));
