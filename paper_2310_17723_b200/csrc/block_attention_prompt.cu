@@ -9,13 +9,13 @@
 //                    from tensor memory once (again only when the maximum moves); P goes back as FP16 into the columns of
 //                    the scores and is the A operand of P V from there.
 //   warps 8-15       codes -> FP16: 16-byte loads one tile ahead in registers, exact conversion, stores in the 128-byte swizzled
-//                    operand layout.  Warp 8 also publishes what the softmax needs of each 16 tokens: key scale, value scale
-//                    relative to the largest so far.
+//                    operand layout
 //   warps 16, 17     issue the products of row tile 0 / 1
+//   warp 18          publishes what the softmax needs of each 16 tokens: key scale, value scale relative to the largest so far
 // The value scale of a page is folded into the exponent, e' = 2^(x + log2 rv), so that it costs nothing per element; the row sum
 // undoes it per 16 tokens (rv is kept above 2^-40, where P is zero anyway).  As in the kernel for few rows, queries are scaled into
-// FP16 by a power of two, P carries a factor 2^11 and the running maximum moves only beyond 2^4: the accumulator in
-// tensor memory is rescaled rarely.
+// FP16 by a power of two.  No maximum is taken per tile: P is formed with the maximum so far, and only if 16 probabilities
+// sum to more than FP16 holds (or in the first half) is the half read again for its maximum, O rescaled in tensor memory.
 #include "block_attention.cuh"
 #include <cmath>
 
@@ -23,9 +23,14 @@ namespace hero {
 
 constexpr int PR_SM_WARPS = 8, PR_CV_WARPS = 8;
 constexpr int PR_MMA_WARP = PR_SM_WARPS + PR_CV_WARPS;         // and the next one
-constexpr int PR_THREADS = (PR_MMA_WARP + 2) * 32;
+constexpr int PR_SCRIBE_WARP = PR_MMA_WARP + 2;
+constexpr int PR_THREADS = (PR_MMA_WARP + 4) * 32;             // whole warpgroups: the register file is dealt out to them
+// 640 threads are launched with 96 registers each; 256 x 136 + 256 x 72 + 128 x 56 = 60416 of those 61440
+constexpr int PR_SM_REGS = 136, PR_CV_REGS = 72, PR_MMA_REGS = 56;
 constexpr int PR_ROWS = 256, PR_KEYS = 128;
 constexpr int PR_INFO = 4;                                     // ring of scale records
+constexpr float PR_SHIFT = 8.0f;                               // P carries a factor 2^8 when the maximum has just moved
+constexpr float PR_MOST = 65504.0f;                            // and 16 of them sum to no more than this, so none overflows FP16
 constexpr float PR_MIN_RV = 9.094947e-13f;                     // 2^-40
 
 
@@ -54,8 +59,8 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
   uint64_t* k_empty = k_full + 2;                // [2] issuers -> converters
   uint64_t* v_full = k_empty + 2;                // [2]
   uint64_t* v_empty = v_full + 2;                // [2]
-  uint64_t* i_full = v_empty + 2;                // [PR_INFO] warp 8 -> softmax
-  uint64_t* i_empty = i_full + PR_INFO;          // [PR_INFO] softmax -> warp 8
+  uint64_t* i_full = v_empty + 2;                // [PR_INFO] scribe -> softmax
+  uint64_t* i_empty = i_full + PR_INFO;          // [PR_INFO] softmax -> scribe
   uint64_t* s_full = i_empty + PR_INFO;          // [tile][half] scores are complete
   uint64_t* p_full = s_full + 4;                 // [tile][half] P is in place (and O rescaled)
   uint64_t* o_full = p_full + 4;                 // [tile] P V of a half is complete
@@ -97,6 +102,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
   if (rb >= total) {
     // nothing of this sequence here
   } else if (warp < PR_SM_WARPS) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(PR_SM_REGS));
     // ------------------------------------------------------------------ softmax of one row tile
     const int t = warp >> 2, quarter = warp & 3, r = quarter * 32 + lane;
     const int n = (keys_of(t) + PR_KEYS - 1) / PR_KEYS;
@@ -139,7 +145,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
     }
     const uint32_t t_lane = tmem_base + ((uint32_t)(quarter * 32) << 16);
     const uint32_t s_col = t_lane + Cfg::S_COL + t * 128, o_col = t_lane + Cfg::O_COL + t * DH;
-    float u = 0.f, l = 0.f, vref = 0.f;            // u = P_SHIFT - running maximum
+    float u = 0.f, l = 0.f, vref = 0.f;            // u = PR_SHIFT - running maximum
     bool ok = true;
     for (int j = 0; j < n_all; ++j) {
       const int slot = j % PR_INFO;
@@ -160,29 +166,29 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
         const float4* info = reinterpret_cast<const float4*>(smem + Cfg::OFF_INFO) + slot * 8 + 4 * h;
         const int valid = lim - j * PR_KEYS - 64 * h;                      // keys of this half that the row sees
         const bool whole = __all_sync(0xffffffffu, valid >= 64), first = (j | h) == 0, turn = h == 0 && ref.y != 1.0f;
-        // ---- e' = 2^(score - maximum + 11 + log2 rv), the row sum and the largest exponent in one reading; P waits in registers
-        // until it is known that the maximum may stay (else it moves and the half is read again; always so for the first one)
+        float4 gi[4];                              // of 16 keys each: key scale, log2 rv, 1 / rv
+#pragma unroll
+        for (int g = 0; g < 4; ++g) gi[g] = info[g];
+        // ---- e' = 2^(score - maximum + 8 + log2 rv) and the row sum in one reading
         uint32_t w[32];
-        float l_new, mx;
+        float l_new;
         for (bool settled = false;; settled = true) {
+          uint32_t x[2][32];
+          ptx::tmem_ld32(s_half, x[0]);
+          ptx::tmem_ld_wait();
+          ptx::tmem_ld32(s_half + 32, x[1]);
           l_new = l;
-          mx = -INFINITY;
-          uint32_t x[2][16];
-          ptx::tmem_ld16(s_half, x[0]);
+          float most = 0.f;
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
-            ptx::tmem_ld_wait();
-            if (g < 3) ptx::tmem_ld16(s_half + 16 * (g + 1), x[(g + 1) & 1]);
-            const uint32_t (&y)[16] = x[g & 1];
-            const float4 gi = info[g];
-            const float fk = f * gi.x, ug = u + gi.y;
+            if (g == 2) ptx::tmem_ld_wait();
+            const uint32_t* y = &x[g >> 1][16 * (g & 1)];
+            const float fk = f * gi[g].x, ug = u + gi[g].y;
             float2 sum = make_float2(0.f, 0.f);
-            float m = -INFINITY;
             if (whole) {
 #pragma unroll
               for (int i = 0; i < 8; ++i) {
                 const float2 a = __ffma2_rn(make_float2(__uint_as_float(y[2 * i]), __uint_as_float(y[2 * i + 1])), make_float2(fk, fk), make_float2(ug, ug));
-                m = ptx::max3(m, a.x, a.y);
                 const float2 e = make_float2(ex2(a.x), ex2(a.y));
                 sum = __fadd2_rn(sum, e);
                 w[8 * g + i] = pack_f16(e.x, e.y);
@@ -191,36 +197,47 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
 #pragma unroll
               for (int i = 0; i < 8; ++i) {
                 const int key = 16 * g + 2 * i;
-                const float a0 = key < valid ? fmaf(__uint_as_float(y[2 * i]), fk, ug) : -INFINITY;
-                const float a1 = key + 1 < valid ? fmaf(__uint_as_float(y[2 * i + 1]), fk, ug) : -INFINITY;
-                m = ptx::max3(m, a0, a1);
-                const float e0 = ex2(a0), e1 = ex2(a1);
+                const float e0 = key < valid ? ex2(fmaf(__uint_as_float(y[2 * i]), fk, ug)) : 0.f;
+                const float e1 = key + 1 < valid ? ex2(fmaf(__uint_as_float(y[2 * i + 1]), fk, ug)) : 0.f;
                 sum.x += e0; sum.y += e1;
                 w[8 * g + i] = pack_f16(e0, e1);
               }
             }
-            l_new = fmaf(sum.x + sum.y, gi.z, l_new);
-            mx = fmaxf(mx, m - gi.y);
+            const float both = sum.x + sum.y;
+            most = fmaxf(most, both);
+            l_new = fmaf(both, gi[g].z, l_new);
           }
-          if (settled || !(__any_sync(0xffffffffu, first || mx > P_SHIFT + MAX_SLACK) || turn)) break;
-          float d = mx - P_SHIFT;
+          if (settled || !(__any_sync(0xffffffffu, first || most > PR_MOST) || turn)) break;
+          // ---- the maximum of this half moves the row's, O and the sum follow, and O the value reference
+          float mx = -INFINITY;
+#pragma unroll 1
+          for (int g = 0; g < 4; ++g) {
+            uint32_t z[16];
+            ptx::tmem_ld16(s_half + 16 * g, z);
+            ptx::tmem_ld_wait();
+            float m = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) m = fmaxf(m, 16 * g + i < valid ? __uint_as_float(z[i]) : -INFINITY);
+            if (m > -INFINITY) mx = fmaxf(mx, fmaf(m, f * info[g].x, u));
+          }
+          float d = mx - PR_SHIFT;
           if (!first) d = fmaxf(d, 0.f);
           if (mx == -INFINITY) d = 0.f;
           u -= d;
           if (!first) {
-            // O and the sum follow the maximum, O the value reference; the previous half's P V has to be complete
-            ok = __all_sync(0xffffffffu, ok && ptx::mbar_wait(&o_full[t], (h + 1) & 1, c.err, 0x8180 | t));
+            ok = __all_sync(0xffffffffu, ok && ptx::mbar_wait(&o_full[t], (h + 1) & 1, c.err, 0x8180 | t));   // the previous half's P V
             ptx::tc_fence_after();
             const float a = ex2(-d);
             l *= a;
             const float ao = turn ? a * ref.y : a;
-#pragma unroll
+#pragma unroll 1
             for (int k = 0; k < DH / 16; ++k) {
-              ptx::tmem_ld16(o_col + 16 * k, x[0]);
+              uint32_t z[16];
+              ptx::tmem_ld16(o_col + 16 * k, z);
               ptx::tmem_ld_wait();
 #pragma unroll
-              for (int i = 0; i < 16; ++i) x[0][i] = __float_as_uint(__uint_as_float(x[0][i]) * ao);
-              ptx::tmem_st16(o_col + 16 * k, x[0]);
+              for (int i = 0; i < 16; ++i) z[i] = __float_as_uint(__uint_as_float(z[i]) * ao);
+              ptx::tmem_st16(o_col + 16 * k, z);
             }
           }
         }
@@ -283,31 +300,39 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
       }
     }
   } else if (warp < PR_MMA_WARP) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(PR_CV_REGS));
     // ------------------------------------------------------------------ codes -> FP16 operands
     constexpr int NP = DH / 32;                    // 16-code pieces of a tile per thread
     constexpr int NSUB = DH / 64;
     // four lanes take 64 features of a row, eight lanes two rows: whole sectors from memory, no bank conflicts in the operand tile
     const int ct = threadIdx.x - PR_SM_WARPS * 32, piece = ct & 3, r0 = ct >> 2;       // rows r0 + 64 i
-    const bool scribe = warp == PR_SM_WARPS;       // publishes the scale records
     const long long mine = (long long)hk * c.head_stride + (long long)(r0 & 15) * c.ld + piece * 16;
-    uint8_t* const to = smem + (r0 >> 3) * 1024 + (r0 & 7) * 128;
-    const uint32_t swz0 = ((2 * piece) ^ (r0 & 7)) << 4, swz1 = ((2 * piece + 1) ^ (r0 & 7)) << 4;
+    uint8_t* const to0 = smem + (r0 >> 3) * 1024 + (r0 & 7) * 128 + (((2 * piece) ^ (r0 & 7)) << 4);
+    uint8_t* const to1 = smem + (r0 >> 3) * 1024 + (r0 & 7) * 128 + (((2 * piece + 1) ^ (r0 & 7)) << 4);
     auto page_of = [&](int j) {                    // lane g < 8: page of tokens 128 j + 16 g ..
       const int tok = j * PR_KEYS + 16 * lane;
       return lane < 8 && tok < L ? page_for_read(c, b, tok >> c.page_shift) : -1;
     };
-    auto offset_of = [&](int j, int id) {          // and where they begin in the pool
-      return (long long)id * c.page_stride + (long long)((j * PR_KEYS + 16 * lane) & (c.page - 1)) * c.ld;
+    long long at[2];                               // where the thread's two rows begin in the pool
+    auto locate = [&](int j, int id) {
+      const long long off = (long long)id * c.page_stride + (long long)((j * PR_KEYS + 16 * lane) & (c.page - 1)) * c.ld;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) at[i] = mine + __shfl_sync(0xffffffffu, off, 4 * i + (r0 >> 4));
     };
-    auto load = [&](const uint8_t* pool, int j, long long off, uint4 (&raw)[NP]) {
+    auto load = [&](const uint8_t* pool, int j, uint4 (&raw)[NP]) {
+      if ((j + 1) * PR_KEYS <= L) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const long long at = mine + __shfl_sync(0xffffffffu, off, 4 * i + (r0 >> 4));
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int h = 0; h < NSUB; ++h) {
-          raw[i * NSUB + h] = make_uint4(0, 0, 0, 0);          // slots behind the end may hold anything (e4m3: NaN)
-          if (j * PR_KEYS + r0 + 64 * i < L) raw[i * NSUB + h] = __ldg(reinterpret_cast<const uint4*>(pool + at + 64 * h));
-        }
+          for (int h = 0; h < NSUB; ++h) raw[i * NSUB + h] = __ldg(reinterpret_cast<const uint4*>(pool + at[i] + 64 * h));
+      } else {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int h = 0; h < NSUB; ++h) {
+            raw[i * NSUB + h] = make_uint4(0, 0, 0, 0);        // slots behind the end may hold anything (e4m3: NaN)
+            if (j * PR_KEYS + r0 + 64 * i < L) raw[i * NSUB + h] = __ldg(reinterpret_cast<const uint4*>(pool + at[i] + 64 * h));
+          }
       }
     };
     auto store = [&](uint32_t tile, const uint4 (&raw)[NP]) {
@@ -321,53 +346,61 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
           codes4_to_f16<F8>(x.y, y[2], y[3]);
           codes4_to_f16<F8>(x.z, y[4], y[5]);
           codes4_to_f16<F8>(x.w, y[6], y[7]);
-          uint8_t* at = to + tile + h * Cfg::SUB + i * 8192;
-          *reinterpret_cast<uint4*>(at + swz0) = make_uint4(y[0], y[1], y[2], y[3]);
-          *reinterpret_cast<uint4*>(at + swz1) = make_uint4(y[4], y[5], y[6], y[7]);
+          *reinterpret_cast<uint4*>(to0 + tile + h * Cfg::SUB + i * 8192) = make_uint4(y[0], y[1], y[2], y[3]);
+          *reinterpret_cast<uint4*>(to1 + tile + h * Cfg::SUB + i * 8192) = make_uint4(y[4], y[5], y[6], y[7]);
         }
       ptx::fence_proxy_async_smem();
       __syncwarp();
     };
     uint4 kr[NP], vr[NP];
     bool ok = true;
-    int ids = page_of(0), ids_next = page_of(1);
-    float2 sc = make_float2(0.f, 0.f);             // scribe's lane g: scales of tokens 128 j + 16 g ..
-    auto scales = [&](int i) { return i >= 0 ? make_float2(__ldg(c.ks + (long long)i * c.nkv + hk), __ldg(c.vs + (long long)i * c.nkv + hk)) : make_float2(0.f, 0.f); };
-    if (n_all > 0) { load(c.k, 0, offset_of(0, ids), kr); load(c.v, 0, offset_of(0, ids), vr); }
-    if (scribe) sc = scales(ids);
-    float vref = 0.f;
+    int ids_next = page_of(1);
+    if (n_all > 0) { locate(0, page_of(0)); load(c.k, 0, kr); load(c.v, 0, vr); }
     for (int j = 0; j < n_all; ++j) {
       const int st = j & 1;
       const uint32_t par = ((j >> 1) & 1) ^ 1;
-      if (scribe) {
-        const int slot = j % PR_INFO;
-        ok = ok && ptx::mbar_wait(&i_empty[slot], ((j / PR_INFO) & 1) ^ 1, c.err, 0x8300 | slot);
-        float top = lane < 8 ? sc.y : 0.f;
-#pragma unroll
-        for (int o = 4; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-        const float now = fmaxf(vref, __shfl_sync(0xffffffffu, top, 0));
-        const float rv = fmaxf(now > 0.f ? sc.y / now : 1.f, PR_MIN_RV);
-        if (lane < 8) *reinterpret_cast<float4*>(smem + Cfg::OFF_INFO + (slot * 8 + lane) * 16) = make_float4(sc.x, __log2f(rv), 1.0f / rv, 0.f);
-        if (lane == 0) reinterpret_cast<float2*>(smem + Cfg::OFF_REF)[slot] = make_float2(now, now > vref ? vref / now : 1.0f);
-        vref = now;
-        __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(&i_full[slot]);
-        sc = scales(ids_next);
-      }
-      const int ids_after = page_of(j + 2);
-      const long long off = offset_of(j + 1, ids_next);
+      locate(j + 1, ids_next);
+      ids_next = page_of(j + 2);
       ok = ok && ptx::mbar_wait(&k_empty[st], par, c.err, 0x8400 | st);
       store(Cfg::OFF_K + st * Cfg::TILE, kr);
       if (lane == 0) ptx::mbar_arrive(&k_full[st]);
-      if (j + 1 < n_all) load(c.k, j + 1, off, kr);
+      if (j + 1 < n_all) load(c.k, j + 1, kr);
       ok = ok && ptx::mbar_wait(&v_empty[st], par, c.err, 0x8500 | st);
       store(Cfg::OFF_V + st * Cfg::TILE, vr);
       if (lane == 0) ptx::mbar_arrive(&v_full[st]);
-      if (j + 1 < n_all) load(c.v, j + 1, off, vr);
-      ids_next = ids_after;
+      if (j + 1 < n_all) load(c.v, j + 1, vr);
       if (!__all_sync(0xffffffffu, ok)) break;
     }
   } else {
+   asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(PR_MMA_REGS));
+   if (warp == PR_SCRIBE_WARP) {
+    // ------------------------------------------------------------------ scale records
+    auto page_of = [&](int j) {                    // lane g < 8: page of tokens 128 j + 16 g ..
+      const int tok = j * PR_KEYS + 16 * lane;
+      return lane < 8 && tok < L ? page_for_read(c, b, tok >> c.page_shift) : -1;
+    };
+    auto scales = [&](int i) { return i >= 0 ? make_float2(__ldg(c.ks + (long long)i * c.nkv + hk), __ldg(c.vs + (long long)i * c.nkv + hk)) : make_float2(0.f, 0.f); };
+    int ids_next = page_of(1);
+    float2 sc = scales(page_of(0));
+    float vref = 0.f;
+    for (int j = 0; j < n_all; ++j) {
+      const int slot = j % PR_INFO;
+      const float2 now_sc = sc;
+      sc = scales(ids_next);
+      ids_next = page_of(j + 2);
+      float top = now_sc.y;
+#pragma unroll
+      for (int o = 4; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+      const float now = fmaxf(vref, __shfl_sync(0xffffffffu, top, 0));
+      const float rv = fmaxf(now > 0.f ? now_sc.y / now : 1.f, PR_MIN_RV);
+      if (!__all_sync(0xffffffffu, ptx::mbar_wait(&i_empty[slot], ((j / PR_INFO) & 1) ^ 1, c.err, 0x8300 | slot))) break;
+      if (lane < 8) *reinterpret_cast<float4*>(smem + Cfg::OFF_INFO + (slot * 8 + lane) * 16) = make_float4(now_sc.x, __log2f(rv), 1.0f / rv, 0.f);
+      if (lane == 0) reinterpret_cast<float2*>(smem + Cfg::OFF_REF)[slot] = make_float2(now, now > vref ? vref / now : 1.0f);
+      vref = now;
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(&i_full[slot]);
+    }
+   } else if (warp < PR_SCRIBE_WARP) {
     // ------------------------------------------------------------------ issuer of one row tile
     const int t = warp - PR_MMA_WARP, n = (keys_of(t) + PR_KEYS - 1) / PR_KEYS;
     const bool issue = ptx::elect_one();
@@ -431,6 +464,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
       if (ok && lane == 0) ptx::mbar_arrive(&v_empty[st]);
     }
     __syncwarp();
+   }
   }
   ptx::tc_fence_before();
   __syncthreads();
