@@ -66,7 +66,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
   uint64_t* o_full = p_full + 4;                 // [tile] P V of a half is complete
   uint64_t* o_last = o_full + 2;                 // [tile] the last one is
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(o_last + 2);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;   // (uniform: addresses by warp stay in uniform registers)
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
