@@ -55,7 +55,7 @@ struct AppendParams {
 
 // NP: passes of the CTA over a page (page * DH / 8 lanes over 128 threads), all held in registers
 template <int DH, int NP, bool BF, bool F8>
-__global__ void __launch_bounds__(APP_THREADS) block_append_kernel(const AppendParams p) {
+__global__ void __launch_bounds__(APP_THREADS) block_append_kernel(const __grid_constant__ AppendParams p) {
   constexpr int LPT = DH / 8;                    // lanes per token
   constexpr int TPP = APP_THREADS / LPT;         // tokens per pass
   constexpr uint32_t INF2 = BF ? 0x7f80u : 0x7c00u;
@@ -70,18 +70,12 @@ __global__ void __launch_bounds__(APP_THREADS) block_append_kernel(const AppendP
   const int pi = (first >> c.page_shift) + blockIdx.x, p0 = pi << c.page_shift;
   if (s.n <= 0 || p0 >= s.len) return;
   const int id = __ldg(c.table + (long long)b * c.ld_table + pi);
-  if ((unsigned)id >= (unsigned)c.n_pages) {
-    if (threadIdx.x == 0) atomicExch(c.err, ERR_BAD_PAGE);
-    return;
-  }
   const int lo = max(first - p0, 0), hi = min(s.len - p0, c.page);   // the page's slots that receive new tokens
-  uint8_t* dst = (is_v ? c.v : c.k) + (long long)id * c.page_stride + (long long)head * c.head_stride;
-  float* scale = (is_v ? c.vs : c.ks) + (long long)id * c.nkv + head;
   const long long ld_x = is_v ? p.ld_v : p.ld_k;
   const uint16_t* src = (is_v ? p.v : p.k) + (s.r0 + (p0 - begin)) * ld_x + (long long)head * DH;   // row of slot 0
   const int sub = threadIdx.x % LPT, tg = threadIdx.x / LPT;
-  const float s_old = lo > 0 ? *scale : 0.f;
 
+  // the rows are requested before the page's number has arrived
   uint4 raw[NP];
   uint32_t top2 = 0;
 #pragma unroll
@@ -90,6 +84,13 @@ __global__ void __launch_bounds__(APP_THREADS) block_append_kernel(const AppendP
     raw[i] = make_uint4(0, 0, 0, 0);
     if (t >= lo && t < hi) raw[i] = __ldg(reinterpret_cast<const uint4*>(src + (long long)t * ld_x + sub * 8));
   }
+  if ((unsigned)id >= (unsigned)c.n_pages) {
+    if (threadIdx.x == 0) atomicExch(c.err, ERR_BAD_PAGE);
+    return;
+  }
+  uint8_t* dst = (is_v ? c.v : c.k) + (long long)id * c.page_stride + (long long)head * c.head_stride;
+  float* scale = (is_v ? c.vs : c.ks) + (long long)id * c.nkv + head;
+  const float s_old = lo > 0 ? *scale : 0.f;
 #pragma unroll
   for (int i = 0; i < NP; ++i)
     top2 = __vmaxu2(top2, __vmaxu2(__vmaxu2(raw[i].x & 0x7fff7fffu, raw[i].y & 0x7fff7fffu), __vmaxu2(raw[i].z & 0x7fff7fffu, raw[i].w & 0x7fff7fffu)));
@@ -153,61 +154,64 @@ __global__ void __launch_bounds__(APP_THREADS) block_append_kernel(const AppendP
   if (threadIdx.x == 0 && (lo == 0 || s_new > s_old)) *scale = s_new;
 }
 
-// ---- read-back: one thread, 16 codes -> 16 values of 16 bits (16 bytes in, 32 out), READ_UNITS of them in flight
-constexpr int READ_THREADS = 256, READ_UNITS = 4;
+// ---- read-back.  One thread turns 16 codes into 16 values of READ_TOKENS tokens, all of them in flight.  The 32 bytes it writes
+// leave in one store where the rows allow it (WIDE: 32-byte aligned); two stores of 16 bytes each are half a sector.
+constexpr int READ_THREADS = 256, READ_TOKENS = 4;
 
 struct ReadParams {
   BlockView c;
   uint16_t* k; long long ld_k;
   uint16_t* v; long long ld_v;
   int ppt;                      // 16-code pieces per token: nkv * DH / 16
-  int tokens;                   // tokens per CTA
+  int tpp;                      // tokens per pass of the CTA
   int first_v;                  // grid y 0 is the values (no keys wanted)
 };
 
-template <int DH, bool BF, bool F8>
-__global__ void __launch_bounds__(READ_THREADS) block_read_kernel(const ReadParams p) {
+template <int DH, bool BF, bool F8, bool WIDE>
+__global__ void __launch_bounds__(READ_THREADS, 4) block_read_kernel(const __grid_constant__ ReadParams p) {
   constexpr int PPH = DH / 16;                   // pieces per head
   ptx::pdl_launch_dependents();
   ptx::pdl_wait();
   const BlockView& c = p.c;
   const int b = blockIdx.z, is_v = blockIdx.y + p.first_v;
   const SeqRows s = seq_rows(c, b);
-  const int i0 = blockIdx.x * p.tokens;
+  const int i0 = blockIdx.x * p.tpp * READ_TOKENS;
   if (i0 >= s.n) return;
-  const int i1 = min(i0 + p.tokens, s.n);
-  const uint8_t* base = is_v ? c.v : c.k;
+  const uint8_t* pool = is_v ? c.v : c.k;
   const float* scales = is_v ? c.vs : c.ks;
   uint16_t* out = is_v ? p.v : p.k;
   const long long ld = is_v ? p.ld_v : p.ld_k;
-  const int units = (i1 - i0) * p.ppt;
-  for (int u0 = threadIdx.x; u0 < units; u0 += READ_THREADS * READ_UNITS) {
-    uint4 code[READ_UNITS];
-    float sc[READ_UNITS];
-    uint16_t* dst[READ_UNITS];
+  const int* table = c.table + (long long)b * c.ld_table;
+  const int tok = p.tpp > 1 ? threadIdx.x / p.ppt : 0;
+  if (tok >= p.tpp) return;
+  for (int piece = threadIdx.x - tok * p.ppt; piece < p.ppt; piece += READ_THREADS) {     // (one pass where a token fits the CTA)
+    const int head = piece / PPH;
+    const uint8_t* from = pool + (long long)head * c.head_stride + (piece % PPH) * 16;
+    uint4 code[READ_TOKENS];
+    float sc[READ_TOKENS];
+    // (no branch between the look-ups and the loads: the pages of all tokens are fetched together, then all codes)
+    int id[READ_TOKENS];
+    bool bad = false;
 #pragma unroll
-    for (int j = 0; j < READ_UNITS; ++j) {
-      const int u = u0 + j * READ_THREADS;
-      dst[j] = nullptr;
-      if (u < units) {
-        const int i = i0 + u / p.ppt, piece = u % p.ppt;
-        const int head = piece / PPH;
-        const int t = s.len - s.n + i;           // token
-        dst[j] = out + (s.r0 + i) * ld + piece * 16;
-        if (t >= 0) {
-          const int id = page_for_read(c, b, t >> c.page_shift);
-          code[j] = __ldg(reinterpret_cast<const uint4*>(base + (long long)id * c.page_stride + (long long)head * c.head_stride +
-                                                         (long long)(t & (c.page - 1)) * c.ld + (piece % PPH) * 16));
-          sc[j] = __ldg(scales + (long long)id * c.nkv + head);
-        } else {
-          code[j] = make_uint4(0, 0, 0, 0);
-          sc[j] = 0.f;
-        }
-      }
+    for (int j = 0; j < READ_TOKENS; ++j) {
+      const int i = i0 + tok + j * p.tpp, t = s.len - s.n + i;             // row of the sequence, its token
+      const int pi = min(max(t, 0), c.max_len - 1) >> c.page_shift;
+      const int n = __ldg(table + pi);
+      id[j] = min(max(n, 0), c.n_pages - 1);
+      bad |= id[j] != n && i < s.n && t >= 0;
     }
 #pragma unroll
-    for (int j = 0; j < READ_UNITS; ++j) {
-      if (dst[j] == nullptr) continue;
+    for (int j = 0; j < READ_TOKENS; ++j) {
+      const int i = i0 + tok + j * p.tpp, t = s.len - s.n + i;
+      code[j] = __ldg(reinterpret_cast<const uint4*>(from + (long long)id[j] * c.page_stride + (long long)(t & (c.page - 1)) * c.ld));
+      sc[j] = __ldg(scales + (long long)id[j] * c.nkv + head);
+      if (i >= s.n || t < 0) { code[j] = make_uint4(0, 0, 0, 0); sc[j] = 0.f; }  // a row without a token
+    }
+    if (bad) atomicExch(c.err, ERR_BAD_PAGE);
+#pragma unroll
+    for (int j = 0; j < READ_TOKENS; ++j) {
+      const int i = i0 + tok + j * p.tpp;
+      if (i >= s.n) break;
       const uint32_t w[4] = {code[j].x, code[j].y, code[j].z, code[j].w};
       uint32_t o[8];
 #pragma unroll
@@ -217,8 +221,14 @@ __global__ void __launch_bounds__(READ_THREADS) block_read_kernel(const ReadPara
         o[2 * q] = f32x2_to_fp16ish<BF>(y[0] * sc[j], y[1] * sc[j]);
         o[2 * q + 1] = f32x2_to_fp16ish<BF>(y[2] * sc[j], y[3] * sc[j]);
       }
-      reinterpret_cast<uint4*>(dst[j])[0] = make_uint4(o[0], o[1], o[2], o[3]);
-      reinterpret_cast<uint4*>(dst[j])[1] = make_uint4(o[4], o[5], o[6], o[7]);
+      uint16_t* at = out + (s.r0 + i) * ld + piece * 16;
+      if constexpr (WIDE) {
+        asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(at), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]), "r"(o[4]), "r"(o[5]),
+                     "r"(o[6]), "r"(o[7]) : "memory");
+      } else {
+        reinterpret_cast<uint4*>(at)[0] = make_uint4(o[0], o[1], o[2], o[3]);
+        reinterpret_cast<uint4*>(at)[1] = make_uint4(o[4], o[5], o[6], o[7]);
+      }
     }
   }
 }
@@ -230,6 +240,16 @@ static hero_status check_rows_matrix(const hero_tensor& t, const char* name, con
   HERO_REQUIRE(t.cols == (int64_t)c->nkv * c->dh, HERO_ERR_INVALID_ARG, "%s: %lld columns, nkv*dh = %lld", name, (long long)t.cols,
                (long long)c->nkv * c->dh);
   return HERO_OK;
+}
+
+typedef void (*read_fn)(const ReadParams);
+template <int DH>
+static read_fn read_kernel(bool bf, bool f8, bool wide) {
+  if (wide)
+    return bf ? (f8 ? block_read_kernel<DH, true, true, true> : block_read_kernel<DH, true, false, true>)
+              : (f8 ? block_read_kernel<DH, false, true, true> : block_read_kernel<DH, false, false, true>);
+  return bf ? (f8 ? block_read_kernel<DH, true, true, false> : block_read_kernel<DH, true, false, false>)
+            : (f8 ? block_read_kernel<DH, false, true, false> : block_read_kernel<DH, false, false, false>);
 }
 
 template <int DH, int NP>
@@ -293,16 +313,15 @@ extern "C" hero_status hero_block_cache_read(hero_handle* h, const hero_block_ca
   p.k = static_cast<uint16_t*>(a->k.data); p.ld_k = a->k.ld;
   p.v = static_cast<uint16_t*>(a->v.data); p.ld_v = a->v.ld;
   p.ppt = cc->nkv * cc->dh / 16;
-  p.tokens = READ_THREADS * READ_UNITS / p.ppt;
-  if (p.tokens < 1) p.tokens = 1;
+  p.tpp = p.ppt < READ_THREADS ? READ_THREADS / p.ppt : 1;
   p.first_v = has_k ? 0 : 1;
-  const dim3 grid((unsigned)((a->max_rows + (long long)p.tokens - 1) / p.tokens), has_k && has_v ? 2 : 1, (unsigned)cc->B);
+  const int per_cta = p.tpp * READ_TOKENS;
+  const dim3 grid((unsigned)((a->max_rows + (long long)per_cta - 1) / per_cta), has_k && has_v ? 2 : 1, (unsigned)cc->B);
   const bool bf = one.dtype == HERO_BF16;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  auto kern = cc->dh == 64 ? (bf ? (p.c.f8 ? block_read_kernel<64, true, true> : block_read_kernel<64, true, false>)
-                                 : (p.c.f8 ? block_read_kernel<64, false, true> : block_read_kernel<64, false, false>))
-                           : (bf ? (p.c.f8 ? block_read_kernel<128, true, true> : block_read_kernel<128, true, false>)
-                                 : (p.c.f8 ? block_read_kernel<128, false, true> : block_read_kernel<128, false, false>));
+  auto wide_rows = [](const hero_tensor& t) { return reinterpret_cast<uintptr_t>(t.data) % 32 == 0 && t.ld % 16 == 0; };
+  const bool wide = (!has_k || wide_rows(a->k)) && (!has_v || wide_rows(a->v));
+  auto kern = cc->dh == 64 ? read_kernel<64>(bf, p.c.f8, wide) : read_kernel<128>(bf, p.c.f8, wide);
   cudaError_t e;
   {
     LaunchScope scope(h, s, KERNEL_CACHE);

@@ -2,7 +2,9 @@
 // kernel is bound by HBM for many rows and by its latency for few.  A head vector is held by LPH lanes of a warp (8 features,
 // 16 bytes each; LPH is the power of two that covers dh), the sum of squares is log2(LPH) shuffles, a rotation partner in
 // the other half of the head is one shuffle per feature and a neighbouring one is the lane's own.  A warp takes ITERS * 32 / LPH
-// heads of ONE row, so that cos and sin of the row's position are loaded once for all of them.
+// heads of ONE row, so that cos and sin of the row's position are loaded once for all of them.  What a feature and its partner are
+// multiplied with (gamma cos, +-gamma sin) is formed once per row too: per head there remain the sum of squares, two products a feature
+// and the norm factor.
 #include "block_cache.cuh"
 
 namespace hero {
@@ -23,65 +25,77 @@ struct RopeParams {
 constexpr int ROPE_WARPS = 4;
 
 template <int LPH, int ITERS, bool BF>
-__global__ void __launch_bounds__(ROPE_WARPS * 32) qk_rope_kernel(const RopeParams p) {
+__global__ void __launch_bounds__(ROPE_WARPS * 32, ITERS == 8 ? 5 : 8) qk_rope_kernel(const __grid_constant__ RopeParams p) {
   constexpr int HPI = 32 / LPH;                  // heads per iteration
   ptx::pdl_launch_dependents();
   ptx::pdl_wait();
-  const int per_row = p.chunks[0] + p.chunks[1];
-  const long long w = (long long)blockIdx.x * ROPE_WARPS + (threadIdx.x >> 5);
-  const long long row = w / per_row;
+  const unsigned per_row = p.chunks[0] + p.chunks[1], unit = blockIdx.x * ROPE_WARPS + (threadIdx.x >> 5);
+  const long long row = unit / per_row;
   if (row >= p.rows) return;
-  int ch = (int)(w - row * per_row);
+  const int this_pos = p.rot > 0 ? __ldg(p.pos + row) : 0;
+  int ch = (int)(unit - (unsigned)row * per_row);
   const int side = ch >= p.chunks[0];            // 0: queries, 1: keys
   if (side) ch -= p.chunks[0];
   const int lane = threadIdx.x & 31, sub = lane % LPH, f0 = sub * 8;
   const bool live = f0 < p.dh;
-  const int h0 = ch * (HPI * ITERS) + lane / LPH, heads = p.heads[side];
-  const uint16_t* x = p.x[side] + row * p.ld_x[side] + f0;
-
+  const int first = ch * (HPI * ITERS), h0 = first + lane / LPH, heads = p.heads[side];
+  const uint16_t* x0 = p.x[side] + row * p.ld_x[side] + f0;
   uint4 raw[ITERS];
 #pragma unroll
   for (int i = 0; i < ITERS; ++i) {
     const int hd = h0 + i * HPI;
     raw[i] = make_uint4(0, 0, 0, 0);
-    if (live && hd < heads) raw[i] = *reinterpret_cast<const uint4*>(x + (long long)hd * p.dh);
+    if (live && hd < heads) raw[i] = *reinterpret_cast<const uint4*>(x0 + (long long)hd * p.dh);
   }
-  // cos and sin of the lane's features: sn carries the sign with which the partner enters
-  float cs[8], sn[8];
-  const bool turns = f0 < p.rot;
+  // what a feature and its partner are multiplied with before the norm factor: gamma cos and +-gamma(partner) sin
+  float2 own[4], mate[4];
+  const bool norm = p.gamma[side] != nullptr, turns = f0 < p.rot;
   const int half = p.rot >> 1;
-  if (p.rot > 0) {
-    long long t = __ldg(p.pos + row);
-    if (t < 0 || t >= p.n_pos) {
-      if (lane == 0) atomicExch(p.err, ERR_BAD_POS);
-      t = t < 0 ? 0 : p.n_pos - 1;
-    }
-    const float* ct = p.cos + t * half;
-    const float* st = p.sin + t * half;
-    if (turns) {
-      if (p.adjacent) {
-        const float4 c = __ldg(reinterpret_cast<const float4*>(ct + f0 / 2)), s = __ldg(reinterpret_cast<const float4*>(st + f0 / 2));
-        cs[0] = cs[1] = c.x; cs[2] = cs[3] = c.y; cs[4] = cs[5] = c.z; cs[6] = cs[7] = c.w;
-        sn[0] = -s.x; sn[1] = s.x; sn[2] = -s.y; sn[3] = s.y; sn[4] = -s.z; sn[5] = s.z; sn[6] = -s.w; sn[7] = s.w;
-      } else {
-        const bool second = f0 >= half;
-        const int j = second ? f0 - half : f0;
-        const float4 c0 = __ldg(reinterpret_cast<const float4*>(ct + j)), c1 = __ldg(reinterpret_cast<const float4*>(ct + j + 4));
-        const float4 s0 = __ldg(reinterpret_cast<const float4*>(st + j)), s1 = __ldg(reinterpret_cast<const float4*>(st + j + 4));
-        cs[0] = c0.x; cs[1] = c0.y; cs[2] = c0.z; cs[3] = c0.w; cs[4] = c1.x; cs[5] = c1.y; cs[6] = c1.z; cs[7] = c1.w;
-        sn[0] = s0.x; sn[1] = s0.y; sn[2] = s0.z; sn[3] = s0.w; sn[4] = s1.x; sn[5] = s1.y; sn[6] = s1.z; sn[7] = s1.w;
-        if (!second) {
+  {
+    const bool second = !p.adjacent && f0 >= half;
+    const int pf = p.adjacent || !turns ? f0 : second ? f0 - half : f0 + half;       // the partner features (adjacent: the lane's own)
+    float g[8], gp[8];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) sn[e] = -sn[e];
+    for (int e = 0; e < 8; ++e) g[e] = gp[e] = 1.f;
+    if (norm && live) {
+      const float* gm = p.gamma[side];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) { g[e] = __ldg(gm + f0 + e); gp[e] = __ldg(gm + pf + e); }
+    }
+    float cs[8], sn[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) { cs[e] = 1.f; sn[e] = 0.f; }
+    if (p.rot > 0) {
+      long long t = this_pos;
+      if (t < 0 || t >= p.n_pos) {
+        if (lane == 0) atomicExch(p.err, ERR_BAD_POS);
+        t = t < 0 ? 0 : p.n_pos - 1;
+      }
+      if (turns) {
+        const float* ct = p.cos + t * half;
+        const float* st = p.sin + t * half;
+        if (p.adjacent) {
+          const float4 x = __ldg(reinterpret_cast<const float4*>(ct + f0 / 2)), y = __ldg(reinterpret_cast<const float4*>(st + f0 / 2));
+          cs[0] = cs[1] = x.x; cs[2] = cs[3] = x.y; cs[4] = cs[5] = x.z; cs[6] = cs[7] = x.w;
+          sn[0] = -y.x; sn[1] = y.x; sn[2] = -y.y; sn[3] = y.y; sn[4] = -y.z; sn[5] = y.z; sn[6] = -y.w; sn[7] = y.w;
+        } else {
+          const int j = second ? f0 - half : f0;
+          const float4 x0 = __ldg(reinterpret_cast<const float4*>(ct + j)), x1 = __ldg(reinterpret_cast<const float4*>(ct + j + 4));
+          const float4 y0 = __ldg(reinterpret_cast<const float4*>(st + j)), y1 = __ldg(reinterpret_cast<const float4*>(st + j + 4));
+          cs[0] = x0.x; cs[1] = x0.y; cs[2] = x0.z; cs[3] = x0.w; cs[4] = x1.x; cs[5] = x1.y; cs[6] = x1.z; cs[7] = x1.w;
+          sn[0] = y0.x; sn[1] = y0.y; sn[2] = y0.z; sn[3] = y0.w; sn[4] = y1.x; sn[5] = y1.y; sn[6] = y1.z; sn[7] = y1.w;
+          if (!second) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sn[e] = -sn[e];
+          }
         }
       }
     }
-  }
-  float g[8];
-  const bool norm = p.gamma[side] != nullptr;
-  if (norm && live) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) g[e] = __ldg(p.gamma[side] + f0 + e);
+    for (int e = 0; e < 4; ++e) {
+      own[e] = make_float2(g[2 * e] * cs[2 * e], g[2 * e + 1] * cs[2 * e + 1]);
+      mate[e] = p.adjacent ? make_float2(gp[2 * e + 1] * sn[2 * e], gp[2 * e] * sn[2 * e + 1]) : make_float2(gp[2 * e] * sn[2 * e], gp[2 * e + 1] * sn[2 * e + 1]);
+    }
   }
   float inv_s = 0.f;
   const bool to_i8 = p.out_scale[side] != nullptr;
@@ -89,64 +103,63 @@ __global__ void __launch_bounds__(ROPE_WARPS * 32) qk_rope_kernel(const RopePara
   const Divider div(inv_s);
   // the lane that holds the partner features under HERO_PAIR_HALVES
   const int r2 = p.rot >> 4;
-  const int mate = (lane - sub) + (turns ? (sub < r2 ? sub + r2 : sub - r2) : sub);
+  const int mate_lane = (lane - sub) + (turns ? (sub < r2 ? sub + r2 : sub - r2) : sub);
 
 #pragma unroll
   for (int i = 0; i < ITERS; ++i) {
+    if (first + i * HPI >= heads) break;         // (uniform)
     const int hd = h0 + i * HPI;
-    float y[8];
-    {
-      const float2 a = fp16ish_to_f32x2<BF>(raw[i].x), b = fp16ish_to_f32x2<BF>(raw[i].y);
-      const float2 c = fp16ish_to_f32x2<BF>(raw[i].z), d = fp16ish_to_f32x2<BF>(raw[i].w);
-      y[0] = a.x; y[1] = a.y; y[2] = b.x; y[3] = b.y; y[4] = c.x; y[5] = c.y; y[6] = d.x; y[7] = d.y;
-    }
+    const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+    float2 x[4], y[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = fp16ish_to_f32x2<BF>(w[e]);
+    float r = 1.f;
     if (norm) {
-      float ss = 0.f;
+      float2 ss = __fmul2_rn(x[0], x[0]);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) ss = fmaf(y[e], y[e], ss);
+      for (int e = 1; e < 4; ++e) ss = __ffma2_rn(x[e], x[e], ss);
+      float sum = ss.x + ss.y;
 #pragma unroll
-      for (int o = LPH / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-      const float r = rsqrtf(fmaf(ss, p.inv_dh, p.eps));
-      if (live) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = y[e] * r * g[e];
-      }
+      for (int o = LPH / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      r = rsqrtf(fmaf(sum, p.inv_dh, p.eps));
     }
-    if (p.rot > 0) {
-      float z[8];
-      if (p.adjacent) {
+    if (p.adjacent) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) z[e] = y[e ^ 1];
-      } else {
+      for (int e = 0; e < 4; ++e) y[e] = __ffma2_rn(make_float2(x[e].y, x[e].x), mate[e], __fmul2_rn(x[e], own[e]));
+    } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) z[e] = __shfl_sync(0xffffffffu, y[e], mate);
-      }
-      if (turns) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = fmaf(z[e], sn[e], y[e] * cs[e]);
-      }
+      for (int e = 0; e < 4; ++e)                // (the 16-bit pairs travel, not the FP32 values)
+        y[e] = __ffma2_rn(fp16ish_to_f32x2<BF>(__shfl_sync(0xffffffffu, w[e], mate_lane)), mate[e], __fmul2_rn(x[e], own[e]));
     }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = __fmul2_rn(y[e], make_float2(r, r));
     if (live && hd < heads) {
       const long long at = row * p.ld_y[side] + (long long)hd * p.dh + f0;
       if (to_i8) {
         uint2 code;
-        code.x = f32_to_codes4<false>(div(y[0]), div(y[1]), div(y[2]), div(y[3]));
-        code.y = f32_to_codes4<false>(div(y[4]), div(y[5]), div(y[6]), div(y[7]));
+        code.x = f32_to_codes4<false>(div(y[0].x), div(y[0].y), div(y[1].x), div(y[1].y));
+        code.y = f32_to_codes4<false>(div(y[2].x), div(y[2].y), div(y[3].x), div(y[3].y));
         *reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.y[side]) + at) = code;
       } else {
         *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.y[side]) + at) =
-            make_uint4(f32x2_to_fp16ish<BF>(y[0], y[1]), f32x2_to_fp16ish<BF>(y[2], y[3]), f32x2_to_fp16ish<BF>(y[4], y[5]), f32x2_to_fp16ish<BF>(y[6], y[7]));
+            make_uint4(f32x2_to_fp16ish<BF>(y[0].x, y[0].y), f32x2_to_fp16ish<BF>(y[1].x, y[1].y), f32x2_to_fp16ish<BF>(y[2].x, y[2].y), f32x2_to_fp16ish<BF>(y[3].x, y[3].y));
       }
     }
   }
 }
 
 template <int LPH, int ITERS>
-static cudaError_t launch_rope(RopeParams& p, bool bf, cudaStream_t s) {
+static cudaError_t launch_rope_steps(RopeParams& p, bool bf, cudaStream_t s) {
   for (int i = 0; i < 2; ++i) p.chunks[i] = (p.heads[i] + (32 / LPH) * ITERS - 1) / ((32 / LPH) * ITERS);
   const long long warps = p.rows * (p.chunks[0] + p.chunks[1]);
-  const unsigned grid = (unsigned)((warps + ROPE_WARPS - 1) / ROPE_WARPS);
-  return launch_dependent(bf ? qk_rope_kernel<LPH, ITERS, true> : qk_rope_kernel<LPH, ITERS, false>, dim3(grid), dim3(ROPE_WARPS * 32), 0, s, p);
+  return launch_dependent(bf ? qk_rope_kernel<LPH, ITERS, true> : qk_rope_kernel<LPH, ITERS, false>, dim3((unsigned)((warps + ROPE_WARPS - 1) / ROPE_WARPS)),
+                          dim3(ROPE_WARPS * 32), 0, s, p);
+}
+// many rows: eight steps a warp, so that what is formed once per row is shared by many heads; few rows: two, more warps
+template <int LPH>
+static cudaError_t launch_rope(const hero_handle* h, RopeParams& p, bool bf, cudaStream_t s) {
+  const bool many = p.rows * (p.heads[0] + p.heads[1]) >= (long long)h->sm_count * 16 * 8 * (32 / LPH);   // 16 warps of eight steps per SM
+  return many ? launch_rope_steps<LPH, 8>(p, bf, s) : launch_rope_steps<LPH, 2>(p, bf, s);
 }
 
 static hero_status check_head_matrix(const hero_tensor& t, const char* name, int64_t rows, int64_t cols) {
@@ -213,8 +226,8 @@ extern "C" hero_status hero_qk_norm_rope(hero_handle* h, const hero_qk_norm_rope
   cudaError_t e;
   {
     LaunchScope scope(h, s, KERNEL_CACHE);
-    e = lph == 2 ? launch_rope<2, 4>(p, bf, s) : lph == 4 ? launch_rope<4, 4>(p, bf, s) : lph == 8 ? launch_rope<8, 4>(p, bf, s)
-      : lph == 16 ? launch_rope<16, 4>(p, bf, s) : launch_rope<32, 4>(p, bf, s);
+    e = lph == 2 ? launch_rope<2>(h, p, bf, s) : lph == 4 ? launch_rope<4>(h, p, bf, s) : lph == 8 ? launch_rope<8>(h, p, bf, s)
+      : lph == 16 ? launch_rope<16>(h, p, bf, s) : launch_rope<32>(h, p, bf, s);
   }
   HERO_CUDA(e);
   return HERO_OK;
