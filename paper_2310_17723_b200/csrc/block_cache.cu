@@ -102,17 +102,13 @@ __global__ void __launch_bounds__(APP_THREADS) block_append_kernel(const __grid_
     amax = f.x;
   } else {
     amax = 0.f;
-    uint32_t* w = reinterpret_cast<uint32_t*>(raw);
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(raw);
 #pragma unroll
     for (int i = 0; i < 4 * NP; ++i) {
-      // a NaN becomes 0 here; an infinity keeps its pattern (it saturates below) but is no part of the maximum
-      uint32_t lo16 = w[i] & 0xffffu, hi16 = w[i] >> 16;
-      if ((lo16 & 0x7fffu) > INF2) lo16 = 0;
-      if ((hi16 & 0x7fffu) > INF2) hi16 = 0;
-      w[i] = lo16 | (hi16 << 16);
+      // the largest finite magnitude
       const float2 f = fp16ish_to_f32x2<BF>(w[i]);
-      if ((lo16 & 0x7fffu) < INF2) amax = fmaxf(amax, fabsf(f.x));
-      if ((hi16 & 0x7fffu) < INF2) amax = fmaxf(amax, fabsf(f.y));
+      if ((w[i] & 0x7fffu) < INF2) amax = fmaxf(amax, fabsf(f.x));
+      if ((w[i] >> 16 & 0x7fffu) < INF2) amax = fmaxf(amax, fabsf(f.y));
     }
   }
 #pragma unroll
@@ -125,16 +121,38 @@ __global__ void __launch_bounds__(APP_THREADS) block_append_kernel(const __grid_
 
   Divider div(s_new);
   if (odd) div.fast = false;                                 // (an infinity has no remainder)
+  if (div.fast) {
+    // no new value exceeds top * s_new, so the codes need no clamping
 #pragma unroll
-  for (int i = 0; i < NP; ++i) {
-    const int t = i * TPP + tg;
-    if (t >= lo && t < hi) {
-      const float2 a = fp16ish_to_f32x2<BF>(raw[i].x), b2 = fp16ish_to_f32x2<BF>(raw[i].y);
-      const float2 c2 = fp16ish_to_f32x2<BF>(raw[i].z), d = fp16ish_to_f32x2<BF>(raw[i].w);
-      uint2 code;
-      code.x = f32_to_codes4<F8>(div(a.x), div(a.y), div(b2.x), div(b2.y));
-      code.y = f32_to_codes4<F8>(div(c2.x), div(c2.y), div(d.x), div(d.y));
-      *reinterpret_cast<uint2*>(dst + (long long)t * c.ld + sub * 8) = code;
+    for (int i = 0; i < NP; ++i) {
+      const int t = i * TPP + tg;
+      if (t >= lo && t < hi) {
+        uint2 code;
+        code.x = f32_to_codes4_inside<F8>(div.pair(fp16ish_to_f32x2<BF>(raw[i].x)), div.pair(fp16ish_to_f32x2<BF>(raw[i].y)));
+        code.y = f32_to_codes4_inside<F8>(div.pair(fp16ish_to_f32x2<BF>(raw[i].z)), div.pair(fp16ish_to_f32x2<BF>(raw[i].w)));
+        *reinterpret_cast<uint2*>(dst + (long long)t * c.ld + sub * 8) = code;
+      }
+    }
+  } else {
+#pragma unroll 1
+    for (int i = 0; i < NP; ++i) {
+      const int t = i * TPP + tg;
+      if (t >= lo && t < hi) {
+        // (reads the row again: indexing the registers here would put them all into memory)
+        const uint4 x = __ldg(reinterpret_cast<const uint4*>(src + (long long)t * ld_x + sub * 8));
+        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+        float y[8];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float2 f = fp16ish_to_f32x2<BF>(w[e]);
+          y[2 * e] = isnan(f.x) ? 0.f : div(f.x);
+          y[2 * e + 1] = isnan(f.y) ? 0.f : div(f.y);
+        }
+        uint2 code;
+        code.x = f32_to_codes4<F8>(y[0], y[1], y[2], y[3]);
+        code.y = f32_to_codes4<F8>(y[4], y[5], y[6], y[7]);
+        *reinterpret_cast<uint2*>(dst + (long long)t * c.ld + sub * 8) = code;
+      }
     }
   }
   if (lo > 0 && s_new > s_old) {

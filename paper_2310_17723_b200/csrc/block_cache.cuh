@@ -99,6 +99,16 @@ __device__ __forceinline__ uint32_t f32_to_codes4(float a, float b, float c, flo
     return __byte_perm(__byte_perm(x, y, 0x0040), __byte_perm(z, w, 0x0040), 0x5410);
   }
 }
+// the same for quotients that are known to lie within the codes' range (|x| <= 127 s (1 + 2^-23)): no clamping
+template <bool F8>
+__device__ __forceinline__ uint32_t f32_to_codes4_inside(float2 a, float2 b) {
+  if constexpr (F8) {
+    return ptx::f32x4_to_e4m3x4(a.x, a.y, b.x, b.y);
+  } else {
+    const float2 magic = make_float2(12582912.0f, 12582912.0f), x = __fadd2_rn(a, magic), y = __fadd2_rn(b, magic);
+    return __byte_perm(__byte_perm(__float_as_uint(x.x), __float_as_uint(x.y), 0x0040), __byte_perm(__float_as_uint(y.x), __float_as_uint(y.y), 0x0040), 0x5410);
+  }
+}
 // x / s rounded to nearest, for many x and one s: with r the correctly rounded reciprocal of s, q = x r is within one unit of the
 // quotient and q + r (x - s q), the remainder formed exactly by a fused multiply-add, is the correctly rounded quotient
 // (P. Markstein, "Computation of elementary functions on the IBM RISC System/6000 processor", 1990).  Scales so small or
@@ -107,6 +117,11 @@ struct Divider {
   float s, r;
   bool fast;
   __device__ __forceinline__ explicit Divider(float s_) : s(s_), r(s_ > 0.f ? 1.0f / s_ : 0.f), fast(s_ > 7.8886e-31f && s_ < 1.2676e30f) {}
+  // two quotients at once; `fast` only
+  __device__ __forceinline__ float2 pair(float2 x) const {
+    const float2 r2 = make_float2(r, r), q = __fmul2_rn(x, r2);
+    return __ffma2_rn(__ffma2_rn(make_float2(-s, -s), q, x), r2, q);
+  }
   __device__ __forceinline__ float operator()(float x) const {
     if (!fast) return s > 0.f ? x / s : 0.f;
     const float q = x * r;
