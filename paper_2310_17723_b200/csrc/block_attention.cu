@@ -25,9 +25,11 @@ namespace hero {
 // and many short ones end at the same time.  A group of units cut by a share's end leaves partial results in the workspace (at
 // most two per CTA), which a second kernel joins.  Short sequences take one CTA per group and no second kernel.
 constexpr int ROWS_WARPS = 4;
-constexpr int ROWS_CTAS = 3;                    // resident per SM
-constexpr int ROWS_GROUP_UNITS = 4;             // what a group costs beside its steps (queries in, partial results out), in steps
-constexpr int ROWS_MIN_UNITS = 12;              // units of a share, at least
+constexpr int rows_ctas(int nt) { return nt == 3 ? 2 : 3; }   // resident per SM (NT = 3: 255 registers a thread)
+// what a group costs beside its steps (page numbers and queries in, partial results joined and out), in steps; with too low a figure
+// the share that holds a batch's shortest sequences ends last (4 for all: 126 us, these: 59 us on ragged drafts for 16 sequences)
+__host__ __device__ constexpr int rows_group_units(int nt) { return 8 + 5 * nt; }
+constexpr int ROWS_MIN_UNITS = 16;              // units of a share, at least
 constexpr int ROWS_DIRECT_STEPS = 16;           // up to this many steps (512 tokens) a group is one CTA's
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -69,7 +71,7 @@ __device__ __forceinline__ int feature_at(int place) { return (DH / 8) * ((place
 template <int R>
 __device__ __forceinline__ int tile_units(const SeqRows& s, int group, int qt) {
   const int total = s.n * group, last = (min((qt + 1) * R, total) - 1) / group;
-  return ((max(s.len - s.n + last + 1, 0) + 31) >> 5) + ROWS_GROUP_UNITS;
+  return ((max(s.len - s.n + last + 1, 0) + 31) >> 5) + rows_group_units(R / 8);
 }
 // A CTA's place in the work (in shared memory: nothing of it is held in registers through the loop over tokens).
 struct Place {
@@ -97,7 +99,7 @@ __device__ __forceinline__ long long seq_units(const BlockView& c, int group, in
 }
 
 template <int DH, int NT, bool BF, bool F8>
-__global__ void __launch_bounds__(ROWS_WARPS * 32, ROWS_CTAS) block_attn_rows_kernel(const __grid_constant__ CUtensorMap tm_k,
+__global__ void __launch_bounds__(ROWS_WARPS * 32, rows_ctas(NT)) block_attn_rows_kernel(const __grid_constant__ CUtensorMap tm_k,
                                                                              const __grid_constant__ CUtensorMap tm_v,
                                                                              const __grid_constant__ BlockAttnParams p) {
   using Smem = RowsSmem<DH, NT>;
@@ -557,12 +559,12 @@ static hero_status plan_rows(const hero_handle* h, const hero_block_cache* cc, i
     *out = r;
     return HERO_OK;
   }
-  r.nt = rows <= 8 ? 1 : 2;
+  r.nt = rows <= 8 ? 1 : rows > 16 && rows <= 24 ? 3 : 2;
   const long long tiles = (rows + 8 * r.nt - 1) / (8 * r.nt), groups = tiles * cc->nkv * cc->B, steps = ((long long)cc->max_len + 31) / 32;
   HERO_REQUIRE(groups <= (1ll << 30), HERO_ERR_UNSUPPORTED, "B=%d nkv=%d max_rows=%d: too many", cc->B, cc->nkv, max_rows);
   r.tiles = (int)tiles;
   r.direct = steps <= ROWS_DIRECT_STEPS;
-  const long long full = (long long)h->sm_count * ROWS_CTAS < JOIN_MAX_PARTS ? (long long)h->sm_count * ROWS_CTAS : JOIN_MAX_PARTS, useful = (groups * (steps + ROWS_GROUP_UNITS) + ROWS_MIN_UNITS - 1) / ROWS_MIN_UNITS;
+  const long long slots = (long long)h->sm_count * rows_ctas(r.nt), full = slots < JOIN_MAX_PARTS ? slots : JOIN_MAX_PARTS, useful = (groups * (steps + rows_group_units(r.nt)) + ROWS_MIN_UNITS - 1) / ROWS_MIN_UNITS;
   r.ctas = (int)(r.direct ? groups : (full < useful ? full : useful));
   r.bytes = r.direct ? 0 : (size_t)r.ctas * (2 * 8 * r.nt * (cc->dh * 4 + 8) + sizeof(JoinRecord));
   *out = r;
@@ -656,6 +658,8 @@ extern "C" hero_status hero_block_attention(hero_handle* h, const hero_block_cac
   p.records = reinterpret_cast<JoinRecord*>(p.part_ml + (size_t)plan.ctas * 2 * 8 * plan.nt);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (cc->dh == 64)
-    return plan.nt == 1 ? launch_rows<64, 1>(h, cc, p, bf, plan.ctas, s) : launch_rows<64, 2>(h, cc, p, bf, plan.ctas, s);
-  return plan.nt == 1 ? launch_rows<128, 1>(h, cc, p, bf, plan.ctas, s) : launch_rows<128, 2>(h, cc, p, bf, plan.ctas, s);
+    return plan.nt == 1 ? launch_rows<64, 1>(h, cc, p, bf, plan.ctas, s) : plan.nt == 2 ? launch_rows<64, 2>(h, cc, p, bf, plan.ctas, s)
+                                                                         : launch_rows<64, 3>(h, cc, p, bf, plan.ctas, s);
+  return plan.nt == 1 ? launch_rows<128, 1>(h, cc, p, bf, plan.ctas, s) : plan.nt == 2 ? launch_rows<128, 2>(h, cc, p, bf, plan.ctas, s)
+                                                                        : launch_rows<128, 3>(h, cc, p, bf, plan.ctas, s);
 }
