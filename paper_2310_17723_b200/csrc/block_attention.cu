@@ -27,9 +27,10 @@ namespace hero {
 constexpr int ROWS_WARPS = 4;
 constexpr int rows_ctas(int nt) { return nt == 3 ? 2 : 3; }   // resident per SM (NT = 3: 255 registers a thread)
 // what a group costs beside its steps (page numbers and queries in, partial results joined and out), in steps; with too low a figure
-// the share that holds a batch's shortest sequences ends last (4 for all: 126 us, these: 59 us on ragged drafts for 16 sequences)
+// the share that holds a batch's shortest sequences ends last (4 for all: 126 us, these: 54 us on ragged drafts for 16 sequences)
 __host__ __device__ constexpr int rows_group_units(int nt) { return 8 + 5 * nt; }
 constexpr int ROWS_MIN_UNITS = 16;              // units of a share, at least
+constexpr int ROWS_KEPT = 256;                  // sequences whose lengths and rows a CTA keeps in shared memory while it walks its share
 constexpr int ROWS_DIRECT_STEPS = 16;           // up to this many steps (512 tokens) a group is one CTA's
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -60,8 +61,9 @@ struct RowsSmem {
   static constexpr int OFF_SCALES = ROWS_WARPS * WARP;                      // float2 [warps][stages][2]: key and value scale of a half
   static constexpr int OFF_BARS = OFF_SCALES + ROWS_WARPS * STAGES * 16;    // uint64 [warps][stages]
   static constexpr int OFF_ML = OFF_BARS + ROWS_WARPS * STAGES * 8;         // float [2][warps][8 NT]
-  static constexpr int OFF_PLACE = OFF_ML + ROWS_WARPS * 8 * NT * 8;        // Place, long long [warps]
-  static constexpr int BYTES = 1024 + OFF_PLACE + 80 + ROWS_WARPS * 8;
+  static constexpr int OFF_PLACE = OFF_ML + ROWS_WARPS * 8 * NT * 8;        // Place, long long [warps], SeqRows [ROWS_KEPT]
+  static constexpr int OFF_SEQ = OFF_PLACE + 80 + ROWS_WARPS * 8;
+  static constexpr int BYTES = 1024 + OFF_SEQ + ROWS_KEPT * (int)sizeof(SeqRows);
 };
 // place of a feature in a partial O: rows of O^T in the order of the lanes that hold them
 template <int DH>
@@ -90,8 +92,7 @@ struct Place {
 struct JoinRecord { int b, qt, hk, parts; };     // a group that starts in this CTA's share and ends in a later one's; parts 0: none
 
 template <int R>
-__device__ __forceinline__ long long seq_units(const BlockView& c, int group, int b) {
-  const SeqRows s = seq_rows(c, b);
+__device__ __forceinline__ long long seq_units(const BlockView& c, int group, const SeqRows& s) {
   const int tiles = (s.n * group + R - 1) / R;
   long long u = 0;
   for (int qt = 0; qt < tiles; ++qt) u += tile_units<R>(s, group, qt);
@@ -126,6 +127,8 @@ __global__ void __launch_bounds__(ROWS_WARPS * 32, rows_ctas(NT)) block_attn_row
   const BlockView& c = p.c;
 
   // ---- this CTA's share of the units and the group it begins in
+  SeqRows* const kept = reinterpret_cast<SeqRows*>(smem + Smem::OFF_SEQ);
+  auto sequence = [&](int b) { return b < ROWS_KEPT ? kept[b] : seq_rows(c, b); };
   Place& at = *reinterpret_cast<Place*>(smem + Smem::OFF_PLACE);
   static_assert(sizeof(Place) <= 80, "");
   if (p.direct) {
@@ -142,7 +145,11 @@ __global__ void __launch_bounds__(ROWS_WARPS * 32, rows_ctas(NT)) block_attn_row
     long long* sums = reinterpret_cast<long long*>(smem + Smem::OFF_PLACE + 80);
     const int chunk = (p.B + ROWS_WARPS * 32 - 1) / (ROWS_WARPS * 32), b0 = min((int)threadIdx.x * chunk, p.B), b1 = min(b0 + chunk, p.B);
     long long own = 0, all = 0;
-    for (int b = b0; b < b1; ++b) own += seq_units<R>(c, p.group, b);
+    for (int b = b0; b < b1; ++b) {
+      const SeqRows s = seq_rows(c, b);
+      if (b < ROWS_KEPT) kept[b] = s;
+      own += seq_units<R>(c, p.group, s);
+    }
     long long incl = own;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -164,11 +171,11 @@ __global__ void __launch_bounds__(ROWS_WARPS * 32, rows_ctas(NT)) block_attn_row
       long long first = incl - own;
       int b = b0;
       for (;; ++b) {
-        const long long n = seq_units<R>(c, p.group, b);
+        const long long n = seq_units<R>(c, p.group, sequence(b));
         if (unit < first + n) break;
         first += n;
       }
-      const SeqRows s = seq_rows(c, b);
+      const SeqRows s = sequence(b);
       at.b = b; at.unit = unit; at.end = end; at.all = all; at.ctas = (int)ctas;
       for (at.qt = 0;; ++at.qt) {
         at.enter<R>(s, p.group);
@@ -212,13 +219,16 @@ __global__ void __launch_bounds__(ROWS_WARPS * 32, rows_ctas(NT)) block_attn_row
       if (n && (n & 15) == 0) load_pages(n);
       if ((lane >> 1) == (n & 15)) {
         const int h = lane & 1;
-        scales[2 * stage + h] = my_scales;         // (before the arrival that releases it)
         if (my_id >= 0) {
+          // (the copies are asked for before the scales have arrived; the bytes may be counted down before they are expected, the
+          // phase cannot end without this lane's arrival, which also releases the scales)
           const uint32_t bar = ptx::smem_u32(&full_bar[stage]), dst = ring_a + stage * Smem::STAGE + h * Smem::HALF;
-          ptx::mbar_expect_tx(&full_bar[stage], 2 * Smem::HALF);
           load_half(dst, &tm_k, my_token, hk, my_id, bar);
           load_half(dst + 2 * Smem::HALF, &tm_v, my_token, hk, my_id, bar);
+          scales[2 * stage + h] = my_scales;
+          ptx::mbar_expect_tx(&full_bar[stage], 2 * Smem::HALF);
         } else {
+          scales[2 * stage + h] = make_float2(0.f, 0.f);
           ptx::mbar_arrive(&full_bar[stage]);
         }
       }
@@ -440,24 +450,31 @@ __global__ void __launch_bounds__(ROWS_WARPS * 32, rows_ctas(NT)) block_attn_row
     const long long group_end = at.first + at.units;
     const bool head = at.unit == at.first, tail = group_end <= at.end, whole = head && tail;   // the group begins / ends in this share
     const long long slot = 2ll * blockIdx.x + (head ? 1 : 0);            // of a partial result: the group goes on / came in
-    for (int i = threadIdx.x; i < R * DH; i += ROWS_WARPS * 32) {
-      const int row = i / DH, place = i % DH, rr = at.qt * R + row;
-      if (rr >= at.total) continue;
-      float mt = sm[row];
+    if (threadIdx.x < R) {                       // one thread per row: the warps' weights, the tile's maximum and sum
+      const int row = threadIdx.x;
+      float mt = sm[row], lt = 0.f, e[ROWS_WARPS];
 #pragma unroll
       for (int w = 1; w < ROWS_WARPS; ++w) mt = fmaxf(mt, sm[w * R + row]);
-      float y = 0.f, lt = 0.f;
 #pragma unroll
       for (int w = 0; w < ROWS_WARPS; ++w) {
-        const float mw = sm[w * R + row], e = mw > -INFINITY ? ex2(mw - mt) : 0.f;
-        y = fmaf(e, reinterpret_cast<const float*>(smem + w * Smem::WARP)[row * Smem::OROW + place], y); lt = fmaf(e, sl[w * R + row], lt);
+        const float mw = sm[w * R + row];
+        e[w] = mw > -INFINITY ? ex2(mw - mt) : 0.f;
+        lt = fmaf(e[w], sl[w * R + row], lt);
       }
-      if (whole) {
-        store_out(p, at.r0 + rr / p.group, (at.hk * p.group + rr % p.group) * DH + feature_at<DH>(place), lt != 0.f ? y / lt : 0.f);
-      } else {
-        p.part_o[slot * (R * DH) + i] = y;
-        if (place == 0) p.part_ml[slot * R + row] = make_float2(mt, lt);
-      }
+      const float inv = whole ? (lt != 0.f ? 1.0f / lt : 0.f) : 1.0f;
+#pragma unroll
+      for (int w = 0; w < ROWS_WARPS; ++w) sm[w * R + row] = e[w] * inv;
+      if (!whole && at.qt * R + row < at.total) p.part_ml[slot * R + row] = make_float2(mt, lt);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < R * DH; i += ROWS_WARPS * 32) {
+      const int row = i / DH, place = i % DH, rr = at.qt * R + row;
+      if (rr >= at.total) break;                 // (rows ascend with i)
+      float y = 0.f;
+#pragma unroll
+      for (int w = 0; w < ROWS_WARPS; ++w) y = fmaf(sm[w * R + row], reinterpret_cast<const float*>(smem + w * Smem::WARP)[row * Smem::OROW + place], y);
+      if (whole) store_out(p, at.r0 + rr / p.group, (at.hk * p.group + rr % p.group) * DH + feature_at<DH>(place), y);
+      else p.part_o[slot * (R * DH) + i] = y;
     }
     const bool done = group_end >= at.end;
     __syncthreads();                             // everybody has read the partial O and the place
@@ -473,7 +490,7 @@ __global__ void __launch_bounds__(ROWS_WARPS * 32, rows_ctas(NT)) block_attn_row
           SeqRows s = SeqRows{at.len, at.n, at.r0};
           if (++at.qt * R >= at.total) {
             at.qt = 0;
-            do s = seq_rows(c, ++at.b); while (s.n == 0);   // (a unit is left, so a sequence with rows is)
+            do s = sequence(++at.b); while (s.n == 0);   // (a unit is left, so a sequence with rows is)
           }
           at.enter<R>(s, p.group);
         }
