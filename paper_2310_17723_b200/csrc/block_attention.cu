@@ -89,7 +89,7 @@ struct Place {
     units = tile_units<R>(s, group, qt);
   }
 };
-struct JoinRecord { int b, qt, hk, parts; };     // a group that starts in this CTA's share and ends in a later one's; parts 0: none
+struct __align__(16) JoinRecord { int parts, share, group, pad; };   // a group cut into `parts`, from share `share` on; parts 0: not cut
 
 template <int R>
 __device__ __forceinline__ long long seq_units(const BlockView& c, int group, const SeqRows& s) {
@@ -164,7 +164,7 @@ __global__ void __launch_bounds__(ROWS_WARPS * 32, rows_ctas(NT)) block_attn_row
     const long long ctas = min((long long)gridDim.x, max(all / ROWS_MIN_UNITS, 1ll));
     const long long unit = all * blockIdx.x / ctas, end = all * (blockIdx.x + 1) / ctas;
     if (blockIdx.x >= ctas || all == 0) {
-      if (threadIdx.x == 0) p.records[blockIdx.x].parts = 0;
+      if (threadIdx.x == 0 && !p.by_group) p.records[blockIdx.x].parts = 0;
       return;
     }
     if (incl - own <= unit && unit < incl) {     // one thread: the sequence, then the row tile and head
@@ -479,11 +479,13 @@ __global__ void __launch_bounds__(ROWS_WARPS * 32, rows_ctas(NT)) block_attn_row
     const bool done = group_end >= at.end;
     __syncthreads();                             // everybody has read the partial O and the place
     if (threadIdx.x == 0) {
-      if (done) {
+      if (!p.direct && (p.by_group ? head : done)) {
         // the CTA that the group's last unit belongs to: shares are [all c / ctas, all (c + 1) / ctas)
-        if (!p.direct)
-          p.records[blockIdx.x] = JoinRecord{at.b, at.qt, at.hk, head && !tail ? (int)((group_end * at.ctas - 1) / at.all) - (int)blockIdx.x + 1 : 0};
-      } else {
+        const int parts = head && !tail ? (int)((group_end * at.ctas - 1) / at.all) - (int)blockIdx.x + 1 : 0;
+        const int group = (at.b * p.tiles + at.qt) * c.nkv + at.hk;
+        p.records[p.by_group ? group : (int)blockIdx.x] = JoinRecord{parts, (int)blockIdx.x, group, 0};
+      }
+      if (!done) {
         at.unit = at.first = group_end;          // the next group: head, row tile, sequence
         if (++at.hk == c.nkv) {
           at.hk = 0;
@@ -502,71 +504,92 @@ __global__ void __launch_bounds__(ROWS_WARPS * 32, rows_ctas(NT)) block_attn_row
   }
 }
 
-// joins the partial results of a group that was cut: CTA (c, row) takes one row of the tile of the group that began in share c.
-// The parts are dealt out to the warps, a lane holds DH / 32 places: the loads of all parts are in flight together.
-constexpr int JOIN_WARPS = 4, JOIN_MAX_PARTS = 1024;
+// joins the partial results of a group that was cut.  CTA (x, row) takes one row of the tile of group x, or, where there are more
+// groups than shares, of the group that began in share x and went on.  What it costs is its chain of loads, so there are two links:
+// the record beside the sequence's rows, then maxima, sums and values of all parts at once (dealt out to the warps, merged with a
+// running maximum).
+constexpr int JOIN_WARPS = 8, JOIN_MAX_PARTS = 1024;
 template <int DH, int NT>
 __global__ void __launch_bounds__(JOIN_WARPS * 32) block_attn_join_kernel(const __grid_constant__ BlockAttnParams p) {
   constexpr int R = 8 * NT, E = DH / 32;
-  __shared__ float weight[JOIN_MAX_PARTS], red[JOIN_WARPS], sum[JOIN_WARPS], part[JOIN_WARPS][DH];
-  ptx::pdl_launch_dependents();
+  __shared__ float part[JOIN_WARPS][DH], ms[JOIN_WARPS], ls[JOIN_WARPS];
+  // (not first thing, as elsewhere: CTAs of the next kernel that took up the SMs of this one's predecessor cost 64 against 54 us on two
+  // sequences of 131072 tokens, step after step)
   ptx::pdl_wait();
-  const JoinRecord rec = p.records[blockIdx.x];
-  if (rec.parts == 0) return;
-  const SeqRows s = seq_rows(p.c, rec.b);
-  const int row = blockIdx.y, rr = rec.qt * R + row, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  if (rr >= s.n * p.group) return;
-  // the first part lies in the second slot of its CTA, the others in the first slots of the CTAs behind it
-  auto slot = [&](int q) { return (2ll * (blockIdx.x + q) + (q == 0 ? 1 : 0)) * R + row; };
-  float mt = -INFINITY;
-  for (int q = threadIdx.x; q < rec.parts; q += JOIN_WARPS * 32) {
-    weight[q] = p.part_ml[slot(q)].x;
-    mt = fmaxf(mt, weight[q]);
+  ptx::pdl_launch_dependents();
+  JoinRecord rec;
+  *reinterpret_cast<int4*>(&rec) = *reinterpret_cast<const int4*>(&p.records[blockIdx.x]);
+  int b, qt, hk;
+  if (p.by_group) {
+    hk = blockIdx.x % p.c.nkv; qt = blockIdx.x / p.c.nkv % p.tiles; b = blockIdx.x / p.c.nkv / p.tiles;
+  } else {
+    if (rec.parts == 0) return;
+    const int rest = rec.group / p.c.nkv;
+    hk = rec.group % p.c.nkv; qt = rest % p.tiles; b = rest / p.tiles;
   }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) mt = fmaxf(mt, __shfl_xor_sync(0xffffffffu, mt, o));
-  if (lane == 0) red[warp] = mt;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < JOIN_WARPS; ++w) mt = fmaxf(mt, red[w]);
-  float lt = 0.f;
-  for (int q = threadIdx.x; q < rec.parts; q += JOIN_WARPS * 32) {
-    const float f = weight[q] > -INFINITY ? ex2(weight[q] - mt) : 0.f;
-    weight[q] = f;
-    lt = fmaf(f, p.part_ml[slot(q)].y, lt);
-  }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) lt += __shfl_xor_sync(0xffffffffu, lt, o);
-  if (lane == 0) sum[warp] = lt;
-  __syncthreads();
-  float y[E];
+  const SeqRows s = seq_rows(p.c, b);
+  const int row = blockIdx.y, rr = qt * R + row, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (rr >= s.n * p.group || rec.parts == 0) return;               // (a record of rows that are not there was never written)
+  constexpr float LEAST = -1e30f;                // below every maximum, and finite: no case for parts without a key
+  float m = LEAST, l = 0.f, y[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) y[e] = 0.f;
-#pragma unroll 8
-  for (int q = warp; q < rec.parts; q += JOIN_WARPS) {
-    const float f = weight[q];
-    const float* src = p.part_o + slot(q) * DH + lane * E;
-    if constexpr (E == 4) {
-      const float4 x = *reinterpret_cast<const float4*>(src);
-      y[0] = fmaf(f, x.x, y[0]); y[1] = fmaf(f, x.y, y[1]); y[2] = fmaf(f, x.z, y[2]); y[3] = fmaf(f, x.w, y[3]);
-    } else {
-      const float2 x = *reinterpret_cast<const float2*>(src);
-      y[0] = fmaf(f, x.x, y[0]); y[1] = fmaf(f, x.y, y[1]);
+  for (int q0 = warp; q0 < rec.parts; q0 += 8 * JOIN_WARPS) {
+    float2 ml[8];
+    float x[8][E];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {                // eight parts in flight per warp (behind the last one: that one again, without weight)
+      const int q = min(q0 + k * JOIN_WARPS, rec.parts - 1);
+      // the first part lies in the second slot of its CTA, the others in the first slots of the CTAs behind it
+      const long long at = (2ll * (rec.share + q) + (q == 0 ? 1 : 0)) * R + row;
+      ml[k] = __ldg(p.part_ml + at);
+      if constexpr (E == 4) {
+        const float4 v = __ldg(reinterpret_cast<const float4*>(p.part_o + at * DH) + lane);
+        x[k][0] = v.x; x[k][1] = v.y; x[k][2] = v.z; x[k][3] = v.w;
+      } else {
+        const float2 v = __ldg(reinterpret_cast<const float2*>(p.part_o + at * DH) + lane);
+        x[k][0] = v.x; x[k][1] = v.y;
+      }
+    }
+    float top = m;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if (q0 + k * JOIN_WARPS >= rec.parts) ml[k] = make_float2(-INFINITY, 0.f);
+      top = fmaxf(top, ml[k].x);
+    }
+    const float old = ex2(m - top);
+    m = top;
+    l *= old;
+#pragma unroll
+    for (int e = 0; e < E; ++e) y[e] *= old;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float f = ex2(ml[k].x - top);
+      l = fmaf(f, ml[k].y, l);
+#pragma unroll
+      for (int e = 0; e < E; ++e) y[e] = fmaf(f, x[k][e], y[e]);
     }
   }
 #pragma unroll
   for (int e = 0; e < E; ++e) part[warp][lane * E + e] = y[e];
+  if (lane == 0) { ms[warp] = m; ls[warp] = l; }
   __syncthreads();
   if (threadIdx.x < DH) {
-    float o = 0.f, l = 0.f;
+    float mt = ms[0], o = 0.f, lt = 0.f;
 #pragma unroll
-    for (int w = 0; w < JOIN_WARPS; ++w) { o += part[w][threadIdx.x]; l += sum[w]; }
-    store_out(p, s.r0 + rr / p.group, (rec.hk * p.group + rr % p.group) * DH + feature_at<DH>(threadIdx.x), l != 0.f ? o / l : 0.f);
+    for (int w = 1; w < JOIN_WARPS; ++w) mt = fmaxf(mt, ms[w]);
+#pragma unroll
+    for (int w = 0; w < JOIN_WARPS; ++w) {
+      const float f = ex2(ms[w] - mt);
+      o = fmaf(f, part[w][threadIdx.x], o);
+      lt = fmaf(f, ls[w], lt);
+    }
+    store_out(p, s.r0 + rr / p.group, (hk * p.group + rr % p.group) * DH + feature_at<DH>(threadIdx.x), lt != 0.f ? o / lt : 0.f);
   }
 }
 
 // How a call is dealt out; the host knows upper bounds of lengths and rows only.
-struct RowsPlan { int nt, tiles, ctas; bool direct, prompt; size_t bytes; };
+struct RowsPlan { int nt, tiles, ctas, records; bool direct, prompt, by_group; size_t bytes; };
 static hero_status plan_rows(const hero_handle* h, const hero_block_cache* cc, int nq, int max_rows, RowsPlan* out) {
   const long long rows = (long long)max_rows * (nq / cc->nkv);
   RowsPlan r;
@@ -583,13 +606,15 @@ static hero_status plan_rows(const hero_handle* h, const hero_block_cache* cc, i
   r.direct = steps <= ROWS_DIRECT_STEPS;
   const long long slots = (long long)h->sm_count * rows_ctas(r.nt), full = slots < JOIN_MAX_PARTS ? slots : JOIN_MAX_PARTS, useful = (groups * (steps + rows_group_units(r.nt)) + ROWS_MIN_UNITS - 1) / ROWS_MIN_UNITS;
   r.ctas = (int)(r.direct ? groups : (full < useful ? full : useful));
-  r.bytes = r.direct ? 0 : (size_t)r.ctas * (2 * 8 * r.nt * (cc->dh * 4 + 8) + sizeof(JoinRecord));
+  r.by_group = groups <= r.ctas;                 // the shorter list of candidates for a join
+  r.records = r.by_group ? (int)groups : r.ctas;
+  r.bytes = r.direct ? 0 : (size_t)r.ctas * 2 * 8 * r.nt * (cc->dh * 4 + 8) + (size_t)r.records * sizeof(JoinRecord);
   *out = r;
   return HERO_OK;
 }
 
 template <int DH, int NT>
-static hero_status launch_rows(hero_handle* h, const hero_block_cache* cc, const BlockAttnParams& p, bool bf, int ctas, cudaStream_t stream) {
+static hero_status launch_rows(hero_handle* h, const hero_block_cache* cc, const BlockAttnParams& p, bool bf, int ctas, int records, cudaStream_t stream) {
   auto kern = bf ? (p.c.f8 ? block_attn_rows_kernel<DH, NT, true, true> : block_attn_rows_kernel<DH, NT, true, false>)
                  : (p.c.f8 ? block_attn_rows_kernel<DH, NT, false, true> : block_attn_rows_kernel<DH, NT, false, false>);
   constexpr int BYTES = RowsSmem<DH, NT>::BYTES;
@@ -608,7 +633,7 @@ static hero_status launch_rows(hero_handle* h, const hero_block_cache* cc, const
   }
   if (!p.direct) {
     LaunchScope scope(h, stream, KERNEL_ATTN);
-    HERO_CUDA(launch_dependent(block_attn_join_kernel<DH, NT>, dim3((unsigned)ctas, 8 * NT), dim3(JOIN_WARPS * 32), 0, stream, p));
+    HERO_CUDA(launch_dependent(block_attn_join_kernel<DH, NT>, dim3((unsigned)records, 8 * NT), dim3(JOIN_WARPS * 32), 0, stream, p));
   }
   return HERO_OK;
 }
@@ -669,14 +694,14 @@ extern "C" hero_status hero_block_attention(hero_handle* h, const hero_block_cac
                a->workspace_bytes, plan.bytes);
   HERO_REQUIRE(plan.bytes == 0 || aligned16(a->workspace), HERO_ERR_ALIGNMENT, "the workspace must be 16-byte aligned");
   if (plan.prompt) return launch_prompt(h, cc, p, bf, static_cast<cudaStream_t>(stream));
-  p.B = cc->B; p.tiles = plan.tiles; p.direct = plan.direct;
+  p.B = cc->B; p.tiles = plan.tiles; p.direct = plan.direct; p.by_group = plan.by_group;
   p.part_o = static_cast<float*>(a->workspace);
   p.part_ml = reinterpret_cast<float2*>(p.part_o + (size_t)plan.ctas * 2 * 8 * plan.nt * cc->dh);
   p.records = reinterpret_cast<JoinRecord*>(p.part_ml + (size_t)plan.ctas * 2 * 8 * plan.nt);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (cc->dh == 64)
-    return plan.nt == 1 ? launch_rows<64, 1>(h, cc, p, bf, plan.ctas, s) : plan.nt == 2 ? launch_rows<64, 2>(h, cc, p, bf, plan.ctas, s)
-                                                                         : launch_rows<64, 3>(h, cc, p, bf, plan.ctas, s);
-  return plan.nt == 1 ? launch_rows<128, 1>(h, cc, p, bf, plan.ctas, s) : plan.nt == 2 ? launch_rows<128, 2>(h, cc, p, bf, plan.ctas, s)
-                                                                        : launch_rows<128, 3>(h, cc, p, bf, plan.ctas, s);
+    return plan.nt == 1 ? launch_rows<64, 1>(h, cc, p, bf, plan.ctas, plan.records, s) : plan.nt == 2 ? launch_rows<64, 2>(h, cc, p, bf, plan.ctas, plan.records, s)
+                                                                         : launch_rows<64, 3>(h, cc, p, bf, plan.ctas, plan.records, s);
+  return plan.nt == 1 ? launch_rows<128, 1>(h, cc, p, bf, plan.ctas, plan.records, s) : plan.nt == 2 ? launch_rows<128, 2>(h, cc, p, bf, plan.ctas, plan.records, s)
+                                                                        : launch_rows<128, 3>(h, cc, p, bf, plan.ctas, plan.records, s);
 }

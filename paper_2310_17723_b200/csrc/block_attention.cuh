@@ -12,7 +12,8 @@ struct BlockAttnParams {
   int nq, group;
   float c2;                      // scale * log2(e)
   int B, tiles, direct;          // direct: CTA index = (sequence, row tile, head); else equal shares of all units
-  struct JoinRecord* records;    // [CTA]
+  int by_group;                  // records of cut groups are listed by group, else by share
+  struct JoinRecord* records;
   float* part_o; float2* part_ml; // partial results [CTA][2]: sum of P V [rows][DH], (maximum, sum of P) [rows]
 };
 

@@ -88,7 +88,8 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
   ptx::pdl_wait();
 
   const BlockView& c = p.c;
-  const int b = blockIdx.y, hk = blockIdx.x % c.nkv, qt = p.tiles - 1 - blockIdx.x / c.nkv;   // late rows (many keys) first
+  // late rows, which see many keys, of all sequences first
+  const int bh = blockIdx.x % (c.nkv * p.B), hk = bh % c.nkv, b = bh / c.nkv, qt = p.tiles - 1 - blockIdx.x / (c.nkv * p.B);
   const SeqRows s = seq_rows(c, b);
   const int total = s.n * p.group, rb = qt * PR_ROWS, base = s.len - s.n;
   // keys of a row tile's last row, and its tiles of keys
@@ -485,7 +486,7 @@ static hero_status launch(hero_handle* h, const hero_block_cache* cc, const Bloc
   const uint32_t idesc_qk = ptx::make_idesc(1, 0, 0, 0, 0, 128, 64), idesc_pv = ptx::make_idesc(1, 0, 0, 0, 1, 128, DH);
   {
     LaunchScope scope(h, stream, KERNEL_ATTN);
-    HERO_CUDA(launch_dependent(kern, dim3((unsigned)(p.tiles * p.c.nkv), (unsigned)cc->B), dim3(PR_THREADS), BYTES, stream, p, idesc_qk, idesc_pv));
+    HERO_CUDA(launch_dependent(kern, dim3((unsigned)((long long)p.tiles * p.c.nkv * cc->B)), dim3(PR_THREADS), BYTES, stream, p, idesc_qk, idesc_pv));
   }
   return HERO_OK;
 }
@@ -493,8 +494,8 @@ static hero_status launch(hero_handle* h, const hero_block_cache* cc, const Bloc
 hero_status launch_prompt(hero_handle* h, const hero_block_cache* cc, const BlockAttnParams& p_, bool bf, cudaStream_t stream) {
   BlockAttnParams p = p_;
   const long long tiles = ((long long)p.c.max_rows * p.group + PR_ROWS - 1) / PR_ROWS;
-  HERO_REQUIRE(tiles * p.c.nkv < (1ll << 31), HERO_ERR_UNSUPPORTED, "max_rows=%d nkv=%d: too many", p.c.max_rows, p.c.nkv);
-  p.tiles = (int)tiles;
+  HERO_REQUIRE(tiles * p.c.nkv * cc->B < (1ll << 31), HERO_ERR_UNSUPPORTED, "max_rows=%d nkv=%d B=%d: too many", p.c.max_rows, p.c.nkv, cc->B);
+  p.tiles = (int)tiles; p.B = cc->B;
   return cc->dh == 64 ? launch<64>(h, cc, p, bf, stream) : launch<128>(h, cc, p, bf, stream);
 }
 
