@@ -1,0 +1,179 @@
+"""GPU parity of hero_block_attention where its work is dealt out differently: row tiles of every size, more sequences than a CTA keeps
+in shared memory, more groups than CTAs, nothing to do, maxima and value scales that move, caches beyond four gigabytes, two
+streams at once.  Bounds as in test_gpu_block_attention.py."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import block_cache as BC
+from paper_2310_17723_b200 import hero
+from block_util import Cache, FP, start_tensor, starts, to_fp
+from test_gpu_block_attention import _compare, _expect, _q, _run
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def h():
+    hd = hero.Handle()
+    yield hd
+    hd.check()
+    hd.close()
+
+
+@pytest.mark.parametrize("group,counts", [(4, [6, 1, 0, 5, 3]), (8, [3, 2, 1, 3, 1]), (1, [20, 24, 1, 0, 17]), (1, [32, 25, 3, 9, 31]), (5, [6, 5, 4, 1, 2]),
+                                          (33, [1, 1, 1, 1, 1]), (40, [2, 1, 2, 0, 1])])
+@pytest.mark.parametrize("dh,kind", [(64, "f8"), (128, "i8")])
+def test_row_tiles_of_every_size(h, group, counts, dh, kind):
+    lens = [700, 40, 9, 1025, 333]
+    c = Cache(80 + group, kind, 32, 2, dh, lens, max_len=1500)
+    qt, qx = _q(1, sum(counts) + 1, 2 * group * dh, "bf16")
+    _compare(c, _run(h, c, qt, counts, 2 * group, "bf16"), qx, counts, 2 * group, "bf16")
+
+
+@pytest.mark.parametrize("layout", ["nhd", "padded"])
+@pytest.mark.parametrize("page", [16, 128])
+def test_prompts_of_several_row_tiles_in_any_layout(h, layout, page):
+    counts, lens = [300, 129, 1, 0, 256], [300, 400, 77, 5, 1000]
+    c = Cache(90 + page, "i8", page, 2, 128, lens, max_len=1200, layout=layout)
+    qt, qx = _q(2, sum(counts) + 2, 4 * 128, "f16")
+    _compare(c, _run(h, c, qt, counts, 4, "f16"), qx, counts, 4, "f16")
+
+
+def test_more_sequences_and_groups_than_are_kept_or_resident(h):
+    B, nkv, dh = 700, 2, 64
+    g = np.random.default_rng(3)
+    lens = [int(x) for x in g.integers(0, 60, B)]
+    lens[5], lens[300], lens[699] = 900, 640, 513
+    counts = [int(x) for x in g.integers(0, 3, B)]
+    c = Cache(95, "i8", 16, nkv, dh, lens, max_len=1000)
+    qt, qx = _q(3, sum(counts), 2 * nkv * dh, "f16")
+    _compare(c, _run(h, c, qt, counts, 2 * nkv, "f16"), qx, counts, 2 * nkv, "f16")
+
+
+@pytest.mark.parametrize("max_rows,max_len", [(1, 100), (1, 9000), (64, 9000)])
+def test_sequences_without_rows_or_tokens(h, max_rows, max_len):
+    # no rows at all: nothing is written; rows without a token: zeros, whatever the kernel
+    c = Cache(96, "f8", 64, 2, 64, [0, 10, 0], max_len=max_len)
+    qt, _ = _q(4, 3, 4 * 64, "bf16")
+    out = _run(h, c, qt, [0, 0, 0], 4, "bf16", max_rows=max_rows)
+    assert torch.all(out == 7.0)
+    c.set_lens([0, 0, 0])
+    out = _run(h, c, qt, [1, 1, 1], 4, "bf16", max_rows=max_rows)
+    assert torch.all(out == 0)
+
+
+@pytest.mark.parametrize("counts", [[1, 1], [5, 2], [100, 60]])
+@pytest.mark.parametrize("kind", ["i8", "f8"])
+def test_maxima_and_value_scales_that_keep_moving(h, counts, kind):
+    # every page's keys are about 1.5 times as large as the page's before, so a row's largest score moves up again and again; the value
+    # scales rise by a factor of 3 a page.  Probabilities below FP16's normal range are off by half of its smallest step, 2^-25, under a factor
+    # of at least 2^8 by which P is formed, in units of the largest value scale: 2^-33 of the largest |v| per key.
+    lens = [500, 380]
+    c = Cache(97, kind, 32, 1, 64, lens)
+    for b in range(2):
+        for i, pid in enumerate(c.table[b]):
+            c.scale["k"][pid] = 0.002 * 1.5 ** i
+            c.scale["v"][pid] = 1e-4 * 3.0 ** i
+    for x in "kv":
+        c.scale_t[x].copy_(torch.from_numpy(c.scale[x]))
+    rows = sum(counts)
+    qt, qx = _q(5, rows, 4 * 64, "bf16")
+    out = _run(h, c, qt, counts, 4, "bf16")
+    want, bar = _expect(c, qx, counts, 4, 64 ** -0.5, rows)
+    reach = np.concatenate([np.full(n, np.abs(c.values("v", b)).max()) for b, n in enumerate(counts)])[:, None]
+    bar = bar + 500 * 2.0 ** -33 * reach
+    bar = bar + torch.finfo(torch.bfloat16).eps / 2 * (np.abs(want) + bar)
+    got = out.double().cpu().numpy()
+    assert np.all(np.abs(got - want) <= bar), np.max(np.abs(got - want) / bar)
+
+
+def test_value_scales_that_begin_with_zero(h):
+    # pages of zeros first (scale 0), loud pages behind them: what was summed under scale 0 counts nothing
+    for counts in ([1], [80]):
+        c = Cache(98, "i8", 16, 1, 128, [200])
+        for i, pid in enumerate(c.table[0]):
+            if i < 9:
+                c.scale["v"][pid] = 0
+        c.scale_t["v"].copy_(torch.from_numpy(c.scale["v"]))
+        qt, qx = _q(6, counts[0], 2 * 128, "f16")
+        _compare(c, _run(h, c, qt, counts, 2, "f16"), qx, counts, 2, "f16")
+
+
+def test_attention_beyond_four_gigabytes(h):
+    page, nkv, dh = 128, 8, 128
+    n = int(4.6e9 // (page * nkv * dh))
+    buf = torch.zeros(n, nkv, page, dh, dtype=torch.int8, device="cuda")
+    scale = torch.zeros(n, nkv, device="cuda")
+    table = torch.tensor([[n - 1, 0], [n // 2, n - 2]], dtype=torch.int32, device="cuda")
+    small = Cache(99, "i8", page, nkv, dh, [200, 130], max_len=256)
+    for b in range(2):
+        for i in range(2):
+            buf[int(table[b, i])] = small.buf["k"][int(small.table[b, i])]
+            scale[int(table[b, i])] = small.scale_t["k"][int(small.table[b, i])]
+    small.codes["v"], small.scale["v"] = small.codes["k"], small.scale["k"]          # one buffer for both
+    small.desc = hero.block_cache(buf, buf, scale, scale, table, small.lens_t, 256)
+    for counts in ([1, 1], [60, 40]):
+        qt, qx = _q(7, sum(counts), 2 * nkv * dh, "bf16")
+        _compare(small, _run(h, small, qt, counts, 2 * nkv, "bf16"), qx, counts, 2 * nkv, "bf16")
+
+
+def test_two_streams_with_a_workspace_each(h):
+    cs = [Cache(100 + i, "i8", 64, 2, 128, [5000, 900, 3000], max_len=6000) for i in range(2)]
+    qs = [_q(8 + i, 3, 8 * 128, "bf16") for i in range(2)]
+    want = [_run(h, c, q[0], [1] * 3, 8, "bf16") for c, q in zip(cs, qs)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = [torch.zeros_like(w) for w in want]
+    wss = [torch.empty(h.hero_block_attention_workspace_bytes(c.desc, 8, 3, 1), dtype=torch.uint8, device="cuda") for c in cs]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for i, s in enumerate(streams):
+            h.hero_block_attention(cs[i].desc, hero.tensor(qs[i][0]), hero.tensor(outs[i]), 8, workspace=wss[i], stream=s)
+    torch.cuda.synchronize()
+    h.check()
+    for o, w in zip(outs, want):
+        assert torch.equal(o, w)
+
+
+def test_a_prompt_and_its_steps_agree(h):
+    # a prompt is appended and attended to in one call; the same tokens one by one, each appended and attended to, on a cache of their own,
+    # see scales that grew differently: both against the oracle on the codes that the device holds
+    nq, nkv, dh, n = 4, 2, 64, 50
+    g = np.random.default_rng(11)
+    kt, _ = to_fp(g.standard_normal((n, nkv * dh)), "f16")
+    vt, _ = to_fp(g.standard_normal((n, nkv * dh)), "f16")
+    qt, qx = _q(12, n, nq * dh, "f16")
+    c = Cache(101, "i8", 16, nkv, dh, [n], max_len=64)
+    s = start_tensor([n])
+    h.hero_block_cache_append(c.desc, hero.tensor(kt), hero.tensor(vt), row_start=s, max_rows=n)
+    out = _run(h, c, qt, [n], nq, "f16")
+    for x in "kv":
+        c.codes[x], c.scale[x] = c.device_codes(x), c.scale_t[x].cpu().numpy()
+    _compare(c, out, qx, [n], nq, "f16")
+    d = Cache(102, "i8", 16, nkv, dh, [n], max_len=64)
+    for i in range(n):
+        d.set_lens([i + 1])
+        h.hero_block_cache_append(d.desc, hero.tensor(kt[i:i + 1]), hero.tensor(vt[i:i + 1]))
+        step = _run(h, d, qt[i:i + 1], [1], nq, "f16")
+        for x in "kv":
+            d.codes[x], d.scale[x] = d.device_codes(x), d.scale_t[x].cpu().numpy()
+        _compare(d, step, qx[i:i + 1], [1], nq, "f16")
+
+
+def test_binding_refusals(h):
+    c = Cache(103, "i8", 16, 1, 64, [5, 5])
+    q = hero.tensor(torch.zeros(2, 64, dtype=torch.bfloat16, device="cuda"))
+    ok = start_tensor([1, 1])
+    for kw in (dict(row_start=ok[:2]), dict(row_start=ok.long()), dict(row_start=ok.cpu()), dict(workspace=torch.zeros(64, dtype=torch.float32, device="cuda")),
+               dict(workspace=torch.zeros(64, dtype=torch.uint8))):
+        with pytest.raises(hero.HeroError):
+            h.hero_block_attention(c.desc, q, q, 1, **kw)
+    k = c.buf["k"]
+    with pytest.raises(hero.HeroError):
+        hero.block_cache(k, k[:, :, :8], c.scale_t["k"], c.scale_t["v"], c.table_t, c.lens_t, 5)
+    with pytest.raises(hero.HeroError):
+        hero.block_cache(k, k, c.scale_t["k"].double(), c.scale_t["v"], c.table_t, c.lens_t, 5)
+    with pytest.raises(hero.HeroError):
+        hero.block_cache(k, k, c.scale_t["k"], c.scale_t["v"], c.table_t, c.lens_t[:1], 5)
+    with pytest.raises(hero.HeroError):
+        hero.block_cache(k, k, c.scale_t["k"], c.scale_t["v"], c.table_t.cpu(), c.lens_t, 5)
