@@ -485,6 +485,7 @@ hero_status hero_static_check(void* stream);
  *   value of (page p, head g, token t, feature c) = code(p, g, t, c) * scale[p * nkv + g]
  *   code at k (or v) + p * page_stride + g * head_stride + t * ld + c, one byte: I8 in [-127, 127] or F8 (e4m3)
  *   token t of sequence b is token t % page of page table[b * ld_table + t / page]
+ *   scales are finite and not negative (0: a page of zeros)
  *
  * Strides are in elements (= bytes), multiples of 16 and at least dh, so that [pages][nkv][page][dh] and
  * [pages][page][nkv][dh] are both expressible; k and v are 16-byte aligned.  `len[b]` counts the tokens that sequence b

@@ -390,7 +390,7 @@ class Handle:
     def _here(self, *descs):
         """Every hero.Tensor of a call lives on the handle's device."""
         for d in descs:
-            if d is not None and getattr(d, "_device", self._device) != self._device:
+            if d is not None and getattr(d, "_device", None) != self._device:
                 _refuse("a tensor is not on the handle's device %d" % self._device)
 
     def _raw_stream(self, stream):
@@ -438,7 +438,7 @@ class Handle:
         """q, k, q_out, k_out: hero.Tensor ([rows, nq*dh] / [rows, nkv*dh]; k and k_out None with nkv = 0; an output may be its
         input); pos: int32 [rows]; cos, sin: float32 [n_pos, rot / 2] (None: no rotation); gammas: float32 [dh] (None: no norm)."""
         self._here(q, k, q_out, k_out)
-        dh, rot, n_pos = q.cols // nq, 0, 0
+        dh, rot, n_pos = q.cols // max(nq, 1), 0, 0
         if cos is not None:
             n_pos, half = cos.shape if cos.dim() == 2 else _refuse("cos, sin: [n_pos, rot / 2]")
             rot = 2 * half

@@ -160,6 +160,43 @@ def test_a_prompt_and_its_steps_agree(h):
         _compare(d, step, qx[i:i + 1], [1], nq, "f16")
 
 
+@pytest.mark.parametrize("counts", [[1, 1, 1], [20, 5, 60]])
+def test_what_is_not_finite_in_a_query_stays_in_its_row(h, counts):
+    c = Cache(104, "i8", 16, 2, 64, [90, 33, 70])
+    rows = sum(counts) + 2
+    qt, qx = _q(13, rows, 4 * 64, "bf16")
+    want = _run(h, c, qt, counts, 4, "bf16")
+    bad = qt.clone()
+    bad[0, 64:128] = float("nan")                                            # head 1 of the first row
+    bad[counts[0], 5] = float("inf")                                         # head 0 of the second sequence's first row
+    bad[-2:] = float("nan")                                                  # rows of nobody
+    got = _run(h, c, bad, counts, 4, "bf16")
+    assert torch.all(torch.isnan(got[0, 64:128]))
+    keep = torch.ones_like(got, dtype=torch.bool)
+    keep[0, 64:128] = keep[counts[0], :64] = False
+    assert torch.equal(got[keep], want[keep])
+
+
+def test_tensors_of_another_device_are_refused(h):
+    # one GPU is visible: the handle is told that it belongs to another one
+    c = Cache(105, "i8", 16, 1, 64, [5, 5])
+    q = hero.tensor(torch.zeros(2, 64, dtype=torch.bfloat16, device="cuda"))
+    pinned = hero.host_tensor(torch.zeros(2, 64, dtype=torch.bfloat16))
+    with pytest.raises(hero.HeroError, match="device"):
+        h.hero_block_attention(c.desc, pinned, q, 1)
+    with pytest.raises(hero.HeroError, match="device"):
+        h.hero_block_cache_append(c.desc, q, pinned)
+    own = h._device
+    try:
+        h._device = own + 1
+        with pytest.raises(hero.HeroError, match="device"):
+            h.hero_block_attention(c.desc, q, q, 1)
+        with pytest.raises(hero.HeroError, match="device"):
+            h.hero_qk_norm_rope(q, None, q, None, 1, 0)
+    finally:
+        h._device = own
+
+
 def test_binding_refusals(h):
     c = Cache(103, "i8", 16, 1, 64, [5, 5])
     q = hero.tensor(torch.zeros(2, 64, dtype=torch.bfloat16, device="cuda"))
