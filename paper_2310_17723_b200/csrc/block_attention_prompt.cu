@@ -7,17 +7,22 @@
 //   warps 0-3, 4-7   softmax of row tile 0 / 1, one row per thread: no reduction across threads.  A tile of keys is two halves of 64
 //                    with a score buffer each, so the softmax of one half runs beside the products of the other.  Scores are read
 //                    from tensor memory once (again only when the maximum moves); P goes back as FP16 into the columns of
-//                    the scores and is the A operand of P V from there.
+//                    the scores and is the A operand of P V from there.  These warps bound the kernel: two on each scheduler, whose
+//                    exponentials take 40 % of the cycles and whose waits and instructions the rest, so they have one barrier to
+//                    wait for per half, the scores'
 //   warps 8-15       codes -> FP16: 16-byte loads one tile ahead in registers, exact conversion, stores in the 128-byte swizzled
 //                    operand layout
 //   warps 16, 17     issue the products of row tile 0 / 1
-//   warp 18          publishes what the softmax needs of each 16 tokens: key scale, value scale relative to the largest so far
+//   warp 18          publishes what the softmax needs of each 16 tokens: key scale, value scale relative to the largest so far.  It
+//                    arrives on the barrier of the keys, which the scores wait for (a barrier of their own cost 319 against 291 us,
+//                    2048 rows on 6000 tokens, heads 32 / 8 of 128)
 // The value scale of a page is folded into the exponent, e' = 2^(x + log2 rv), so that it costs nothing per element; the row sum
 // undoes it per 16 tokens (rv is kept above 2^-40, where P is zero anyway).  As in the kernel for few rows, queries are scaled into
 // FP16 by a power of two.  No maximum is taken per tile: P is formed with the maximum so far, and only if 16 probabilities
 // sum to more than FP16 holds (or in the first half) is the half read again for its maximum, O rescaled in tensor memory.
 #include "block_attention.cuh"
 #include <cmath>
+#include <type_traits>
 
 namespace hero {
 
@@ -31,6 +36,7 @@ constexpr int PR_ROWS = 256, PR_KEYS = 128;
 constexpr int PR_INFO = 4;                                     // ring of scale records
 constexpr float PR_SHIFT = 8.0f;                               // P carries a factor 2^8 when the maximum has just moved
 constexpr float PR_MOST = 65504.0f;                            // and 16 of them sum to no more than this, so none overflows FP16
+constexpr float PR_HIGH = 11.9f;                               // 16 x 2^PR_HIGH stays below that
 constexpr float PR_MIN_RV = 9.094947e-13f;                     // 2^-40
 
 
@@ -42,7 +48,7 @@ struct PromptCfg {
   static constexpr int OFF_INFO = OFF_V + 2 * TILE;            // float4 [PR_INFO][8], of 16 tokens each: key scale, log2 and reciprocal of the relative value scale
   static constexpr int OFF_REF = OFF_INFO + PR_INFO * 8 * 16;  // float2 [PR_INFO]: largest value scale so far, its old / new ratio
   static constexpr int OFF_BARS = OFF_REF + PR_INFO * 8;
-  static constexpr int NBARS = 2 + 4 + 4 + 2 * PR_INFO + 12;
+  static constexpr int NBARS = 2 + 4 + 4 + 12;
   static constexpr int BYTES = 1024 + OFF_BARS + NBARS * 8 + 16;
   static constexpr int S_COL = 0, O_COL = 256;                 // scores (then P) 2 x 128 columns, O 2 x DH columns
 };
@@ -55,13 +61,11 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + Cfg::OFF_BARS);
   uint64_t* q_full = bars;                       // [2] softmax warps of a tile -> its issuer
-  uint64_t* k_full = q_full + 2;                 // [2] converters -> issuers
+  uint64_t* k_full = q_full + 2;                 // [2] converters and scribe -> issuers
   uint64_t* k_empty = k_full + 2;                // [2] issuers -> converters
   uint64_t* v_full = k_empty + 2;                // [2]
   uint64_t* v_empty = v_full + 2;                // [2]
-  uint64_t* i_full = v_empty + 2;                // [PR_INFO] scribe -> softmax
-  uint64_t* i_empty = i_full + PR_INFO;          // [PR_INFO] softmax -> scribe
-  uint64_t* s_full = i_empty + PR_INFO;          // [tile][half] scores are complete
+  uint64_t* s_full = v_empty + 2;                // [tile][half] scores are complete
   uint64_t* p_full = s_full + 4;                 // [tile][half] P is in place (and O rescaled)
   uint64_t* o_full = p_full + 4;                 // [tile] P V of a half is complete
   uint64_t* o_last = o_full + 2;                 // [tile] the last one is
@@ -71,12 +75,11 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
       ptx::mbar_init(&q_full[i], 4);
-      ptx::mbar_init(&k_full[i], PR_CV_WARPS); ptx::mbar_init(&k_empty[i], 2);
+      ptx::mbar_init(&k_full[i], PR_CV_WARPS + 1); ptx::mbar_init(&k_empty[i], 2);
       ptx::mbar_init(&v_full[i], PR_CV_WARPS); ptx::mbar_init(&v_empty[i], 2);
       ptx::mbar_init(&o_full[i], 1); ptx::mbar_init(&o_last[i], 1);
     }
     for (int i = 0; i < 4; ++i) { ptx::mbar_init(&s_full[i], 1); ptx::mbar_init(&p_full[i], 4); }
-    for (int i = 0; i < PR_INFO; ++i) { ptx::mbar_init(&i_full[i], 1); ptx::mbar_init(&i_empty[i], PR_SM_WARPS); }
     ptx::fence_mbar_init();
   }
   if (warp == PR_MMA_WARP) { ptx::tmem_alloc(tmem_slot, 512); ptx::tmem_relinquish(); }
@@ -148,68 +151,83 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
     const uint32_t s_col = t_lane + Cfg::S_COL + t * 128, o_col = t_lane + Cfg::O_COL + t * DH;
     float u = 0.f, l = 0.f, vref = 0.f;            // u = PR_SHIFT - running maximum
     bool ok = true;
-    for (int j = 0; j < n_all; ++j) {
+    // The first 32 scores of the next half can be read beside the second half's work on this one: 452 -> 403 us with 64 features (2 x 16
+    // heads, 4096 rows on 4096 tokens); with 128 the products of the two row tiles keep tensor memory busier, and it cost 1 %.
+    constexpr bool AHEAD = DH == 64;
+    bool ahead = false;
+    uint32_t x[2][32];
+    for (int j = 0; j < n && ok; ++j) {
       const int slot = j % PR_INFO;
-      ok = __all_sync(0xffffffffu, ok && ptx::mbar_wait(&i_full[slot], (j / PR_INFO) & 1, c.err, 0x8000 | slot));
-      if (j >= n || !ok) {                         // the other row tile's keys: only hand the record back
-        __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(&i_empty[slot]);
-        continue;
-      }
-      const float2 ref = reinterpret_cast<const float2*>(smem + Cfg::OFF_REF)[slot];
-      vref = ref.x;
 #pragma unroll 1
       for (int h = 0; h < 2; ++h) {
-        ok = __all_sync(0xffffffffu, ok && ptx::mbar_wait(&s_full[2 * t + h], j & 1, c.err, 0x8100 | t));
-        if (!ok) break;
-        ptx::tc_fence_after();
+        if (!AHEAD || !ahead) {
+          ok = __all_sync(0xffffffffu, ok && ptx::mbar_wait(&s_full[2 * t + h], j & 1, c.err, 0x8100 | t));
+          if (!ok) break;
+          ptx::tc_fence_after();
+          if (AHEAD) ptx::tmem_ld32(s_col + 64 * h, x[0]);
+        }
+        // (the record was there before the tile's keys were announced, so before its scores)
+        const float2 ref = reinterpret_cast<const float2*>(smem + Cfg::OFF_REF)[slot];
+        vref = ref.x;
         const uint32_t s_half = s_col + 64 * h;
         const float4* info = reinterpret_cast<const float4*>(smem + Cfg::OFF_INFO) + slot * 8 + 4 * h;
         const int valid = lim - j * PR_KEYS - 64 * h;                      // keys of this half that the row sees
         const bool whole = __all_sync(0xffffffffu, valid >= 64), first = (j | h) == 0, turn = h == 0 && ref.y != 1.0f;
-        float4 gi[4];                              // of 16 keys each: key scale, log2 rv, 1 / rv
+        // e' = 2^(score - maximum + 8 + log2 rv) and the row sum in one reading; false, with nothing changed, if a sum outgrows FP16.
+        // (Compiled for each case by itself: chosen at every 16 keys it took 291 against 285 us, 2048 rows on 6000 tokens.)
+        auto one_reading = [&](auto masked) {
+          float4 gi[4];                            // of 16 keys each: key scale, log2 rv, 1 / rv
 #pragma unroll
-        for (int g = 0; g < 4; ++g) gi[g] = info[g];
-        // ---- e' = 2^(score - maximum + 8 + log2 rv) and the row sum in one reading
-        uint32_t w[32];
-        float l_new;
-        for (bool settled = false;; settled = true) {
-          uint32_t x[2][32];
-          ptx::tmem_ld32(s_half, x[0]);
+          for (int g = 0; g < 4; ++g) gi[g] = info[g];
+          uint32_t w[32];
+          if (!AHEAD) ptx::tmem_ld32(s_half, x[0]);
           ptx::tmem_ld_wait();
           ptx::tmem_ld32(s_half + 32, x[1]);
-          l_new = l;
-          float most = 0.f;
+          float l_new = l, most = 0.f;
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
-            if (g == 2) ptx::tmem_ld_wait();
+            if (g == 2) {
+              ptx::tmem_ld_wait();
+              if (AHEAD) {
+                const bool more = h == 0 || j + 1 < n;
+                ahead = __all_sync(0xffffffffu, more && ptx::mbar_test(&s_full[2 * t + (h ^ 1)], (j + h) & 1));
+                if (ahead) {
+                  ptx::tc_fence_after();
+                  ptx::tmem_ld32(s_col + 64 * (h ^ 1), x[0]);
+                }
+              }
+            }
             const uint32_t* y = &x[g >> 1][16 * (g & 1)];
             const float fk = f * gi[g].x, ug = u + gi[g].y;
             float2 sum = make_float2(0.f, 0.f);
-            if (whole) {
 #pragma unroll
-              for (int i = 0; i < 8; ++i) {
-                const float2 a = __ffma2_rn(make_float2(__uint_as_float(y[2 * i]), __uint_as_float(y[2 * i + 1])), make_float2(fk, fk), make_float2(ug, ug));
-                const float2 e = make_float2(ex2(a.x), ex2(a.y));
-                sum = __fadd2_rn(sum, e);
-                w[8 * g + i] = pack_f16(e.x, e.y);
+            for (int i = 0; i < 8; ++i) {
+              const float2 a = __ffma2_rn(make_float2(__uint_as_float(y[2 * i]), __uint_as_float(y[2 * i + 1])), make_float2(fk, fk), make_float2(ug, ug));
+              float2 e = make_float2(ex2(a.x), ex2(a.y));
+              if constexpr (decltype(masked)::value) {
+                if (16 * g + 2 * i >= valid) e.x = 0.f;
+                if (16 * g + 2 * i + 1 >= valid) e.y = 0.f;
               }
-            } else {
-#pragma unroll
-              for (int i = 0; i < 8; ++i) {
-                const int key = 16 * g + 2 * i;
-                const float e0 = key < valid ? ex2(fmaf(__uint_as_float(y[2 * i]), fk, ug)) : 0.f;
-                const float e1 = key + 1 < valid ? ex2(fmaf(__uint_as_float(y[2 * i + 1]), fk, ug)) : 0.f;
-                sum.x += e0; sum.y += e1;
-                w[8 * g + i] = pack_f16(e0, e1);
-              }
+              sum = __fadd2_rn(sum, e);
+              w[8 * g + i] = pack_f16(e.x, e.y);
             }
             const float both = sum.x + sum.y;
             most = fmaxf(most, both);
             l_new = fmaf(both, gi[g].z, l_new);
           }
-          if (settled || !(__any_sync(0xffffffffu, first || most > PR_MOST) || turn)) break;
-          // ---- the maximum of this half moves the row's, O and the sum follow, and O the value reference
+          const bool fits = !__any_sync(0xffffffffu, most > PR_MOST);
+          if (AHEAD) ptx::tmem_ld_wait();
+          if (fits) {
+            l = l_new;
+            // P over the scores' columns
+#pragma unroll
+            for (int k = 0; k < 2; ++k) ptx::tmem_st16(s_half + 16 * k, *reinterpret_cast<const uint32_t(*)[16]>(&w[16 * k]));
+          }
+          return fits;
+        };
+        if (first || turn || !(whole ? one_reading(std::false_type()) : one_reading(std::true_type()))) {
+          if (AHEAD) { ahead = false; ptx::tmem_ld_wait(); }
+          // ---- the first keys, a larger value scale, or probabilities that outgrow FP16: the half's maximum first
           float mx = -INFINITY;
 #pragma unroll 1
           for (int g = 0; g < 4; ++g) {
@@ -221,37 +239,55 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
             for (int i = 0; i < 16; ++i) m = fmaxf(m, 16 * g + i < valid ? __uint_as_float(z[i]) : -INFINITY);
             if (m > -INFINITY) mx = fmaxf(mx, fmaf(m, f * info[g].x, u));
           }
-          float d = mx - PR_SHIFT;
-          if (!first) d = fmaxf(d, 0.f);
-          if (mx == -INFINITY) d = 0.f;
-          u -= d;
-          if (!first) {
-            ok = __all_sync(0xffffffffu, ok && ptx::mbar_wait(&o_full[t], (h + 1) & 1, c.err, 0x8180 | t));   // the previous half's P V
-            ptx::tc_fence_after();
-            const float a = ex2(-d);
-            l *= a;
-            const float ao = turn ? a * ref.y : a;
+          // where it calls for it, it moves the row's, O and the sum follow, and O the value reference
+          if (__any_sync(0xffffffffu, first || mx > PR_HIGH) || turn) {
+            float d = mx - PR_SHIFT;
+            if (!first) d = fmaxf(d, 0.f);
+            if (mx == -INFINITY) d = 0.f;
+            u -= d;
+            if (!first) {
+              ok = __all_sync(0xffffffffu, ok && ptx::mbar_wait(&o_full[t], (h + 1) & 1, c.err, 0x8180 | t));   // the previous half's P V
+              ptx::tc_fence_after();
+              const float a = ex2(-d);
+              l *= a;
+              const float ao = turn ? a * ref.y : a;
 #pragma unroll 1
-            for (int k = 0; k < DH / 16; ++k) {
-              uint32_t z[16];
-              ptx::tmem_ld16(o_col + 16 * k, z);
-              ptx::tmem_ld_wait();
+              for (int k = 0; k < DH / 16; ++k) {
+                uint32_t z[16];
+                ptx::tmem_ld16(o_col + 16 * k, z);
+                ptx::tmem_ld_wait();
 #pragma unroll
-              for (int i = 0; i < 16; ++i) z[i] = __float_as_uint(__uint_as_float(z[i]) * ao);
-              ptx::tmem_st16(o_col + 16 * k, z);
+                for (int i = 0; i < 16; ++i) z[i] = __float_as_uint(__uint_as_float(z[i]) * ao);
+                ptx::tmem_st16(o_col + 16 * k, z);
+              }
             }
           }
-        }
-        l = l_new;
-        // P over the scores' columns
+          // P of 16 keys takes the place of scores that have been read: columns 8 g .. 8 g + 7, after 16 g .. 16 g + 15
+#pragma unroll 1
+          for (int g = 0; g < 4; ++g) {
+            const float4 gi = info[g];
+            const float fk = f * gi.x, ug = u + gi.y;
+            uint32_t z[16], w[8];
+            ptx::tmem_ld16(s_half + 16 * g, z);
+            ptx::tmem_ld_wait();
+            float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
-        for (int k = 0; k < 2; ++k) ptx::tmem_st16(s_half + 16 * k, *reinterpret_cast<const uint32_t(*)[16]>(&w[16 * k]));
+            for (int i = 0; i < 8; ++i) {
+              const int key = 16 * g + 2 * i;
+              const float e0 = key < valid ? ex2(fmaf(__uint_as_float(z[2 * i]), fk, ug)) : 0.f;
+              const float e1 = key + 1 < valid ? ex2(fmaf(__uint_as_float(z[2 * i + 1]), fk, ug)) : 0.f;
+              sum.x += e0; sum.y += e1;
+              w[i] = pack_f16(e0, e1);
+            }
+            l = fmaf(sum.x + sum.y, gi.z, l);
+            ptx::tmem_st8(s_half + 8 * g, w);
+          }
+        }
         ptx::tmem_st_wait();
         ptx::tc_fence_before();
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(&p_full[2 * t + h]);
       }
-      if (lane == 0) ptx::mbar_arrive(&i_empty[slot]);
     }
     // ---- output
     float scale_o = 0.f;
@@ -394,12 +430,13 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
       for (int o = 4; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
       const float now = fmaxf(vref, __shfl_sync(0xffffffffu, top, 0));
       const float rv = fmaxf(now > 0.f ? now_sc.y / now : 1.f, PR_MIN_RV);
-      if (!__all_sync(0xffffffffu, ptx::mbar_wait(&i_empty[slot], ((j / PR_INFO) & 1) ^ 1, c.err, 0x8300 | slot))) break;
+      // the keys' place is free: the scores two tiles back are complete, so nobody reads records four tiles back any more
+      if (!__all_sync(0xffffffffu, ptx::mbar_wait(&k_empty[j & 1], ((j >> 1) & 1) ^ 1, c.err, 0x8300 | slot))) break;
       if (lane < 8) *reinterpret_cast<float4*>(smem + Cfg::OFF_INFO + (slot * 8 + lane) * 16) = make_float4(now_sc.x, __log2f(rv), 1.0f / rv, 0.f);
       if (lane == 0) reinterpret_cast<float2*>(smem + Cfg::OFF_REF)[slot] = make_float2(now, now > vref ? vref / now : 1.0f);
       vref = now;
       __syncwarp();
-      if (lane == 0) ptx::mbar_arrive(&i_full[slot]);
+      if (lane == 0) ptx::mbar_arrive(&k_full[j & 1]);
     }
    } else if (warp < PR_SCRIBE_WARP) {
     // ------------------------------------------------------------------ issuer of one row tile
