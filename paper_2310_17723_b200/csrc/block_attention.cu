@@ -595,9 +595,9 @@ static hero_status plan_rows(const hero_handle* h, const hero_block_cache* cc, i
   RowsPlan r;
   r.prompt = rows > 32;
   if (r.prompt) {
-    r.bytes = 0;
+    hero_status st = prompt_workspace_bytes(h, cc, nq, max_rows, &r.bytes);
     *out = r;
-    return HERO_OK;
+    return st;
   }
   r.nt = rows <= 8 ? 1 : rows > 16 && rows <= 24 ? 3 : 2;
   const long long tiles = (rows + 8 * r.nt - 1) / (8 * r.nt), groups = tiles * cc->nkv * cc->B, steps = ((long long)cc->max_len + 31) / 32;
@@ -693,7 +693,7 @@ extern "C" hero_status hero_block_attention(hero_handle* h, const hero_block_cac
   HERO_REQUIRE(plan.bytes == 0 || (a->workspace && a->workspace_bytes >= plan.bytes), HERO_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed",
                a->workspace_bytes, plan.bytes);
   HERO_REQUIRE(plan.bytes == 0 || aligned16(a->workspace), HERO_ERR_ALIGNMENT, "the workspace must be 16-byte aligned");
-  if (plan.prompt) return launch_prompt(h, cc, p, bf, static_cast<cudaStream_t>(stream));
+  if (plan.prompt) return launch_prompt(h, cc, p, bf, a->workspace, static_cast<cudaStream_t>(stream));
   p.B = cc->B; p.tiles = plan.tiles; p.direct = plan.direct; p.by_group = plan.by_group;
   p.part_o = static_cast<float*>(a->workspace);
   p.part_ml = reinterpret_cast<float2*>(p.part_o + (size_t)plan.ctas * 2 * 8 * plan.nt * cc->dh);

@@ -14,7 +14,8 @@ struct BlockAttnParams {
   int B, tiles, direct;          // direct: CTA index = (sequence, row tile, head); else equal shares of all units
   int by_group;                  // records of cut groups are listed by group, else by share
   struct JoinRecord* records;
-  float* part_o; float2* part_ml; // partial results [CTA][2]: sum of P V [rows][DH], (maximum, sum of P) [rows]
+  int splits;                    // many rows: parts of a group's keys, a CTA each
+  float* part_o; float2* part_ml; // partial results ([CTA][2]; many rows: [CTA]): sum of P V [rows][DH], (maximum, sum of P) [rows]
 };
 
 __device__ __forceinline__ void store_out(const BlockAttnParams& p, long long row, int col, float y) {
@@ -56,6 +57,7 @@ __device__ __forceinline__ void codes4_to_f16(uint32_t w, uint32_t& lo, uint32_t
 }
 
 // many rows per key / value head (block_attention_prompt.cu)
-hero_status launch_prompt(hero_handle* h, const hero_block_cache* cc, const BlockAttnParams& p, bool bf, cudaStream_t stream);
+hero_status prompt_workspace_bytes(const hero_handle* h, const hero_block_cache* cc, int nq, int max_rows, size_t* bytes);
+hero_status launch_prompt(hero_handle* h, const hero_block_cache* cc, const BlockAttnParams& p, bool bf, void* workspace, cudaStream_t stream);
 
 }  // namespace hero

@@ -2,7 +2,7 @@
 // on tcgen05 (kind::f16, FP32 accumulators in tensor memory) and everything else is arranged around keeping them fed.
 //
 // One CTA takes 256 rows ((row of the sequence, query head of the group) pairs, two tiles of 128) of one (sequence, key / value head)
-// and walks its keys in tiles of 128.  Keys and values have to become FP16 operands in shared memory on the way: done once per CTA,
+// and walks its keys, or one of several equal parts of them where CTAs are few, in tiles of 128.  Keys and values have to become FP16 operands in shared memory on the way: done once per CTA,
 // for both row tiles.  Roles:
 //   warps 0-3, 4-7   softmax of row tile 0 / 1, one row per thread: no reduction across threads.  A tile of keys is two halves of 64
 //                    with a score buffer each, so the softmax of one half runs beside the products of the other.  Scores are read
@@ -33,6 +33,7 @@ constexpr int PR_THREADS = (PR_MMA_WARP + 4) * 32;             // whole warpgrou
 // 640 threads are launched with 96 registers each; 256 x 136 + 256 x 72 + 128 x 56 = 60416 of those 61440
 constexpr int PR_SM_REGS = 136, PR_CV_REGS = 72, PR_MMA_REGS = 56;
 constexpr int PR_ROWS = 256, PR_KEYS = 128;
+constexpr int PR_PART = 4;                                     // tiles of keys of a part, at least, where a group's keys are split
 constexpr int PR_INFO = 4;                                     // ring of scale records
 constexpr float PR_SHIFT = 8.0f;                               // P carries a factor 2^8 when the maximum has just moved
 constexpr float PR_MOST = 65504.0f;                            // and 16 of them sum to no more than this, so none overflows FP16
@@ -52,6 +53,12 @@ struct PromptCfg {
   static constexpr int BYTES = 1024 + OFF_BARS + NBARS * 8 + 16;
   static constexpr int S_COL = 0, O_COL = 256;                 // scores (then P) 2 x 128 columns, O 2 x DH columns
 };
+
+// sequence, head and row tile of a group: late rows, which see many keys, of all sequences first
+__device__ __forceinline__ void prompt_group(const BlockAttnParams& p, int group, int& b, int& hk, int& qt) {
+  const int bh = group % (p.c.nkv * p.B);
+  hk = bh % p.c.nkv; b = bh / p.c.nkv; qt = p.tiles - 1 - group / (p.c.nkv * p.B);
+}
 
 template <int DH, bool BF, bool F8>
 __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const __grid_constant__ BlockAttnParams p, const uint32_t idesc_qk,
@@ -91,8 +98,8 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
   ptx::pdl_wait();
 
   const BlockView& c = p.c;
-  // late rows, which see many keys, of all sequences first
-  const int bh = blockIdx.x % (c.nkv * p.B), hk = bh % c.nkv, b = bh / c.nkv, qt = p.tiles - 1 - blockIdx.x / (c.nkv * p.B);
+  int b, hk, qt;
+  prompt_group(p, blockIdx.x / p.splits, b, hk, qt);
   const SeqRows s = seq_rows(c, b);
   const int total = s.n * p.group, rb = qt * PR_ROWS, base = s.len - s.n;
   // keys of a row tile's last row, and its tiles of keys
@@ -101,7 +108,11 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
     return first >= total ? 0 : max(base + (min(first + 128, total) - 1) / p.group + 1, 0);
   };
   const int L = max(keys_of(0), keys_of(1));
-  const int n_all = (L + PR_KEYS - 1) / PR_KEYS;
+  // of its tiles of keys this CTA has one part: n_all tiles from key0 on
+  const int n_group = (L + PR_KEYS - 1) / PR_KEYS, part = blockIdx.x % p.splits;
+  const int per = p.splits == 1 ? n_group : max((n_group + p.splits - 1) / p.splits, PR_PART);
+  const int j0 = min(part * per, n_group), n_all = min(per, n_group - j0), key0 = j0 * PR_KEYS;
+  auto tiles_of = [&](int t) { return min(max((keys_of(t) + PR_KEYS - 1) / PR_KEYS - j0, 0), n_all); };
 
   if (rb >= total) {
     // nothing of this sequence here
@@ -109,10 +120,10 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(PR_SM_REGS));
     // ------------------------------------------------------------------ softmax of one row tile
     const int t = warp >> 2, quarter = warp & 3, r = quarter * 32 + lane;
-    const int n = (keys_of(t) + PR_KEYS - 1) / PR_KEYS;
+    const int n = tiles_of(t);
     const int rr = rb + 128 * t + r;
     const bool row_ok = rr < total;
-    const int lim = row_ok ? base + rr / p.group + 1 : 0;
+    const int lim = row_ok ? base + rr / p.group + 1 - key0 : 0;
     const long long row_g = s.r0 + (row_ok ? rr / p.group : 0);
     const int hq = hk * p.group + (row_ok ? rr % p.group : 0);
     float f = 0.f;
@@ -289,13 +300,16 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
         if (lane == 0) ptx::mbar_arrive(&p_full[2 * t + h]);
       }
     }
-    // ---- output
+    // ---- output, or the part's sums
     float scale_o = 0.f;
     if (n > 0) {
       ok = __all_sync(0xffffffffu, ok && ptx::mbar_wait(&o_last[t], 0, c.err, 0x8200 | t));
       ptx::tc_fence_after();
-      scale_o = l != 0.f ? vref / l : 0.f;
+      scale_o = l != 0.f ? (p.splits > 1 ? vref : vref / l) : 0.f;
     }
+    const long long own = (long long)blockIdx.x * PR_ROWS + 128 * t + r;   // the row's place among the parts
+    const bool seen = n > 0 && l != 0.f;
+    if (p.splits > 1 && row_ok && ok) p.part_ml[own] = make_float2(seen ? -u : -INFINITY, l);
 #pragma unroll
     for (int k = 0; k < DH / 32; ++k) {
       uint32_t x[32];
@@ -305,8 +319,14 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
       }
       float y[32];
 #pragma unroll
-      for (int i = 0; i < 32; ++i) y[i] = n > 0 && l != 0.f ? __uint_as_float(x[i]) * scale_o : 0.f;
-      if (row_ok && ok) {
+      for (int i = 0; i < 32; ++i) y[i] = seen ? __uint_as_float(x[i]) * scale_o : 0.f;
+      if (p.splits > 1) {
+        if (seen && row_ok && ok) {
+          float4* dst = reinterpret_cast<float4*>(p.part_o + own * DH + 32 * k);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) dst[i] = make_float4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
+        }
+      } else if (row_ok && ok) {
         const int col = hq * DH + 32 * k;
         const long long at = row_g * p.ld_out + col;
         if (p.out_dt == HERO_F16 || p.out_dt == HERO_BF16) {
@@ -346,8 +366,8 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
     const long long mine = (long long)hk * c.head_stride + (long long)(r0 & 15) * c.ld + piece * 16;
     uint8_t* const to0 = smem + (r0 >> 3) * 1024 + (r0 & 7) * 128 + (((2 * piece) ^ (r0 & 7)) << 4);
     uint8_t* const to1 = smem + (r0 >> 3) * 1024 + (r0 & 7) * 128 + (((2 * piece + 1) ^ (r0 & 7)) << 4);
-    auto page_of = [&](int j) {                    // lane g < 8: page of tokens 128 j + 16 g ..
-      const int tok = j * PR_KEYS + 16 * lane;
+    auto page_of = [&](int j) {                    // lane g < 8: page of tokens key0 + 128 j + 16 g ..
+      const int tok = key0 + j * PR_KEYS + 16 * lane;
       return lane < 8 && tok < L ? page_for_read(c, b, tok >> c.page_shift) : -1;
     };
     long long at[2];                               // where the thread's two rows begin in the pool
@@ -357,7 +377,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
       for (int i = 0; i < 2; ++i) at[i] = mine + __shfl_sync(0xffffffffu, off, 4 * i + (r0 >> 4));
     };
     auto load = [&](const uint8_t* pool, int j, uint4 (&raw)[NP]) {
-      if ((j + 1) * PR_KEYS <= L) {
+      if (key0 + (j + 1) * PR_KEYS <= L) {
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -368,7 +388,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
 #pragma unroll
           for (int h = 0; h < NSUB; ++h) {
             raw[i * NSUB + h] = make_uint4(0, 0, 0, 0);        // slots behind the end may hold anything (e4m3: NaN)
-            if (j * PR_KEYS + r0 + 64 * i < L) raw[i * NSUB + h] = __ldg(reinterpret_cast<const uint4*>(pool + at[i] + 64 * h));
+            if (key0 + j * PR_KEYS + r0 + 64 * i < L) raw[i * NSUB + h] = __ldg(reinterpret_cast<const uint4*>(pool + at[i] + 64 * h));
           }
       }
     };
@@ -412,8 +432,8 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(PR_MMA_REGS));
    if (warp == PR_SCRIBE_WARP) {
     // ------------------------------------------------------------------ scale records
-    auto page_of = [&](int j) {                    // lane g < 8: page of tokens 128 j + 16 g ..
-      const int tok = j * PR_KEYS + 16 * lane;
+    auto page_of = [&](int j) {                    // lane g < 8: page of tokens key0 + 128 j + 16 g ..
+      const int tok = key0 + j * PR_KEYS + 16 * lane;
       return lane < 8 && tok < L ? page_for_read(c, b, tok >> c.page_shift) : -1;
     };
     auto scales = [&](int i) { return i >= 0 ? make_float2(__ldg(c.ks + (long long)i * c.nkv + hk), __ldg(c.vs + (long long)i * c.nkv + hk)) : make_float2(0.f, 0.f); };
@@ -440,7 +460,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
     }
    } else if (warp < PR_SCRIBE_WARP) {
     // ------------------------------------------------------------------ issuer of one row tile
-    const int t = warp - PR_MMA_WARP, n = (keys_of(t) + PR_KEYS - 1) / PR_KEYS;
+    const int t = warp - PR_MMA_WARP, n = tiles_of(t);
     const bool issue = ptx::elect_one();
     constexpr uint64_t kmaj = ptx::smem_desc_base(16, 1024, ptx::SWZ_128B);            // Q, K: K-major, 128-byte rows
     constexpr uint64_t vmaj = ptx::smem_desc_base(Cfg::SUB, 1024, ptx::SWZ_128B);      // V: MN-major; 64-feature chunks SUB apart
@@ -509,8 +529,74 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
   if (warp == PR_MMA_WARP) ptx::tmem_dealloc(tmem_base, 512);
 }
 
+// joins the parts of a group whose keys were split: CTA (x, y) takes 32 rows of group x, a warp four of them, side by side
+constexpr int PJ_WARPS = 8, PJ_EACH = 4, PJ_ROWS = PJ_WARPS * PJ_EACH;
 template <int DH>
-static hero_status launch(hero_handle* h, const hero_block_cache* cc, const BlockAttnParams& p, bool bf, cudaStream_t stream) {
+__global__ void __launch_bounds__(PJ_WARPS * 32) block_attn_prompt_join_kernel(const __grid_constant__ BlockAttnParams p) {
+  constexpr int E = DH / 32;
+  ptx::pdl_wait();
+  ptx::pdl_launch_dependents();
+  int b, hk, qt;
+  prompt_group(p, blockIdx.x, b, hk, qt);
+  const SeqRows s = seq_rows(p.c, b);
+  const int total = s.n * p.group, lane = threadIdx.x & 31, row0 = blockIdx.y * PJ_ROWS + (threadIdx.x >> 5) * PJ_EACH;
+  float m[PJ_EACH], l[PJ_EACH], y[PJ_EACH][E];
+#pragma unroll
+  for (int i = 0; i < PJ_EACH; ++i) {
+    m[i] = -1e30f; l[i] = 0.f;                     // below every maximum, and finite: no case for rows without a key
+#pragma unroll
+    for (int e = 0; e < E; ++e) y[i][e] = 0.f;
+  }
+#pragma unroll 2
+  for (int q = 0; q < p.splits; ++q) {
+#pragma unroll
+    for (int i = 0; i < PJ_EACH; ++i) {
+      if (qt * PR_ROWS + row0 + i >= total) continue;              // rows that are not there were not written
+      const long long at = ((long long)blockIdx.x * p.splits + q) * PR_ROWS + row0 + i;
+      const float2 ml = __ldcg(p.part_ml + at);
+      if (ml.x == -INFINITY) continue;                             // nor were sums of no keys
+      const float now = fmaxf(m[i], ml.x), old = ex2(m[i] - now), w = ex2(ml.x - now);
+      m[i] = now;
+      l[i] = fmaf(l[i], old, w * ml.y);
+#pragma unroll
+      for (int e = 0; e < E; ++e) y[i][e] = fmaf(y[i][e], old, w * __ldcg(p.part_o + at * DH + 32 * e + lane));
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < PJ_EACH; ++i) {
+    const int rr = qt * PR_ROWS + row0 + i;
+    if (rr >= total) break;
+    const float inv = l[i] != 0.f ? 1.0f / l[i] : 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) store_out(p, s.r0 + rr / p.group, (hk * p.group + rr % p.group) * DH + 32 * e + lane, y[i][e] * inv);
+  }
+}
+
+// Where there are fewer groups than half the SMs, each group's keys are split over as many CTAs as fit, and a second kernel joins them:
+// 592 -> 104 us for 64 rows of one sequence on 32768 tokens (heads 32 / 8 of 128; 8 groups, 18 parts), 605 -> 329 for 512 rows (64 groups, 2
+// parts), 66 -> 52 for 4 x 128 rows on 4096 tokens (64 groups of 64 features).
+struct PromptPlan { long long tiles, groups; int splits; size_t bytes; };
+static hero_status plan_prompt(const hero_handle* h, const hero_block_cache* cc, int nq, int max_rows, PromptPlan* out) {
+  PromptPlan r;
+  r.tiles = ((long long)max_rows * (nq / cc->nkv) + PR_ROWS - 1) / PR_ROWS;
+  r.groups = r.tiles * cc->nkv * cc->B;
+  HERO_REQUIRE(r.groups < (1ll << 31), HERO_ERR_UNSUPPORTED, "max_rows=%d nkv=%d B=%d: too many", max_rows, cc->nkv, cc->B);
+  const long long fit = h->sm_count / r.groups, steps = ((long long)cc->max_len + PR_KEYS - 1) / PR_KEYS, useful = steps / PR_PART;
+  const long long splits = fit < useful ? fit : useful;
+  r.splits = splits > 1 ? (int)splits : 1;
+  r.bytes = r.splits > 1 ? (size_t)r.groups * r.splits * PR_ROWS * (cc->dh * 4 + 8) : 0;
+  *out = r;
+  return HERO_OK;
+}
+hero_status prompt_workspace_bytes(const hero_handle* h, const hero_block_cache* cc, int nq, int max_rows, size_t* bytes) {
+  PromptPlan plan;
+  hero_status st = plan_prompt(h, cc, nq, max_rows, &plan);
+  if (st == HERO_OK) *bytes = plan.bytes;
+  return st;
+}
+
+template <int DH>
+static hero_status launch(hero_handle* h, const PromptPlan& plan, const BlockAttnParams& p, bool bf, cudaStream_t stream) {
   auto kern = bf ? (p.c.f8 ? block_attn_prompt_kernel<DH, true, true> : block_attn_prompt_kernel<DH, true, false>)
                  : (p.c.f8 ? block_attn_prompt_kernel<DH, false, true> : block_attn_prompt_kernel<DH, false, false>);
   constexpr int BYTES = PromptCfg<DH>::BYTES;
@@ -523,17 +609,24 @@ static hero_status launch(hero_handle* h, const hero_block_cache* cc, const Bloc
   const uint32_t idesc_qk = ptx::make_idesc(1, 0, 0, 0, 0, 128, 64), idesc_pv = ptx::make_idesc(1, 0, 0, 0, 1, 128, DH);
   {
     LaunchScope scope(h, stream, KERNEL_ATTN);
-    HERO_CUDA(launch_dependent(kern, dim3((unsigned)((long long)p.tiles * p.c.nkv * cc->B)), dim3(PR_THREADS), BYTES, stream, p, idesc_qk, idesc_pv));
+    HERO_CUDA(launch_dependent(kern, dim3((unsigned)(plan.groups * plan.splits)), dim3(PR_THREADS), BYTES, stream, p, idesc_qk, idesc_pv));
+  }
+  if (plan.splits > 1) {
+    LaunchScope scope(h, stream, KERNEL_ATTN);
+    HERO_CUDA(launch_dependent(block_attn_prompt_join_kernel<DH>, dim3((unsigned)plan.groups, PR_ROWS / PJ_ROWS), dim3(PJ_WARPS * 32), 0, stream, p));
   }
   return HERO_OK;
 }
 
-hero_status launch_prompt(hero_handle* h, const hero_block_cache* cc, const BlockAttnParams& p_, bool bf, cudaStream_t stream) {
+hero_status launch_prompt(hero_handle* h, const hero_block_cache* cc, const BlockAttnParams& p_, bool bf, void* workspace, cudaStream_t stream) {
   BlockAttnParams p = p_;
-  const long long tiles = ((long long)p.c.max_rows * p.group + PR_ROWS - 1) / PR_ROWS;
-  HERO_REQUIRE(tiles * p.c.nkv * cc->B < (1ll << 31), HERO_ERR_UNSUPPORTED, "max_rows=%d nkv=%d B=%d: too many", p.c.max_rows, p.c.nkv, cc->B);
-  p.tiles = (int)tiles; p.B = cc->B;
-  return cc->dh == 64 ? launch<64>(h, cc, p, bf, stream) : launch<128>(h, cc, p, bf, stream);
+  PromptPlan plan;
+  hero_status st = plan_prompt(h, cc, p.nq, p.c.max_rows, &plan);
+  if (st != HERO_OK) return st;
+  p.tiles = (int)plan.tiles; p.B = cc->B; p.splits = plan.splits;
+  p.part_o = static_cast<float*>(workspace);
+  p.part_ml = reinterpret_cast<float2*>(p.part_o + (size_t)plan.groups * plan.splits * PR_ROWS * cc->dh);
+  return cc->dh == 64 ? launch<64>(h, plan, p, bf, stream) : launch<128>(h, plan, p, bf, stream);
 }
 
 }  // namespace hero

@@ -214,3 +214,85 @@ def test_binding_refusals(h):
         hero.block_cache(k, k, c.scale_t["k"], c.scale_t["v"], c.table_t, c.lens_t[:1], 5)
     with pytest.raises(hero.HeroError):
         hero.block_cache(k, k, c.scale_t["k"], c.scale_t["v"], c.table_t.cpu(), c.lens_t, 5)
+
+
+@pytest.mark.parametrize("kind", ["i8", "f8"])
+@pytest.mark.parametrize("counts,lens,group,nkv,dh,page,max_len,layout", [
+    ([40], [5000], 4, 2, 128, 64, 5000, "hnd"),                  # ten parts of a group
+    ([70, 33], [2100, 150], 1, 1, 64, 16, 2100, "nhd"),          # fewer tiles of keys than parts
+    ([300, 0, 3], [3001, 2000, 3], 2, 2, 128, 32, 3100, "padded"),   # several row tiles, the rows of one end inside the last part
+    ([50, 40], [20, 1281], 3, 2, 64, 128, 1400, "hnd"),          # rows from before the first token: zeros
+])
+def test_few_groups_whose_keys_are_split(h, kind, counts, lens, group, nkv, dh, page, max_len, layout):
+    c = Cache(105 + len(counts) + page, kind, page, nkv, dh, lens, max_len=max_len, layout=layout)
+    nq = group * nkv
+    qt, qx = _q(15, sum(counts) + 2, nq * dh, "bf16")
+    assert h.hero_block_attention_workspace_bytes(c.desc, nq, qt.shape[0], max(counts)) > 0
+    out = _run(h, c, qt, counts, nq, "bf16")
+    _compare(c, out, qx, counts, nq, "bf16")
+    assert torch.equal(out, _run(h, c, qt, counts, nq, "bf16"))
+
+
+@pytest.mark.parametrize("kind", ["i8", "f8"])
+def test_split_keys_with_maxima_and_value_scales_that_move(h, kind):
+    # bound as in test_maxima_and_value_scales_that_keep_moving: 2^-33 of the largest |v| per key for probabilities below FP16's normal range
+    counts, lens, page, nkv, dh = [64], [2600], 32, 1, 128
+    c = Cache(120, kind, page, nkv, dh, lens)
+    g = np.random.default_rng(16)
+    for x, lo, hi in (("k", -6, 3), ("v", -20, 8)):
+        c.scale[x] = (c.scale[x] * np.exp2(g.uniform(lo, hi, c.scale[x].shape))).astype(np.float32)
+        c.scale_t[x].copy_(torch.from_numpy(c.scale[x]))
+    qt, qx = _q(17, 64, 2 * dh, "bf16", size=2.0)
+    got = _run(h, c, qt, counts, 2, "bf16").double().cpu().numpy()
+    want, bar = _expect(c, qx, counts, 2, dh ** -0.5, 64)
+    bar = bar + lens[0] * 2.0 ** -33 * np.abs(c.values("v", 0)).max()
+    bar = bar + torch.finfo(torch.bfloat16).eps / 2 * (np.abs(want) + bar)
+    assert np.all(np.abs(got - want) <= bar), np.max(np.abs(got - want) / bar)
+
+
+def test_split_keys_not_finite_queries_and_eight_bit_outputs(h):
+    counts, lens, nkv, dh, nq = [60, 45], [2000, 1100], 2, 64, 4
+    c = Cache(121, "i8", 16, nkv, dh, lens)
+    rows = sum(counts)
+    qt, qx = _q(18, rows, nq * dh, "bf16")
+    want, bar = _expect(c, qx, counts, nq, dh ** -0.5, rows)
+    bad = qt.clone()
+    bad[7, dh:2 * dh] = float("nan")
+    bad[60, 5] = float("inf")
+    out = _run(h, c, bad, counts, nq, "bf16")
+    assert torch.all(torch.isnan(out[7, dh:2 * dh]))
+    keep = np.ones(want.shape, dtype=bool)
+    keep[7, dh:2 * dh] = keep[60, :dh] = False
+    near = bar + torch.finfo(torch.bfloat16).eps / 2 * (np.abs(want) + bar)
+    assert np.all(np.abs(out.double().cpu().numpy() - want)[keep] <= near[keep])
+    step = np.float32(np.abs(want).max() / 127 * 0.9)                        # some saturate
+    codes = torch.zeros(rows, nq * dh, dtype=torch.int8, device="cuda")
+    _run(h, c, qt, counts, nq, "bf16", out=codes, gran="sq", out_scale=torch.tensor([step], device="cuda"))
+    y, d = want / step, bar / step * 1.01 + 1e-5
+    got = codes.double().cpu().numpy()
+    assert np.all((got >= BC.to_codes(y - d, "i8")) & (got <= BC.to_codes(y + d, "i8")))   # rounding is monotonic
+
+
+def test_split_keys_captured_and_replayed_at_other_lengths(h):
+    counts, nkv, dh, nq = [48], 2, 64, 4
+    c = Cache(122, "i8", 64, nkv, dh, [4000])
+    qt, qx = _q(19, 48, nq * dh, "f16")
+    out = torch.full((48, nq * dh), 7.0, dtype=torch.float16, device="cuda")
+    s = start_tensor(counts)
+    ws = torch.full((h.hero_block_attention_workspace_bytes(c.desc, nq, 48, 48),), 0xff, dtype=torch.uint8, device="cuda")
+
+    def call():
+        h.hero_block_attention(c.desc, hero.tensor(qt), hero.tensor(out), nq, row_start=s, max_rows=48, workspace=ws)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        call()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            call()
+    torch.cuda.synchronize()
+    for n in (4000, 130, 60, 3333):
+        c.set_lens([n])
+        graph.replay()
+        torch.cuda.synchronize()
+        h.check()
+        _compare(c, out, qx, counts, nq, "f16")
