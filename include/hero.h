@@ -554,7 +554,7 @@ typedef struct {
   hero_tensor q;
   hero_tensor out;
   const int32_t* row_start;  /* device [B + 1] or NULL */
-  int32_t max_rows;          /* host-side upper bound on n_b */
+  int32_t max_rows;          /* host-side upper bound on n_b; times nq / nkv at most 2^30 */
   int32_t nq;
   float scale;
   void* workspace;

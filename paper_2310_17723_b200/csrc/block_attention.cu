@@ -642,6 +642,9 @@ static hero_status attn_check(hero_handle* h, const hero_block_cache* cc, int32_
   HERO_REQUIRE(h && cc, HERO_ERR_INVALID_ARG, "hero_block_attention: NULL handle or cache");
   HERO_REQUIRE(cc->nkv >= 1 && nq >= cc->nkv && nq % cc->nkv == 0 && nq <= 65535, HERO_ERR_INVALID_ARG, "nq=%d must be a multiple of nkv=%d", nq, cc->nkv);
   HERO_REQUIRE(rows >= 0 && max_rows >= 1, HERO_ERR_INVALID_ARG, "rows=%lld max_rows=%d", (long long)rows, max_rows);
+  // (rows of a key / value head are numbered in 32 bits, up to a row tile behind the last one)
+  HERO_REQUIRE((long long)max_rows * (nq / cc->nkv) <= (1ll << 30), HERO_ERR_UNSUPPORTED, "max_rows=%d with %d query heads each: more than 2^30 rows",
+               max_rows, nq / cc->nkv);
   return HERO_OK;
 }
 

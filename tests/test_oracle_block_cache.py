@@ -140,6 +140,17 @@ def test_bad_attention_arguments_are_refused(call, kw):
     assert call("hero_block_attention", _cache(), hero.BlockAttnArgs(**d))[0] not in (hero.OK, hero.ERR_CUDA)
 
 
+@pytest.mark.parametrize("max_rows,nq", [(1 << 30, 4), ((1 << 31) - 1, 4), (1 << 24, 256)])
+def test_a_row_bound_beyond_32_bit_row_numbers_is_refused(call, max_rows, nq):
+    # rows of a key / value head are numbered (row of the sequence, query head of the group): 2^30 of them at most
+    q = _t(4, nq * 128)
+    args = hero.BlockAttnArgs(q, q, P, max_rows, nq, 0.0, P, 1 << 30)
+    assert call("hero_block_attention", _cache(), args)[0] == hero.ERR_UNSUPPORTED
+    n = C.c_size_t()
+    blank = (C.c_uint8 * (1 << 20))()
+    assert hero.lib().hero_block_attention_workspace_bytes(C.cast(blank, C.c_void_p), C.byref(_cache()), nq, 4, max_rows, C.byref(n)) == hero.ERR_UNSUPPORTED
+
+
 def _rope(**kw):
     d = dict(q=_t(4, 512), k=_t(4, 256), q_out=_t(4, 512, data=2 * P), k_out=_t(4, 256, data=2 * P), nq=4, nkv=2, dh=128, rot=128, pairing=0,
              eps=1e-6, q_gamma=P, k_gamma=P, pos=P, cos=P, sin=P, n_pos=8)
