@@ -333,7 +333,8 @@ __global__ void __launch_bounds__(ROWS_WARPS * 32, rows_ctas(NT)) block_attn_row
       }
       // ---- probabilities
       if (fmaxf(sv.y, sv.w) > vref) {              // uniform over the warp
-        const float now = fmaxf(sv.y, sv.w), up = vref / now;
+        // (a normal number, so that its reciprocal is finite: BF16 values of 1e-37 have scales of 1e-39)
+        const float now = fmaxf(fmaxf(sv.y, sv.w), 0x1p-126f), up = vref / now;
 #pragma unroll
         for (int r = 0; r < NT; ++r)
 #pragma unroll

@@ -1,0 +1,52 @@
+"""GPU parity of hero_block_attention at the ends of its number range: value scales below FP32's normal numbers, values near the largest
+and the smallest that BF16 holds, scores far below zero or so large that their own rounding counts, subnormal queries.  Each on the
+kernel for few rows (one CTA per group, and shares that are joined) and on the one for many (whole, and keys in parts).  Bounds as in
+test_gpu_block_attention.py; where an output is itself subnormal, half a step of it (2^-134 in BF16) is added."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import block_cache as BC
+from paper_2310_17723_b200 import hero
+from block_util import Cache, start_tensor, starts, to_fp
+from test_gpu_block_attention import _compare, _expect, _q, _run
+
+pytestmark = pytest.mark.gpu
+
+LENS = [200, 150]
+# (rows of each sequence, host-side bound on the lengths): few rows direct and in shares, many rows whole and in parts
+FORMS = [([1, 1], 300), ([1, 1], 5000), ([6, 2], 5000), ([80, 60], 300), ([80, 60], 5000)]
+
+
+@pytest.fixture(scope="module")
+def h():
+    hd = hero.Handle()
+    yield hd
+    hd.check()
+    hd.close()
+
+
+def _cache(kind, dh, max_len, k_scale=None, v_scale=None, page=16):
+    c = Cache(7, kind, page, 1, dh, LENS, max_len=max_len)
+    for x, s in (("k", k_scale), ("v", v_scale)):
+        if s is not None:
+            c.scale[x][:] = s
+            _renew(c, x)
+    return c
+
+
+def _renew(c, x):
+    c.scale_t[x].copy_(torch.from_numpy(c.scale[x]))
+
+
+@pytest.mark.parametrize("counts,max_len", FORMS)
+@pytest.mark.parametrize("kind,dh", [("i8", 64), ("f8", 128)])
+def test_value_scales_below_the_normal_range_beside_ordinary_ones(h, kind, dh, counts, max_len):
+    # what the append makes of values of 1e-37: a scale whose reciprocal is beyond FP32; a page of zeros beside it, ordinary pages behind it
+    c = _cache(kind, dh, max_len)
+    for b in range(2):
+        for i, pid in enumerate(c.table[b][:6]):
+            c.scale["v"][pid] = 0.0 if i in (1, 4) else 1e-39 * (i + 1)
+    _renew(c, "v")
+    qt, qx = _q(1, sum(counts), 2 * dh, "bf16")
+    _compare(c, _run(h, c, qt, counts, 2, "bf16"), qx, counts, 2, "bf16")
