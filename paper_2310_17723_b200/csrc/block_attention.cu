@@ -61,7 +61,7 @@ struct RowsSmem {
   static constexpr int OFF_SCALES = ROWS_WARPS * WARP;                      // float2 [warps][stages][2]: key and value scale of a half
   static constexpr int OFF_BARS = OFF_SCALES + ROWS_WARPS * STAGES * 16;    // uint64 [warps][stages]
   static constexpr int OFF_ML = OFF_BARS + ROWS_WARPS * STAGES * 8;         // float [2][warps][8 NT]
-  static constexpr int OFF_PLACE = OFF_ML + ROWS_WARPS * 8 * NT * 8;        // Place, long long [warps], SeqRows [ROWS_KEPT]
+  static constexpr int OFF_PLACE = OFF_ML + ROWS_WARPS * 8 * NT * 8 + 16;   // (behind them: float [warps]) Place, long long [warps], SeqRows [ROWS_KEPT]
   static constexpr int OFF_SEQ = OFF_PLACE + 80 + ROWS_WARPS * 8;
   static constexpr int BYTES = 1024 + OFF_SEQ + ROWS_KEPT * (int)sizeof(SeqRows);
 };
@@ -113,6 +113,7 @@ __global__ void __launch_bounds__(ROWS_WARPS * 32, rows_ctas(NT)) block_attn_row
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   float* sm = reinterpret_cast<float*>(smem + Smem::OFF_ML);               // [warps][R] maxima
   float* sl = sm + ROWS_WARPS * R;                                         // [warps][R] sums
+  float* refs = sl + ROWS_WARPS * R;                                       // [warps] largest value scales
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   uint64_t* full_bar = reinterpret_cast<uint64_t*>(smem + Smem::OFF_BARS) + warp * STAGES;
   float2* scales = reinterpret_cast<float2*>(smem + Smem::OFF_SCALES) + warp * STAGES * 2;
@@ -444,13 +445,20 @@ __global__ void __launch_bounds__(ROWS_WARPS * 32, rows_ctas(NT)) block_attn_row
         if (g == 0) { sm[warp * R + row] = l[n][r] != 0.f ? P_SHIFT - u[n][r] : -INFINITY; sl[warp * R + row] = l[n][r]; }
 #pragma unroll
         for (int k = 0; k < MT; ++k)
-          *reinterpret_cast<float2*>(my_o + row * Smem::OROW + 16 * k + 2 * g) = make_float2(acc[n][k][r] * vref, acc[n][k][2 + r] * vref);
+          *reinterpret_cast<float2*>(my_o + row * Smem::OROW + 16 * k + 2 * g) = make_float2(acc[n][k][r], acc[n][k][2 + r]);
       }
     }
+    if (lane == 0) refs[warp] = vref;
     __syncthreads();
     const long long group_end = at.first + at.units;
     const bool head = at.unit == at.first, tail = group_end <= at.end, whole = head && tail;   // the group begins / ends in this share
     const long long slot = 2ll * blockIdx.x + (head ? 1 : 0);            // of a partial result: the group goes on / came in
+    // Sums of P V are divided by the row's sum before the value scale enters: P carries up to 2^15 a key, so near the largest BF16 value FP32
+    // holds the quotient alone, and near the smallest a scale divided by the row's sum would lose its bits.  The warps' weights carry
+    // their scale relative to the largest.
+    float ref = refs[0];
+#pragma unroll
+    for (int w = 1; w < ROWS_WARPS; ++w) ref = fmaxf(ref, refs[w]);
     if (threadIdx.x < R) {                       // one thread per row: the warps' weights, the tile's maximum and sum
       const int row = threadIdx.x;
       float mt = sm[row], lt = 0.f, e[ROWS_WARPS];
@@ -462,9 +470,9 @@ __global__ void __launch_bounds__(ROWS_WARPS * 32, rows_ctas(NT)) block_attn_row
         e[w] = mw > -INFINITY ? ex2(mw - mt) : 0.f;
         lt = fmaf(e[w], sl[w * R + row], lt);
       }
-      const float inv = whole ? (lt != 0.f ? 1.0f / lt : 0.f) : 1.0f;
+      const float inv = lt != 0.f ? 1.0f / lt : 0.f, inv_ref = ref > 0.f ? 1.0f / ref : 0.f;
 #pragma unroll
-      for (int w = 0; w < ROWS_WARPS; ++w) sm[w * R + row] = e[w] * inv;
+      for (int w = 0; w < ROWS_WARPS; ++w) sm[w * R + row] = e[w] * inv * (refs[w] * inv_ref);
       if (!whole && at.qt * R + row < at.total) p.part_ml[slot * R + row] = make_float2(mt, lt);
     }
     __syncthreads();
@@ -474,6 +482,7 @@ __global__ void __launch_bounds__(ROWS_WARPS * 32, rows_ctas(NT)) block_attn_row
       float y = 0.f;
 #pragma unroll
       for (int w = 0; w < ROWS_WARPS; ++w) y = fmaf(sm[w * R + row], reinterpret_cast<const float*>(smem + w * Smem::WARP)[row * Smem::OROW + place], y);
+      y *= ref;
       if (whole) store_out(p, at.r0 + rr / p.group, (at.hk * p.group + rr % p.group) * DH + feature_at<DH>(place), y);
       else p.part_o[slot * (R * DH) + i] = y;
     }
@@ -558,15 +567,22 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) block_attn_join_kernel(const 
       if (q0 + k * JOIN_WARPS >= rec.parts) ml[k] = make_float2(-INFINITY, 0.f);
       top = fmaxf(top, ml[k].x);
     }
-    const float old = ex2(m - top);
+    // (a part is divided by its own sum, so what is merged is their mean under weights that add up to one)
+    l *= ex2(m - top);
     m = top;
-    l *= old;
-#pragma unroll
-    for (int e = 0; e < E; ++e) y[e] *= old;
+    float sum = l;
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      const float f = ex2(ml[k].x - top);
-      l = fmaf(f, ml[k].y, l);
+      ml[k].y *= ex2(ml[k].x - top);
+      sum += ml[k].y;
+    }
+    const float inv = sum != 0.f ? __fdividef(1.0f, sum) : 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) y[e] *= l * inv;
+    l = sum;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float f = ml[k].y * inv;
 #pragma unroll
       for (int e = 0; e < E; ++e) y[e] = fmaf(f, x[k][e], y[e]);
     }
@@ -576,16 +592,18 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) block_attn_join_kernel(const 
   if (lane == 0) { ms[warp] = m; ls[warp] = l; }
   __syncthreads();
   if (threadIdx.x < DH) {
-    float mt = ms[0], o = 0.f, lt = 0.f;
+    float mt = ms[0], o = 0.f, lt = 0.f, f[JOIN_WARPS];
 #pragma unroll
     for (int w = 1; w < JOIN_WARPS; ++w) mt = fmaxf(mt, ms[w]);
 #pragma unroll
     for (int w = 0; w < JOIN_WARPS; ++w) {
-      const float f = ex2(ms[w] - mt);
-      o = fmaf(f, part[w][threadIdx.x], o);
-      lt = fmaf(f, ls[w], lt);
+      f[w] = ex2(ms[w] - mt) * ls[w];
+      lt += f[w];
     }
-    store_out(p, s.r0 + rr / p.group, (hk * p.group + rr % p.group) * DH + feature_at<DH>(threadIdx.x), lt != 0.f ? o / lt : 0.f);
+    const float inv = lt != 0.f ? __fdividef(1.0f, lt) : 0.f;
+#pragma unroll
+    for (int w = 0; w < JOIN_WARPS; ++w) o = fmaf(f[w] * inv, part[w][threadIdx.x], o);
+    store_out(p, s.r0 + rr / p.group, (hk * p.group + rr % p.group) * DH + feature_at<DH>(threadIdx.x), o);
   }
 }
 

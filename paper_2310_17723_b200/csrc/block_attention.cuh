@@ -15,7 +15,7 @@ struct BlockAttnParams {
   int by_group;                  // records of cut groups are listed by group, else by share
   struct JoinRecord* records;
   int splits;                    // many rows: parts of a group's keys, a CTA each
-  float* part_o; float2* part_ml; // partial results ([CTA][2]; many rows: [CTA]): sum of P V [rows][DH], (maximum, sum of P) [rows]
+  float* part_o; float2* part_ml; // partial results ([CTA][2]; many rows: [CTA]): output of the part's keys alone [rows][DH], (maximum, sum of P) [rows]
 };
 
 __device__ __forceinline__ void store_out(const BlockAttnParams& p, long long row, int col, float y) {

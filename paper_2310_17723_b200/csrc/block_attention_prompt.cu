@@ -301,11 +301,13 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
       }
     }
     // ---- output, or the part's sums
-    float scale_o = 0.f;
+    // (O is divided by the row's sum before the value scale enters: near the ends of BF16's range neither O times the scale nor the scale
+    // over the sum is a number that FP32 holds)
+    float inv_l = 0.f;
     if (n > 0) {
       ok = __all_sync(0xffffffffu, ok && ptx::mbar_wait(&o_last[t], 0, c.err, 0x8200 | t));
       ptx::tc_fence_after();
-      scale_o = l != 0.f ? (p.splits > 1 ? vref : vref / l) : 0.f;
+      inv_l = l != 0.f ? 1.0f / l : 0.f;
     }
     const long long own = (long long)blockIdx.x * PR_ROWS + 128 * t + r;   // the row's place among the parts
     const bool seen = n > 0 && l != 0.f;
@@ -319,7 +321,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
       }
       float y[32];
 #pragma unroll
-      for (int i = 0; i < 32; ++i) y[i] = seen ? __uint_as_float(x[i]) * scale_o : 0.f;
+      for (int i = 0; i < 32; ++i) y[i] = seen ? __uint_as_float(x[i]) * inv_l * vref : 0.f;
       if (p.splits > 1) {
         if (seen && row_ok && ok) {
           float4* dst = reinterpret_cast<float4*>(p.part_o + own * DH + 32 * k);
@@ -555,20 +557,20 @@ __global__ void __launch_bounds__(PJ_WARPS * 32) block_attn_prompt_join_kernel(c
       const long long at = ((long long)blockIdx.x * p.splits + q) * PR_ROWS + row0 + i;
       const float2 ml = __ldcg(p.part_ml + at);
       if (ml.x == -INFINITY) continue;                             // nor were sums of no keys
-      const float now = fmaxf(m[i], ml.x), old = ex2(m[i] - now), w = ex2(ml.x - now);
+      // (a part is divided by its own sum: their mean, under weights that add up to one)
+      const float now = fmaxf(m[i], ml.x), old = l[i] * ex2(m[i] - now), w = ex2(ml.x - now) * ml.y, inv = 1.0f / (old + w);
       m[i] = now;
-      l[i] = fmaf(l[i], old, w * ml.y);
+      l[i] = old + w;
 #pragma unroll
-      for (int e = 0; e < E; ++e) y[i][e] = fmaf(y[i][e], old, w * __ldcg(p.part_o + at * DH + 32 * e + lane));
+      for (int e = 0; e < E; ++e) y[i][e] = fmaf(y[i][e], old * inv, w * inv * __ldcg(p.part_o + at * DH + 32 * e + lane));
     }
   }
 #pragma unroll
   for (int i = 0; i < PJ_EACH; ++i) {
     const int rr = qt * PR_ROWS + row0 + i;
     if (rr >= total) break;
-    const float inv = l[i] != 0.f ? 1.0f / l[i] : 0.f;
 #pragma unroll
-    for (int e = 0; e < E; ++e) store_out(p, s.r0 + rr / p.group, (hk * p.group + rr % p.group) * DH + 32 * e + lane, y[i][e] * inv);
+    for (int e = 0; e < E; ++e) store_out(p, s.r0 + rr / p.group, (hk * p.group + rr % p.group) * DH + 32 * e + lane, y[i][e]);
   }
 }
 

@@ -50,3 +50,23 @@ def test_value_scales_below_the_normal_range_beside_ordinary_ones(h, kind, dh, c
     _renew(c, "v")
     qt, qx = _q(1, sum(counts), 2 * dh, "bf16")
     _compare(c, _run(h, c, qt, counts, 2, "bf16"), qx, counts, 2, "bf16")
+
+
+@pytest.mark.parametrize("counts,max_len", FORMS)
+@pytest.mark.parametrize("kind,dh", [("i8", 128), ("f8", 64)])
+@pytest.mark.parametrize("unit", [5e35, 2.0 ** -130])
+def test_values_near_the_ends_of_the_range(h, kind, dh, counts, max_len, unit):
+    # sums of P V before their division by the row's sum are up to 2^15 keys times the values: FP32 does not hold them at one end, and
+    # a factor divided by the row's sum loses its bits at the other
+    g = np.random.default_rng(2)
+    c = _cache(kind, dh, max_len)
+    c.scale["v"][:] = unit * g.uniform(0.3, 1.0, c.scale["v"].shape)
+    _renew(c, "v")
+    qt, qx = _q(3, sum(counts), 2 * dh, "bf16")
+    got = _run(h, c, qt, counts, 2, "bf16").double().cpu().numpy()
+    want, bar = _expect(c, qx, counts, 2, dh ** -0.5, sum(counts))
+    # probabilities are held relative to the largest value scale, a normal number: 2^-36 of 2^-126 times the largest code per key; partial
+    # results in FP32's subnormal numbers are off by 2^-150 each, sixteen of them at most
+    bar = bar + max(LENS) * 2.0 ** -36 * 448 * 2.0 ** -126 + 16 * 2.0 ** -150
+    bar = bar + torch.finfo(torch.bfloat16).eps / 2 * (np.abs(want) + bar) + 2.0 ** -134
+    assert np.all(np.abs(got - want) <= bar), np.nanmax(np.abs(got - want) / bar)
