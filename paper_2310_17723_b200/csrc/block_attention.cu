@@ -540,8 +540,7 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) block_attn_join_kernel(const 
   const SeqRows s = seq_rows(p.c, b);
   const int row = blockIdx.y, rr = qt * R + row, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (rr >= s.n * p.group || rec.parts == 0) return;               // (a record of rows that are not there was never written)
-  constexpr float LEAST = -1e30f;                // below every maximum, and finite: no case for parts without a key
-  float m = LEAST, l = 0.f, y[E];
+  float m = -INFINITY, l = 0.f, y[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) y[e] = 0.f;
   for (int q0 = warp; q0 < rec.parts; q0 += 8 * JOIN_WARPS) {
@@ -568,12 +567,13 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) block_attn_join_kernel(const 
       top = fmaxf(top, ml[k].x);
     }
     // (a part is divided by its own sum, so what is merged is their mean under weights that add up to one)
-    l *= ex2(m - top);
+    const float base = top == -INFINITY ? 0.f : top;               // (parts without a key have no maximum)
+    l *= ex2(m - base);
     m = top;
     float sum = l;
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      ml[k].y *= ex2(ml[k].x - top);
+      ml[k].y *= ex2(ml[k].x - base);
       sum += ml[k].y;
     }
     const float inv = sum != 0.f ? __fdividef(1.0f, sum) : 0.f;
@@ -595,6 +595,7 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) block_attn_join_kernel(const 
     float mt = ms[0], o = 0.f, lt = 0.f, f[JOIN_WARPS];
 #pragma unroll
     for (int w = 1; w < JOIN_WARPS; ++w) mt = fmaxf(mt, ms[w]);
+    if (mt == -INFINITY) mt = 0.f;
 #pragma unroll
     for (int w = 0; w < JOIN_WARPS; ++w) {
       f[w] = ex2(ms[w] - mt) * ls[w];

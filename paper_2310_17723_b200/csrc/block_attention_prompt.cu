@@ -545,7 +545,7 @@ __global__ void __launch_bounds__(PJ_WARPS * 32) block_attn_prompt_join_kernel(c
   float m[PJ_EACH], l[PJ_EACH], y[PJ_EACH][E];
 #pragma unroll
   for (int i = 0; i < PJ_EACH; ++i) {
-    m[i] = -1e30f; l[i] = 0.f;                     // below every maximum, and finite: no case for rows without a key
+    m[i] = -INFINITY; l[i] = 0.f;
 #pragma unroll
     for (int e = 0; e < E; ++e) y[i][e] = 0.f;
   }

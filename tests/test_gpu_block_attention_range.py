@@ -70,3 +70,32 @@ def test_values_near_the_ends_of_the_range(h, kind, dh, counts, max_len, unit):
     bar = bar + max(LENS) * 2.0 ** -36 * 448 * 2.0 ** -126 + 16 * 2.0 ** -150
     bar = bar + torch.finfo(torch.bfloat16).eps / 2 * (np.abs(want) + bar) + 2.0 ** -134
     assert np.all(np.abs(got - want) <= bar), np.nanmax(np.abs(got - want) / bar)
+
+
+def _one_loud_token(kind, dh, max_len, k_unit):
+    """Keys of one sign in which token 3 of each sequence is small: against queries of the other sign its score is the largest by far."""
+    c = _cache(kind, dh, max_len, k_scale=k_unit)
+    codes = BC.to_codes(np.maximum(np.abs(c.codes["k"]), 50.0), kind)
+    for b in range(2):
+        codes[c.table[b][0], :, 3] = 1.0
+    c.codes["k"] = codes
+    c.buf["k"].copy_(torch.from_numpy(codes.astype(np.float32)).to(c.buf["k"].dtype))
+    return c
+
+
+def _is_the_value_of_its_one_token(h, kind, dh, counts, max_len, k_unit, q_unit):
+    c = _one_loud_token(kind, dh, max_len, k_unit)
+    rows = sum(counts)
+    qt, _ = to_fp(-q_unit * np.random.default_rng(4).uniform(1.0, 1.5, (rows, 2 * dh)), "bf16")
+    got = _run(h, c, qt, counts, 2, "bf16").double().cpu().numpy()
+    for b, (n, at) in enumerate(zip(counts, starts(counts))):
+        want = np.tile(c.values("v", b)[3, 0], (n, 2))
+        # half a step of BF16, and two roundings of FP16 (the probability and its product with the value scale)
+        assert np.all(np.abs(got[at:at + n] - want) <= (2.0 ** -8 + 2.0 ** -10) * np.abs(want)), b
+
+
+@pytest.mark.parametrize("counts,max_len", FORMS[:3])
+@pytest.mark.parametrize("kind,dh", [("i8", 64), ("f8", 128)])
+def test_few_rows_whose_scores_all_lie_below_a_large_negative_number(h, kind, dh, counts, max_len):
+    # the largest score is about -1e32, the next fifty times as far
+    _is_the_value_of_its_one_token(h, kind, dh, counts, max_len, 1e14, 1e17)
