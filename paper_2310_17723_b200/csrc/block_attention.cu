@@ -383,7 +383,13 @@ __global__ void __launch_bounds__(ROWS_WARPS * 32, rows_ctas(NT)) block_attn_row
             for (int k = 0; k < MT; ++k) { acc[r][k][0] *= a0; acc[r][k][2] *= a0; acc[r][k][1] *= a1; acc[r][k][3] *= a1; }
           }
 #pragma unroll
-          for (int h = 0; h < 2; ++h) { x[h][0] -= d0; x[h][2] -= d0; x[h][1] -= d1; x[h][3] -= d1; }
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              // (a maximum beyond 2^26 is itself rounded by more than 4: without the bound a score of 2^27 left P at 2^16, beyond FP16)
+              const float moved = x[h][i] - ((i & 1) ? d1 : d0);
+              x[h][i] = moved > P_SHIFT + MAX_SLACK ? P_SHIFT + MAX_SLACK : moved;
+            }
         }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {

@@ -99,3 +99,11 @@ def _is_the_value_of_its_one_token(h, kind, dh, counts, max_len, k_unit, q_unit)
 def test_few_rows_whose_scores_all_lie_below_a_large_negative_number(h, kind, dh, counts, max_len):
     # the largest score is about -1e32, the next fifty times as far
     _is_the_value_of_its_one_token(h, kind, dh, counts, max_len, 1e14, 1e17)
+
+
+@pytest.mark.parametrize("counts,max_len", FORMS[:3])
+@pytest.mark.parametrize("kind,dh", [("i8", 64), ("f8", 128)])
+@pytest.mark.parametrize("q_unit", [1e6, 3e6, 1e7, 2e7, 4e7, 1e9, 1e12])
+def test_few_rows_whose_scores_are_rounded_by_more_than_the_probabilities_reach(h, kind, dh, counts, max_len, q_unit):
+    # scores of 2^27: FP32 holds them in steps of 16, more than FP16 has above the place that the largest probability is given
+    _is_the_value_of_its_one_token(h, kind, dh, counts, max_len, 1.0, q_unit)
