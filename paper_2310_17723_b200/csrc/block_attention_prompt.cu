@@ -38,6 +38,7 @@ constexpr int PR_INFO = 4;                                     // ring of scale 
 constexpr float PR_SHIFT = 8.0f;                               // P carries a factor 2^8 when the maximum has just moved
 constexpr float PR_MOST = 65504.0f;                            // and 16 of them sum to no more than this, so none overflows FP16
 constexpr float PR_HIGH = 11.9f;                               // 16 x 2^PR_HIGH stays below that
+constexpr float PR_COARSE = 524288.0f;                         // 2^19: maxima up to here are rounded by less than 2^-4
 constexpr float PR_MIN_RV = 9.094947e-13f;                     // 2^-40
 
 
@@ -251,11 +252,20 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
             if (m > -INFINITY) mx = fmaxf(mx, fmaf(m, f * info[g].x, u));
           }
           // where it calls for it, it moves the row's, O and the sum follow, and O the value reference
-          if (__any_sync(0xffffffffu, first || mx > PR_HIGH) || turn) {
+          // (A maximum beyond 2^PR_COARSE is itself rounded by more than the places above the largest probability can take.  Such a row's
+          // reference is put eight of its roundings too low, so that no rounding leaves the largest key without weight, keys up
+          // there count alike (the bound on e0, e1 below), and the maximum moves for a key above all of them only.)
+          const float slack = fabsf(u) > PR_COARSE ? fabsf(u) * 0x1p-20f : 0.f;
+          if (__any_sync(0xffffffffu, first || mx > PR_HIGH + slack) || turn) {
             float d = mx - PR_SHIFT;
-            if (!first) d = fmaxf(d, 0.f);
+            if (!first) d = slack == 0.f ? fmaxf(d, 0.f) : mx > PR_HIGH + slack ? d : 0.f;
             if (mx == -INFINITY) d = 0.f;
+            const float from = u;
             u -= d;
+            if (d != 0.f && fabsf(u) > PR_COARSE) {
+              u = fmaf(fabsf(u), 0x1p-21f, u);
+              d = from - u;
+            }
             if (!first) {
               ok = __all_sync(0xffffffffu, ok && ptx::mbar_wait(&o_full[t], (h + 1) & 1, c.err, 0x8180 | t));   // the previous half's P V
               ptx::tc_fence_after();
@@ -285,8 +295,9 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
               const int key = 16 * g + 2 * i;
-              const float e0 = key < valid ? ex2(fmaf(__uint_as_float(z[2 * i]), fk, ug)) : 0.f;
-              const float e1 = key + 1 < valid ? ex2(fmaf(__uint_as_float(z[2 * i + 1]), fk, ug)) : 0.f;
+              const float x0 = fmaf(__uint_as_float(z[2 * i]), fk, ug), x1 = fmaf(__uint_as_float(z[2 * i + 1]), fk, ug);
+              const float e0 = key < valid ? ex2(x0 > PR_HIGH ? PR_HIGH : x0) : 0.f;
+              const float e1 = key + 1 < valid ? ex2(x1 > PR_HIGH ? PR_HIGH : x1) : 0.f;
               sum.x += e0; sum.y += e1;
               w[i] = pack_f16(e0, e1);
             }

@@ -90,8 +90,10 @@ def _is_the_value_of_its_one_token(h, kind, dh, counts, max_len, k_unit, q_unit)
     got = _run(h, c, qt, counts, 2, "bf16").double().cpu().numpy()
     for b, (n, at) in enumerate(zip(counts, starts(counts))):
         want = np.tile(c.values("v", b)[3, 0], (n, 2))
+        t = LENS[b] - n + np.arange(n)             # the rows' tokens: those before the loud one do not see it, rows without one are zeros
+        assert np.all(got[at:at + n][t < 0] == 0)
         # half a step of BF16, and two roundings of FP16 (the probability and its product with the value scale)
-        assert np.all(np.abs(got[at:at + n] - want) <= (2.0 ** -8 + 2.0 ** -10) * np.abs(want)), b
+        assert np.all((np.abs(got[at:at + n] - want) <= (2.0 ** -8 + 2.0 ** -10) * np.abs(want))[t >= 3]), b
 
 
 @pytest.mark.parametrize("counts,max_len", FORMS[:3])
@@ -107,3 +109,27 @@ def test_few_rows_whose_scores_all_lie_below_a_large_negative_number(h, kind, dh
 def test_few_rows_whose_scores_are_rounded_by_more_than_the_probabilities_reach(h, kind, dh, counts, max_len, q_unit):
     # scores of 2^27: FP32 holds them in steps of 16, more than FP16 has above the place that the largest probability is given
     _is_the_value_of_its_one_token(h, kind, dh, counts, max_len, 1.0, q_unit)
+
+
+@pytest.mark.parametrize("counts,max_len", FORMS[3:] + [([700, 60], 900)])
+@pytest.mark.parametrize("kind,dh", [("i8", 64), ("f8", 128)])
+@pytest.mark.parametrize("k_unit,q_unit", [(1.0, 1e5), (1.0, 1e6), (1.0, 3e6), (1.0, 1e7), (1.0, 2e7), (1.0, 4e7), (1.0, 1e9), (1.0, 1e12), (1e14, 1e17)])
+def test_many_rows_whose_scores_are_rounded_by_more_than_the_probabilities_reach(h, kind, dh, counts, max_len, k_unit, q_unit):
+    _is_the_value_of_its_one_token(h, kind, dh, counts, max_len, k_unit, q_unit)
+
+
+@pytest.mark.parametrize("counts,max_len", FORMS)
+@pytest.mark.parametrize("q_unit", [1.0, 1e3])
+def test_keys_that_are_all_alike_share_a_row(h, counts, max_len, q_unit):
+    # equal keys have equal scores: the row is the mean of the values (P in FP16, sums and the mean in FP32)
+    c = _cache("i8", 64, max_len, k_scale=1.0)
+    c.codes["k"][:] = 3.0
+    c.buf["k"].fill_(3)
+    qt, _ = to_fp(-q_unit * np.random.default_rng(4).uniform(1.0, 1.5, (sum(counts), 2 * 64)), "bf16")
+    got = _run(h, c, qt, counts, 2, "bf16").double().cpu().numpy()
+    for b, (n, at) in enumerate(zip(counts, starts(counts))):
+        v = c.values("v", b)[:, 0]
+        for i in range(n):
+            seen = v[:LENS[b] - n + i + 1]
+            bar = 2.0 ** -10 * np.abs(seen).mean(0) + 2.0 ** -8 * np.abs(seen.mean(0))
+            assert np.all(np.abs(got[at + i] - np.tile(seen.mean(0), 2)) <= np.tile(bar, 2)), (b, i)
