@@ -259,10 +259,7 @@ __global__ void __launch_bounds__(ROWS_WARPS * 32, rows_ctas(NT)) block_attn_row
       top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
       top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
       const float amax = fp16ish_to_f32x2<BF>(top).x;
-      // 2^(14 - exponent of the maximum); zero, infinite and NaN rows are left as they are
-      const int e = (int)(__float_as_uint(amax) >> 23);
-      const float up = e == 0 || e == 255 ? 1.0f : __uint_as_float((uint32_t)min(127 + 14 + 127 - e, 253) << 23);
-      const float down = p.c2 / up;                // a power of two within the normal range: exact
+      const float up = query_factor(amax), down = p.c2 / up;
 #pragma unroll
       for (int i = 0; i < KC * 8; ++i) {
         const float2 x = fp16ish_to_f32x2<BF>(raw[i]);

@@ -32,6 +32,13 @@ __device__ __forceinline__ void store_out(const BlockAttnParams& p, long long ro
 // of two, so P stays below 2^15 and a probability 2^-25 of the largest is still a normal FP16 number.
 constexpr float P_SHIFT = 11.0f, MAX_SLACK = 4.0f;
 
+// Factor that brings a query row of this largest magnitude into FP16: 2^(14 - its exponent), at most 2^126 (which BF16's subnormal rows
+// need, and which leaves the score factor divided by it within three bits of FP32's subnormal numbers); infinite and NaN rows are left alone.
+__device__ __forceinline__ float query_factor(float amax) {
+  const int e = (int)(__float_as_uint(amax) >> 23);
+  return e == 255 ? 1.0f : __uint_as_float((uint32_t)min(127 + 14 + 127 - e, 253) << 23);
+}
+
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

@@ -140,8 +140,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
 #pragma unroll
       for (int i = 0; i < DH / 2; ++i) top = __vmaxu2(top, w[i] & 0x7fff7fffu);
       const float amax = fp16ish_to_f32x2<BF>(max(top & 0xffffu, top >> 16)).x;
-      const int e = (int)(__float_as_uint(amax) >> 23);
-      const float up = e == 0 || e == 255 ? 1.0f : __uint_as_float((uint32_t)min(127 + 14 + 127 - e, 253) << 23);
+      const float up = query_factor(amax);
       f = fabsf(p.c2) / up;
       const float up_s = p.c2 < 0.f ? -up : up;
       uint8_t* row = smem + t * Cfg::TILE + (r >> 3) * 1024 + (r & 7) * 128;

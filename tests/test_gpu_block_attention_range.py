@@ -133,3 +133,15 @@ def test_keys_that_are_all_alike_share_a_row(h, counts, max_len, q_unit):
             seen = v[:LENS[b] - n + i + 1]
             bar = 2.0 ** -10 * np.abs(seen).mean(0) + 2.0 ** -8 * np.abs(seen.mean(0))
             assert np.all(np.abs(got[at + i] - np.tile(seen.mean(0), 2)) <= np.tile(bar, 2)), (b, i)
+
+
+@pytest.mark.parametrize("counts,max_len", FORMS)
+@pytest.mark.parametrize("kind,dh", [("i8", 64), ("f8", 128)])
+def test_subnormal_queries(h, kind, dh, counts, max_len):
+    # BF16 queries of 1e-39 against keys of 1e37: scores of about one
+    c = _cache(kind, dh, max_len)
+    c.scale["k"][:] = np.float32(5e35) * np.random.default_rng(5).uniform(0.3, 1.0, c.scale["k"].shape)
+    _renew(c, "k")
+    qt, qx = to_fp(1e-39 * np.random.default_rng(6).standard_normal((sum(counts), 2 * dh)), "bf16")
+    assert qx.any()
+    _compare(c, _run(h, c, qt, counts, 2, "bf16", scale=20.0), qx, counts, 2, "bf16", scale=20.0)
