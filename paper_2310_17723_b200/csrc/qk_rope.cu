@@ -77,8 +77,9 @@ __global__ void __launch_bounds__(ROPE_MAX_WARPS * 32, 4) qk_rope_kernel(const _
     }
   }
   __syncthreads();
-  // the lane that holds the partner features under HERO_PAIR_HALVES
-  const int r2 = p.rot >> 4, mate_lane = (lane - sub) + (f0 < p.rot ? (sub < r2 ? sub + r2 : sub - r2) : sub);
+  // the lane that holds the partner features under HERO_PAIR_HALVES (all eight features of a lane turn, or none)
+  const bool turned = f0 < p.rot;
+  const int r2 = p.rot >> 4, mate_lane = (lane - sub) + (turned ? (sub < r2 ? sub + r2 : sub - r2) : sub);
   for (int unit = warp; unit < per_row;) {
     const bool norm = p.gamma[side] != nullptr;
     float2 o[4], m[4];
@@ -113,11 +114,15 @@ __global__ void __launch_bounds__(ROPE_MAX_WARPS * 32, 4) qk_rope_kernel(const _
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         y[e] = __fmul2_rn(x[e], o[e]);
+        // (what does not turn has no partner: a factor of zero would let an infinite or NaN neighbour in)
         if constexpr (ADJ) {
-          y[e].x = fmaf(x[e].y, m[e].x, y[e].x);
-          y[e].y = fmaf(x[e].x, m[e].y, y[e].y);
+          if (turned) {
+            y[e].x = fmaf(x[e].y, m[e].x, y[e].x);
+            y[e].y = fmaf(x[e].x, m[e].y, y[e].y);
+          }
         } else {
-          y[e] = __ffma2_rn(fp16ish_to_f32x2<BF>(__shfl_sync(0xffffffffu, w[e], mate_lane)), m[e], y[e]);
+          const uint32_t partner = __shfl_sync(0xffffffffu, w[e], mate_lane);
+          if (turned) y[e] = __ffma2_rn(fp16ish_to_f32x2<BF>(partner), m[e], y[e]);
         }
         y[e] = __fmul2_rn(y[e], make_float2(r, r));
       }

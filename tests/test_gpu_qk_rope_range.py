@@ -1,0 +1,60 @@
+"""GPU parity of hero_qk_norm_rope where values are not finite or leave the range of the INT8 output, and of its INT8 outputs for
+keys, both pairings and a scale for each output.  Bounds as in test_gpu_qk_rope.py."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import block_cache as BC
+from paper_2310_17723_b200 import hero
+from block_util import to_fp
+from test_gpu_qk_rope import _tables
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def h():
+    hd = hero.Handle()
+    yield hd
+    hd.check()
+    hd.close()
+
+
+@pytest.mark.parametrize("fp", ["f16", "bf16"])
+@pytest.mark.parametrize("pairing", ["halves", "adjacent"])
+@pytest.mark.parametrize("dh,rot", [(128, 64), (64, 0), (80, 32), (256, 128)])
+@pytest.mark.parametrize("norm", [False, True])
+def test_what_is_not_finite_stays_where_the_definition_leaves_it(h, fp, pairing, dh, rot, norm):
+    # infinities and NaN in features that pass through and in features that turn, zeros of either sign; a row each, and one of all
+    g = np.random.default_rng(dh + rot)
+    rows, nq = 6, 3
+    x = g.standard_normal((rows, nq, dh))
+    x[:, :, 5 % max(rot, 8)] = -0.0
+    x[:, :, dh - 3] = -0.0
+    x[0, 0, dh - 6] = np.inf
+    x[1, 1, dh - 7] = np.nan
+    x[2, 2, [dh - 1, dh - 2]] = -np.inf, np.inf
+    x[3, 0, 2] = np.inf                                        # turned where there is a rotation
+    x[4, 1, 1] = np.nan
+    x[5, :, dh - 5], x[5, 0, 0] = np.inf, -np.inf
+    t, xr = to_fp(x.reshape(rows, nq * dh), fp)
+    c, s, ct, st = _tables(50, rot, seed=0.3) if rot else (None,) * 4
+    pos = g.integers(0, 50, rows).astype(np.int32)
+    gm = (1 + 0.2 * g.standard_normal(dh)).astype(np.float32) if norm else None
+    out = torch.zeros_like(t)
+    h.hero_qk_norm_rope(hero.tensor(t), None, hero.tensor(out), None, nq, 0, torch.from_numpy(pos).cuda() if rot else None, ct, st,
+                        torch.from_numpy(gm).cuda() if norm else None, pairing=pairing)
+    h.check()
+    with np.errstate(invalid="ignore"):
+        want = BC.norm_rope(xr, nq, gm, 1e-6, c, s, pos, pairing)
+        size = np.abs(BC.norm_rope(np.where(np.isfinite(xr), xr, 0.0), nq, gm, 1e-6, None, None, None, pairing)).max()
+    got = out.double().cpu().numpy()
+    assert np.array_equal(np.isnan(got), np.isnan(want))
+    assert np.array_equal(got[np.isinf(want)], want[np.isinf(want)]) and np.array_equal(np.isinf(got), np.isinf(want))
+    fin = np.isfinite(want)
+    # half a step of the type, and 16 units of 2^-24 on the two products, each at most the largest magnitude
+    assert np.all(np.abs(got - want)[fin] <= torch.finfo(t.dtype).eps / 2 * np.abs(want[fin]) + 32 * 2.0 ** -24 * size + 2.0 ** -25)
+    if not norm:                                               # what passes through is the input, signs of zeros and all
+        a, b = (y.view(torch.int16).reshape(rows, nq, dh)[..., rot:] for y in (out, t))
+        keep = ~torch.isnan(t.reshape(rows, nq, dh)[..., rot:])
+        assert torch.equal(a[keep], b[keep])
