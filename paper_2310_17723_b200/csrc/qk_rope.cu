@@ -130,9 +130,12 @@ __global__ void __launch_bounds__(ROPE_MAX_WARPS * 32, 4) qk_rope_kernel(const _
         const long long at = at0 + i * HPI * p.dh;
         if (to_i8) {
           const Divider div(i8_scale);
+          // (bounded before the division: a quotient beyond FP32, an infinity's too, would leave a remainder that is NaN)
+          const float most = 128.f * i8_scale;
+          auto code_of = [&](float x) { return div(fminf(fmaxf(x, -most), most)); };
           uint2 code;
-          code.x = f32_to_codes4<false>(div(y[0].x), div(y[0].y), div(y[1].x), div(y[1].y));
-          code.y = f32_to_codes4<false>(div(y[2].x), div(y[2].y), div(y[3].x), div(y[3].y));
+          code.x = f32_to_codes4<false>(code_of(y[0].x), code_of(y[0].y), code_of(y[1].x), code_of(y[1].y));
+          code.y = f32_to_codes4<false>(code_of(y[2].x), code_of(y[2].y), code_of(y[3].x), code_of(y[3].y));
           *reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.y[side]) + at) = code;
         } else {
           *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.y[side]) + at) =

@@ -58,3 +58,27 @@ def test_what_is_not_finite_stays_where_the_definition_leaves_it(h, fp, pairing,
         a, b = (y.view(torch.int16).reshape(rows, nq, dh)[..., rot:] for y in (out, t))
         keep = ~torch.isnan(t.reshape(rows, nq, dh)[..., rot:])
         assert torch.equal(a[keep], b[keep])
+
+
+@pytest.mark.parametrize("pairing", ["halves", "adjacent"])
+def test_int8_outputs_saturate(h, pairing):
+    # infinities, and quotients beyond FP32: the largest code of their sign
+    rows, dh, rot = 4, 64, 32
+    g = np.random.default_rng(1)
+    x = g.standard_normal((rows, 2 * dh))
+    x[0, [40, 41, 63]] = np.inf, -np.inf, np.inf               # pass through
+    x[1, [dh + 33, dh + 50]] = 3e38, -3e38
+    x[2] *= 1e30
+    x[3, 10] = np.inf                                          # turned: its pair is infinite
+    t, xr = to_fp(x, "bf16")
+    c, s, ct, st = _tables(50, rot, seed=0.3)
+    pos = np.array([3, 7, 11, 19], np.int32)
+    for step in (0.02, 1e-5, 1e-25, 1e-35):
+        out = torch.zeros(rows, 2 * dh, dtype=torch.int8, device="cuda")
+        sc = torch.tensor([step], device="cuda")
+        h.hero_qk_norm_rope(hero.tensor(t), None, hero.tensor(out, "sq", sc), None, 2, 0, torch.from_numpy(pos).cuda(), ct, st, pairing=pairing)
+        h.check()
+        y = BC.norm_rope(xr, 2, None, 0.0, c, s, pos, pairing)
+        sign = BC.to_codes(np.clip(y / float(sc[0]), -1e9, 1e9), "i8")
+        far = np.abs(y) > 200 * step
+        assert np.array_equal(out.double().cpu().numpy()[far], sign[far]), step
