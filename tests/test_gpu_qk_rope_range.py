@@ -82,3 +82,32 @@ def test_int8_outputs_saturate(h, pairing):
         sign = BC.to_codes(np.clip(y / float(sc[0]), -1e9, 1e9), "i8")
         far = np.abs(y) > 200 * step
         assert np.array_equal(out.double().cpu().numpy()[far], sign[far]), step
+
+
+@pytest.mark.parametrize("fp", ["f16", "bf16"])
+@pytest.mark.parametrize("pairing", ["halves", "adjacent"])
+@pytest.mark.parametrize("dh,rot,nq,nkv", [(128, 128, 8, 2), (64, 32, 3, 3), (96, 96, 2, 1)])
+def test_int8_queries_and_keys_with_a_scale_each(h, fp, pairing, dh, rot, nq, nkv):
+    rows = 23
+    g = np.random.default_rng(dh)
+    (qt, qx), (kt, kx) = (to_fp(g.standard_normal((rows, n * dh)) * z, fp) for n, z in ((nq, 2.0), (nkv, 0.3)))
+    c, s, ct, st = _tables(64, rot)
+    pos = g.integers(0, 64, rows).astype(np.int32)
+    gq, gk = ((1 + 0.2 * g.standard_normal(dh)).astype(np.float32) for _ in range(2))
+    sq, sk = torch.tensor([0.021], device="cuda"), torch.tensor([0.034], device="cuda")
+    qo, ko = (torch.zeros(rows, n * dh, dtype=torch.int8, device="cuda") for n in (nq, nkv))
+    h.hero_qk_norm_rope(hero.tensor(qt), hero.tensor(kt), hero.tensor(qo, "sq", sq), hero.tensor(ko, "sq", sk), nq, nkv, torch.from_numpy(pos).cuda(),
+                        ct, st, torch.from_numpy(gq).cuda(), torch.from_numpy(gk).cuda(), pairing=pairing)
+    h.check()
+    for got, x, heads, gm, sc in ((qo, qx, nq, gq, sq), (ko, kx, nkv, gk, sk)):
+        y = BC.norm_rope(x, heads, gm, 1e-6, c, s, pos, pairing) / float(sc[0])
+        # half a step; FP32 noise of 32 units of 2^-24 on two products of at most sqrt(dh) * 2 each over the scale
+        assert np.all(np.abs(got.double().cpu().numpy() - np.clip(y, -127, 127)) <= 0.5 + 32 * 2.0 ** -24 * 4 * dh ** 0.5 / float(sc[0]))
+    # one of the two in the input's type
+    k16 = torch.zeros_like(kt)
+    h.hero_qk_norm_rope(hero.tensor(qt), hero.tensor(kt), hero.tensor(qo, "sq", sq), hero.tensor(k16), nq, nkv, torch.from_numpy(pos).cuda(),
+                        ct, st, torch.from_numpy(gq).cuda(), torch.from_numpy(gk).cuda(), pairing=pairing)
+    h.check()
+    y = BC.norm_rope(kx, nkv, gk, 1e-6, c, s, pos, pairing)
+    got = k16.double().cpu().numpy()
+    assert np.all(np.abs(got - y) <= torch.finfo(kt.dtype).eps / 2 * np.abs(y) + 32 * 2.0 ** -24 * 4 * dh ** 0.5 + 2.0 ** -25)
