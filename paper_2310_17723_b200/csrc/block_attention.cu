@@ -1,5 +1,6 @@
 // Attention over the 8-bit block cache (hero_block_attention): o = softmax(scale q K^T) V, causal in a sequence's new rows.
 #include "block_attention.cuh"
+#include "block_ring.cuh"
 #include <cmath>
 
 namespace hero {
@@ -189,16 +190,14 @@ __global__ void __launch_bounds__(ROWS_WARPS * 32, rows_ctas(NT)) block_attn_row
   }
   __syncthreads();
 
-  int stage = 0;                                 // ring position and parity go on from group to group
-  uint32_t phase = 0;
-  bool ok = true;
+  CopyRing<STAGES> ring;                         // its position and parity go on from group to group
   for (;;) {
     const int b = at.b, hk = at.hk, total = at.total, rb = at.qt * R;
     const int last = (min(rb + R, total) - 1) / p.group, base = at.len - at.n;
     const int L = max(base + last + 1, 0);       // keys of the tile's last row
     const int open = base + rb / p.group + 1;    // keys of its first row: steps below need no mask
     const int k0 = (int)min((long long)L, 32 * (at.unit - at.first)), k1 = (int)min((long long)L, 32 * (at.end - at.first));
-    const int steps = (k1 - k0 + 31) >> 5, mine = steps > warp ? (steps - warp + ROWS_WARPS - 1) / ROWS_WARPS : 0;
+    const int steps = (k1 - k0 + 31) >> 5, mine = ring.steps_of(steps > warp ? (steps - warp + ROWS_WARPS - 1) / ROWS_WARPS : 0);
 
     // lane i looks after half i % 2 of the warp's step i / 2 of every batch of 16: page id, scales, requests
     int my_token = 0, my_id = -1;
@@ -235,8 +234,7 @@ __global__ void __launch_bounds__(ROWS_WARPS * 32, rows_ctas(NT)) block_attn_row
       }
     };
     load_pages(0);
-#pragma unroll
-    for (int i = 0; i < STAGES; ++i) request(i, (stage + i) % STAGES);
+    ring.open(request);
 
     // query fragments: lane (g, t) holds features 64 c + 16 t .. + 15 of row g of each N tile, scaled by a power of two
     uint32_t qf[NT][KC * 8];
@@ -291,16 +289,11 @@ __global__ void __launch_bounds__(ROWS_WARPS * 32, rows_ctas(NT)) block_attn_row
       for (int r = 0; r < 2; ++r) v_off[r] = (2 * t + r) * 64 + (((g >> 1) ^ t) << 4) + (g & 1) * 8;
     }
 
-    for (int n = 0; n < mine; ++n) {
-      const int tb = k0 + 32 * (warp + ROWS_WARPS * n);
-      ok = ok && ptx::mbar_wait(&full_bar[stage], phase, c.err, 0x7000 | stage);
-      if (!__all_sync(0xffffffffu, ok)) {          // a copy never arrived (reported): wait, bounded, for the others before the ring is reused
-        for (int i = 1; i < STAGES && n + i < mine; ++i) {
-          if (++stage == STAGES) { stage = 0; phase ^= 1; }
-          ptx::mbar_wait(&full_bar[stage], phase, c.err, 0x7100 | stage);
-        }
-        break;
-      }
+    auto wait = [&](bool go, int stage, uint32_t phase) {
+      return __all_sync(0xffffffffu, go && ptx::mbar_wait(&full_bar[stage], phase, c.err, 0x7000 | stage)) != 0;
+    };
+    for (int n = 0; n < mine && ring.arrive(n, mine, wait); ++n) {
+      const int stage = ring.stage, tb = k0 + 32 * (warp + ROWS_WARPS * n);
       const uint8_t* tile = smem + warp * Smem::WARP + stage * Smem::STAGE;
       const float4 sv = *reinterpret_cast<const float4*>(&scales[2 * stage]);   // key and value scale of either half
       // ---- scores, one chain of products per half and 64 features
@@ -431,8 +424,7 @@ __global__ void __launch_bounds__(ROWS_WARPS * 32, rows_ctas(NT)) block_attn_row
         }
       }
       __syncwarp();                                // every lane has read the stage
-      request(n + STAGES, stage);
-      if (++stage == STAGES) { stage = 0; phase ^= 1; }
+      ring.leave(n, request);
     }
 
     // ---- join the warps of the CTA; a warp's partial O takes the place of its ring (every copy it asked for has been waited for)
@@ -452,7 +444,7 @@ __global__ void __launch_bounds__(ROWS_WARPS * 32, rows_ctas(NT)) block_attn_row
       }
     }
     if (lane == 0) refs[warp] = vref;
-    __syncthreads();
+    const bool complete = __syncthreads_and(ring.ok);     // (a warp whose copies did not arrive, which is reported, has summed some keys only)
     const long long group_end = at.first + at.units;
     const bool head = at.unit == at.first, tail = group_end <= at.end, whole = head && tail;   // the group begins / ends in this share
     const long long slot = 2ll * blockIdx.x + (head ? 1 : 0);            // of a partial result: the group goes on / came in
@@ -476,10 +468,11 @@ __global__ void __launch_bounds__(ROWS_WARPS * 32, rows_ctas(NT)) block_attn_row
       const float inv = lt != 0.f ? 1.0f / lt : 0.f, inv_ref = ref > 0.f ? 1.0f / ref : 0.f;
 #pragma unroll
       for (int w = 0; w < ROWS_WARPS; ++w) sm[w * R + row] = e[w] * inv * (refs[w] * inv_ref);
-      if (!whole && at.qt * R + row < at.total) p.part_ml[slot * R + row] = make_float2(mt, lt);
+      // (a part that is not complete makes its rows NaN, a group that is not leaves them as they were)
+      if (!whole && at.qt * R + row < at.total) p.part_ml[slot * R + row] = complete ? make_float2(mt, lt) : make_float2(NAN, NAN);
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < R * DH; i += ROWS_WARPS * 32) {
+    for (int i = complete ? threadIdx.x : R * DH; i < R * DH; i += ROWS_WARPS * 32) {
       const int row = i / DH, place = i % DH, rr = at.qt * R + row;
       if (rr >= at.total) break;                 // (rows ascend with i)
       float y = 0.f;
