@@ -469,7 +469,7 @@ __global__ void __launch_bounds__(ROWS_WARPS * 32, rows_ctas(NT)) block_attn_row
 #pragma unroll
       for (int w = 0; w < ROWS_WARPS; ++w) sm[w * R + row] = e[w] * inv * (refs[w] * inv_ref);
       // (a part that is not complete makes its rows NaN, a group that is not leaves them as they were)
-      if (!whole && at.qt * R + row < at.total) p.part_ml[slot * R + row] = complete ? make_float2(mt, lt) : make_float2(NAN, NAN);
+      if (!whole && at.qt * R + row < at.total) p.part_ml[slot * R + row] = make_float2(part_maximum(complete, lt != 0.f, mt), lt);
     }
     __syncthreads();
     for (int i = complete ? threadIdx.x : R * DH; i < R * DH; i += ROWS_WARPS * 32) {

@@ -21,6 +21,7 @@
 // FP16 by a power of two.  No maximum is taken per tile: P is formed with the maximum so far, and only if 16 probabilities
 // sum to more than FP16 holds (or in the first half) is the half read again for its maximum, O rescaled in tensor memory.
 #include "block_attention.cuh"
+#include "block_ring.cuh"
 #include <cmath>
 #include <type_traits>
 
@@ -321,7 +322,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
     }
     const long long own = (long long)blockIdx.x * PR_ROWS + 128 * t + r;   // the row's place among the parts
     const bool seen = n > 0 && l != 0.f;
-    if (p.splits > 1 && row_ok && ok) p.part_ml[own] = make_float2(seen ? -u : -INFINITY, l);
+    if (p.splits > 1 && row_ok) p.part_ml[own] = make_float2(part_maximum(ok, seen, -u), l);
 #pragma unroll
     for (int k = 0; k < DH / 32; ++k) {
       uint32_t x[32];

@@ -1,6 +1,7 @@
-// The order of a warp's copies through its ring of shared-memory stages, apart from what moves and what is computed, so that it can be
-// compiled for the host too and followed there through waits that run out.
+// The order of a warp's copies through its ring of shared-memory stages, and what becomes of a part of a row's keys, apart from what moves and
+// what is computed, so that both can be compiled for the host too and followed there through waits that run out.
 #pragma once
+#include <cmath>
 
 #if defined(__CUDACC__)
 #define HERO_RING_FN __host__ __device__ __forceinline__
@@ -51,5 +52,9 @@ struct CopyRing {
     advance();
   }
 };
+
+// What a part of a row's keys tells the join beside its sum: its maximum; minus infinity where the row saw none of them; NaN, which makes the
+// row NaN, where copies or products did not arrive, so that what the workspace happened to hold is never taken for a result.
+HERO_RING_FN float part_maximum(bool complete, bool seen, float maximum) { return complete ? (seen ? maximum : -INFINITY) : NAN; }
 
 }  // namespace hero

@@ -33,6 +33,10 @@ template <int STAGES> static void go(int fail, int groups, char** steps) {
   }
 }
 int main(int argc, char** argv) {
+  if (argc == 1) {
+    for (int i = 0; i < 4; ++i) printf("%g\n", hero::part_maximum(i & 1, i & 2, -3.5f));
+    return 0;
+  }
   if (atoi(argv[1]) == 2) go<2>(atoi(argv[2]), argc - 3, argv + 3);
   else go<4>(atoi(argv[2]), argc - 3, argv + 3);
 }
@@ -47,7 +51,9 @@ def ring(tmp_path_factory):
     assert compiler, "a C++ compiler is needed"
     subprocess.run([compiler, "-std=c++17", "-Wall", "-Werror", "-I", B.CSRC, "-o", str(d / "ring"), str(d / "ring.cpp")], check=True)
 
-    def run(stages, fail, groups):
+    def run(stages=None, fail=None, groups=()):
+        if stages is None:
+            return subprocess.run([str(d / "ring")], check=True, capture_output=True, text=True).stdout.split()
         out = subprocess.run([str(d / "ring"), str(stages), str(fail), *map(str, groups)], check=True, capture_output=True, text=True).stdout
         return [(w[0], *map(int, w[1:])) for w in (line.split() for line in out.splitlines())]
     return run
@@ -80,3 +86,9 @@ def test_every_copy_is_waited_for_and_nothing_follows_a_wait_that_ran_out(ring, 
                 assert not pending and rest == [0 if dead else 1]
         want = [(g, n) for g, steps in enumerate(groups) for n in range(steps)]
         assert stepped == (want if fail < 0 else want[:fail])
+
+
+def test_a_part_that_is_not_complete_makes_its_row_nan_whatever_the_workspace_held(ring):
+    # (complete, seen) = (0, 0), (1, 0), (0, 1), (1, 1)
+    parts = [float(x) for x in ring()]
+    assert parts[0] != parts[0] and parts[2] != parts[2] and parts[1] == -float("inf") and parts[3] == -3.5
