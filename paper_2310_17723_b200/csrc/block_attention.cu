@@ -210,7 +210,7 @@ __global__ void __launch_bounds__(ROWS_WARPS * 32, rows_ctas(NT)) block_attn_row
       if (tok < k1) {
         my_id = page_for_read(c, b, tok >> c.page_shift);
         const long long sc = (long long)my_id * c.nkv + hk;
-        my_scales = make_float2(__ldg(c.ks + sc), __ldg(c.vs + sc));
+        my_scales = make_float2(written(c.ks + sc), written(c.vs + sc));
       }
     };
     const uint32_t ring_a = ptx::smem_u32(smem + warp * Smem::WARP);
@@ -247,7 +247,7 @@ __global__ void __launch_bounds__(ROWS_WARPS * 32, rows_ctas(NT)) block_attn_row
       uint32_t raw[KC * 8], top = 0;
 #pragma unroll
       for (int k = 0; k < KC; ++k) {
-        const uint4 x = __ldg(reinterpret_cast<const uint4*>(q + 64 * k)), y = __ldg(reinterpret_cast<const uint4*>(q + 64 * k + 8));
+        const uint4 x = written(reinterpret_cast<const uint4*>(q + 64 * k)), y = written(reinterpret_cast<const uint4*>(q + 64 * k + 8));
         raw[8 * k] = x.x; raw[8 * k + 1] = x.y; raw[8 * k + 2] = x.z; raw[8 * k + 3] = x.w;
         raw[8 * k + 4] = y.x; raw[8 * k + 5] = y.y; raw[8 * k + 6] = y.z; raw[8 * k + 7] = y.w;
       }
@@ -547,12 +547,12 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) block_attn_join_kernel(const 
       const int q = min(q0 + k * JOIN_WARPS, rec.parts - 1);
       // the first part lies in the second slot of its CTA, the others in the first slots of the CTAs behind it
       const long long at = (2ll * (rec.share + q) + (q == 0 ? 1 : 0)) * R + row;
-      ml[k] = __ldg(p.part_ml + at);
+      ml[k] = written(p.part_ml + at);
       if constexpr (E == 4) {
-        const float4 v = __ldg(reinterpret_cast<const float4*>(p.part_o + at * DH) + lane);
+        const float4 v = written(reinterpret_cast<const float4*>(p.part_o + at * DH) + lane);
         x[k][0] = v.x; x[k][1] = v.y; x[k][2] = v.z; x[k][3] = v.w;
       } else {
-        const float2 v = __ldg(reinterpret_cast<const float2*>(p.part_o + at * DH) + lane);
+        const float2 v = written(reinterpret_cast<const float2*>(p.part_o + at * DH) + lane);
         x[k][0] = v.x; x[k][1] = v.y;
       }
     }

@@ -135,7 +135,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
       const uint4* q = reinterpret_cast<const uint4*>(p.q + row_g * p.ld_q + (long long)hq * DH);
 #pragma unroll
       for (int i = 0; i < DH / 8; ++i) {
-        const uint4 x = row_ok ? __ldg(q + i) : make_uint4(0, 0, 0, 0);
+        const uint4 x = row_ok ? written(q + i) : make_uint4(0, 0, 0, 0);
         w[4 * i] = x.x; w[4 * i + 1] = x.y; w[4 * i + 2] = x.z; w[4 * i + 3] = x.w;
       }
 #pragma unroll
@@ -394,14 +394,14 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
-          for (int h = 0; h < NSUB; ++h) raw[i * NSUB + h] = __ldg(reinterpret_cast<const uint4*>(pool + at[i] + 64 * h));
+          for (int h = 0; h < NSUB; ++h) raw[i * NSUB + h] = written(reinterpret_cast<const uint4*>(pool + at[i] + 64 * h));
       } else {
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
           for (int h = 0; h < NSUB; ++h) {
             raw[i * NSUB + h] = make_uint4(0, 0, 0, 0);        // slots behind the end may hold anything (e4m3: NaN)
-            if (key0 + j * PR_KEYS + r0 + 64 * i < L) raw[i * NSUB + h] = __ldg(reinterpret_cast<const uint4*>(pool + at[i] + 64 * h));
+            if (key0 + j * PR_KEYS + r0 + 64 * i < L) raw[i * NSUB + h] = written(reinterpret_cast<const uint4*>(pool + at[i] + 64 * h));
           }
       }
     };
@@ -449,7 +449,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
       const int tok = key0 + j * PR_KEYS + 16 * lane;
       return lane < 8 && tok < L ? page_for_read(c, b, tok >> c.page_shift) : -1;
     };
-    auto scales = [&](int i) { return i >= 0 ? make_float2(__ldg(c.ks + (long long)i * c.nkv + hk), __ldg(c.vs + (long long)i * c.nkv + hk)) : make_float2(0.f, 0.f); };
+    auto scales = [&](int i) { return i >= 0 ? make_float2(written(c.ks + (long long)i * c.nkv + hk), written(c.vs + (long long)i * c.nkv + hk)) : make_float2(0.f, 0.f); };
     int ids_next = page_of(1);
     float2 sc = scales(page_of(0));
     float vref = 0.f;
@@ -566,14 +566,14 @@ __global__ void __launch_bounds__(PJ_WARPS * 32) block_attn_prompt_join_kernel(c
     for (int i = 0; i < PJ_EACH; ++i) {
       if (qt * PR_ROWS + row0 + i >= total) continue;              // rows that are not there were not written
       const long long at = ((long long)blockIdx.x * p.splits + q) * PR_ROWS + row0 + i;
-      const float2 ml = __ldcg(p.part_ml + at);
+      const float2 ml = written(p.part_ml + at);
       if (ml.x == -INFINITY) continue;                             // nor were sums of no keys
       // (a part is divided by its own sum: their mean, under weights that add up to one)
       const float now = fmaxf(m[i], ml.x), old = l[i] * ex2(m[i] - now), w = ex2(ml.x - now) * ml.y, inv = 1.0f / (old + w);
       m[i] = now;
       l[i] = old + w;
 #pragma unroll
-      for (int e = 0; e < E; ++e) y[i][e] = fmaf(y[i][e], old * inv, w * inv * __ldcg(p.part_o + at * DH + 32 * e + lane));
+      for (int e = 0; e < E; ++e) y[i][e] = fmaf(y[i][e], old * inv, w * inv * written(p.part_o + at * DH + 32 * e + lane));
     }
   }
 #pragma unroll

@@ -69,7 +69,7 @@ __global__ void __launch_bounds__(APP_THREADS) block_append_kernel(const __grid_
   const int begin = s.len - s.n, first = max(begin, 0);      // first new token (rows before token 0 store nothing)
   const int pi = (first >> c.page_shift) + blockIdx.x, p0 = pi << c.page_shift;
   if (s.n <= 0 || p0 >= s.len) return;
-  const int id = __ldg(c.table + (long long)b * c.ld_table + pi);
+  const int id = written(c.table + (long long)b * c.ld_table + pi);
   const int lo = max(first - p0, 0), hi = min(s.len - p0, c.page);   // the page's slots that receive new tokens
   const long long ld_x = is_v ? p.ld_v : p.ld_k;
   const uint16_t* src = (is_v ? p.v : p.k) + (s.r0 + (p0 - begin)) * ld_x + (long long)head * DH;   // row of slot 0
@@ -82,7 +82,7 @@ __global__ void __launch_bounds__(APP_THREADS) block_append_kernel(const __grid_
   for (int i = 0; i < NP; ++i) {
     const int t = i * TPP + tg;
     raw[i] = make_uint4(0, 0, 0, 0);
-    if (t >= lo && t < hi) raw[i] = __ldg(reinterpret_cast<const uint4*>(src + (long long)t * ld_x + sub * 8));
+    if (t >= lo && t < hi) raw[i] = written(reinterpret_cast<const uint4*>(src + (long long)t * ld_x + sub * 8));
   }
   if ((unsigned)id >= (unsigned)c.n_pages) {
     if (threadIdx.x == 0) atomicExch(c.err, ERR_BAD_PAGE);
@@ -139,7 +139,7 @@ __global__ void __launch_bounds__(APP_THREADS) block_append_kernel(const __grid_
       const int t = i * TPP + tg;
       if (t >= lo && t < hi) {
         // (reads the row again: indexing the registers here would put them all into memory)
-        const uint4 x = __ldg(reinterpret_cast<const uint4*>(src + (long long)t * ld_x + sub * 8));
+        const uint4 x = written(reinterpret_cast<const uint4*>(src + (long long)t * ld_x + sub * 8));
         const uint32_t w[4] = {x.x, x.y, x.z, x.w};
         float y[8];
 #pragma unroll
@@ -214,15 +214,15 @@ __global__ void __launch_bounds__(READ_THREADS, 4) block_read_kernel(const __gri
     for (int j = 0; j < READ_TOKENS; ++j) {
       const int i = i0 + tok + j * p.tpp, t = s.len - s.n + i;             // row of the sequence, its token
       const int pi = min(max(t, 0), c.max_len - 1) >> c.page_shift;
-      const int n = __ldg(table + pi);
+      const int n = written(table + pi);
       id[j] = min(max(n, 0), c.n_pages - 1);
       bad |= id[j] != n && i < s.n && t >= 0;
     }
 #pragma unroll
     for (int j = 0; j < READ_TOKENS; ++j) {
       const int i = i0 + tok + j * p.tpp, t = s.len - s.n + i;
-      code[j] = __ldg(reinterpret_cast<const uint4*>(from + (long long)id[j] * c.page_stride + (long long)(t & (c.page - 1)) * c.ld));
-      sc[j] = __ldg(scales + (long long)id[j] * c.nkv + head);
+      code[j] = written(reinterpret_cast<const uint4*>(from + (long long)id[j] * c.page_stride + (long long)(t & (c.page - 1)) * c.ld));
+      sc[j] = written(scales + (long long)id[j] * c.nkv + head);
       if (i >= s.n || t < 0) { code[j] = make_uint4(0, 0, 0, 0); sc[j] = 0.f; }  // a row without a token
     }
     if (bad) atomicExch(c.err, ERR_BAD_PAGE);

@@ -28,18 +28,24 @@ struct BlockView {
 // checks shared by every entry point of the cache; `rows` / `max_rows` describe the call's matrices
 hero_status block_view(hero_handle* h, const hero_block_cache* c, const int32_t* row_start, int64_t rows, int32_t max_rows, BlockView* out);
 
+// A load of what an earlier call of the stream may have written: codes, scales, tables, lengths, rows, partial results.  These kernels may be
+// resident while the one before them still runs, so such data is not read-only for their whole life, which a non-coherent load
+// (__ldg) takes for granted: it may be moved ahead of the wait for that kernel.
+template <typename T>
+__device__ __forceinline__ T written(const T* p) { return *p; }
+
 struct SeqRows {
   int len, n;                   // tokens held, rows of the call
   long long r0;                 // first row
 };
 __device__ __forceinline__ SeqRows seq_rows(const BlockView& v, int b) {
   SeqRows s;
-  s.len = min(max(__ldg(v.len + b), 0), v.max_len);
+  s.len = min(max(written(v.len + b), 0), v.max_len);
   if (v.row_start == nullptr) {
     s.r0 = b; s.n = 1;
     return s;
   }
-  long long r0 = __ldg(v.row_start + b), r1 = __ldg(v.row_start + b + 1);
+  long long r0 = written(v.row_start + b), r1 = written(v.row_start + b + 1);
   if (r0 < 0 || r1 < r0 || r1 > v.rows || r1 - r0 > v.max_rows) {
     atomicExch(v.err, ERR_BAD_ROWS);
     r0 = min(max(r0, 0ll), v.rows);
@@ -51,7 +57,7 @@ __device__ __forceinline__ SeqRows seq_rows(const BlockView& v, int b) {
 }
 // page id of the sequence's page `pi`, clamped into the pool (and reported) for reading
 __device__ __forceinline__ int page_for_read(const BlockView& v, int b, int pi) {
-  int id = __ldg(v.table + (long long)b * v.ld_table + pi);
+  int id = written(v.table + (long long)b * v.ld_table + pi);
   if ((unsigned)id >= (unsigned)v.n_pages) {
     atomicExch(v.err, ERR_BAD_PAGE);
     id = id < 0 ? 0 : v.n_pages - 1;

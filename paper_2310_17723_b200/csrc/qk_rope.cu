@@ -33,7 +33,7 @@ __global__ void __launch_bounds__(ROPE_MAX_WARPS * 32, 4) qk_rope_kernel(const _
   const long long row = blockIdx.x;
   const int per_row = p.chunks[0] + p.chunks[1], warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = lane % LPH, f0 = sub * 8;
   const bool live = f0 < p.dh;
-  const long long t0 = p.rot > 0 ? __ldg(p.pos + row) : 0;
+  const long long t0 = p.rot > 0 ? written(p.pos + row) : 0;
   uint4 raw[ROPE_ITERS];
   int side = 0, first = 0, heads = 0;
   auto request = [&](int unit) {
