@@ -544,8 +544,8 @@ hero_status hero_block_cache_read(hero_handle* h, const hero_block_cache* c, con
  *   out : [rows][nq*dh] F16 / BF16, or I8 / F8 with gran FWQ (scale[nq*dh]) or SQ (scale[1]): the quantised input of the
  *         attention-output linear (clip(Round(o / s)); for F8 the saturating conversion of o / s)
  *   scale : factor of the scores; 0 selects 1 / sqrt(dh)
- *   workspace : device scratch of hero_block_attention_workspace_bytes() for the same cache, heads and max_rows (a smaller max_rows may
- *         need more), 16-byte aligned, for the partial results of sequences split over several CTAs; it needs no clearing and holds
+ *   workspace : device scratch of hero_block_attention_workspace_bytes() for the same cache and heads and this or a larger max_rows,
+ *         16-byte aligned, for the partial results of sequences split over several CTAs; it needs no clearing and holds
  *         nothing between calls.  Calls that may overlap on the GPU (two
  *         streams, two graphs) need a workspace each.
  * Arithmetic: codes and queries enter the products exactly (a query row is scaled by a power of two into FP16), scores,

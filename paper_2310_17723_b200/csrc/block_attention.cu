@@ -676,8 +676,20 @@ extern "C" hero_status hero_block_attention_workspace_bytes(hero_handle* h, cons
   HERO_REQUIRE(cc->B >= 0 && cc->max_len >= 1 && (cc->dh == 64 || cc->dh == 128), HERO_ERR_UNSUPPORTED, "B=%d max_len=%d dh=%d", cc->B, cc->max_len, cc->dh);
   if (cc->B == 0) return HERO_OK;
   RowsPlan plan;
-  if ((st = plan_rows(h, cc, nq, max_rows, &plan)) == HERO_OK) *bytes = plan.bytes;
-  return st;
+  if ((st = plan_rows(h, cc, nq, max_rows, &plan)) != HERO_OK) return st;
+  // a call with a smaller row bound may be dealt out differently and need more: the answer serves it too
+  size_t most = plan.bytes;
+  for (int m = 1; m < max_rows && (long long)m * (nq / cc->nkv) <= 32; ++m) {
+    RowsPlan fewer;
+    if ((st = plan_rows(h, cc, nq, m, &fewer)) != HERO_OK) return st;
+    most = fewer.bytes > most ? fewer.bytes : most;
+  }
+  if (plan.prompt) {
+    const size_t fewer = prompt_workspace_most(h, cc, nq, max_rows);
+    most = fewer > most ? fewer : most;
+  }
+  *bytes = most;
+  return HERO_OK;
 }
 
 extern "C" hero_status hero_block_attention(hero_handle* h, const hero_block_cache* cc, const hero_block_attn_args* a, void* stream) {

@@ -65,6 +65,7 @@ __device__ __forceinline__ void codes4_to_f16(uint32_t w, uint32_t& lo, uint32_t
 
 // many rows per key / value head (block_attention_prompt.cu)
 hero_status prompt_workspace_bytes(const hero_handle* h, const hero_block_cache* cc, int nq, int max_rows, size_t* bytes);
+size_t prompt_workspace_most(const hero_handle* h, const hero_block_cache* cc, int nq, int max_rows);
 hero_status launch_prompt(hero_handle* h, const hero_block_cache* cc, const BlockAttnParams& p, bool bf, void* workspace, cudaStream_t stream);
 
 }  // namespace hero

@@ -589,16 +589,21 @@ __global__ void __launch_bounds__(PJ_WARPS * 32) block_attn_prompt_join_kernel(c
 // 592 -> 104 us for 64 rows of one sequence on 32768 tokens (heads 32 / 8 of 128; 8 groups, 18 parts), 605 -> 329 for 512 rows (64 groups, 2
 // parts), 66 -> 52 for 4 x 128 rows on 4096 tokens (64 groups of 64 features).
 struct PromptPlan { long long tiles, groups; int splits; size_t bytes; };
-static hero_status plan_prompt(const hero_handle* h, const hero_block_cache* cc, int nq, int max_rows, PromptPlan* out) {
+static PromptPlan plan_tiles(const hero_handle* h, const hero_block_cache* cc, long long tiles) {
   PromptPlan r;
-  r.tiles = ((long long)max_rows * (nq / cc->nkv) + PR_ROWS - 1) / PR_ROWS;
+  r.tiles = tiles;
   r.groups = r.tiles * cc->nkv * cc->B;
-  HERO_REQUIRE(r.groups < (1ll << 31), HERO_ERR_UNSUPPORTED, "max_rows=%d nkv=%d B=%d: too many", max_rows, cc->nkv, cc->B);
   const long long fit = h->sm_count / r.groups, steps = ((long long)cc->max_len + PR_KEYS - 1) / PR_KEYS, useful = steps / PR_PART;
   const long long splits = fit < useful ? fit : useful;
   r.splits = splits > 1 ? (int)splits : 1;
   r.bytes = r.splits > 1 ? (size_t)r.groups * r.splits * PR_ROWS * (cc->dh * 4 + 8) : 0;
-  *out = r;
+  return r;
+}
+static long long tiles_of(const hero_block_cache* cc, int nq, int max_rows) { return ((long long)max_rows * (nq / cc->nkv) + PR_ROWS - 1) / PR_ROWS; }
+static hero_status plan_prompt(const hero_handle* h, const hero_block_cache* cc, int nq, int max_rows, PromptPlan* out) {
+  const long long groups = tiles_of(cc, nq, max_rows) * cc->nkv * cc->B;
+  HERO_REQUIRE(groups < (1ll << 31), HERO_ERR_UNSUPPORTED, "max_rows=%d nkv=%d B=%d: too many", max_rows, cc->nkv, cc->B);
+  *out = plan_tiles(h, cc, tiles_of(cc, nq, max_rows));
   return HERO_OK;
 }
 hero_status prompt_workspace_bytes(const hero_handle* h, const hero_block_cache* cc, int nq, int max_rows, size_t* bytes) {
@@ -606,6 +611,16 @@ hero_status prompt_workspace_bytes(const hero_handle* h, const hero_block_cache*
   hero_status st = plan_prompt(h, cc, nq, max_rows, &plan);
   if (st == HERO_OK) *bytes = plan.bytes;
   return st;
+}
+// the most that any row bound up to max_rows needs here (keys are split up to half the SMs' groups only, so there are few to look at)
+size_t prompt_workspace_most(const hero_handle* h, const hero_block_cache* cc, int nq, int max_rows) {
+  const long long last = tiles_of(cc, nq, max_rows), split = h->sm_count / 2 / ((long long)cc->nkv * cc->B);
+  size_t most = 0;
+  for (long long t = 1; t <= last && t <= split; ++t) {
+    const size_t bytes = plan_tiles(h, cc, t).bytes;
+    most = bytes > most ? bytes : most;
+  }
+  return most;
 }
 
 template <int DH>

@@ -418,6 +418,7 @@ class Handle:
         _check(self._lib.hero_block_cache_read(self._h, C.byref(cache), C.byref(a), self._raw_stream(stream)))
 
     def hero_block_attention_workspace_bytes(self, cache, nq, rows, max_rows=1):
+        """Bytes that serve every call on this cache with these heads and at most max_rows rows a sequence."""
         n = C.c_size_t()
         _check(self._lib.hero_block_attention_workspace_bytes(self._h, C.byref(cache), nq, rows, max_rows, C.byref(n)))
         return int(n.value)
