@@ -43,6 +43,12 @@ constexpr float PR_COARSE = 524288.0f;                         // 2^19: maxima u
 constexpr float PR_MIN_RV = 9.094947e-13f;                     // 2^-40
 
 
+__device__ __forceinline__ float min_or_nan(float a, float b) {
+  float y;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+  return y;
+}
+
 template <int DH>
 struct PromptCfg {
   static constexpr int SUB = 128 * 128;                        // one [128 rows x 64 features] FP16 sub-tile, 128-byte rows
@@ -258,14 +264,13 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
           const float slack = fabsf(u) > PR_COARSE ? fabsf(u) * 0x1p-20f : 0.f;
           if (__any_sync(0xffffffffu, first || mx > PR_HIGH + slack) || turn) {
             float d = mx - PR_SHIFT;
-            if (!first) d = slack == 0.f ? fmaxf(d, 0.f) : mx > PR_HIGH + slack ? d : 0.f;
+            if (!first) d = fmaxf(d, 0.f);
             if (mx == -INFINITY) d = 0.f;
-            const float from = u;
-            u -= d;
-            if (d != 0.f && fabsf(u) > PR_COARSE) {
-              u = fmaf(fabsf(u), 0x1p-21f, u);
-              d = from - u;
+            if (fabsf(u - d) > PR_COARSE) {
+              if (!first && slack != 0.f && mx <= PR_HIGH + slack) d = 0.f;
+              if (d != 0.f) d = u - fmaf(fabsf(u - d), 0x1p-21f, u - d);
             }
+            u -= d;
             if (!first) {
               ok = __all_sync(0xffffffffu, ok && ptx::mbar_wait(&o_full[t], (h + 1) & 1, c.err, 0x8180 | t));   // the previous half's P V
               ptx::tc_fence_after();
@@ -296,8 +301,8 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
             for (int i = 0; i < 8; ++i) {
               const int key = 16 * g + 2 * i;
               const float x0 = fmaf(__uint_as_float(z[2 * i]), fk, ug), x1 = fmaf(__uint_as_float(z[2 * i + 1]), fk, ug);
-              const float e0 = key < valid ? ex2(x0 > PR_HIGH ? PR_HIGH : x0) : 0.f;
-              const float e1 = key + 1 < valid ? ex2(x1 > PR_HIGH ? PR_HIGH : x1) : 0.f;
+              const float e0 = key < valid ? ex2(min_or_nan(x0, PR_HIGH)) : 0.f;
+              const float e1 = key + 1 < valid ? ex2(min_or_nan(x1, PR_HIGH)) : 0.f;
               sum.x += e0; sum.y += e1;
               w[i] = pack_f16(e0, e1);
             }
@@ -314,11 +319,12 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
     // ---- output, or the part's sums
     // (O is divided by the row's sum before the value scale enters: near the ends of BF16's range neither O times the scale nor the scale
     // over the sum is a number that FP32 holds)
-    float inv_l = 0.f;
+    float scale_o = 0.f;
+    const bool tiny = vref < 0x1p-60f;
     if (n > 0) {
       ok = __all_sync(0xffffffffu, ok && ptx::mbar_wait(&o_last[t], 0, c.err, 0x8200 | t));
       ptx::tc_fence_after();
-      inv_l = l != 0.f ? 1.0f / l : 0.f;
+      scale_o = l != 0.f ? (tiny ? 1.0f : vref) / l : 0.f;
     }
     const long long own = (long long)blockIdx.x * PR_ROWS + 128 * t + r;   // the row's place among the parts
     const bool seen = n > 0 && l != 0.f;
@@ -332,7 +338,11 @@ __global__ void __launch_bounds__(PR_THREADS, 1) block_attn_prompt_kernel(const 
       }
       float y[32];
 #pragma unroll
-      for (int i = 0; i < 32; ++i) y[i] = seen ? __uint_as_float(x[i]) * inv_l * vref : 0.f;
+      for (int i = 0; i < 32; ++i) y[i] = seen ? __uint_as_float(x[i]) * scale_o : 0.f;
+      if (tiny) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) y[i] *= vref;
+      }
       if (p.splits > 1) {
         if (seen && row_ok && ok) {
           float4* dst = reinterpret_cast<float4*>(p.part_o + own * DH + 32 * k);
