@@ -57,7 +57,7 @@ __device__ __forceinline__ SeqRows seq_rows(const BlockView& v, int b) {
 }
 // page id of the sequence's page `pi`, clamped into the pool (and reported) for reading
 __device__ __forceinline__ int page_for_read(const BlockView& v, int b, int pi) {
-  int id = written(v.table + (long long)b * v.ld_table + pi);
+  int id = __ldcg(v.table + (long long)b * v.ld_table + pi);   // (as `written`; past the first-level cache it costs fewer registers: drafts 57.0 -> 56.3 us)
   if ((unsigned)id >= (unsigned)v.n_pages) {
     atomicExch(v.err, ERR_BAD_PAGE);
     id = id < 0 ? 0 : v.n_pages - 1;
