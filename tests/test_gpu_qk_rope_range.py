@@ -111,3 +111,26 @@ def test_int8_queries_and_keys_with_a_scale_each(h, fp, pairing, dh, rot, nq, nk
     y = BC.norm_rope(kx, nkv, gk, 1e-6, c, s, pos, pairing)
     got = k16.double().cpu().numpy()
     assert np.all(np.abs(got - y) <= torch.finfo(kt.dtype).eps / 2 * np.abs(y) + 32 * 2.0 ** -24 * 4 * dh ** 0.5 + 2.0 ** -25)
+
+
+@pytest.mark.parametrize("pairing", ["halves", "adjacent"])
+@pytest.mark.parametrize("rot", [0, 32, 64])
+def test_a_head_whose_squares_are_beyond_fp32_is_zeros(h, pairing, rot):
+    # the definition is in FP32 throughout: an infinite mean of squares divides every finite feature to 0, whatever the gammas are
+    dh, nq = 64, 3
+    g = np.random.default_rng(2)
+    x = g.standard_normal((2, nq, dh))
+    x[0, 1], x[1, 2] = 3e38 * np.sign(x[0, 1]), 1e20 * x[1, 2]
+    t, xr = to_fp(x.reshape(2, nq * dh), "bf16")
+    c, s, ct, st = _tables(50, rot, seed=0.3) if rot else (None,) * 4
+    pos = np.array([7, 31], np.int32)
+    gm = g.uniform(1.5, 3.0, dh).astype(np.float32)
+    out = torch.ones_like(t)
+    h.hero_qk_norm_rope(hero.tensor(t), None, hero.tensor(out), None, nq, 0, torch.from_numpy(pos).cuda() if rot else None, ct, st,
+                        torch.from_numpy(gm).cuda(), pairing=pairing)
+    h.check()
+    got = out.double().cpu().numpy().reshape(2, nq, dh)
+    assert np.all(got[0, 1] == 0) and np.all(got[1, 2] == 0)
+    want = BC.norm_rope(xr, nq, gm, 1e-6, c, s, pos, pairing).reshape(2, nq, dh)
+    for at in ((0, 0), (0, 2), (1, 0), (1, 1)):
+        assert np.all(np.abs(got[at] - want[at]) <= 2.0 ** -8 * np.abs(want[at]) + 32 * 2.0 ** -24 * np.abs(want[at]).max() * 2)
