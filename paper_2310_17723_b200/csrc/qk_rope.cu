@@ -97,7 +97,7 @@ __global__ void __launch_bounds__(ROPE_MAX_WARPS * 32, 4) qk_rope_kernel(const _
     for (int i = 0; i < ROPE_ITERS; ++i) {
       if (first + i * HPI >= heads) break;       // (uniform)
       const int hd = first + lane / LPH + i * HPI;
-      uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+      const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
       float2 x[4], y[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) x[e] = fp16ish_to_f32x2<BF>(w[e]);
@@ -110,18 +110,10 @@ __global__ void __launch_bounds__(ROPE_MAX_WARPS * 32, 4) qk_rope_kernel(const _
 #pragma unroll
         for (int k = LPH / 2; k > 0; k >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, k);
         r = rsqrtf(fmaf(sum, p.inv_dh, p.eps));
-        if (r == 0.f) {
-          // squares beyond FP32: x over an infinite root is 0, and NaN for an infinite x, before a factor can make it infinite
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            constexpr uint32_t INF = BF ? 0x7f80u : 0x7c00u;
-            w[e] = ((w[e] & 0x7fffu) >= INF ? 0x7fffu : 0u) | ((w[e] >> 16 & 0x7fffu) >= INF ? 0x7fff0000u : 0u);
-            x[e] = fp16ish_to_f32x2<BF>(w[e]);
-          }
-        }
       }
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
+        x[e] = __fmul2_rn(x[e], make_float2(r, r));              // first: a norm factor of 0 (squares beyond FP32) meets no infinite product
         y[e] = __fmul2_rn(x[e], o[e]);
         // (what does not turn has no partner: a factor of zero would let an infinite or NaN neighbour in)
         if constexpr (ADJ) {
@@ -131,9 +123,8 @@ __global__ void __launch_bounds__(ROPE_MAX_WARPS * 32, 4) qk_rope_kernel(const _
           }
         } else {
           const uint32_t partner = __shfl_sync(0xffffffffu, w[e], mate_lane);
-          if (turned) y[e] = __ffma2_rn(fp16ish_to_f32x2<BF>(partner), m[e], y[e]);
+          if (turned) y[e] = __ffma2_rn(__fmul2_rn(fp16ish_to_f32x2<BF>(partner), make_float2(r, r)), m[e], y[e]);
         }
-        y[e] = __fmul2_rn(y[e], make_float2(r, r));
       }
       if (live && hd < heads) {
         const long long at = at0 + i * HPI * p.dh;
