@@ -130,12 +130,20 @@ __global__ void __launch_bounds__(ROPE_MAX_WARPS * 32, 4) qk_rope_kernel(const _
         const long long at = at0 + i * HPI * p.dh;
         if (to_i8) {
           const Divider div(i8_scale);
-          // (bounded before the division: a quotient beyond FP32, an infinity's too, would leave a remainder that is NaN)
-          const float most = 128.f * i8_scale;
-          auto code_of = [&](float x) { return div(fminf(fmaxf(x, -most), most)); };
+          // (bounded before the division: a quotient beyond FP32, an infinity's too, would leave a remainder that is NaN; and then the codes
+          // need no bound of their own)
+          const float most = 127.f * i8_scale;
+          float2 b[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) b[e] = make_float2(fminf(fmaxf(y[e].x, -most), most), fminf(fmaxf(y[e].y, -most), most));
           uint2 code;
-          code.x = f32_to_codes4<false>(code_of(y[0].x), code_of(y[0].y), code_of(y[1].x), code_of(y[1].y));
-          code.y = f32_to_codes4<false>(code_of(y[2].x), code_of(y[2].y), code_of(y[3].x), code_of(y[3].y));
+          if (div.fast) {
+            code.x = f32_to_codes4_inside<false>(div.pair(b[0]), div.pair(b[1]));
+            code.y = f32_to_codes4_inside<false>(div.pair(b[2]), div.pair(b[3]));
+          } else {
+            code.x = f32_to_codes4<false>(div(b[0].x), div(b[0].y), div(b[1].x), div(b[1].y));
+            code.y = f32_to_codes4<false>(div(b[2].x), div(b[2].y), div(b[3].x), div(b[3].y));
+          }
           *reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.y[side]) + at) = code;
         } else {
           *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.y[side]) + at) =
