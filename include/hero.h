@@ -548,8 +548,15 @@ hero_status hero_block_cache_read(hero_handle* h, const hero_block_cache* c, con
  *         16-byte aligned, for the partial results of sequences split over several CTAs; it needs no clearing and holds
  *         nothing between calls.  Calls that may overlap on the GPU (two
  *         streams, two graphs) need a workspace each.
- * Arithmetic: codes and queries enter the products exactly (a query row is scaled by a power of two into FP16), scores,
- * maxima, sums and outputs are FP32, probabilities are FP16 relative to the running maximum. */
+ * Arithmetic: codes enter the products exactly, a query feature within 2^-39 of its row's largest (a row is scaled by a power of
+ * two into FP16); scores, maxima, sums and outputs are FP32 (a score of size s is resolved to 2^-24 s); what meets the values is
+ * the probability times its page's value scale over the largest value scale of the sequence's tokens up to the call's end, rounded to FP16:
+ * half a step, 2^-11, and at most 2^-33 of the largest |v| that such a scale allows for each token, which is all that is left of pages whose
+ * value scales are so much smaller than the loudest page's.
+ * The kernel is chosen for the whole call: up to 32 rows per key / value head (max_rows * nq / nkv) one that is bound by
+ * the cache's bytes, above that one whose tiles hold 256 rows, in which a sequence with a single row costs a tile; there, keys are split over CTAs
+ * only where max_rows and B allow few tiles.  A batch of single tokens beside a piece of a prompt is better made two calls, each on its
+ * own rows of table and len: 31 tokens on 4096 and a piece of 512 (heads 32 / 8 of 128) take 259 us in one call, 135 in two. */
 typedef struct {
   hero_tensor q;
   hero_tensor out;
@@ -569,6 +576,8 @@ hero_status hero_block_attention(hero_handle* h, const hero_block_cache* c, cons
  *     y = x / sqrt(mean(x^2) + eps) * gamma            (no norm where the head's gamma is NULL: y = x)
  *     (y[a], y[b]) -> (y[a] cos - y[b] sin, y[b] cos + y[a] sin) for the rot / 2 pairs j, with cos[pos[i]][j], sin[pos[i]][j]
  *       HERO_PAIR_HALVES: a = j, b = j + rot / 2;  HERO_PAIR_ADJACENT: a = 2 j, b = 2 j + 1;  features >= rot pass through
+ *   Infinities and NaN reach the features that these formulas give them to and no others; a head whose squares sum beyond FP32 is
+ *   divided by infinity.  INT8 outputs saturate at the value's sign.
  *   q, k         : F16 / BF16 of one type, [rows][nq*dh] and [rows][nkv*dh]; k may be absent (nkv = 0)
  *   q_out, k_out : the same type, or I8 with gran SQ (clip(Round(y / scale[0])): the operands of hero_int8_attention).  An output
  *                  of the input's type may be its input (same pointer and ld); other overlaps are not allowed.

@@ -6,8 +6,9 @@
 namespace hero {
 
 // ------------------------------------------------------------------------------------------------------------------
-// Few rows per key / value head (decode steps, drafts).  Every cached byte is read once and meets at most 16 query rows, so
-// the kernel is bound by HBM and is built to keep loads in flight and the chains between them short.  Each warp walks steps of 32
+// Few rows per key / value head (decode steps, drafts).  Every cached byte is read once and meets at most 24 query rows (25 to 32 rows
+// are two tiles of 16, each of which reads it), so the kernel is built to keep loads in flight and the chains between them short;
+// up to 8 rows it is bound by HBM, with 24 by the latency of 8 warps per SM (issue slots 36 %, DRAM 37 %, tensor pipe 30 %).  Each warp walks steps of 32
 // tokens of its own (two halves of 16, each within a page) through a ring that bulk tensor copies fill: keys and values of a half are
 // one box each of a map over [pages][heads][tokens][features], swizzled so that the fragment loads below do not collide.
 // The operands need no transposition because a contraction's index may be permuted at will as long as both sides agree:
@@ -17,10 +18,13 @@ namespace hero {
 //       of M tile j stand for features (DH / 8) g + 2 j and + 1.  P^T is S^T's fragment, transposed by movmatrix.
 // Rows are the N dimension (8, the smallest there is), so a single query row does not pad a tile to 16.  Codes become FP16
 // exactly (INT8: byte permute into 1024 + u, subtract; e4m3: conversion instruction).  A query row is scaled by a power of two
-// into FP16 (exact for F16, for BF16 down to 2^-39 of the row's maximum).  The page's key scale multiplies the scores; the value
-// scale enters P relative to the largest one the warp has met (P is formed with a factor 2^11, so pages whose scale is 2^-25 of
-// the largest still meet FP16's normal range).  The running maximum moves only when a score exceeds it by more than 4 in
-// the exponent (P <= 2^15), so that most steps need no reduction over tokens.
+// into FP16: a feature is off by at most 2^-39 of the row's largest (and exact from 2^-31 of it on).  The page's key scale multiplies the
+// scores; the value scale enters P relative to the largest one the warp has met.  P is rounded to FP16, because the matrix instruction
+// takes 16 bits on both sides and FP16 has eight times BF16's precision: half a step, 2^-11, for each probability, 2.0e-4 ->
+// 2.9e-4 against 64 bits in F16 outputs (one token on 384), nothing in BF16 ones.  It is formed with a factor 2^11, so a probability times its
+// page's relative scale is in FP16's normal range down to 2^-25 and rounded by 2^-36 of the largest value scale below that.  The
+// running maximum moves only when a score exceeds it by more than 4 in the exponent (P <= 2^15), so that most steps need no
+// reduction over tokens.
 // Work is dealt out in units of one step of one (sequence, row tile, key / value head).  The lengths are on the device, so each CTA of
 // one full GPU takes an equal, consecutive share of all units, whatever the lengths are: ragged batches, a long document
 // and many short ones end at the same time.  A group of units cut by a share's end leaves partial results in the workspace (at
@@ -28,7 +32,8 @@ namespace hero {
 constexpr int ROWS_WARPS = 4;
 constexpr int rows_ctas(int nt) { return nt == 3 ? 2 : 3; }   // resident per SM (NT = 3: 255 registers a thread)
 // what a group costs beside its steps (page numbers and queries in, partial results joined and out), in steps; with too low a figure
-// the share that holds a batch's shortest sequences ends last (4 for all: 126 us, these: 54 us on ragged drafts for 16 sequences)
+// the share that holds a batch's shortest sequences ends last (4 for all: 116 us, these: 56 us on ragged drafts for 16 sequences; 45 and 39 on
+// ragged steps for 32)
 __host__ __device__ constexpr int rows_group_units(int nt) { return 8 + 5 * nt; }
 constexpr int ROWS_MIN_UNITS = 16;              // units of a share, at least
 constexpr int ROWS_KEPT = 256;                  // sequences whose lengths and rows a CTA keeps in shared memory while it walks its share
@@ -609,12 +614,16 @@ struct RowsPlan { int nt, tiles, ctas, records; bool direct, prompt, by_group; s
 static hero_status plan_rows(const hero_handle* h, const hero_block_cache* cc, int nq, int max_rows, RowsPlan* out) {
   const long long rows = (long long)max_rows * (nq / cc->nkv);
   RowsPlan r;
+  // Up to 32 rows per key / value head this kernel, more the one for many.  us for 16 sequences of 6000 tokens (heads 32 / 8 of 128) here and
+  // there: 24 rows 78 and 114, 32 rows 100 and 120, 36 rows 138 and 121, 64 rows 179 and 120; for 2 sequences of 32768: 32 rows 63 and 103,
+  // 36 rows 85 and 104, 64 rows 109 and 104; 16 x 16 heads of 64 on 6000: 32 rows 120 and 189, 64 rows 204 and 186.
   r.prompt = rows > 32;
   if (r.prompt) {
     hero_status st = prompt_workspace_bytes(h, cc, nq, max_rows, &r.bytes);
     *out = r;
     return st;
   }
+  // rows of a tile: 8, 16 or 24.  us on the same 16 sequences: 24 rows in one tile 78, in two of 16 97; 28 rows in two of 16 99, of 24 125
   r.nt = rows <= 8 ? 1 : rows > 16 && rows <= 24 ? 3 : 2;
   const long long tiles = (rows + 8 * r.nt - 1) / (8 * r.nt), groups = tiles * cc->nkv * cc->B, steps = ((long long)cc->max_len + 31) / 32;
   HERO_REQUIRE(groups <= (1ll << 30), HERO_ERR_UNSUPPORTED, "B=%d nkv=%d max_rows=%d: too many", cc->B, cc->nkv, max_rows);

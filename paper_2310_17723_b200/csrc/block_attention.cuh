@@ -28,7 +28,7 @@ __device__ __forceinline__ void store_out(const BlockAttnParams& p, long long ro
   }
 }
 
-// P is formed with a factor 2^P_SHIFT; the running maximum moves when a score exceeds it by more than MAX_SLACK in the exponent
+// Few rows: P is formed with a factor 2^P_SHIFT; the running maximum moves when a score exceeds it by more than MAX_SLACK in the exponent
 // of two, so P stays below 2^15 and a probability 2^-25 of the largest is still a normal FP16 number.
 constexpr float P_SHIFT = 11.0f, MAX_SLACK = 4.0f;
 

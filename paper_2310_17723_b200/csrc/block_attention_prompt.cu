@@ -18,7 +18,8 @@
 //                    2048 rows on 6000 tokens, heads 32 / 8 of 128)
 // The value scale of a page is folded into the exponent, e' = 2^(x + log2 rv), so that it costs nothing per element; the row sum
 // undoes it per 16 tokens (rv is kept above 2^-40, where P is zero anyway).  As in the kernel for few rows, queries are scaled into
-// FP16 by a power of two.  No maximum is taken per tile: P is formed with the maximum so far, and only if 16 probabilities
+// FP16 by a power of two and P is rounded to FP16 (the products take 16 bits on both sides): half a step, and 2^-33 of the largest
+// value scale met where a probability times its page's relative scale is below 2^-22.  No maximum is taken per tile: P is formed with the maximum so far, and only if 16 probabilities
 // sum to more than FP16 holds (or in the first half) is the half read again for its maximum, O rescaled in tensor memory.
 #include "block_attention.cuh"
 #include "block_ring.cuh"
