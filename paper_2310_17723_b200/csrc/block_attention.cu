@@ -689,9 +689,8 @@ extern "C" hero_status hero_block_attention_workspace_bytes(hero_handle* h, cons
   // a call with a smaller row bound may be dealt out differently and need more: the answer serves it too
   size_t most = plan.bytes;
   for (int m = 1; m < max_rows && (long long)m * (nq / cc->nkv) <= 32; ++m) {
-    RowsPlan fewer;
-    if ((st = plan_rows(h, cc, nq, m, &fewer)) != HERO_OK) return st;
-    most = fewer.bytes > most ? fewer.bytes : most;
+    RowsPlan fewer;                              // (a row bound that is refused needs nothing)
+    if (plan_rows(h, cc, nq, m, &fewer) == HERO_OK && fewer.bytes > most) most = fewer.bytes;
   }
   if (plan.prompt) {
     const size_t fewer = prompt_workspace_most(h, cc, nq, max_rows);
