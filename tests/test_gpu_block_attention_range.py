@@ -145,3 +145,51 @@ def test_subnormal_queries(h, kind, dh, counts, max_len):
     qt, qx = to_fp(1e-39 * np.random.default_rng(6).standard_normal((sum(counts), 2 * dh)), "bf16")
     assert qx.any()
     _compare(c, _run(h, c, qt, counts, 2, "bf16", scale=20.0), qx, counts, 2, "bf16", scale=20.0)
+
+
+@pytest.mark.parametrize("counts,max_len", FORMS)
+@pytest.mark.parametrize("kind,dh", [("i8", 64), ("f8", 128)])
+@pytest.mark.parametrize("q_unit", [1e3, 1e5, 1e6, 3e6, 1e7, 4e7, 1e9, 1e12])
+def test_large_scores_whose_maximum_comes_late(h, kind, dh, counts, max_len, q_unit):
+    # positive scores that grow from page to page, the last tokens' but for one that is larger than all: the maximum moves at many places
+    c = _cache(kind, dh, max_len, k_scale=1.0)
+    late = [130, 100]
+    codes = c.codes["k"]
+    for b in range(2):
+        for i, pid in enumerate(c.table[b]):
+            codes[pid] = BC.to_codes(np.full(codes[pid].shape, 4.0 + 3.0 * min(i, 12)), kind)
+        codes[c.table[b][late[b] // 16], :, late[b] % 16] = 112.0
+    c.buf["k"].copy_(torch.from_numpy(codes.astype(np.float32)).to(c.buf["k"].dtype))
+    qt, _ = to_fp(q_unit * np.random.default_rng(8).uniform(1.0, 1.5, (sum(counts), 2 * dh)), "bf16")
+    got = _run(h, c, qt, counts, 2, "bf16").double().cpu().numpy()
+    for b, (n, at) in enumerate(zip(counts, starts(counts))):
+        want = np.tile(c.values("v", b)[late[b], 0], (n, 2))
+        sees = LENS[b] - n + np.arange(n) >= late[b]
+        assert sees.any() and np.all((np.abs(got[at:at + n] - want) <= (2.0 ** -8 + 2.0 ** -10) * np.abs(want))[sees]), b
+
+
+@pytest.mark.parametrize("counts,max_len", FORMS)
+@pytest.mark.parametrize("kind,dh", [("i8", 128), ("f8", 64)])
+def test_rows_of_very_different_size_side_by_side(h, kind, dh, counts, max_len):
+    # ordinary rows beside rows a billion times as large, whose largest key is all that counts (where the next is 2^-12 of the scores away)
+    c = _cache(kind, dh, max_len)
+    rows = sum(counts)
+    q = np.random.default_rng(9).standard_normal((rows, 2, dh))
+    q[:, 1] *= 10.0 ** (3 * (np.arange(rows) % 4))[:, None]                  # head 1: 1, 1e3, 1e6, 1e9
+    qt, qx = to_fp(q.reshape(rows, 2 * dh), "bf16")
+    got = _run(h, c, qt, counts, 2, "bf16").double().cpu().numpy().reshape(rows, 2, dh)
+    want, bar = (x.reshape(rows, 2, dh) for x in _expect(c, qx, counts, 2, dh ** -0.5, rows))
+    bar = bar + 2.0 ** -8 * (np.abs(want) + bar)
+    assert np.all(np.abs(got - want)[:, 0] <= bar[:, 0])
+    sure = 0
+    for b, (n, at) in enumerate(zip(counts, starts(counts))):
+        k, v = c.values("k", b)[:, 0], c.values("v", b)[:, 0]
+        for i in range(n):
+            m = LENS[b] - n + i + 1
+            s = k[:m] @ qx.reshape(rows, 2, dh)[at + i, 1] * dh ** -0.5
+            top, runner = np.sort(s)[-1], np.sort(s)[-2] if m > 1 else -np.inf
+            if (at + i) % 4 >= 2 and top - runner > 2.0 ** -12 * np.abs(s).max():
+                sure += 1
+                one = v[int(np.argmax(s))]
+                assert np.all(np.abs(got[at + i, 1] - one) <= (2.0 ** -8 + 2.0 ** -10) * np.abs(one)), (b, i)
+    assert sure or rows < 4
