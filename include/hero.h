@@ -24,8 +24,8 @@
  * (text via hero_last_error()).  A device-side wait that exceeded its bound (a pipeline bug, never
  * expected) sets a device error word; hero_check() synchronizes the stream and returns
  * HERO_ERR_DEVICE_TIMEOUT if it is set.  The same word reports an embedding id outside its table (the gather of
- * hero_layernorm_quant clamps such an id, so nothing is read out of bounds), a page id or row range of a block cache or a
- * position outside its bounds: hero_check() then returns HERO_ERR_INVALID_ARG.
+ * hero_layernorm_quant clamps such an id, so nothing is read out of bounds), a page id or row range of a block cache, a
+ * position, or a row, token or expert of a mixture of experts outside its bounds: hero_check() then returns HERO_ERR_INVALID_ARG.
  */
 #ifndef HERO_H_
 #define HERO_H_
@@ -56,7 +56,8 @@ typedef enum { HERO_I8 = 0, HERO_U8 = 1, HERO_I32 = 2, HERO_F16 = 3, HERO_BF16 =
 /* Granularity of the scale attached to an INT8 tensor (Eq. 3-5). */
 typedef enum { HERO_GRAN_NONE = 0, HERO_GRAN_TWQ = 1, HERO_GRAN_FWQ = 2, HERO_GRAN_SQ = 3 } hero_gran;
 
-typedef enum { HERO_ACT_NONE = 0, HERO_ACT_GELU_ERF = 1, HERO_ACT_GELU_TANH = 2 } hero_act;
+/* HERO_ACT_SILU (v / (1 + exp(-v))): hero_moe_linear only. */
+typedef enum { HERO_ACT_NONE = 0, HERO_ACT_GELU_ERF = 1, HERO_ACT_GELU_TANH = 2, HERO_ACT_SILU = 3 } hero_act;
 typedef enum { HERO_MASK_NONE = 0, HERO_MASK_CAUSAL = 1 } hero_mask;
 typedef enum { HERO_POST_LN = 0, HERO_PRE_LN = 1 } hero_arch;
 /* Table 1: a module runs INT8 or stays in FP16/BF16 (the layer's fp_dtype). */
@@ -602,10 +603,123 @@ typedef struct {
 } hero_qk_norm_rope_args;
 hero_status hero_qk_norm_rope(hero_handle* h, const hero_qk_norm_rope_args* a, void* stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * A mixture of experts in place of the layer's MLP (no counterpart in the paper; Eq. 28-32 for each expert).  A router gives each
+ * of T tokens a logit for each of E experts; the k experts with the largest ones work on the token, and the weighted sum
+ * of what they give is the branch that the residual LN^quant takes.  Three calls:
+ *
+ *     hero_moe_route    logits -> experts and weights of each token, and the order of the (token, expert) pairs by expert
+ *     hero_moe_linear   GeMM^quant of each expert's rows with that expert's weights (twice: FC1 with its activation, FC2)
+ *     hero_moe_combine  residual + weighted sum of each token's rows, LN^quant of the result
+ *
+ * "Sorted rows" are the pairs ordered by expert, then by token.  offset (device int32 [E + 1]): expert e has the sorted rows
+ * offset[e] .. offset[e + 1] - 1.  A tensor of sorted rows has T k rows, of which offset[E] are in use; the others are neither read nor
+ * written.  How many rows an expert gets is known on the device alone, so that the calls can be captured in a CUDA graph
+ * and replayed with other tokens.
+ *
+ * What the host cannot see is bounded on the device and reported by the next hero_check() as HERO_ERR_INVALID_ARG: an expert whose rows are
+ * decreasing or outside the tensor (taken as empty), a token outside A (clamped), a row or expert outside its tensor (that pair adds
+ * nothing). */
+
+/* hero_moe_route.  Per token t, with x its logits:
+ *     score[e] = softmax(x)[e] or sigmoid(x[e]);   key[e] = x[e], or score[e] + select_bias[e] when a bias is given
+ *     expert[t][0 .. k-1] = the experts of the k largest keys, largest first, ties to the lowest index
+ *     weight[t][j] = score (divided by the sum of the chosen ones when renorm is set) * scale
+ *   The choice is the one of exact arithmetic (a bias: keys that FP32 cannot tell apart are compared in FP64; scores and weights are FP32).  A logit (or
+ *   bias) of -inf or NaN never takes part: not in the choice, not in the softmax.  Where a token has fewer than k experts left,
+ *   the other places hold expert -1, weight 0 and row -1.  Several logits of +inf share a softmax equally.
+ *   logits      : F16 / BF16 / F32 [T][E], E <= 512, any ld >= E, aligned to its elements
+ *   n_tokens    : device int32 [1] or NULL: only the first n_tokens rows are tokens (a padded batch); the others get expert -1
+ *   expert, weight, row : device [T][k] int32 / float32 / int32, contiguous; row[t][j]: sorted row of the pair
+ *   offset      : device int32 [E + 1];  token : device int32 [T k]: the token of each sorted row (written up to offset[E])
+ *   top_k       : 1 .. 16, at most E;  T k < 2^31
+ *   workspace   : device scratch of hero_moe_route_workspace_bytes(), 16-byte aligned; no clearing, nothing held between calls; calls
+ *                 that may overlap on the GPU need one each.  The answer serves any smaller number of tokens as well. */
+typedef enum { HERO_SCORE_SOFTMAX = 0, HERO_SCORE_SIGMOID = 1 } hero_score;
+typedef struct {
+  hero_tensor logits;
+  const int32_t* n_tokens;
+  const float* select_bias;  /* device [E] or NULL */
+  int32_t top_k;
+  int32_t score;             /* hero_score */
+  int32_t renorm;
+  float scale;
+  int32_t* expert;
+  float* weight;
+  int32_t* offset;
+  int32_t* token;
+  int32_t* row;
+  void* workspace;
+  size_t workspace_bytes;
+} hero_moe_route_args;
+hero_status hero_moe_route_workspace_bytes(hero_handle* h, int64_t n_tokens, int32_t n_experts, int32_t top_k, size_t* bytes);
+hero_status hero_moe_route(hero_handle* h, const hero_moe_route_args* a, void* stream);
+
+/* hero_moe_linear.  For the sorted rows r of expert e (i = token[r], or r when token is NULL):
+ *     v[r,j] = sum_c A[i,c] W[e][j,c] * rs[i] * w_scale[e][j] + bias[e][j]      rs = TWQ scale of A, or 1
+ *     a[r,j] = act(v[r,j]);  gated: a[r,j] = act(v[r,j]) * v[r, N/2 + j], j < N/2
+ *     a     *= post_scale[e][j]                                                 (1 / S_a of the quantised hidden features; NULL = skip)
+ *     out    = I8: clip(Round(a), -127, 127);  F8: saturating e4m3;  F16 / BF16: a rounded
+ *   With one expert and no token the result is hero_w8a8_linear's (INT8 operands: bit for bit).
+ *   A      : I8 / F8 (TWQ: scale[rows], else no row factor) or F16 / BF16, [rows][K]; K times the element size a multiple of 16 bytes
+ *   W      : device [E][N][K] of A's type, K contiguous, row pitch ldw, expert_stride elements from one expert to the next (both
+ *            multiples of 16 bytes); N a multiple of 16, gated a multiple of 32 (rows 0 .. N/2 - 1: gate, the others: up).
+ *            W is a constant of the model, as for hero_w8a8_linear.
+ *   w_scale, bias : device [E][N] (8-bit operands: w_scale required; 16-bit: ignored);  post_scale : device [E][N, gated N/2]
+ *   token  : device int32 [out.rows] or NULL (then A has out.rows rows)
+ *   out    : [T k][N, gated N/2]; I8 from I8 or 16-bit operands, F8 from F8 or 16-bit operands, F16 / BF16 from any
+ *   out_col_absmax : device float[E][columns of out] or NULL: running per-expert column maxima of |out| as stored (F16 / BF16 outputs), from
+ *            which calibration takes the static scale of an expert's hidden features (zero it before the first batch)
+ *   act    : hero_act, HERO_ACT_SILU included;  E <= 512 */
+typedef struct {
+  hero_tensor A;
+  const int32_t* token;
+  const int32_t* offset;
+  const void* W;
+  int64_t N;
+  int64_t ldw;
+  int64_t expert_stride;
+  int32_t n_experts;
+  const float* w_scale;
+  const float* bias;
+  int32_t act;
+  int32_t gated;
+  const float* post_scale;
+  hero_tensor out;
+  float* out_col_absmax;
+} hero_moe_linear_args;
+hero_status hero_moe_linear(hero_handle* h, const hero_moe_linear_args* a, void* stream);
+
+/* hero_moe_combine.  LN^quant of a residual and a token's expert rows, FP32 throughout:
+ *     r[t] = residual[t] + shared[t] + sum_j weight[t][j] * y[row[t][j]]        (each dequantised; pairs in the order of j; row -1: no pair)
+ *     fp_out = r;   out = LN^quant(r) as hero_layernorm_quant defines it (of the stored r when there is an fp_out)
+ *   y        : [T k][H] F16 / BF16, or I8 / F8 with gran FWQ (scale [E][H]: one per expert and feature), SQ or NONE
+ *   row, weight, expert : device [T][k] as hero_moe_route leaves them; expert is needed for an FWQ y only (else NULL)
+ *   residual, shared : optional, [T][H] I8 / F8 (TWQ / FWQ / SQ / NONE) or F16 / BF16; shared: the output of experts that every token visits
+ *   out      : optional, I8 / F8 (TWQ: scale written; FWQ / SQ: read) or F16 / BF16; needs gamma and beta (device [H])
+ *   fp_out   : optional F16 / BF16; at least one of out and fp_out.  An output of the residual's or of shared's type may be that tensor.
+ *   H a multiple of 16, at most 16384; top_k 1 .. 16; T any size (rows of the larger of out and fp_out) */
+typedef struct {
+  hero_tensor y;
+  const int32_t* row;
+  const float* weight;
+  const int32_t* expert;
+  int32_t top_k;
+  int32_t n_experts;         /* for an FWQ y */
+  hero_tensor residual;
+  hero_tensor shared;
+  const float* gamma;
+  const float* beta;
+  float eps;
+  hero_tensor out;
+  hero_tensor fp_out;
+} hero_moe_combine_args;
+hero_status hero_moe_combine(hero_handle* h, const hero_moe_combine_args* a, void* stream);
+
 /* Per-launch device timing for benchmarks (no counterpart in the paper, which measured nothing): between
  * _begin and _end every kernel the handle launches is bracketed by a pair of CUDA events on its stream.
  * _end waits for them and returns, per launch in order, the elapsed milliseconds and the kernel family
- * (1 = LN^quant, 2 = GeMM^quant, 3 = attention core, 4 = block cache and rotation).  Arrays must hold max_launches entries. */
+ * (1 = LN^quant, 2 = GeMM^quant, 3 = attention core, 4 = block cache and rotation, 5 = routing of experts).  Arrays must hold max_launches entries. */
 hero_status hero_profile_begin(hero_handle* h, int32_t max_launches);
 hero_status hero_profile_end(hero_handle* h, float* ms_out, int32_t* tag_out, int32_t* n_out);
 

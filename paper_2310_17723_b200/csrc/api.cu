@@ -128,6 +128,38 @@ hero_status make_tmap_pages(const hero_handle* h, CUtensorMap* out, const void* 
   return HERO_OK;
 }
 
+hero_status make_tmap_experts(const hero_handle* h, CUtensorMap* out, const void* base, int dtype, bool gated, int64_t N, int64_t K, int64_t E,
+                              int64_t ldw, int64_t expert_stride) {
+  HERO_REQUIRE(h && h->encode_tiled, HERO_ERR_CUDA, "tensor-map encoder unavailable");
+  const int eb = (int)dtype_size(dtype);
+  const uint64_t key[6] = {reinterpret_cast<uint64_t>(base), (uint64_t)N | ((uint64_t)E << 32), (uint64_t)K, (uint64_t)ldw, (uint64_t)expert_stride,
+                           5 | ((uint64_t)dtype << 8) | ((uint64_t)(gated ? 1 : 0) << 16)};
+  hero_handle* hm = const_cast<hero_handle*>(h);
+  hero_tmap_slot& slot = tmap_slot(hm, key);
+  std::lock_guard<std::mutex> guard(hm->tmap_mu);
+  if (slot.used && memcmp(slot.key, key, sizeof(key)) == 0) {
+    *out = slot.map;
+    return HERO_OK;
+  }
+  const cuuint32_t halves = gated ? 2 : 1;
+  cuuint64_t dims[5] = {(cuuint64_t)K, 8, halves, (cuuint64_t)(N / (8 * halves)), (cuuint64_t)E};
+  cuuint64_t strides[4] = {(cuuint64_t)(ldw * eb), (cuuint64_t)(gated ? N / 2 * ldw * eb : ldw * eb), (cuuint64_t)(8 * ldw * eb),
+                           (cuuint64_t)(expert_stride * eb)};
+  cuuint32_t box[5] = {(cuuint32_t)(128 / eb), 8, halves, 16 / halves, 1};
+  cuuint32_t estr[5] = {1, 1, 1, 1, 1};
+  const CUtensorMapDataType dt = eb == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8
+                                         : dtype == HERO_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+  CUresult r = reinterpret_cast<encode_tiled_fn>(h->encode_tiled)(
+      out, dt, 5, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+      CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  HERO_REQUIRE(r == CUDA_SUCCESS, HERO_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d) for experts' weights: N=%lld K=%lld E=%lld ldw=%lld stride=%lld",
+               (int)r, (long long)N, (long long)K, (long long)E, (long long)ldw, (long long)expert_stride);
+  memcpy(slot.key, key, sizeof(key));
+  slot.map = *out;
+  slot.used = true;
+  return HERO_OK;
+}
+
 }  // namespace hero
 
 extern "C" {
@@ -227,6 +259,10 @@ hero_status hero_check(hero_handle* h, void* stream) {
       hero::set_error(code == hero::ERR_BAD_PAGE ? "a page table named a page outside the cache; it was clamped (read) or skipped (written)"
                       : code == hero::ERR_BAD_ROWS ? "a row range was decreasing, outside the matrices or longer than max_rows; it was cut"
                                                    : "a position was outside the rotation tables; it was clamped");
+      return HERO_ERR_INVALID_ARG;
+    }
+    if (code == hero::ERR_BAD_EXPERT) {
+      hero::set_error("an expert's row range, a token, a row or an expert of a mixture of experts was outside its tensor; it was left out or clamped");
       return HERO_ERR_INVALID_ARG;
     }
     hero::set_error("a bounded device-side wait gave up (code 0x%x)", code);

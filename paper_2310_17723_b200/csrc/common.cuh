@@ -85,9 +85,11 @@ hero_status check_matrix(const hero_tensor& t, const char* name);
 constexpr int ERR_BAD_ID = 0x1D000001;
 // ... a page id outside its pool, a row range outside its matrix, a position outside the rotation tables
 constexpr int ERR_BAD_PAGE = 0x1D000002, ERR_BAD_ROWS = 0x1D000003, ERR_BAD_POS = 0x1D000004;
+// ... a row range, token, row or expert of a mixture of experts outside its tensor
+constexpr int ERR_BAD_EXPERT = 0x1D000005;
 
 // Kernel families for the per-launch timing records.
-enum { KERNEL_LN = 1, KERNEL_GEMM = 2, KERNEL_ATTN = 3, KERNEL_CACHE = 4 };
+enum { KERNEL_LN = 1, KERNEL_GEMM = 2, KERNEL_ATTN = 3, KERNEL_CACHE = 4, KERNEL_ROUTE = 5 };
 // Brackets one kernel launch with events when timing is on; counts the launch either way.
 struct LaunchScope {
   hero_handle* h; cudaStream_t s; int slot;
@@ -182,5 +184,10 @@ hero_status make_tmap_2d(const hero_handle* h, CUtensorMap* out, const void* bas
 // 4-D TMA descriptor {features, tokens of a page, heads, pages} over the keys or values of a block cache; box = dh x box_tokens
 // bytes of one page and head, swizzled over rows of dh (64 or 128) bytes.
 hero_status make_tmap_pages(const hero_handle* h, CUtensorMap* out, const void* base, const hero_block_cache* c, uint32_t box_tokens);
+
+// 5-D TMA descriptor {K, 8 rows, gate / up, groups of 8 rows, experts} over weights [E][N][K] of a mixture of experts; box = 128 bytes of
+// K x 128 rows of one expert, where `gated` takes eight rows of the first half of N and eight of the second in turn.
+hero_status make_tmap_experts(const hero_handle* h, CUtensorMap* out, const void* base, int dtype, bool gated, int64_t N, int64_t K, int64_t E,
+                              int64_t ldw, int64_t expert_stride);
 
 }  // namespace hero

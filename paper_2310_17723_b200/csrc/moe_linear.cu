@@ -1,0 +1,565 @@
+// Products grouped by expert (hero_moe_linear): GeMM^quant (Eq. 14, 28-30, 32) of each expert's rows with that expert's weights, over groups whose
+// sizes only the device knows.
+//
+// The operands change sides on the tensor core: 128 output features (rows of W) are the M side of a product and the rows of an
+// expert its N side, which an instruction may have in any multiple of 16 (of a CTA pair: 32).  A group of 17 rows then costs 32 columns and
+// not a tile of 128 or 256 rows, and the accumulator's lane is a feature, so that the scale, bias and output factor of a thread are three
+// registers and the row factors are broadcasts.
+//
+// A CTA (or a pair of them, tcgen05 cta_group::2, 128 features each) is persistent over tiles of (expert, rows of the expert, features).  The
+// rows of an expert are dealt evenly to as few tiles as they need.  Twelve working warps and two that issue:
+//   warps 0-7   epilogue: tensor memory -> registers -> scales, activation, rounding -> shared memory (turned) -> whole row segments out
+//   warps 8-11  rows of A, picked by token, to shared memory (cp.async, in the operand's 128-byte swizzle)
+//   warp  12    W tiles (TMA)
+//   warp  13    products (one elected lane) and the owner of the tensor memory
+// The accumulator is double-buffered.  Every wait is bounded; on expiry the CTA records a code and unwinds.
+//
+// Gated products (act(gate) * up): a tile's 128 rows of W are eight rows of the gate's half and eight of the other in turn (one
+// tensor map does that), so that gate and up of a feature lie eight lanes apart in the same warp.  The two lanes exchange one value for each
+// pair of rows; each then finishes one row of the pair.
+#include "gemm_common.cuh"
+
+namespace hero {
+
+constexpr int MOE_MAX_E = 512;
+constexpr int MOE_EPI_WARPS = 8, MOE_ROW_WARPS = 4, MOE_W_WARP = 12, MOE_MMA_WARP = 13, MOE_THREADS = 14 * 32;
+constexpr int MOE_CHUNK = 32;                 // rows that an epilogue group turns at a time
+constexpr int MOE_LAG = 3;                    // k-blocks of rows in flight per row warp before the oldest is announced
+
+struct MoeLinearParams {
+  int R, a_rows, E, N, n_out, K;              // K in elements
+  int num_kb, num_nt;                         // 128-byte steps of K, feature tiles of an expert
+  const int* offset; const int* token;
+  const uint8_t* A; long long a_ld;           // bytes
+  int k_bytes;
+  const float* rs; const float* cs; const float* bias; const float* post;
+  void* out; long long out_ld; int out_dt;
+  int act, f8;                                // f8: e4m3 operands
+  uint32_t idesc;                             // without the N field
+  int kelems;                                 // elements of 128 bytes
+  float* obs;
+  int* err;
+};
+
+template <bool PAIR>
+struct MoeCfg {
+  static constexpr int MT = PAIR ? 256 : 64;              // rows of a tile at most
+  static constexpr int ROWS = PAIR ? MT / 2 : MT;         // ... that this CTA loads
+  static constexpr int STEP = PAIR ? 32 : 16;             // granularity of the N side
+  static constexpr int FEAT = 128;                        // features of this CTA
+  static constexpr int W_BYTES = FEAT * GEMM_BK_BYTES, X_BYTES = ROWS * GEMM_BK_BYTES, STAGE_BYTES = W_BYTES + X_BYTES;
+  static constexpr int STAGES = PAIR ? 5 : 7;
+  static constexpr int TURN_BYTES = 2 * MOE_CHUNK * FEAT * 2;             // per epilogue group: two buffers of 32 rows of 16-bit outputs
+  static constexpr int TMEM_COLS = 2 * MT;
+  static constexpr int TURN_AT = STAGES * STAGE_BYTES;
+  static constexpr int RS_AT = TURN_AT + 2 * TURN_BYTES;                  // [8 warps][MT / 2] row factors
+  static constexpr int TABLE_AT = RS_AT + 8 * (MT / 2) * 4;               // first row [E + 1] and first tile [E + 1] of each expert
+  static constexpr int BARS_AT = TABLE_AT + 2 * (MOE_MAX_E + 4) * 4;
+  static constexpr int SMEM_BYTES = 1024 + BARS_AT + 256;
+  static_assert(SMEM_BYTES <= 227 * 1024, "shared memory");
+};
+
+struct MoeTile { int e, row0, rows, nt; };    // rows 0: none
+
+// tile t of the launch; lo[e], tiles[e]: first sorted row of expert e and its first row tile (tables in shared memory)
+template <int MT, int STEP>
+__device__ __forceinline__ MoeTile moe_tile(const MoeLinearParams& p, const int* first, const int* tiles, int t) {
+  MoeTile r;
+  const int rt = t / p.num_nt;
+  r.nt = t - rt * p.num_nt;
+  int lo = 0, hi = p.E;                       // the last expert whose first tile is not behind rt
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (tiles[mid] <= rt) lo = mid; else hi = mid;
+  }
+  r.e = lo;
+  const int n = first[lo + 1] - first[lo], k = tiles[lo + 1] - tiles[lo], i = rt - tiles[lo];
+  const int per = ((n + k - 1) / k + STEP - 1) / STEP * STEP;
+  r.row0 = first[lo] + i * per;
+  r.rows = min(per, n - i * per);             // may be 0 or less where an even share rounds up: such a tile is skipped
+  return r;
+}
+
+// (a denominator beyond 2^126 gives 0, which is what v e^v rounds to there)
+__device__ __forceinline__ float silu_f(float v) { return __fdividef(v, 1.0f + __expf(-v)); }
+
+template <int ACT>
+__device__ __forceinline__ float moe_act(float v) {
+  if constexpr (ACT == HERO_ACT_GELU_ERF) return gelu_erf_f(v);
+  if constexpr (ACT == HERO_ACT_GELU_TANH) return gelu_tanh_f(v);
+  if constexpr (ACT == HERO_ACT_SILU) return silu_f(v);
+  return v;
+}
+
+struct MoeLane {                              // what a lane knows of its feature
+  float cs, bias, post;
+  bool ok;                                    // the feature exists
+  bool up;                                    // gated: this lane holds the second half's product
+  int turn;                                   // its column in the turned chunk
+};
+
+template <int OUTK>                           // OUT_I8, OUT_F8, OUT_FP
+__device__ __forceinline__ void moe_put(uint8_t* at, float y, int dt, float& most, bool count) {
+  if constexpr (OUTK == OUT_I8) {
+    const float r = fminf(fmaxf(y + ROUND_MAGIC, ROUND_MAGIC - 127.0f), ROUND_MAGIC + 127.0f);   // RNE in the adder, then clip
+    *at = (uint8_t)(__float_as_uint(r) & 0xff);
+  } else if constexpr (OUTK == OUT_F8) {
+    *at = (uint8_t)(ptx::f32x2_to_e4m3x2(y, 0.0f) & 0xff);
+  } else {
+    unsigned short b;
+    if (dt == HERO_F16) b = __half_as_ushort(__float2half_rn(y));
+    else b = __bfloat16_as_ushort(__float2bfloat16_rn(y));
+    *reinterpret_cast<unsigned short*>(at) = b;
+    const float a = dt == HERO_F16 ? __half2float(__ushort_as_half(b & 0x7fff)) : __uint_as_float((uint32_t)(b & 0x7fff) << 16);
+    if (count) most = fmaxf(most, a);
+  }
+}
+
+// 32 rows of this lane's feature: products, activation, rounding, into the turned chunk [32 rows][columns of the CTA]
+template <bool INT8, bool GATED, int ACT, int OUTK>
+__device__ __forceinline__ void moe_chunk(const MoeLinearParams& p, const uint32_t (&r)[32], const float* rs, const MoeLane& l, uint8_t* buf, int rows,
+                                          float& most) {
+  constexpr int ES = OUTK == OUT_FP ? 2 : 1, COLS = GATED ? 64 : 128, PITCH = COLS * ES;
+  uint8_t* at = buf + l.turn * ES;
+#pragma unroll
+  for (int j = 0; j < 32; j += 4) {
+    const float4 f = *reinterpret_cast<const float4*>(rs + j);
+    const float rsj[4] = {f.x, f.y, f.z, f.w};
+    float v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float acc = INT8 ? (float)(int)r[j + i] : __uint_as_float(r[j + i]);
+      if constexpr (!GATED && ACT == HERO_ACT_NONE) v[i] = fmaf(acc * rsj[i], l.cs, l.bias);      // (cs and bias carry the output factor)
+      else v[i] = fmaf(acc * rsj[i], l.cs, l.bias);
+    }
+    if constexpr (GATED) {
+#pragma unroll
+      for (int i = 0; i < 4; i += 2) {
+        // the gate's lane keeps the first row of the two and gives its second, the other lane the other way round
+        const float other = __shfl_xor_sync(0xffffffffu, l.up ? v[i] : v[i + 1], 8);
+        const float gate = l.up ? other : v[i], up = l.up ? v[i + 1] : other;
+        const int row = j + i + (l.up ? 1 : 0);
+        moe_put<OUTK>(at + row * PITCH, moe_act<ACT>(gate) * up * l.post, p.out_dt, most, row < rows);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float y = ACT == HERO_ACT_NONE ? v[i] : moe_act<ACT>(v[i]) * l.post;
+        moe_put<OUTK>(at + (j + i) * PITCH, y, p.out_dt, most, j + i < rows);
+      }
+    }
+  }
+}
+
+template <bool INT8, bool GATED, int ACT>
+__device__ __forceinline__ void moe_chunk_out(const MoeLinearParams& p, const uint32_t (&r)[32], const float* rs, const MoeLane& l, uint8_t* buf, int rows,
+                                              float& most) {
+  if (p.out_dt == HERO_I8) moe_chunk<INT8, GATED, ACT, OUT_I8>(p, r, rs, l, buf, rows, most);
+  else if (p.out_dt == HERO_F8) moe_chunk<INT8, GATED, ACT, OUT_F8>(p, r, rs, l, buf, rows, most);
+  else moe_chunk<INT8, GATED, ACT, OUT_FP>(p, r, rs, l, buf, rows, most);
+}
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, uint32_t bytes) {   // the other 16 - bytes become zero
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+__device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap* m, int x, int g, int e, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
+      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(x), "r"(0), "r"(0), "r"(g), "r"(e), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void tma_load_5d_pair(uint32_t dst, const CUtensorMap* m, int x, int g, int e, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.5d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
+      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(x), "r"(0), "r"(0), "r"(g), "r"(e), "r"(bar) : "memory");
+}
+
+template <bool INT8, bool GATED, bool PAIR>
+__device__ __forceinline__ void moe_linear_body(const CUtensorMap& tmW, const MoeLinearParams& p) {
+  using Cfg = MoeCfg<PAIR>;
+  constexpr int MT = Cfg::MT, STAGES = Cfg::STAGES;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  int* first = reinterpret_cast<int*>(smem + Cfg::TABLE_AT);        // [E + 1]
+  int* tiles = first + MOE_MAX_E + 4;                               // [E + 1]
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + Cfg::BARS_AT);   // [STAGES] operands there (of a pair: the leader's)
+  uint64_t* empty = full + STAGES;                                  // [STAGES] operands read
+  uint64_t* acc_full = empty + STAGES;                              // [2]
+  uint64_t* acc_empty = acc_full + 2;                               // [2] (of a pair: the leader's)
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = PAIR ? ptx::cluster_ctarank() : 0u;
+  const int group_id = PAIR ? blockIdx.x >> 1 : blockIdx.x, groups = PAIR ? gridDim.x >> 1 : gridDim.x;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < STAGES; ++i) { ptx::mbar_init(&full[i], 1 + MOE_ROW_WARPS * (PAIR ? 2 : 1)); ptx::mbar_init(&empty[i], 1); }
+    for (int i = 0; i < 2; ++i) { ptx::mbar_init(&acc_full[i], 1); ptx::mbar_init(&acc_empty[i], MOE_EPI_WARPS * (PAIR ? 2 : 1)); }
+    ptx::fence_mbar_init();
+  }
+  if (warp == MOE_MMA_WARP) {
+    if constexpr (PAIR) { ptx::tmem_alloc_pair(tmem_slot, Cfg::TMEM_COLS); ptx::tmem_relinquish_pair(); }
+    else { ptx::tmem_alloc(tmem_slot, Cfg::TMEM_COLS); ptx::tmem_relinquish(); }
+  }
+  if (warp == MOE_W_WARP && lane == 0) ptx::prefetch_tmap(&tmW);
+  ptx::pdl_launch_dependents();
+  ptx::pdl_wait();                                                  // the router's offsets (and all else) are there from here on
+
+  // ---- the experts' first rows and first tiles
+  for (int e = threadIdx.x; e <= p.E; e += blockDim.x) first[e] = p.offset[e];
+  __syncthreads();
+  if (warp == 0) {
+    int run = 0;
+    for (int e0 = 0; e0 < p.E; e0 += 32) {
+      const int e = e0 + lane;
+      int k = 0;
+      if (e < p.E) {
+        const int lo = first[e], hi = first[e + 1];
+        if (lo < 0 || hi < lo || hi > p.R) atomicExch(p.err, ERR_BAD_EXPERT);
+        else k = (hi - lo + MT - 1) / MT;
+      }
+      int s = k;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int u = __shfl_up_sync(0xffffffffu, s, o);
+        if (lane >= o) s += u;
+      }
+      if (e < p.E) tiles[e] = run + s - k;
+      run += __shfl_sync(0xffffffffu, s, 31);
+    }
+    if (lane == 0) tiles[p.E] = run;
+  }
+  ptx::tc_fence_before();
+  __syncthreads();
+  if constexpr (PAIR) ptx::cluster_sync();                          // both CTAs' barriers exist before any remote arrive
+  ptx::tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  const int num_tiles = tiles[p.E] * p.num_nt;
+  auto tile_at = [&](int t) { return moe_tile<MT, Cfg::STEP>(p, first, tiles, t); };
+
+  if (warp == MOE_W_WARP) {
+    // ------------------------------------------------------------------ weights
+    const bool issue = ptx::elect_one();
+    const uint32_t dst0 = PAIR ? ptx::mapa(ptx::smem_u32(smem), rank) : ptx::smem_u32(smem);
+    const uint32_t bar0 = PAIR ? ptx::mapa(ptx::smem_u32(full), 0) : ptx::smem_u32(full);
+    int stage = 0; uint32_t phase = 0; bool ok = true;
+    for (int t = group_id; t < num_tiles && ok; t += groups) {
+      const MoeTile w = tile_at(t);
+      if (w.rows <= 0) continue;
+      const int g = (w.nt * (PAIR ? 2 : 1) + (int)rank) * (GATED ? 8 : 16);     // first group of eight rows (of each half)
+      for (int kb = 0; kb < p.num_kb; ++kb) {
+        if (!ptx::mbar_wait(&empty[stage], phase ^ 1, p.err, 0xC00 | stage)) { ok = false; break; }
+        if (issue) {
+          if (rank == 0) ptx::mbar_expect_tx(&full[stage], (PAIR ? 2 : 1) * Cfg::W_BYTES);
+          if constexpr (PAIR) tma_load_5d_pair(dst0 + stage * Cfg::STAGE_BYTES, &tmW, kb * p.kelems, g, w.e, bar0 + 8 * stage);
+          else tma_load_5d(dst0 + stage * Cfg::STAGE_BYTES, &tmW, kb * p.kelems, g, w.e, bar0 + 8 * stage);
+        }
+        if (++stage == STAGES) { stage = 0; phase ^= 1; }
+      }
+    }
+    for (int i = 0; i < STAGES; ++i) {                              // every copy started here has been consumed
+      if (!ptx::mbar_wait(&empty[stage], phase ^ 1, p.err, 0xC80 | stage)) break;
+      if (++stage == STAGES) { stage = 0; phase ^= 1; }
+    }
+    __syncwarp();
+  } else if (warp >= MOE_EPI_WARPS && warp < MOE_EPI_WARPS + MOE_ROW_WARPS) {
+    // ------------------------------------------------------------------ rows of A
+    constexpr int PER = Cfg::ROWS / 16;                             // rows of a thread
+    const int i = threadIdx.x - MOE_EPI_WARPS * 32, c16 = i & 7, r0 = i >> 3;     // 16-byte column, first row
+    const uint32_t dst0 = ptx::smem_u32(smem) + Cfg::W_BYTES + r0 * GEMM_BK_BYTES + ((c16 ^ (r0 & 7)) << 4);
+    const uint32_t bar0 = PAIR ? ptx::mapa(ptx::smem_u32(full), 0) : ptx::smem_u32(full);
+    int stage = 0; uint32_t phase = 0; bool ok = true;
+    int said = 0, behind = 0;                                       // stage to announce next, k-blocks not announced yet
+    auto announce = [&]() {
+      ptx::fence_proxy_async_smem();                                // this thread's copies, seen by the tensor core
+      __syncwarp();
+      if (lane == 0) {
+        if constexpr (PAIR) ptx::mbar_arrive_cluster(bar0 + 8 * said);
+        else ptx::mbar_arrive(&full[said]);
+      }
+      if (++said == STAGES) said = 0;
+      --behind;
+    };
+    for (int t = group_id; t < num_tiles && ok; t += groups) {
+      const MoeTile w = tile_at(t);
+      if (w.rows <= 0) continue;
+      // of a pair, each CTA loads half of the N side
+      const int half = (w.rows + Cfg::STEP - 1) / Cfg::STEP * (Cfg::STEP / (PAIR ? 2 : 1));
+      const int lo = (int)rank * half, n = min(half, w.rows - lo);
+      const uint8_t* src[PER];
+#pragma unroll
+      for (int s = 0; s < PER; ++s) {
+        const int r = r0 + 16 * s;
+        src[s] = nullptr;
+        if (r < n) {
+          int at = w.row0 + lo + r;
+          if (p.token) {
+            at = p.token[at];
+            if ((unsigned)at >= (unsigned)p.a_rows) {
+              if (c16 == 0) atomicExch(p.err, ERR_BAD_EXPERT);
+              at = at < 0 ? 0 : p.a_rows - 1;
+            }
+          }
+          src[s] = p.A + (long long)at * p.a_ld + c16 * 16;
+        }
+      }
+      for (int kb = 0; kb < p.num_kb; ++kb) {
+        if (!__all_sync(0xffffffffu, ptx::mbar_wait(&empty[stage], phase ^ 1, p.err, 0xD00 | stage))) { ok = false; break; }
+        const int x = kb * GEMM_BK_BYTES;
+        const uint32_t bytes = x + c16 * 16 < p.k_bytes ? 16u : 0u;  // beyond K: zeros
+        const int xs = bytes ? x : 0;
+#pragma unroll
+        for (int s = 0; s < PER; ++s)
+          if (src[s]) cp_async16(dst0 + stage * Cfg::STAGE_BYTES + s * (16 * GEMM_BK_BYTES), src[s] + xs, bytes);
+        cp_async_commit();
+        ++behind;
+        if (behind > MOE_LAG) { cp_async_wait<MOE_LAG>(); announce(); }
+        if (++stage == STAGES) { stage = 0; phase ^= 1; }
+      }
+    }
+    cp_async_wait<0>();
+    while (behind > 0) announce();
+  } else if (warp == MOE_MMA_WARP) {
+    // ------------------------------------------------------------------ products (of a pair: the leader's)
+    if (rank == 0) {
+      const bool issue = ptx::elect_one();
+      constexpr uint64_t desc_base = ptx::smem_desc_base(16, 1024, ptx::SWZ_128B);
+      const uint64_t ad0 = ptx::smem_desc(desc_base, ptx::smem_u32(smem));
+      const uint64_t bd0 = ptx::smem_desc(desc_base, ptx::smem_u32(smem) + Cfg::W_BYTES);
+      int stage = 0; uint32_t phase = 0; bool ok = true;
+      int it = 0;
+      for (int t = group_id; t < num_tiles && ok; t += groups) {
+        const MoeTile w = tile_at(t);
+        if (w.rows <= 0) continue;
+        const uint32_t idesc = p.idesc | ((uint32_t)((w.rows + Cfg::STEP - 1) / Cfg::STEP * (Cfg::STEP / 8)) << 17);
+        const int as = it & 1;
+        const uint32_t aphase = (it >> 1) & 1;
+        ++it;
+        if (!ptx::mbar_wait(&acc_empty[as], aphase ^ 1, p.err, 0xE00 | as)) { ok = false; break; }
+        ptx::tc_fence_after();
+        const uint32_t d_tmem = tmem_base + as * MT;
+        for (int kb = 0; kb < p.num_kb; ++kb) {
+          if (!ptx::mbar_wait(&full[stage], phase, p.err, 0xE80 | stage)) { ok = false; break; }
+          ptx::tc_fence_after();
+          if (issue) {
+            const uint32_t so = (uint32_t)(stage * Cfg::STAGE_BYTES) >> 4;
+#pragma unroll
+            for (int k = 0; k < GEMM_BK_BYTES / 32; ++k) {
+              const uint64_t ad = ad0 + (so + 2 * k), bd = bd0 + (so + 2 * k);
+              const uint32_t acc = (kb | k) != 0 ? 1u : 0u;
+              if constexpr (PAIR) {
+                if constexpr (INT8) ptx::umma_i8_pair(d_tmem, ad, bd, idesc, acc);
+                else if (p.f8) ptx::umma_f8_pair(d_tmem, ad, bd, idesc, acc);
+                else ptx::umma_f16_pair(d_tmem, ad, bd, idesc, acc);
+              } else {
+                if constexpr (INT8) ptx::umma_i8(d_tmem, ad, bd, idesc, acc);
+                else if (p.f8) ptx::umma_f8(d_tmem, ad, bd, idesc, acc);
+                else ptx::umma_f16(d_tmem, ad, bd, idesc, acc);
+              }
+            }
+            if constexpr (PAIR) ptx::umma_commit_pair(&empty[stage], 3);
+            else ptx::umma_commit(&empty[stage]);
+          }
+          if (++stage == STAGES) { stage = 0; phase ^= 1; }
+        }
+        if (ok && issue) {
+          if constexpr (PAIR) ptx::umma_commit_pair(&acc_full[as], 3);
+          else ptx::umma_commit(&acc_full[as]);
+        }
+      }
+    }
+    __syncwarp();
+  } else if (warp < MOE_EPI_WARPS) {
+    // ------------------------------------------------------------------ epilogue
+    constexpr int COLS = GATED ? 64 : 128;                          // output columns of this CTA
+    constexpr int SHARE = MT / (2 * MOE_CHUNK);                     // chunks of a tile that this group takes, at most
+    const int quarter = warp & 3, group = warp >> 2, nl = quarter * 32 + lane;
+    float* rs_mine = reinterpret_cast<float*>(smem + Cfg::RS_AT) + warp * (MT / 2);
+    uint8_t* turn = smem + Cfg::TURN_AT + group * Cfg::TURN_BYTES;
+    const int es = p.out_dt == HERO_F16 || p.out_dt == HERO_BF16 ? 2 : 1;
+    MoeLane l;
+    l.up = GATED && (nl & 8);
+    l.turn = GATED ? ((nl >> 4) << 3) + (nl & 7) : nl;
+    bool ok = true;
+    int it = 0, turned = 0;
+    for (int t = group_id; t < num_tiles; t += groups) {
+      const MoeTile w = tile_at(t);
+      if (w.rows <= 0) continue;
+      const int c0 = (w.nt * (PAIR ? 2 : 1) + (int)rank) * COLS;    // first output column of this CTA
+      const int col = c0 + l.turn;
+      l.ok = col < p.n_out;
+      {
+        const long long at = (long long)w.e * p.N + col + (l.up ? p.n_out : 0);
+        l.cs = l.ok && p.cs ? __ldg(p.cs + at) : 1.0f;
+        l.bias = l.ok && p.bias ? __ldg(p.bias + at) : 0.0f;
+        l.post = l.ok && p.post ? __ldg(p.post + (long long)w.e * p.n_out + col) : 1.0f;
+        if (!GATED && p.act == HERO_ACT_NONE) { l.cs *= l.post; l.bias *= l.post; }   // (acc rs cs + b) post = acc rs (cs post) + b post
+      }
+      __syncwarp();                                                 // every lane is through with the last tile's row factors
+#pragma unroll
+      for (int k = 0; k < SHARE; ++k) {
+        const int r = (2 * k + group) * MOE_CHUNK + lane;
+        float f = 1.0f;
+        if (p.rs && r < w.rows) {
+          int at = w.row0 + r;
+          if (p.token) at = min(max(p.token[at], 0), p.a_rows - 1);
+          f = p.rs[at];
+        }
+        rs_mine[k * MOE_CHUNK + lane] = f;
+      }
+      __syncwarp();
+      const int as = it & 1;
+      const uint32_t aphase = (it >> 1) & 1;
+      ++it;
+      // a wait that gave up has recorded its code; the warp runs on without waiting again so that the kernel ends promptly
+      if (ok && !ptx::mbar_wait(&acc_full[as], aphase, p.err, 0xF00 | as)) ok = false;
+      ptx::tc_fence_after();
+      const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + as * MT;
+      float most = 0.f;
+      const int chunks = (w.rows + MOE_CHUNK - 1) / MOE_CHUNK;
+      for (int c = group, k = 0; c < chunks; c += 2, ++k) {
+        uint32_t r[32];
+        ptx::tmem_ld32(taddr + c * MOE_CHUNK, r);
+        ptx::tmem_ld_wait();
+        uint8_t* buf = turn + (turned & 1) * (MOE_CHUNK * Cfg::FEAT * 2);
+        ++turned;
+        const int rows = min(MOE_CHUNK, w.rows - c * MOE_CHUNK);
+        const float* rs = rs_mine + k * MOE_CHUNK;
+        switch (p.act) {
+          case HERO_ACT_GELU_ERF: moe_chunk_out<INT8, GATED, HERO_ACT_GELU_ERF>(p, r, rs, l, buf, rows, most); break;
+          case HERO_ACT_GELU_TANH: moe_chunk_out<INT8, GATED, HERO_ACT_GELU_TANH>(p, r, rs, l, buf, rows, most); break;
+          case HERO_ACT_SILU: moe_chunk_out<INT8, GATED, HERO_ACT_SILU>(p, r, rs, l, buf, rows, most); break;
+          default: moe_chunk_out<INT8, GATED, HERO_ACT_NONE>(p, r, rs, l, buf, rows, most); break;
+        }
+        // the group's four warps have written the chunk (the barrier also says that the buffer of two chunks ago is free)
+        asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory");
+        const int row_bytes = COLS * es, per_row = row_bytes >> 4;  // 16-byte pieces of a row
+        uint8_t* out = static_cast<uint8_t*>(p.out) + ((long long)(w.row0 + c * MOE_CHUNK) * p.out_ld + c0) * es;
+        const int left = (p.n_out - c0) * es;                       // bytes of a row inside the matrix
+        const int shift = __ffs(per_row) - 1;
+        for (int q = quarter * 32 + lane; q < rows * per_row; q += 128) {
+          const int row = q >> shift, piece = (q & (per_row - 1)) << 4;
+          if (piece < left)
+            *reinterpret_cast<uint4*>(out + (long long)row * p.out_ld * es + piece) = *reinterpret_cast<const uint4*>(buf + row * row_bytes + piece);
+        }
+      }
+      if (p.obs && l.ok && most > 0.f) atomicMax(reinterpret_cast<unsigned int*>(p.obs) + (long long)w.e * p.n_out + col, __float_as_uint(most));
+      // hand the accumulator back
+      ptx::tc_fence_before();
+      __syncwarp();
+      if (lane == 0) {
+        if constexpr (PAIR) ptx::mbar_arrive_cluster_relaxed(ptx::mapa(ptx::smem_u32(&acc_empty[as]), 0));
+        else ptx::mbar_arrive(&acc_empty[as]);
+      }
+    }
+  }
+
+  ptx::tc_fence_before();
+  __syncthreads();
+  if constexpr (PAIR) ptx::cluster_sync();                          // the peer may still be reading this CTA's shared memory / barriers
+  if (warp == MOE_MMA_WARP) {
+    if constexpr (PAIR) ptx::tmem_dealloc_pair(tmem_base, Cfg::TMEM_COLS);
+    else ptx::tmem_dealloc(tmem_base, Cfg::TMEM_COLS);
+  }
+}
+
+template <bool INT8, bool GATED>
+__global__ void __launch_bounds__(MOE_THREADS, 1) moe_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ MoeLinearParams p) {
+  moe_linear_body<INT8, GATED, false>(tmW, p);
+}
+template <bool INT8, bool GATED>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MOE_THREADS, 1)
+moe_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ MoeLinearParams p) {
+  moe_linear_body<INT8, GATED, true>(tmW, p);
+}
+
+template <bool INT8, bool GATED>
+static hero_status launch_moe_linear(hero_handle* h, const CUtensorMap& tmW, MoeLinearParams& p, bool pair, cudaStream_t s) {
+  const int feat = (pair ? 256 : 128) / (GATED ? 2 : 1);
+  p.num_nt = (p.n_out + feat - 1) / feat;
+  // a launch never needs more CTAs than an even deal of all rows over all experts could make tiles of
+  const int mt = pair ? MoeCfg<true>::MT : MoeCfg<false>::MT;
+  const long long most = ((long long)p.R / mt + (p.E < p.R ? p.E : p.R)) * p.num_nt;
+  const long long room = pair ? h->sm_count / 2 : h->sm_count;
+  const unsigned groups = (unsigned)(most < room ? most : room);
+  LaunchScope scope(h, s, KERNEL_GEMM);
+  if (pair) {
+    auto kern = moe_linear_pair_kernel<INT8, GATED>;
+    HERO_SMEM_OPT_IN(h, kern, MoeCfg<true>::SMEM_BYTES);
+    HERO_CUDA(launch_dependent(kern, dim3(2 * groups), dim3(MOE_THREADS), MoeCfg<true>::SMEM_BYTES, s, tmW, p));
+  } else {
+    auto kern = moe_linear_kernel<INT8, GATED>;
+    HERO_SMEM_OPT_IN(h, kern, MoeCfg<false>::SMEM_BYTES);
+    HERO_CUDA(launch_dependent(kern, dim3(groups), dim3(MOE_THREADS), MoeCfg<false>::SMEM_BYTES, s, tmW, p));
+  }
+  return HERO_OK;
+}
+
+}  // namespace hero
+
+extern "C" hero_status hero_moe_linear(hero_handle* h, const hero_moe_linear_args* a, void* stream) {
+  using namespace hero;
+  HERO_REQUIRE(h && a, HERO_ERR_INVALID_ARG, "hero_moe_linear: NULL handle or args");
+  hero_status st;
+  if ((st = check_matrix(a->A, "A")) != HERO_OK) return st;
+  if ((st = check_matrix(a->out, "out")) != HERO_OK) return st;
+  const bool int8 = a->A.dtype == HERO_I8, f8 = a->A.dtype == HERO_F8, q8 = int8 || f8;
+  HERO_REQUIRE(q8 || is_fp16ish(a->A.dtype), HERO_ERR_UNSUPPORTED, "A dtype %d: INT8, e4m3, F16 or BF16 expected", a->A.dtype);
+  const int eb = q8 ? 1 : 2;
+  const int64_t K = a->A.cols, N = a->N, E = a->n_experts, R = a->out.rows;
+  HERO_REQUIRE(E >= 1 && E <= MOE_MAX_E, HERO_ERR_UNSUPPORTED, "n_experts=%lld: 1 to %d", (long long)E, MOE_MAX_E);
+  HERO_REQUIRE(a->gated == 0 || a->gated == 1, HERO_ERR_INVALID_ARG, "gated=%d", a->gated);
+  HERO_REQUIRE(N > 0 && N % (a->gated ? 32 : 16) == 0, HERO_ERR_UNSUPPORTED, "N=%lld must be a positive multiple of %d", (long long)N, a->gated ? 32 : 16);
+  HERO_REQUIRE((K * eb) % 16 == 0, HERO_ERR_UNSUPPORTED, "K=%lld: K * element size must be a multiple of 16 bytes", (long long)K);
+  HERO_REQUIRE(a->W != nullptr && aligned16(a->W), a->W ? HERO_ERR_ALIGNMENT : HERO_ERR_INVALID_ARG, "W must be a 16-byte aligned device pointer");
+  HERO_REQUIRE(K < (1ll << 30) && N < (1ll << 30) && R < (1ll << 31) && a->A.rows < (1ll << 31), HERO_ERR_UNSUPPORTED, "dimension too large");
+  HERO_REQUIRE(a->ldw >= K && (a->ldw * eb) % 16 == 0, HERO_ERR_ALIGNMENT, "ldw=%lld invalid", (long long)a->ldw);
+  HERO_REQUIRE(E == 1 || (a->expert_stride >= K && (a->expert_stride * eb) % 16 == 0), HERO_ERR_ALIGNMENT, "expert_stride=%lld invalid",
+               (long long)a->expert_stride);
+  HERO_REQUIRE(a->ldw < (1ll << 38) / N && a->expert_stride < (1ll << 38), HERO_ERR_UNSUPPORTED, "weights too far apart");
+  const int64_t n_out = a->gated ? N / 2 : N;
+  HERO_REQUIRE(a->out.cols == n_out, HERO_ERR_INVALID_ARG, "out has %lld columns, %lld expected", (long long)a->out.cols, (long long)n_out);
+  HERO_REQUIRE(a->token || a->A.rows == R, HERO_ERR_INVALID_ARG, "without token A and out have the same rows (%lld, %lld)", (long long)a->A.rows, (long long)R);
+  HERO_REQUIRE(is_q8(a->out.dtype) || is_fp16ish(a->out.dtype), HERO_ERR_UNSUPPORTED, "out dtype %d", a->out.dtype);
+  HERO_REQUIRE(a->out.dtype != HERO_F8 || !int8, HERO_ERR_UNSUPPORTED, "an e4m3 output needs e4m3 or FP operands");
+  HERO_REQUIRE(a->out.dtype != HERO_I8 || !f8, HERO_ERR_UNSUPPORTED, "an INT8 output needs INT8 or FP operands");
+  HERO_REQUIRE(!(is_q8(a->out.dtype) && a->out.gran == HERO_GRAN_TWQ), HERO_ERR_UNSUPPORTED,
+               "a token-wise (TWQ) output needs a row reduction, which is kept out of GEMM epilogues (Sec. 2.1)");
+  HERO_REQUIRE(!q8 || a->w_scale, HERO_ERR_INVALID_ARG, "w_scale is required");
+  HERO_REQUIRE(a->act >= HERO_ACT_NONE && a->act <= HERO_ACT_SILU, HERO_ERR_INVALID_ARG, "unknown activation %d", a->act);
+  HERO_REQUIRE(a->out_col_absmax == nullptr || is_fp16ish(a->out.dtype), HERO_ERR_UNSUPPORTED, "out_col_absmax observes an F16 / BF16 output");
+  HERO_REQUIRE(a->offset, HERO_ERR_INVALID_ARG, "offset is required");
+  if (R == 0) return HERO_OK;
+  HERO_REQUIRE(a->A.rows > 0, HERO_ERR_INVALID_ARG, "A has no rows");
+  if ((st = check_device(h)) != HERO_OK) return st;
+
+  MoeLinearParams p;
+  memset(&p, 0, sizeof(p));
+  p.R = (int)R; p.a_rows = (int)a->A.rows; p.E = (int)E; p.N = (int)N; p.n_out = (int)n_out; p.K = (int)K;
+  p.k_bytes = (int)(K * eb);
+  p.num_kb = (p.k_bytes + GEMM_BK_BYTES - 1) / GEMM_BK_BYTES;
+  p.offset = a->offset; p.token = a->token;
+  p.A = static_cast<const uint8_t*>(a->A.data); p.a_ld = a->A.ld * eb;
+  p.rs = q8 && a->A.gran == HERO_GRAN_TWQ ? a->A.scale : nullptr;
+  p.cs = q8 ? a->w_scale : nullptr;
+  p.bias = a->bias; p.post = a->post_scale;
+  p.out = a->out.data; p.out_ld = a->out.ld; p.out_dt = a->out.dtype;
+  p.act = a->act; p.f8 = f8 ? 1 : 0;
+  p.kelems = GEMM_BK_BYTES / eb;
+  p.obs = a->out_col_absmax;
+  p.err = h->d_error;
+  CUtensorMap tmW;
+  st = make_tmap_experts(h, &tmW, a->W, a->A.dtype, a->gated != 0, N, K, E, a->ldw, E == 1 ? N * a->ldw : a->expert_stride);
+  if (st != HERO_OK) return st;
+  // A pair's tile takes up to 256 rows of an expert, a single CTA's 64: few rows an expert leave the pair's column half idle
+  const bool pair = R > 32 * E;
+  const uint32_t bf = a->A.dtype == HERO_BF16 ? 1 : 0;
+  const int m = pair ? 256 : 128;
+  p.idesc = int8 ? ptx::make_idesc(2, 1, 1, 0, 0, m, 0) : f8 ? ptx::make_idesc(1, 0, 0, 0, 0, m, 0) : ptx::make_idesc(1, bf, bf, 0, 0, m, 0);
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (int8) return a->gated ? launch_moe_linear<true, true>(h, tmW, p, pair, s) : launch_moe_linear<true, false>(h, tmW, p, pair, s);
+  return a->gated ? launch_moe_linear<false, true>(h, tmW, p, pair, s) : launch_moe_linear<false, false>(h, tmW, p, pair, s);
+}

@@ -15,7 +15,7 @@ _LIB_PATH = os.path.join(_HERE, "libhero.so")
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_ALIGNMENT, ERR_WORKSPACE, ERR_CUDA, ERR_DEVICE_TIMEOUT = range(7)
 I8, U8, I32, F16, BF16, F32 = range(6)
 GRAN_NONE, GRAN_TWQ, GRAN_FWQ, GRAN_SQ = range(4)
-ACT_NONE, ACT_GELU_ERF, ACT_GELU_TANH = range(3)
+ACT_NONE, ACT_GELU_ERF, ACT_GELU_TANH, ACT_SILU = range(4)
 MASK_NONE, MASK_CAUSAL = range(2)
 POST_LN, PRE_LN = range(2)
 MODE_INT8, MODE_FP = range(2)
@@ -26,7 +26,7 @@ F8 = 6                      # e4m3 payload of the FP8 variant
 _DT = {torch.int8: I8, torch.uint8: U8, torch.int32: I32, torch.float16: F16, torch.bfloat16: BF16,
        torch.float32: F32, torch.float8_e4m3fn: F8}
 GRAN = {"none": GRAN_NONE, "twq": GRAN_TWQ, "fwq": GRAN_FWQ, "sq": GRAN_SQ, "fp": GRAN_NONE}
-ACT = {"none": ACT_NONE, "gelu_erf": ACT_GELU_ERF, "gelu_tanh": ACT_GELU_TANH}
+ACT = {"none": ACT_NONE, "gelu_erf": ACT_GELU_ERF, "gelu_tanh": ACT_GELU_TANH, "silu": ACT_SILU}   # silu: hero_moe_linear only
 MASK = {"none": MASK_NONE, "causal": MASK_CAUSAL}
 FPDT = {"f16": F16, "bf16": BF16}
 TORCH_FP = {"f16": torch.float16, "bf16": torch.bfloat16}
@@ -125,6 +125,24 @@ class QkNormRopeArgs(C.Structure):
                 ("k_gamma", C.c_void_p), ("pos", C.c_void_p), ("cos", C.c_void_p), ("sin", C.c_void_p), ("n_pos", C.c_int64)]
 
 
+class MoeRouteArgs(C.Structure):
+    _fields_ = [("logits", Tensor), ("n_tokens", C.c_void_p), ("select_bias", C.c_void_p), ("top_k", C.c_int32), ("score", C.c_int32),
+                ("renorm", C.c_int32), ("scale", C.c_float), ("expert", C.c_void_p), ("weight", C.c_void_p), ("offset", C.c_void_p),
+                ("token", C.c_void_p), ("row", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
+class MoeLinearArgs(C.Structure):
+    _fields_ = [("A", Tensor), ("token", C.c_void_p), ("offset", C.c_void_p), ("W", C.c_void_p), ("N", C.c_int64), ("ldw", C.c_int64),
+                ("expert_stride", C.c_int64), ("n_experts", C.c_int32), ("w_scale", C.c_void_p), ("bias", C.c_void_p), ("act", C.c_int32),
+                ("gated", C.c_int32), ("post_scale", C.c_void_p), ("out", Tensor), ("out_col_absmax", C.c_void_p)]
+
+
+class MoeCombineArgs(C.Structure):
+    _fields_ = [("y", Tensor), ("row", C.c_void_p), ("weight", C.c_void_p), ("expert", C.c_void_p), ("top_k", C.c_int32), ("n_experts", C.c_int32),
+                ("residual", Tensor), ("shared", Tensor), ("gamma", C.c_void_p), ("beta", C.c_void_p), ("eps", C.c_float), ("out", Tensor),
+                ("fp_out", Tensor)]
+
+
 class LayerLayout(C.Structure):
     _fields_ = [(n, C.c_size_t) for n in ("qkv", "x_attn", "x_o", "x_mid", "x_mid_scale", "a", "x_2", "x_in", "x_in_scale",
                                           "h_in", "h_mid", "total")]
@@ -132,6 +150,7 @@ class LayerLayout(C.Structure):
 
 P_MODE = {"static": 0, "rowmax": 1}
 PAIRING = {"halves": 0, "adjacent": 1}
+SCORE = {"softmax": 0, "sigmoid": 1}
 HIST_BINS = 2048
 
 EXPORTS = ("hero_create", "hero_destroy", "hero_last_error", "hero_check", "hero_launch_count",
@@ -140,7 +159,8 @@ EXPORTS = ("hero_create", "hero_destroy", "hero_last_error", "hero_check", "hero
            "hero_profile_end", "hero_layer_forward_static", "hero_absmax_observe", "hero_quantize_weight", "hero_abs_histogram",
            "hero_int8_decode_attention", "hero_layer_decode", "hero_static_check", "hero_int8_attention_probe", "hero_stack_forward",
            "hero_stack_forward_host_async", "hero_quantize_weight_f8", "hero_block_cache_append", "hero_block_cache_read",
-           "hero_block_attention_workspace_bytes", "hero_block_attention", "hero_qk_norm_rope")
+           "hero_block_attention_workspace_bytes", "hero_block_attention", "hero_qk_norm_rope", "hero_moe_route_workspace_bytes",
+           "hero_moe_route", "hero_moe_linear", "hero_moe_combine")
 
 _lib = None
 
@@ -199,6 +219,10 @@ def lib():
                                                            C.POINTER(C.c_size_t)]
         L.hero_block_attention.argtypes = [C.c_void_p, C.POINTER(BlockCache), C.POINTER(BlockAttnArgs), C.c_void_p]
         L.hero_qk_norm_rope.argtypes = [C.c_void_p, C.POINTER(QkNormRopeArgs), C.c_void_p]
+        L.hero_moe_route_workspace_bytes.argtypes = [C.c_void_p, C.c_int64, C.c_int32, C.c_int32, C.POINTER(C.c_size_t)]
+        L.hero_moe_route.argtypes = [C.c_void_p, C.POINTER(MoeRouteArgs), C.c_void_p]
+        L.hero_moe_linear.argtypes = [C.c_void_p, C.POINTER(MoeLinearArgs), C.c_void_p]
+        L.hero_moe_combine.argtypes = [C.c_void_p, C.POINTER(MoeCombineArgs), C.c_void_p]
         L.hero_profile_begin.argtypes = [C.c_void_p, C.c_int32]
         L.hero_profile_end.argtypes = [C.c_void_p, C.POINTER(C.c_float), C.POINTER(C.c_int32), C.POINTER(C.c_int32)]
         _lib = L
@@ -452,6 +476,75 @@ class Handle:
                            eps, at(q_gamma, f32, "q_gamma"), at(k_gamma, f32, "k_gamma"), at(pos, torch.int32, "pos"), at(cos, f32, "cos"),
                            at(sin, f32, "sin"), n_pos)
         _check(self._lib.hero_qk_norm_rope(self._h, C.byref(a), self._raw_stream(stream)))
+
+    # ---- a mixture of experts (lean for the same reason)
+    def _pairs(self, t, dtype, shape, name):
+        """Address of a contiguous table of the given type and shape on the handle's device; None -> absent."""
+        if t is not None and tuple(t.shape) != shape:
+            _refuse("%s: shape %s is needed, got %s" % (name, shape, tuple(t.shape)))
+        return self._address(t, dtype, name)
+
+    def hero_moe_route_workspace_bytes(self, tokens, n_experts, top_k):
+        """Bytes that serve every call with these experts and at most this many tokens."""
+        n = C.c_size_t()
+        _check(self._lib.hero_moe_route_workspace_bytes(self._h, tokens, n_experts, top_k, C.byref(n)))
+        return int(n.value)
+
+    def hero_moe_route(self, logits, expert, weight, offset, token, row, score="softmax", renorm=True, scale=1.0, select_bias=None,
+                       n_tokens=None, workspace=None, stream=None):
+        """logits: hero.Tensor (F32 / F16 / BF16 [tokens, experts]); written: expert, row int32 [tokens, k], weight float32 [tokens, k],
+        offset int32 [experts + 1], token int32 [tokens * k]; select_bias: float32 [experts]; n_tokens: int32 [1] device tensor (a padded
+        batch); workspace: 1-D uint8 tensor of hero_moe_route_workspace_bytes (may be empty or None when that is 0)."""
+        self._here(logits)
+        T, E, at, i32 = logits.rows, logits.cols, self._pairs, torch.int32
+        if expert.dim() != 2 or expert.shape[0] != T:
+            _refuse("expert: [tokens, k]")
+        k, ws, n = expert.shape[1], None, 0
+        if workspace is not None and workspace.numel():
+            ws, n = self._address(workspace, torch.uint8, "workspace"), workspace.numel()
+        a = MoeRouteArgs(logits, at(n_tokens, i32, (1,), "n_tokens"), at(select_bias, torch.float32, (E,), "select_bias"), k,
+                         SCORE[score] if isinstance(score, str) else score, int(renorm), scale, at(expert, i32, (T, k), "expert"),
+                         at(weight, torch.float32, (T, k), "weight"), at(offset, i32, (E + 1,), "offset"), at(token, i32, (T * k,), "token"),
+                         at(row, i32, (T, k), "row"), ws, n)
+        _check(self._lib.hero_moe_route(self._h, C.byref(a), self._raw_stream(stream)))
+
+    def hero_moe_linear(self, A, W, out, offset, token=None, w_scale=None, bias=None, act="none", gated=False, post_scale=None,
+                        out_col_absmax=None, stream=None):
+        """A, out: hero.Tensor; W: [experts, N, K] of A's type (K contiguous); offset: int32 [experts + 1]; token: int32 [rows of out] (None: A is in
+        sorted order); w_scale, bias: float32 [experts, N]; post_scale, out_col_absmax: float32 [experts, columns of out]."""
+        self._here(A, out)
+        if W.dim() != 3 or W.stride(2) != 1 or W.shape[2] != A.cols or W.get_device() != self._device or _DT.get(W.dtype) != A.dtype:
+            _refuse("W: [experts, N, K = %d] of A's type on the handle's device, K contiguous" % A.cols)
+        E, N, K = W.shape
+        at, f32 = self._pairs, torch.float32
+        a = MoeLinearArgs(A, at(token, torch.int32, (out.rows,), "token"), at(offset, torch.int32, (E + 1,), "offset"), W.data_ptr(), N,
+                          W.stride(1) if N > 1 else max(W.stride(1), K), W.stride(0), E, at(w_scale, f32, (E, N), "w_scale"), at(bias, f32, (E, N), "bias"),
+                          ACT[act] if isinstance(act, str) else act, int(gated), at(post_scale, f32, (E, out.cols), "post_scale"), out,
+                          at(out_col_absmax, f32, (E, out.cols), "out_col_absmax"))
+        _check(self._lib.hero_moe_linear(self._h, C.byref(a), self._raw_stream(stream)))
+
+    def hero_moe_combine(self, y, row, weight, expert=None, residual=None, shared=None, out=None, fp_out=None, gamma=None, beta=None, eps=1e-5,
+                         stream=None):
+        """y: hero.Tensor of the sorted rows (F16 / BF16, or I8 / F8 with a static scale or, "fwq", one of [experts, H]); row, expert: int32 [tokens, k],
+        weight: float32 [tokens, k], as hero_moe_route leaves them; residual, shared, out, fp_out: hero.Tensor [tokens, H] or None;
+        gamma, beta: float32 [H], with out."""
+        self._here(y, *(t for t in (residual, shared, out, fp_out) if t is not None))
+        like, at, i32, f32 = out or fp_out, self._pairs, torch.int32, torch.float32
+        if like is None or row.dim() != 2 or row.shape[0] != like.rows:
+            _refuse("out or fp_out is needed, row: [tokens, k]")
+        E, shape = 0, tuple(row.shape)
+        if y.gran == GRAN_FWQ:
+            scale = y._keep[1]
+            if scale is None or scale.dim() != 2 or scale.shape[1] != y.cols:
+                _refuse("y: the feature-wise scale is [experts, H]")
+            E = scale.shape[0]
+        for t, n in ((residual, like.rows), (shared, like.rows), (out, like.rows)):
+            if t is not None and t.gran in (GRAN_TWQ, GRAN_FWQ) and t._keep[1] is not None and t._keep[1].numel() != (n if t.gran == GRAN_TWQ else t.cols):
+                _refuse("a token-wise scale has one entry per token, a feature-wise one per feature")
+        a = MoeCombineArgs(y, at(row, i32, shape, "row"), at(weight, f32, shape, "weight"), at(expert, i32, shape, "expert"), shape[1], E,
+                           residual or _ABSENT, shared or _ABSENT, at(gamma, f32, (like.cols,), "gamma"), at(beta, f32, (like.cols,), "beta"), eps,
+                           out or _ABSENT, fp_out or _ABSENT)
+        _check(self._lib.hero_moe_combine(self._h, C.byref(a), self._raw_stream(stream)))
 
     def hero_layer_workspace_bytes(self, desc, M):
         n = C.c_size_t()
