@@ -141,16 +141,16 @@ hero_status make_tmap_experts(const hero_handle* h, CUtensorMap* out, const void
     *out = slot.map;
     return HERO_OK;
   }
-  const cuuint32_t halves = gated ? 2 : 1;
-  cuuint64_t dims[5] = {(cuuint64_t)K, 8, halves, (cuuint64_t)(N / (8 * halves)), (cuuint64_t)E};
-  cuuint64_t strides[4] = {(cuuint64_t)(ldw * eb), (cuuint64_t)(gated ? N / 2 * ldw * eb : ldw * eb), (cuuint64_t)(8 * ldw * eb),
-                           (cuuint64_t)(expert_stride * eb)};
-  cuuint32_t box[5] = {(cuuint32_t)(128 / eb), 8, halves, 16 / halves, 1};
-  cuuint32_t estr[5] = {1, 1, 1, 1, 1};
+  const cuuint64_t row = (cuuint64_t)(ldw * eb), expert = (cuuint64_t)(expert_stride * eb);
+  const cuuint32_t inner = (cuuint32_t)(128 / eb), rank = gated ? 5 : 3;
+  const cuuint64_t dims3[3] = {(cuuint64_t)K, (cuuint64_t)N, (cuuint64_t)E}, strides3[2] = {row, expert};
+  const cuuint64_t dims5[5] = {(cuuint64_t)K, 8, 2, (cuuint64_t)(N / 16), (cuuint64_t)E}, strides5[4] = {row, (cuuint64_t)(N / 2) * row, 8 * row, expert};
+  const cuuint32_t box3[3] = {inner, 128, 1}, box5[5] = {inner, 8, 2, 8, 1}, estr[5] = {1, 1, 1, 1, 1};
   const CUtensorMapDataType dt = eb == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8
                                          : dtype == HERO_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
   CUresult r = reinterpret_cast<encode_tiled_fn>(h->encode_tiled)(
-      out, dt, 5, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+      out, dt, rank, const_cast<void*>(base), gated ? dims5 : dims3, gated ? strides5 : strides3, gated ? box5 : box3, estr,
+      CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
       CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   HERO_REQUIRE(r == CUDA_SUCCESS, HERO_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d) for experts' weights: N=%lld K=%lld E=%lld ldw=%lld stride=%lld",
                (int)r, (long long)N, (long long)K, (long long)E, (long long)ldw, (long long)expert_stride);

@@ -7,11 +7,13 @@
 // registers and the row factors are broadcasts.
 //
 // A CTA (or a pair of them, tcgen05 cta_group::2, 128 features each) is persistent over tiles of (expert, rows of the expert, features).  The
-// rows of an expert are dealt evenly to as few tiles as they need.  Twelve working warps and two that issue:
+// rows of an expert are dealt evenly to as few tiles as they need.  Twelve working warps and three that pass work on:
 //   warps 0-7   epilogue: tensor memory -> registers -> scales, activation, rounding -> shared memory (turned) -> whole row segments out
-//   warps 8-11  rows of A, picked by token, to shared memory (cp.async, in the operand's 128-byte swizzle)
+//   warps 8-11  rows of A, picked by token (TMA, four rows a copy)
 //   warp  12    W tiles (TMA)
 //   warp  13    products (one elected lane) and the owner of the tensor memory
+// Rows that warps copy themselves (cp.async) need a hand-off from those warps to the tensor core, whose chain is longer than five stages hide: 1850
+// cycles a k-block, against 512 that the products take.
 // The accumulator is double-buffered.  Every wait is bounded; on expiry the CTA records a code and unwinds.
 //
 // Gated products (act(gate) * up): a tile's 128 rows of W are eight rows of the gate's half and eight of the other in turn (one
@@ -24,14 +26,11 @@ namespace hero {
 constexpr int MOE_MAX_E = 512;
 constexpr int MOE_EPI_WARPS = 8, MOE_ROW_WARPS = 4, MOE_W_WARP = 12, MOE_MMA_WARP = 13, MOE_THREADS = 14 * 32;
 constexpr int MOE_CHUNK = 32;                 // rows that an epilogue group turns at a time
-constexpr int MOE_LAG = 3;                    // k-blocks of rows in flight per row warp before the oldest is announced
 
 struct MoeLinearParams {
   int R, a_rows, E, N, n_out, K;              // K in elements
   int num_kb, num_nt;                         // 128-byte steps of K, feature tiles of an expert
   const int* offset; const int* token;
-  const uint8_t* A; long long a_ld;           // bytes
-  int k_bytes;
   const float* rs; const float* cs; const float* bias; const float* post;
   void* out; long long out_ld; int out_dt;
   int act, f8;                                // f8: e4m3 operands
@@ -78,6 +77,19 @@ __device__ __forceinline__ MoeTile moe_tile(const MoeLinearParams& p, const int*
   r.row0 = first[lo] + i * per;
   r.rows = min(per, n - i * per);             // may be 0 or less where an even share rounds up: such a tile is skipped
   return r;
+}
+
+// Rows of a tile that a CTA loads, in groups of four: of a pair, each has half of the N side.  Every row warp takes part in every stage, with a group
+// that nobody needs if there are too few: a warp without one could fall two uses of a stage behind, where a barrier's parity repeats.
+struct MoeShare { int lo, fours; };           // first row in the tile, groups
+template <bool PAIR>
+__device__ __forceinline__ MoeShare moe_share(const MoeTile& w, int rank) {
+  constexpr int STEP = MoeCfg<PAIR>::STEP;
+  const int half = (w.rows + STEP - 1) / STEP * (STEP / (PAIR ? 2 : 1));
+  MoeShare s;
+  s.lo = rank * half;
+  s.fours = max(MOE_ROW_WARPS, (min(half, w.rows - s.lo) + 3) >> 2);
+  return s;
 }
 
 // (a denominator beyond 2^126 gives 0, which is what v e^v rounds to there)
@@ -159,26 +171,39 @@ __device__ __forceinline__ void moe_chunk_out(const MoeLinearParams& p, const ui
   else moe_chunk<INT8, GATED, ACT, OUT_FP>(p, r, rs, l, buf, rows, most);
 }
 
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, uint32_t bytes) {   // the other 16 - bytes become zero
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+// four rows of A, 128 bytes of each
+template <bool PAIR>
+__device__ __forceinline__ void load_rows(uint32_t dst, const CUtensorMap* m, int x, const int (&r)[4], uint32_t bar) {
+  if constexpr (PAIR)
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
+                 ::"r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(x), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(bar) : "memory");
+  else
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
+                 ::"r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(x), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(bar) : "memory");
 }
-__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
-__device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap* m, int x, int g, int e, uint32_t bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
-      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(x), "r"(0), "r"(0), "r"(g), "r"(e), "r"(bar) : "memory");
-}
-__device__ __forceinline__ void tma_load_5d_pair(uint32_t dst, const CUtensorMap* m, int x, int g, int e, uint32_t bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.5d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
-      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(x), "r"(0), "r"(0), "r"(g), "r"(e), "r"(bar) : "memory");
+// 128 rows of one expert's W: row r0, or (gated) the r0-th group of eight rows of each half
+template <bool GATED, bool PAIR>
+__device__ __forceinline__ void load_w(uint32_t dst, const CUtensorMap* m, int x, int r0, int e, uint32_t bar) {
+  const uint64_t map = reinterpret_cast<uint64_t>(m);
+  if constexpr (GATED) {
+    if constexpr (PAIR)
+      asm volatile("cp.async.bulk.tensor.5d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %3, %4, %5}], [%6];"
+                   ::"r"(dst), "l"(map), "r"(x), "r"(0), "r"(r0), "r"(e), "r"(bar) : "memory");
+    else
+      asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %3, %4, %5}], [%6];"
+                   ::"r"(dst), "l"(map), "r"(x), "r"(0), "r"(r0), "r"(e), "r"(bar) : "memory");
+  } else {
+    if constexpr (PAIR)
+      asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                   ::"r"(dst), "l"(map), "r"(x), "r"(r0), "r"(e), "r"(bar) : "memory");
+    else
+      asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                   ::"r"(dst), "l"(map), "r"(x), "r"(r0), "r"(e), "r"(bar) : "memory");
+  }
 }
 
 template <bool INT8, bool GATED, bool PAIR>
-__device__ __forceinline__ void moe_linear_body(const CUtensorMap& tmW, const MoeLinearParams& p) {
+__device__ __forceinline__ void moe_linear_body(const CUtensorMap& tmW, const CUtensorMap& tmA, const MoeLinearParams& p) {
   using Cfg = MoeCfg<PAIR>;
   constexpr int MT = Cfg::MT, STAGES = Cfg::STAGES;
   extern __shared__ uint8_t smem_raw[];
@@ -196,7 +221,7 @@ __device__ __forceinline__ void moe_linear_body(const CUtensorMap& tmW, const Mo
   const int group_id = PAIR ? blockIdx.x >> 1 : blockIdx.x, groups = PAIR ? gridDim.x >> 1 : gridDim.x;
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < STAGES; ++i) { ptx::mbar_init(&full[i], 1 + MOE_ROW_WARPS * (PAIR ? 2 : 1)); ptx::mbar_init(&empty[i], 1); }
+    for (int i = 0; i < STAGES; ++i) { ptx::mbar_init(&full[i], 1); ptx::mbar_init(&empty[i], 1); }
     for (int i = 0; i < 2; ++i) { ptx::mbar_init(&acc_full[i], 1); ptx::mbar_init(&acc_empty[i], MOE_EPI_WARPS * (PAIR ? 2 : 1)); }
     ptx::fence_mbar_init();
   }
@@ -204,7 +229,7 @@ __device__ __forceinline__ void moe_linear_body(const CUtensorMap& tmW, const Mo
     if constexpr (PAIR) { ptx::tmem_alloc_pair(tmem_slot, Cfg::TMEM_COLS); ptx::tmem_relinquish_pair(); }
     else { ptx::tmem_alloc(tmem_slot, Cfg::TMEM_COLS); ptx::tmem_relinquish(); }
   }
-  if (warp == MOE_W_WARP && lane == 0) ptx::prefetch_tmap(&tmW);
+  if (warp == MOE_W_WARP && lane == 0) { ptx::prefetch_tmap(&tmW); ptx::prefetch_tmap(&tmA); }
   ptx::pdl_launch_dependents();
   ptx::pdl_wait();                                                  // the router's offsets (and all else) are there from here on
 
@@ -249,13 +274,15 @@ __device__ __forceinline__ void moe_linear_body(const CUtensorMap& tmW, const Mo
     for (int t = group_id; t < num_tiles && ok; t += groups) {
       const MoeTile w = tile_at(t);
       if (w.rows <= 0) continue;
-      const int g = (w.nt * (PAIR ? 2 : 1) + (int)rank) * (GATED ? 8 : 16);     // first group of eight rows (of each half)
+      const int r0 = (w.nt * (PAIR ? 2 : 1) + (int)rank) * (GATED ? 8 : 128);
+      // what both CTAs' copies of a k-block bring: whole groups of four rows
+      const MoeShare s0 = moe_share<PAIR>(w, 0), s1 = moe_share<PAIR>(w, 1);
+      const uint32_t bytes = (PAIR ? 2 : 1) * Cfg::W_BYTES + (uint32_t)(s0.fours + (PAIR ? s1.fours : 0)) * (4 * GEMM_BK_BYTES);
       for (int kb = 0; kb < p.num_kb; ++kb) {
         if (!ptx::mbar_wait(&empty[stage], phase ^ 1, p.err, 0xC00 | stage)) { ok = false; break; }
         if (issue) {
-          if (rank == 0) ptx::mbar_expect_tx(&full[stage], (PAIR ? 2 : 1) * Cfg::W_BYTES);
-          if constexpr (PAIR) tma_load_5d_pair(dst0 + stage * Cfg::STAGE_BYTES, &tmW, kb * p.kelems, g, w.e, bar0 + 8 * stage);
-          else tma_load_5d(dst0 + stage * Cfg::STAGE_BYTES, &tmW, kb * p.kelems, g, w.e, bar0 + 8 * stage);
+          if (rank == 0) ptx::mbar_expect_tx(&full[stage], bytes);
+          load_w<GATED, PAIR>(dst0 + stage * Cfg::STAGE_BYTES, &tmW, kb * p.kelems, r0, w.e, bar0 + 8 * stage);
         }
         if (++stage == STAGES) { stage = 0; phase ^= 1; }
       }
@@ -267,61 +294,52 @@ __device__ __forceinline__ void moe_linear_body(const CUtensorMap& tmW, const Mo
     __syncwarp();
   } else if (warp >= MOE_EPI_WARPS && warp < MOE_EPI_WARPS + MOE_ROW_WARPS) {
     // ------------------------------------------------------------------ rows of A
-    constexpr int PER = Cfg::ROWS / 16;                             // rows of a thread
-    const int i = threadIdx.x - MOE_EPI_WARPS * 32, c16 = i & 7, r0 = i >> 3;     // 16-byte column, first row
-    const uint32_t dst0 = ptx::smem_u32(smem) + Cfg::W_BYTES + r0 * GEMM_BK_BYTES + ((c16 ^ (r0 & 7)) << 4);
+    // warp ww has the groups ww, ww + 4, ..
+    constexpr int PER = Cfg::ROWS / (4 * MOE_ROW_WARPS);
+    const int ww = warp - MOE_EPI_WARPS;
+    const bool issue = ptx::elect_one();
+    const uint32_t dst0 = (PAIR ? ptx::mapa(ptx::smem_u32(smem), rank) : ptx::smem_u32(smem)) + Cfg::W_BYTES + ww * (4 * GEMM_BK_BYTES);
     const uint32_t bar0 = PAIR ? ptx::mapa(ptx::smem_u32(full), 0) : ptx::smem_u32(full);
     int stage = 0; uint32_t phase = 0; bool ok = true;
-    int said = 0, behind = 0;                                       // stage to announce next, k-blocks not announced yet
-    auto announce = [&]() {
-      ptx::fence_proxy_async_smem();                                // this thread's copies, seen by the tensor core
-      __syncwarp();
-      if (lane == 0) {
-        if constexpr (PAIR) ptx::mbar_arrive_cluster(bar0 + 8 * said);
-        else ptx::mbar_arrive(&full[said]);
-      }
-      if (++said == STAGES) said = 0;
-      --behind;
-    };
-    for (int t = group_id; t < num_tiles && ok; t += groups) {
+    int fours = 0, mine = 0;                                        // this warp's groups in the tile asked for (-1: no tile), this lane's row of A
+    auto ask = [&](int t) {
       const MoeTile w = tile_at(t);
-      if (w.rows <= 0) continue;
-      // of a pair, each CTA loads half of the N side
-      const int half = (w.rows + Cfg::STEP - 1) / Cfg::STEP * (Cfg::STEP / (PAIR ? 2 : 1));
-      const int lo = (int)rank * half, n = min(half, w.rows - lo);
-      const uint8_t* src[PER];
-#pragma unroll
-      for (int s = 0; s < PER; ++s) {
-        const int r = r0 + 16 * s;
-        src[s] = nullptr;
-        if (r < n) {
-          int at = w.row0 + lo + r;
-          if (p.token) {
-            at = p.token[at];
-            if ((unsigned)at >= (unsigned)p.a_rows) {
-              if (c16 == 0) atomicExch(p.err, ERR_BAD_EXPERT);
-              at = at < 0 ? 0 : p.a_rows - 1;
-            }
-          }
-          src[s] = p.A + (long long)at * p.a_ld + c16 * 16;
+      fours = -1;
+      if (w.rows <= 0) return;
+      const MoeShare sh = moe_share<PAIR>(w, (int)rank);
+      fours = (sh.fours - ww + MOE_ROW_WARPS - 1) / MOE_ROW_WARPS;
+      // (a group that is not full ends with other rows of the tile)
+      const int at = w.row0 + min(sh.lo + 4 * (ww + MOE_ROW_WARPS * (lane >> 2)) + (lane & 3), w.rows - 1);
+      mine = 0;
+      if (lane < 4 * fours) {
+        mine = p.token ? p.token[at] : at;
+        if ((unsigned)mine >= (unsigned)p.a_rows) {
+          atomicExch(p.err, ERR_BAD_EXPERT);
+          mine = mine < 0 ? 0 : p.a_rows - 1;
         }
       }
-      for (int kb = 0; kb < p.num_kb; ++kb) {
-        if (!__all_sync(0xffffffffu, ptx::mbar_wait(&empty[stage], phase ^ 1, p.err, 0xD00 | stage))) { ok = false; break; }
-        const int x = kb * GEMM_BK_BYTES;
-        const uint32_t bytes = x + c16 * 16 < p.k_bytes ? 16u : 0u;  // beyond K: zeros
-        const int xs = bytes ? x : 0;
+    };
+    if (group_id < num_tiles) ask(group_id);
+    for (int t = group_id; t < num_tiles && ok; t += groups) {
+      const int n4 = fours;
+      int r[PER][4];
 #pragma unroll
-        for (int s = 0; s < PER; ++s)
-          if (src[s]) cp_async16(dst0 + stage * Cfg::STAGE_BYTES + s * (16 * GEMM_BK_BYTES), src[s] + xs, bytes);
-        cp_async_commit();
-        ++behind;
-        if (behind > MOE_LAG) { cp_async_wait<MOE_LAG>(); announce(); }
+      for (int s = 0; s < PER; ++s)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[s][i] = __shfl_sync(0xffffffffu, mine, 4 * s + i);
+      if (t + groups < num_tiles) ask(t + groups);                  // the next tile's rows, while this one's are copied
+      if (n4 < 0) continue;
+      for (int kb = 0; kb < p.num_kb; ++kb) {
+        if (!ptx::mbar_wait(&empty[stage], phase ^ 1, p.err, 0xD00 | stage)) { ok = false; break; }
+        if (issue) {
+#pragma unroll
+          for (int s = 0; s < PER; ++s)
+            if (s < n4) load_rows<PAIR>(dst0 + stage * Cfg::STAGE_BYTES + s * (4 * GEMM_BK_BYTES * MOE_ROW_WARPS), &tmA, kb * p.kelems, r[s], bar0 + 8 * stage);
+        }
         if (++stage == STAGES) { stage = 0; phase ^= 1; }
       }
     }
-    cp_async_wait<0>();
-    while (behind > 0) announce();
+    __syncwarp();
   } else if (warp == MOE_MMA_WARP) {
     // ------------------------------------------------------------------ products (of a pair: the leader's)
     if (rank == 0) {
@@ -467,17 +485,18 @@ __device__ __forceinline__ void moe_linear_body(const CUtensorMap& tmW, const Mo
 }
 
 template <bool INT8, bool GATED>
-__global__ void __launch_bounds__(MOE_THREADS, 1) moe_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ MoeLinearParams p) {
-  moe_linear_body<INT8, GATED, false>(tmW, p);
+__global__ void __launch_bounds__(MOE_THREADS, 1) moe_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmA,
+                                                                    const __grid_constant__ MoeLinearParams p) {
+  moe_linear_body<INT8, GATED, false>(tmW, tmA, p);
 }
 template <bool INT8, bool GATED>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MOE_THREADS, 1)
-moe_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ MoeLinearParams p) {
-  moe_linear_body<INT8, GATED, true>(tmW, p);
+moe_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmA, const __grid_constant__ MoeLinearParams p) {
+  moe_linear_body<INT8, GATED, true>(tmW, tmA, p);
 }
 
 template <bool INT8, bool GATED>
-static hero_status launch_moe_linear(hero_handle* h, const CUtensorMap& tmW, MoeLinearParams& p, bool pair, cudaStream_t s) {
+static hero_status launch_moe_linear(hero_handle* h, const CUtensorMap& tmW, const CUtensorMap& tmA, MoeLinearParams& p, bool pair, cudaStream_t s) {
   const int feat = (pair ? 256 : 128) / (GATED ? 2 : 1);
   p.num_nt = (p.n_out + feat - 1) / feat;
   // a launch never needs more CTAs than an even deal of all rows over all experts could make tiles of
@@ -489,11 +508,11 @@ static hero_status launch_moe_linear(hero_handle* h, const CUtensorMap& tmW, Moe
   if (pair) {
     auto kern = moe_linear_pair_kernel<INT8, GATED>;
     HERO_SMEM_OPT_IN(h, kern, MoeCfg<true>::SMEM_BYTES);
-    HERO_CUDA(launch_dependent(kern, dim3(2 * groups), dim3(MOE_THREADS), MoeCfg<true>::SMEM_BYTES, s, tmW, p));
+    HERO_CUDA(launch_dependent(kern, dim3(2 * groups), dim3(MOE_THREADS), MoeCfg<true>::SMEM_BYTES, s, tmW, tmA, p));
   } else {
     auto kern = moe_linear_kernel<INT8, GATED>;
     HERO_SMEM_OPT_IN(h, kern, MoeCfg<false>::SMEM_BYTES);
-    HERO_CUDA(launch_dependent(kern, dim3(groups), dim3(MOE_THREADS), MoeCfg<false>::SMEM_BYTES, s, tmW, p));
+    HERO_CUDA(launch_dependent(kern, dim3(groups), dim3(MOE_THREADS), MoeCfg<false>::SMEM_BYTES, s, tmW, tmA, p));
   }
   return HERO_OK;
 }
@@ -539,10 +558,8 @@ extern "C" hero_status hero_moe_linear(hero_handle* h, const hero_moe_linear_arg
   MoeLinearParams p;
   memset(&p, 0, sizeof(p));
   p.R = (int)R; p.a_rows = (int)a->A.rows; p.E = (int)E; p.N = (int)N; p.n_out = (int)n_out; p.K = (int)K;
-  p.k_bytes = (int)(K * eb);
-  p.num_kb = (p.k_bytes + GEMM_BK_BYTES - 1) / GEMM_BK_BYTES;
+  p.num_kb = (int)((K * eb + GEMM_BK_BYTES - 1) / GEMM_BK_BYTES);
   p.offset = a->offset; p.token = a->token;
-  p.A = static_cast<const uint8_t*>(a->A.data); p.a_ld = a->A.ld * eb;
   p.rs = q8 && a->A.gran == HERO_GRAN_TWQ ? a->A.scale : nullptr;
   p.cs = q8 ? a->w_scale : nullptr;
   p.bias = a->bias; p.post = a->post_scale;
@@ -554,12 +571,16 @@ extern "C" hero_status hero_moe_linear(hero_handle* h, const hero_moe_linear_arg
   CUtensorMap tmW;
   st = make_tmap_experts(h, &tmW, a->W, a->A.dtype, a->gated != 0, N, K, E, a->ldw, E == 1 ? N * a->ldw : a->expert_stride);
   if (st != HERO_OK) return st;
+  CUtensorMap tmA;
+  st = make_tmap_2d(h, &tmA, a->A.data, eb, a->A.dtype == HERO_F16, a->A.dtype == HERO_BF16, (uint64_t)a->A.rows, (uint64_t)K, (uint64_t)a->A.ld * eb,
+                    GEMM_BK_BYTES / eb, 1, 128);
+  if (st != HERO_OK) return st;
   // A pair's tile takes up to 256 rows of an expert, a single CTA's 64: few rows an expert leave the pair's column half idle
   const bool pair = R > 32 * E;
   const uint32_t bf = a->A.dtype == HERO_BF16 ? 1 : 0;
   const int m = pair ? 256 : 128;
   p.idesc = int8 ? ptx::make_idesc(2, 1, 1, 0, 0, m, 0) : f8 ? ptx::make_idesc(1, 0, 0, 0, 0, m, 0) : ptx::make_idesc(1, bf, bf, 0, 0, m, 0);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (int8) return a->gated ? launch_moe_linear<true, true>(h, tmW, p, pair, s) : launch_moe_linear<true, false>(h, tmW, p, pair, s);
-  return a->gated ? launch_moe_linear<false, true>(h, tmW, p, pair, s) : launch_moe_linear<false, false>(h, tmW, p, pair, s);
+  if (int8) return a->gated ? launch_moe_linear<true, true>(h, tmW, tmA, p, pair, s) : launch_moe_linear<true, false>(h, tmW, tmA, p, pair, s);
+  return a->gated ? launch_moe_linear<false, true>(h, tmW, tmA, p, pair, s) : launch_moe_linear<false, false>(h, tmW, tmA, p, pair, s);
 }

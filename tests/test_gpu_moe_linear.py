@@ -170,3 +170,29 @@ def test_refusals_of_the_binding(h):
         with pytest.raises(hero.HeroError):
             h.hero_moe_linear(hero.tensor(A), out=hero.tensor(out), **dict(good, **bad))
     h.check()
+
+
+@pytest.mark.parametrize("gated", [False, True])
+def test_long_runs_of_ragged_tiles_repeat_themselves(h, gated):
+    # many tiles per CTA with few rows between full ones, in both forms of the kernel, launched behind one another and as a graph
+    g = np.random.default_rng(20)
+    K, N, E = 1040, 512, 64
+    for top in (600, 40):
+        counts = g.integers(0, top, E) * (g.random(E) < 0.8)
+        counts[:3] = 1, 257, 5
+        offset, token, offset_t, token_t = deal(g, counts, 500)
+        at, wt = to(g.standard_normal((500, K)) * 36, "i8")[0], to(g.standard_normal((E, N, K)) * 36, "i8")[0]
+        cs = torch.full((E, N), 1 / (36 * 36 * np.sqrt(K)), device="cuda")
+        ys = [torch.zeros(len(token), N // 2 if gated else N, dtype=torch.float16, device="cuda") for _ in range(2)]
+        call = lambda y: h.hero_moe_linear(hero.tensor(at), wt, hero.tensor(y), offset_t, token=token_t, w_scale=cs, act="silu", gated=gated)  # noqa: E731
+        call(ys[0])
+        side = torch.cuda.Stream()
+        with torch.cuda.stream(side):
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=side):
+                for _ in range(20):
+                    call(ys[1])
+        for _ in range(20):
+            graph.replay()
+        h.check()
+        assert torch.equal(*ys)
