@@ -660,7 +660,7 @@ hero_status hero_moe_route(hero_handle* h, const hero_moe_route_args* a, void* s
  *     a[r,j] = act(v[r,j]);  gated: a[r,j] = act(v[r,j]) * v[r, N/2 + j], j < N/2
  *     a     *= post_scale[e][j]                                                 (1 / S_a of the quantised hidden features; NULL = skip)
  *     out    = I8: clip(Round(a), -127, 127);  F8: saturating e4m3;  F16 / BF16: a rounded
- *   With one expert and no token the result is hero_w8a8_linear's (INT8 operands: bit for bit).
+ *   With one expert and no token the result is hero_w8a8_linear's (INT8 operands, no activation or GELU(erf): bit for bit).
  *   A      : I8 / F8 (TWQ: scale[rows], else no row factor) or F16 / BF16, [rows][K]; K times the element size a multiple of 16 bytes
  *   W      : device [E][N][K] of A's type, K contiguous, row pitch ldw, expert_stride elements from one expert to the next (both
  *            multiples of 16 bytes); N a multiple of 16, gated a multiple of 32 (rows 0 .. N/2 - 1: gate, the others: up).

@@ -7,25 +7,25 @@
 // registers and the row factors are broadcasts.
 //
 // A CTA (or a pair of them, tcgen05 cta_group::2, 128 features each) is persistent over tiles of (expert, rows of the expert, features).  The
-// rows of an expert are dealt evenly to as few tiles as they need.  Twelve working warps and three that pass work on:
-//   warps 0-7   epilogue: tensor memory -> registers -> scales, activation, rounding -> shared memory (turned) -> whole row segments out
-//   warps 8-11  rows of A, picked by token (TMA, four rows a copy)
-//   warp  12    W tiles (TMA)
-//   warp  13    products (one elected lane) and the owner of the tensor memory
+// rows of an expert are dealt evenly to as few tiles as they need.
+//   epilogue warps (8)  tensor memory -> registers -> scales, activation, rounding -> shared memory (turned) -> whole row segments out
+//   row warps (8; 2)    rows of A picked by token: TMA gathers of four rows.  One warp starts one every 80 cycles or so, a k-block takes 32 in 512
+//                       cycles: two row warps for each four gave 197 us where four gave 231 (8192 tokens, top 8 of 64, 2048 x 2048)
+//   load warp           W tiles, and A where its rows are in order (TMA)
+//   product warp        products (one elected lane); owns the tensor memory
 // Rows that warps copy themselves (cp.async) need a hand-off from those warps to the tensor core, whose chain is longer than five stages hide: 1850
-// cycles a k-block, against 512 that the products take.
-// The accumulator is double-buffered.  Every wait is bounded; on expiry the CTA records a code and unwinds.
+// cycles a k-block.  The accumulator is double-buffered.  Every wait is bounded; on expiry the CTA records a code and unwinds.
 //
-// Gated products (act(gate) * up): a tile's 128 rows of W are eight rows of the gate's half and eight of the other in turn (one
-// tensor map does that), so that gate and up of a feature lie eight lanes apart in the same warp.  The two lanes exchange one value for each
-// pair of rows; each then finishes one row of the pair.
+// Gated products (act(gate) * up): a tile's 128 rows of W are eight rows of the gate's half and eight of the other in turn (one tensor map does
+// that).  Read in the shape of 16 lanes x 256 bits, tensor memory then gives a thread both products of a feature for the same two rows.
 #include "gemm_common.cuh"
 
 namespace hero {
 
 constexpr int MOE_MAX_E = 512;
-constexpr int MOE_EPI_WARPS = 8, MOE_ROW_WARPS = 4, MOE_W_WARP = 12, MOE_MMA_WARP = 13, MOE_THREADS = 14 * 32;
+constexpr int MOE_EPI_WARPS = 8;
 constexpr int MOE_CHUNK = 32;                 // rows that an epilogue group turns at a time
+constexpr int MOE_TURN_PITCH = 2 * 128 + 16;  // bytes of a turned row at most (16 more than its values: rows two apart on banks of their own)
 
 struct MoeLinearParams {
   int R, a_rows, E, N, n_out, K;              // K in elements
@@ -48,7 +48,10 @@ struct MoeCfg {
   static constexpr int FEAT = 128;                        // features of this CTA
   static constexpr int W_BYTES = FEAT * GEMM_BK_BYTES, X_BYTES = ROWS * GEMM_BK_BYTES, STAGE_BYTES = W_BYTES + X_BYTES;
   static constexpr int STAGES = PAIR ? 5 : 7;
-  static constexpr int TURN_BYTES = 2 * MOE_CHUNK * FEAT * 2;             // per epilogue group: two buffers of 32 rows of 16-bit outputs
+  static constexpr int ROW_WARPS = PAIR ? 8 : 2;
+  static constexpr int ROW_WARP = MOE_EPI_WARPS, LOAD_WARP = ROW_WARP + ROW_WARPS, MMA_WARP = LOAD_WARP + 1, THREADS = (MMA_WARP + 1) * 32;
+  static constexpr int BOX = PAIR ? 64 : 16;              // rows of a copy where A is in order
+  static constexpr int TURN_BYTES = 2 * MOE_CHUNK * MOE_TURN_PITCH;       // per epilogue group: two buffers of 32 rows
   static constexpr int TMEM_COLS = 2 * MT;
   static constexpr int TURN_AT = STAGES * STAGE_BYTES;
   static constexpr int RS_AT = TURN_AT + 2 * TURN_BYTES;                  // [8 warps][MT / 2] row factors
@@ -81,35 +84,34 @@ __device__ __forceinline__ MoeTile moe_tile(const MoeLinearParams& p, const int*
 
 // Rows of a tile that a CTA loads, in groups of four: of a pair, each has half of the N side.  Every row warp takes part in every stage, with a group
 // that nobody needs if there are too few: a warp without one could fall two uses of a stage behind, where a barrier's parity repeats.
-struct MoeShare { int lo, fours; };           // first row in the tile, groups
+struct MoeShare { int lo, n, fours; };        // first row in the tile, rows (0 or less: none), groups
 template <bool PAIR>
 __device__ __forceinline__ MoeShare moe_share(const MoeTile& w, int rank) {
   constexpr int STEP = MoeCfg<PAIR>::STEP;
   const int half = (w.rows + STEP - 1) / STEP * (STEP / (PAIR ? 2 : 1));
   MoeShare s;
   s.lo = rank * half;
-  s.fours = max(MOE_ROW_WARPS, (min(half, w.rows - s.lo) + 3) >> 2);
+  s.n = min(half, w.rows - s.lo);
+  s.fours = max(MoeCfg<PAIR>::ROW_WARPS, (s.n + 3) >> 2);
   return s;
 }
 
 // (a denominator beyond 2^126 gives 0, which is what v e^v rounds to there)
 __device__ __forceinline__ float silu_f(float v) { return __fdividef(v, 1.0f + __expf(-v)); }
 
+// 0.5 v (1 + tanh(u)) = v / (1 + e^-2u), u = sqrt(2 / pi) (v + 0.044715 v^3)
+__device__ __forceinline__ float gelu_tanh_quotient(float v) {
+  return __fdividef(v, 1.0f + __expf(-1.59576912160573071176f * v * fmaf(0.044715f * v, v, 1.0f)));
+}
 template <int ACT>
 __device__ __forceinline__ float moe_act(float v) {
   if constexpr (ACT == HERO_ACT_GELU_ERF) return gelu_erf_f(v);
-  if constexpr (ACT == HERO_ACT_GELU_TANH) return gelu_tanh_f(v);
+  if constexpr (ACT == HERO_ACT_GELU_TANH) return gelu_tanh_quotient(v);
   if constexpr (ACT == HERO_ACT_SILU) return silu_f(v);
   return v;
 }
 
-struct MoeLane {                              // what a lane knows of its feature
-  float cs, bias, post;
-  bool ok;                                    // the feature exists
-  bool up;                                    // gated: this lane holds the second half's product
-  int turn;                                   // its column in the turned chunk
-};
-
+// y, the value before its rounding, to the turned chunk; 16-bit outputs: the largest magnitude as stored
 template <int OUTK>                           // OUT_I8, OUT_F8, OUT_FP
 __device__ __forceinline__ void moe_put(uint8_t* at, float y, int dt, float& most, bool count) {
   if constexpr (OUTK == OUT_I8) {
@@ -122,53 +124,75 @@ __device__ __forceinline__ void moe_put(uint8_t* at, float y, int dt, float& mos
     if (dt == HERO_F16) b = __half_as_ushort(__float2half_rn(y));
     else b = __bfloat16_as_ushort(__float2bfloat16_rn(y));
     *reinterpret_cast<unsigned short*>(at) = b;
-    const float a = dt == HERO_F16 ? __half2float(__ushort_as_half(b & 0x7fff)) : __uint_as_float((uint32_t)(b & 0x7fff) << 16);
-    if (count) most = fmaxf(most, a);
+    if (count) most = fmaxf(most, dt == HERO_F16 ? __half2float(__ushort_as_half(b & 0x7fff)) : __uint_as_float((uint32_t)(b & 0x7fff) << 16));
   }
 }
 
-// 32 rows of this lane's feature: products, activation, rounding, into the turned chunk [32 rows][columns of the CTA]
+template <bool INT8>
+__device__ __forceinline__ float2 moe_acc2(uint32_t a, uint32_t b) {
+  return INT8 ? make_float2((float)(int)a, (float)(int)b) : make_float2(__uint_as_float(a), __uint_as_float(b));
+}
+
+// What a thread knows of its features: one (its lane), or two gated ones (lane / 4 of each half of 16 lanes).
+template <bool GATED>
+struct MoeFeature {
+  float cs[GATED ? 4 : 1], bias[GATED ? 4 : 1], post[GATED ? 2 : 1];      // gated: gate and up of the first, of the second
+};
+
+// A chunk of 32 rows: products, activation, rounding, into the turned chunk.  `rs`: the chunk's row factors; count: rows that exist, or 0 (no observer)
 template <bool INT8, bool GATED, int ACT, int OUTK>
-__device__ __forceinline__ void moe_chunk(const MoeLinearParams& p, const uint32_t (&r)[32], const float* rs, const MoeLane& l, uint8_t* buf, int rows,
-                                          float& most) {
-  constexpr int ES = OUTK == OUT_FP ? 2 : 1, COLS = GATED ? 64 : 128, PITCH = COLS * ES;
-  uint8_t* at = buf + l.turn * ES;
+__device__ __forceinline__ void moe_chunk(const MoeLinearParams& p, const uint32_t (&r)[32], const float* rs, const MoeFeature<GATED>& l, uint8_t* buf, int lane,
+                                          int count, float (&most)[2]) {
+  constexpr int ES = OUTK == OUT_FP ? 2 : 1, PITCH = (GATED ? 64 : 128) * ES + 16;
+  if constexpr (GATED) {
+    uint8_t* at = buf + (2 * (lane & 3)) * PITCH + (lane >> 2) * ES;
 #pragma unroll
-  for (int j = 0; j < 32; j += 4) {
-    const float4 f = *reinterpret_cast<const float4*>(rs + j);
-    const float rsj[4] = {f.x, f.y, f.z, f.w};
-    float v[4];
+    for (int b = 0; b < 4; ++b) {
+      const int row = 8 * b + 2 * (lane & 3);
+      const float2 f = *reinterpret_cast<const float2*>(rs + row);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float acc = INT8 ? (float)(int)r[j + i] : __uint_as_float(r[j + i]);
-      if constexpr (!GATED && ACT == HERO_ACT_NONE) v[i] = fmaf(acc * rsj[i], l.cs, l.bias);      // (cs and bias carry the output factor)
-      else v[i] = fmaf(acc * rsj[i], l.cs, l.bias);
+      for (int half = 0; half < 2; ++half) {
+        const uint32_t* q = &r[half * 16 + b * 4];
+        const float2 g = __ffma2_rn(__fmul2_rn(moe_acc2<INT8>(q[0], q[1]), f), make_float2(l.cs[2 * half], l.cs[2 * half]), make_float2(l.bias[2 * half], l.bias[2 * half]));
+        const float2 u = __ffma2_rn(__fmul2_rn(moe_acc2<INT8>(q[2], q[3]), f), make_float2(l.cs[2 * half + 1], l.cs[2 * half + 1]), make_float2(l.bias[2 * half + 1], l.bias[2 * half + 1]));
+        moe_put<OUTK>(at + (8 * b) * PITCH + half * 8 * ES, moe_act<ACT>(g.x) * u.x * l.post[half], p.out_dt, most[half], row < count);
+        moe_put<OUTK>(at + (8 * b + 1) * PITCH + half * 8 * ES, moe_act<ACT>(g.y) * u.y * l.post[half], p.out_dt, most[half], row + 1 < count);
+      }
     }
-    if constexpr (GATED) {
+  } else {
+    uint8_t* at = buf + lane * ES;
+#pragma unroll
+    for (int j = 0; j < 32; j += 4) {
+      const float4 f = *reinterpret_cast<const float4*>(rs + j);
 #pragma unroll
       for (int i = 0; i < 4; i += 2) {
-        // the gate's lane keeps the first row of the two and gives its second, the other lane the other way round
-        const float other = __shfl_xor_sync(0xffffffffu, l.up ? v[i] : v[i + 1], 8);
-        const float gate = l.up ? other : v[i], up = l.up ? v[i + 1] : other;
-        const int row = j + i + (l.up ? 1 : 0);
-        moe_put<OUTK>(at + row * PITCH, moe_act<ACT>(gate) * up * l.post, p.out_dt, most, row < rows);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float y = ACT == HERO_ACT_NONE ? v[i] : moe_act<ACT>(v[i]) * l.post;
-        moe_put<OUTK>(at + (j + i) * PITCH, y, p.out_dt, most, j + i < rows);
+        // (without an activation cs and bias carry the output factor)
+        const float2 v = __ffma2_rn(__fmul2_rn(moe_acc2<INT8>(r[j + i], r[j + i + 1]), i ? make_float2(f.z, f.w) : make_float2(f.x, f.y)),
+                                    make_float2(l.cs[0], l.cs[0]), make_float2(l.bias[0], l.bias[0]));
+        moe_put<OUTK>(at + (j + i) * PITCH, ACT == HERO_ACT_NONE ? v.x : moe_act<ACT>(v.x) * l.post[0], p.out_dt, most[0], j + i < count);
+        moe_put<OUTK>(at + (j + i + 1) * PITCH, ACT == HERO_ACT_NONE ? v.y : moe_act<ACT>(v.y) * l.post[0], p.out_dt, most[0], j + i + 1 < count);
       }
     }
   }
 }
 
-template <bool INT8, bool GATED, int ACT>
-__device__ __forceinline__ void moe_chunk_out(const MoeLinearParams& p, const uint32_t (&r)[32], const float* rs, const MoeLane& l, uint8_t* buf, int rows,
-                                              float& most) {
-  if (p.out_dt == HERO_I8) moe_chunk<INT8, GATED, ACT, OUT_I8>(p, r, rs, l, buf, rows, most);
-  else if (p.out_dt == HERO_F8) moe_chunk<INT8, GATED, ACT, OUT_F8>(p, r, rs, l, buf, rows, most);
-  else moe_chunk<INT8, GATED, ACT, OUT_FP>(p, r, rs, l, buf, rows, most);
+// 32 columns of this warp's 32 lanes; gated: in two halves of 16 lanes, a thread having lanes l / 4 and l / 4 + 8, columns 2 (l % 4) and one more, of
+// each eight columns
+template <bool GATED>
+__device__ __forceinline__ void moe_tmem_ld(uint32_t taddr, uint32_t (&r)[32]) {
+  if constexpr (GATED) {
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      uint32_t* q = &r[16 * half];
+      asm volatile(
+          "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+          : "=r"(q[0]), "=r"(q[1]), "=r"(q[2]), "=r"(q[3]), "=r"(q[4]), "=r"(q[5]), "=r"(q[6]), "=r"(q[7]), "=r"(q[8]), "=r"(q[9]), "=r"(q[10]),
+            "=r"(q[11]), "=r"(q[12]), "=r"(q[13]), "=r"(q[14]), "=r"(q[15])
+          : "r"(taddr + ((uint32_t)(16 * half) << 16)) : "memory");
+    }
+  } else {
+    ptx::tmem_ld32(taddr, r);
+  }
 }
 
 // four rows of A, 128 bytes of each
@@ -180,6 +204,16 @@ __device__ __forceinline__ void load_rows(uint32_t dst, const CUtensorMap* m, in
   else
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
                  ::"r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(x), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(bar) : "memory");
+}
+// a box of rows of A that lie behind one another, 128 bytes of each
+template <bool PAIR>
+__device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* m, int x, int y, uint32_t bar) {
+  if constexpr (PAIR)
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 ::"r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(x), "r"(y), "r"(bar) : "memory");
+  else
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 ::"r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(x), "r"(y), "r"(bar) : "memory");
 }
 // 128 rows of one expert's W: row r0, or (gated) the r0-th group of eight rows of each half
 template <bool GATED, bool PAIR>
@@ -199,6 +233,99 @@ __device__ __forceinline__ void load_w(uint32_t dst, const CUtensorMap* m, int x
     else
       asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
                    ::"r"(dst), "l"(map), "r"(x), "r"(r0), "r"(e), "r"(bar) : "memory");
+  }
+}
+
+// The epilogue warps' walk over the CTA's tiles.
+template <bool INT8, bool GATED, bool PAIR, int ACT, int OUTK>
+__device__ __forceinline__ void moe_epilogue(const MoeLinearParams& p, uint8_t* smem, const int* first, const int* tiles, uint64_t* acc_full, uint64_t* acc_empty,
+                                             uint32_t tmem_base, int first_tile, int tile_stride, int num_tiles, int rank) {
+  using Cfg = MoeCfg<PAIR>;
+  constexpr int MT = Cfg::MT, COLS = GATED ? 64 : 128, ES = OUTK == OUT_FP ? 2 : 1;    // COLS: output columns of this CTA
+  constexpr int PITCH = COLS * ES + 16, PIECES = COLS * ES / 16;                       // of a turned row: bytes, 16-byte pieces
+  constexpr int SHARE = MT / (2 * MOE_CHUNK);                                          // chunks of a tile that a group of four warps takes, at most
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int quarter = warp & 3, group = warp >> 2;
+  float* rs_mine = reinterpret_cast<float*>(smem + Cfg::RS_AT) + warp * (MT / 2);
+  uint8_t* turn = smem + Cfg::TURN_AT + group * Cfg::TURN_BYTES;
+  const int warp_col = quarter * (GATED ? 16 : 32);                                    // first output column of this warp in the CTA's
+  bool ok = true;
+  int it = 0, turned = 0;
+  for (int t = first_tile; t < num_tiles; t += tile_stride) {
+    const MoeTile w = moe_tile<MT, Cfg::STEP>(p, first, tiles, t);
+    if (w.rows <= 0) continue;
+    const int c0 = (w.nt * (PAIR ? 2 : 1) + rank) * COLS;
+    MoeFeature<GATED> l;
+    const float* cs = p.cs ? p.cs + (long long)w.e * p.N : nullptr;
+    const float* bias = p.bias ? p.bias + (long long)w.e * p.N : nullptr;
+    const float* post = p.post ? p.post + (long long)w.e * p.n_out : nullptr;
+#pragma unroll
+    for (int i = 0; i < (GATED ? 2 : 1); ++i) {
+      const int col = c0 + warp_col + (GATED ? i * 8 + (lane >> 2) : lane);
+      const bool in = col < p.n_out;
+      l.post[i] = in && post ? __ldg(post + col) : 1.0f;
+#pragma unroll
+      for (int k = 0; k < (GATED ? 2 : 1); ++k) {
+        l.cs[2 * i + k] = in && cs ? __ldg(cs + col + k * p.n_out) : 1.0f;
+        l.bias[2 * i + k] = in && bias ? __ldg(bias + col + k * p.n_out) : 0.0f;
+      }
+      if (!GATED && ACT == HERO_ACT_NONE) { l.cs[0] *= l.post[0]; l.bias[0] *= l.post[0]; }   // (acc rs cs + b) post = acc rs (cs post) + b post
+    }
+    __syncwarp();                                                   // every lane is through with the last tile's row factors
+#pragma unroll
+    for (int k = 0; k < SHARE; ++k) {
+      const int r = (2 * k + group) * MOE_CHUNK + lane;
+      float f = 1.0f;
+      if (p.rs && r < w.rows) {
+        int at = w.row0 + r;
+        if (p.token) at = min(max(p.token[at], 0), p.a_rows - 1);
+        f = p.rs[at];
+      }
+      rs_mine[k * MOE_CHUNK + lane] = f;
+    }
+    __syncwarp();
+    const int as = it & 1;
+    const uint32_t aphase = (it >> 1) & 1;
+    ++it;
+    // a wait that gave up has recorded its code; the warp runs on without waiting again so that the kernel ends promptly
+    if (ok && !ptx::mbar_wait(&acc_full[as], aphase, p.err, 0xF00 | as)) ok = false;
+    ptx::tc_fence_after();
+    const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + as * MT;
+    float most[2] = {0.f, 0.f};
+    const int chunks = (w.rows + MOE_CHUNK - 1) / MOE_CHUNK;
+    for (int c = group, k = 0; c < chunks; c += 2, ++k) {
+      uint32_t r[32];
+      moe_tmem_ld<GATED>(taddr + c * MOE_CHUNK, r);
+      ptx::tmem_ld_wait();
+      uint8_t* buf = turn + (turned & 1) * (MOE_CHUNK * MOE_TURN_PITCH);
+      ++turned;
+      const int rows = min(MOE_CHUNK, w.rows - c * MOE_CHUNK);
+      moe_chunk<INT8, GATED, ACT, OUTK>(p, r, rs_mine + k * MOE_CHUNK, l, buf + warp_col * ES, lane, p.obs ? rows : 0, most);
+      // the group's four warps have written the chunk (the barrier also says that the buffer of two chunks ago is free)
+      asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory");
+      uint8_t* out = static_cast<uint8_t*>(p.out) + ((long long)(w.row0 + c * MOE_CHUNK) * p.out_ld + c0) * ES;
+      const long long pitch = p.out_ld * ES;
+      const int left = (p.n_out - c0) * ES;                         // bytes of a row inside the matrix
+#pragma unroll
+      for (int q0 = 0; q0 < MOE_CHUNK * PIECES; q0 += 128) {
+        const int q = q0 + quarter * 32 + lane, row = q / PIECES, piece = q % PIECES * 16;
+        if (row < rows && piece < left) *reinterpret_cast<uint4*>(out + row * pitch + piece) = *reinterpret_cast<const uint4*>(buf + row * PITCH + piece);
+      }
+    }
+    if (p.obs) {
+#pragma unroll
+      for (int i = 0; i < (GATED ? 2 : 1); ++i) {
+        const int col = c0 + warp_col + (GATED ? i * 8 + (lane >> 2) : lane);
+        if (col < p.n_out && most[i] > 0.f) atomicMax(reinterpret_cast<unsigned int*>(p.obs) + (long long)w.e * p.n_out + col, __float_as_uint(most[i]));
+      }
+    }
+    // hand the accumulator back
+    ptx::tc_fence_before();
+    __syncwarp();
+    if (lane == 0) {
+      if constexpr (PAIR) ptx::mbar_arrive_cluster_relaxed(ptx::mapa(ptx::smem_u32(&acc_empty[as]), 0));
+      else ptx::mbar_arrive(&acc_empty[as]);
+    }
   }
 }
 
@@ -225,11 +352,11 @@ __device__ __forceinline__ void moe_linear_body(const CUtensorMap& tmW, const CU
     for (int i = 0; i < 2; ++i) { ptx::mbar_init(&acc_full[i], 1); ptx::mbar_init(&acc_empty[i], MOE_EPI_WARPS * (PAIR ? 2 : 1)); }
     ptx::fence_mbar_init();
   }
-  if (warp == MOE_MMA_WARP) {
+  if (warp == Cfg::MMA_WARP) {
     if constexpr (PAIR) { ptx::tmem_alloc_pair(tmem_slot, Cfg::TMEM_COLS); ptx::tmem_relinquish_pair(); }
     else { ptx::tmem_alloc(tmem_slot, Cfg::TMEM_COLS); ptx::tmem_relinquish(); }
   }
-  if (warp == MOE_W_WARP && lane == 0) { ptx::prefetch_tmap(&tmW); ptx::prefetch_tmap(&tmA); }
+  if (warp == Cfg::LOAD_WARP && lane == 0) { ptx::prefetch_tmap(&tmW); ptx::prefetch_tmap(&tmA); }
   ptx::pdl_launch_dependents();
   ptx::pdl_wait();                                                  // the router's offsets (and all else) are there from here on
 
@@ -265,7 +392,7 @@ __device__ __forceinline__ void moe_linear_body(const CUtensorMap& tmW, const CU
   const int num_tiles = tiles[p.E] * p.num_nt;
   auto tile_at = [&](int t) { return moe_tile<MT, Cfg::STEP>(p, first, tiles, t); };
 
-  if (warp == MOE_W_WARP) {
+  if (warp == Cfg::LOAD_WARP) {
     // ------------------------------------------------------------------ weights
     const bool issue = ptx::elect_one();
     const uint32_t dst0 = PAIR ? ptx::mapa(ptx::smem_u32(smem), rank) : ptx::smem_u32(smem);
@@ -275,14 +402,20 @@ __device__ __forceinline__ void moe_linear_body(const CUtensorMap& tmW, const CU
       const MoeTile w = tile_at(t);
       if (w.rows <= 0) continue;
       const int r0 = (w.nt * (PAIR ? 2 : 1) + (int)rank) * (GATED ? 8 : 128);
-      // what both CTAs' copies of a k-block bring: whole groups of four rows
-      const MoeShare s0 = moe_share<PAIR>(w, 0), s1 = moe_share<PAIR>(w, 1);
-      const uint32_t bytes = (PAIR ? 2 : 1) * Cfg::W_BYTES + (uint32_t)(s0.fours + (PAIR ? s1.fours : 0)) * (4 * GEMM_BK_BYTES);
+      // what both CTAs' copies of a k-block bring: whole groups of four rows, or whole boxes of rows in order
+      const MoeShare s0 = moe_share<PAIR>(w, 0), s1 = moe_share<PAIR>(w, 1), sh = rank ? s1 : s0;
+      auto rows_in = [&](const MoeShare& s) { return p.token ? 4 * s.fours : max(0, (s.n + Cfg::BOX - 1) / Cfg::BOX) * Cfg::BOX; };
+      const uint32_t bytes = (PAIR ? 2 : 1) * Cfg::W_BYTES + (uint32_t)(rows_in(s0) + (PAIR ? rows_in(s1) : 0)) * GEMM_BK_BYTES;
+      const int in_order = p.token ? 0 : sh.n;
       for (int kb = 0; kb < p.num_kb; ++kb) {
         if (!ptx::mbar_wait(&empty[stage], phase ^ 1, p.err, 0xC00 | stage)) { ok = false; break; }
         if (issue) {
           if (rank == 0) ptx::mbar_expect_tx(&full[stage], bytes);
           load_w<GATED, PAIR>(dst0 + stage * Cfg::STAGE_BYTES, &tmW, kb * p.kelems, r0, w.e, bar0 + 8 * stage);
+#pragma unroll
+          for (int r = 0; r < Cfg::ROWS; r += Cfg::BOX)
+            if (r < in_order)
+              load_box<PAIR>(dst0 + stage * Cfg::STAGE_BYTES + Cfg::W_BYTES + r * GEMM_BK_BYTES, &tmA, kb * p.kelems, w.row0 + sh.lo + r, bar0 + 8 * stage);
         }
         if (++stage == STAGES) { stage = 0; phase ^= 1; }
       }
@@ -292,11 +425,11 @@ __device__ __forceinline__ void moe_linear_body(const CUtensorMap& tmW, const CU
       if (++stage == STAGES) { stage = 0; phase ^= 1; }
     }
     __syncwarp();
-  } else if (warp >= MOE_EPI_WARPS && warp < MOE_EPI_WARPS + MOE_ROW_WARPS) {
+  } else if (warp >= Cfg::ROW_WARP && warp < Cfg::LOAD_WARP) {
     // ------------------------------------------------------------------ rows of A
-    // warp ww has the groups ww, ww + 4, ..
-    constexpr int PER = Cfg::ROWS / (4 * MOE_ROW_WARPS);
-    const int ww = warp - MOE_EPI_WARPS;
+    // warp ww has the groups ww, ww + ROW_WARPS, ..
+    constexpr int ROW_WARPS = Cfg::ROW_WARPS, PER = Cfg::ROWS / (4 * ROW_WARPS);
+    const int ww = warp - Cfg::ROW_WARP;
     const bool issue = ptx::elect_one();
     const uint32_t dst0 = (PAIR ? ptx::mapa(ptx::smem_u32(smem), rank) : ptx::smem_u32(smem)) + Cfg::W_BYTES + ww * (4 * GEMM_BK_BYTES);
     const uint32_t bar0 = PAIR ? ptx::mapa(ptx::smem_u32(full), 0) : ptx::smem_u32(full);
@@ -307,20 +440,20 @@ __device__ __forceinline__ void moe_linear_body(const CUtensorMap& tmW, const CU
       fours = -1;
       if (w.rows <= 0) return;
       const MoeShare sh = moe_share<PAIR>(w, (int)rank);
-      fours = (sh.fours - ww + MOE_ROW_WARPS - 1) / MOE_ROW_WARPS;
+      fours = (sh.fours - ww + ROW_WARPS - 1) / ROW_WARPS;
       // (a group that is not full ends with other rows of the tile)
-      const int at = w.row0 + min(sh.lo + 4 * (ww + MOE_ROW_WARPS * (lane >> 2)) + (lane & 3), w.rows - 1);
+      const int at = w.row0 + min(sh.lo + 4 * (ww + ROW_WARPS * (lane >> 2)) + (lane & 3), w.rows - 1);
       mine = 0;
       if (lane < 4 * fours) {
-        mine = p.token ? p.token[at] : at;
+        mine = p.token[at];
         if ((unsigned)mine >= (unsigned)p.a_rows) {
           atomicExch(p.err, ERR_BAD_EXPERT);
           mine = mine < 0 ? 0 : p.a_rows - 1;
         }
       }
     };
-    if (group_id < num_tiles) ask(group_id);
-    for (int t = group_id; t < num_tiles && ok; t += groups) {
+    if (p.token && group_id < num_tiles) ask(group_id);
+    for (int t = group_id; p.token && t < num_tiles && ok; t += groups) {
       const int n4 = fours;
       int r[PER][4];
 #pragma unroll
@@ -334,13 +467,13 @@ __device__ __forceinline__ void moe_linear_body(const CUtensorMap& tmW, const CU
         if (issue) {
 #pragma unroll
           for (int s = 0; s < PER; ++s)
-            if (s < n4) load_rows<PAIR>(dst0 + stage * Cfg::STAGE_BYTES + s * (4 * GEMM_BK_BYTES * MOE_ROW_WARPS), &tmA, kb * p.kelems, r[s], bar0 + 8 * stage);
+            if (s < n4) load_rows<PAIR>(dst0 + stage * Cfg::STAGE_BYTES + s * (4 * GEMM_BK_BYTES * ROW_WARPS), &tmA, kb * p.kelems, r[s], bar0 + 8 * stage);
         }
         if (++stage == STAGES) { stage = 0; phase ^= 1; }
       }
     }
     __syncwarp();
-  } else if (warp == MOE_MMA_WARP) {
+  } else if (warp == Cfg::MMA_WARP) {
     // ------------------------------------------------------------------ products (of a pair: the leader's)
     if (rank == 0) {
       const bool issue = ptx::elect_one();
@@ -390,107 +523,42 @@ __device__ __forceinline__ void moe_linear_body(const CUtensorMap& tmW, const CU
       }
     }
     __syncwarp();
-  } else if (warp < MOE_EPI_WARPS) {
+  } else {
     // ------------------------------------------------------------------ epilogue
-    constexpr int COLS = GATED ? 64 : 128;                          // output columns of this CTA
-    constexpr int SHARE = MT / (2 * MOE_CHUNK);                     // chunks of a tile that this group takes, at most
-    const int quarter = warp & 3, group = warp >> 2, nl = quarter * 32 + lane;
-    float* rs_mine = reinterpret_cast<float*>(smem + Cfg::RS_AT) + warp * (MT / 2);
-    uint8_t* turn = smem + Cfg::TURN_AT + group * Cfg::TURN_BYTES;
-    const int es = p.out_dt == HERO_F16 || p.out_dt == HERO_BF16 ? 2 : 1;
-    MoeLane l;
-    l.up = GATED && (nl & 8);
-    l.turn = GATED ? ((nl >> 4) << 3) + (nl & 7) : nl;
-    bool ok = true;
-    int it = 0, turned = 0;
-    for (int t = group_id; t < num_tiles; t += groups) {
-      const MoeTile w = tile_at(t);
-      if (w.rows <= 0) continue;
-      const int c0 = (w.nt * (PAIR ? 2 : 1) + (int)rank) * COLS;    // first output column of this CTA
-      const int col = c0 + l.turn;
-      l.ok = col < p.n_out;
-      {
-        const long long at = (long long)w.e * p.N + col + (l.up ? p.n_out : 0);
-        l.cs = l.ok && p.cs ? __ldg(p.cs + at) : 1.0f;
-        l.bias = l.ok && p.bias ? __ldg(p.bias + at) : 0.0f;
-        l.post = l.ok && p.post ? __ldg(p.post + (long long)w.e * p.n_out + col) : 1.0f;
-        if (!GATED && p.act == HERO_ACT_NONE) { l.cs *= l.post; l.bias *= l.post; }   // (acc rs cs + b) post = acc rs (cs post) + b post
-      }
-      __syncwarp();                                                 // every lane is through with the last tile's row factors
-#pragma unroll
-      for (int k = 0; k < SHARE; ++k) {
-        const int r = (2 * k + group) * MOE_CHUNK + lane;
-        float f = 1.0f;
-        if (p.rs && r < w.rows) {
-          int at = w.row0 + r;
-          if (p.token) at = min(max(p.token[at], 0), p.a_rows - 1);
-          f = p.rs[at];
-        }
-        rs_mine[k * MOE_CHUNK + lane] = f;
-      }
-      __syncwarp();
-      const int as = it & 1;
-      const uint32_t aphase = (it >> 1) & 1;
-      ++it;
-      // a wait that gave up has recorded its code; the warp runs on without waiting again so that the kernel ends promptly
-      if (ok && !ptx::mbar_wait(&acc_full[as], aphase, p.err, 0xF00 | as)) ok = false;
-      ptx::tc_fence_after();
-      const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + as * MT;
-      float most = 0.f;
-      const int chunks = (w.rows + MOE_CHUNK - 1) / MOE_CHUNK;
-      for (int c = group, k = 0; c < chunks; c += 2, ++k) {
-        uint32_t r[32];
-        ptx::tmem_ld32(taddr + c * MOE_CHUNK, r);
-        ptx::tmem_ld_wait();
-        uint8_t* buf = turn + (turned & 1) * (MOE_CHUNK * Cfg::FEAT * 2);
-        ++turned;
-        const int rows = min(MOE_CHUNK, w.rows - c * MOE_CHUNK);
-        const float* rs = rs_mine + k * MOE_CHUNK;
-        switch (p.act) {
-          case HERO_ACT_GELU_ERF: moe_chunk_out<INT8, GATED, HERO_ACT_GELU_ERF>(p, r, rs, l, buf, rows, most); break;
-          case HERO_ACT_GELU_TANH: moe_chunk_out<INT8, GATED, HERO_ACT_GELU_TANH>(p, r, rs, l, buf, rows, most); break;
-          case HERO_ACT_SILU: moe_chunk_out<INT8, GATED, HERO_ACT_SILU>(p, r, rs, l, buf, rows, most); break;
-          default: moe_chunk_out<INT8, GATED, HERO_ACT_NONE>(p, r, rs, l, buf, rows, most); break;
-        }
-        // the group's four warps have written the chunk (the barrier also says that the buffer of two chunks ago is free)
-        asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory");
-        const int row_bytes = COLS * es, per_row = row_bytes >> 4;  // 16-byte pieces of a row
-        uint8_t* out = static_cast<uint8_t*>(p.out) + ((long long)(w.row0 + c * MOE_CHUNK) * p.out_ld + c0) * es;
-        const int left = (p.n_out - c0) * es;                       // bytes of a row inside the matrix
-        const int shift = __ffs(per_row) - 1;
-        for (int q = quarter * 32 + lane; q < rows * per_row; q += 128) {
-          const int row = q >> shift, piece = (q & (per_row - 1)) << 4;
-          if (piece < left)
-            *reinterpret_cast<uint4*>(out + (long long)row * p.out_ld * es + piece) = *reinterpret_cast<const uint4*>(buf + row * row_bytes + piece);
-        }
-      }
-      if (p.obs && l.ok && most > 0.f) atomicMax(reinterpret_cast<unsigned int*>(p.obs) + (long long)w.e * p.n_out + col, __float_as_uint(most));
-      // hand the accumulator back
-      ptx::tc_fence_before();
-      __syncwarp();
-      if (lane == 0) {
-        if constexpr (PAIR) ptx::mbar_arrive_cluster_relaxed(ptx::mapa(ptx::smem_u32(&acc_empty[as]), 0));
-        else ptx::mbar_arrive(&acc_empty[as]);
-      }
+#define MOE_EPILOGUE(ACT, OUTK) \
+  moe_epilogue<INT8, GATED, PAIR, ACT, OUTK>(p, smem, first, tiles, acc_full, acc_empty, tmem_base, group_id, groups, num_tiles, (int)rank)
+#define MOE_EPILOGUE_OUT(ACT)                                        \
+  do {                                                               \
+    if (p.out_dt == HERO_I8) MOE_EPILOGUE(ACT, OUT_I8);              \
+    else if (p.out_dt != HERO_F8) MOE_EPILOGUE(ACT, OUT_FP);         \
+    else if constexpr (!INT8) MOE_EPILOGUE(ACT, OUT_F8);             \
+  } while (0)
+    switch (p.act) {
+      case HERO_ACT_GELU_ERF: MOE_EPILOGUE_OUT(HERO_ACT_GELU_ERF); break;
+      case HERO_ACT_GELU_TANH: MOE_EPILOGUE_OUT(HERO_ACT_GELU_TANH); break;
+      case HERO_ACT_SILU: MOE_EPILOGUE_OUT(HERO_ACT_SILU); break;
+      default: MOE_EPILOGUE_OUT(HERO_ACT_NONE); break;
     }
+#undef MOE_EPILOGUE_OUT
+#undef MOE_EPILOGUE
   }
 
   ptx::tc_fence_before();
   __syncthreads();
   if constexpr (PAIR) ptx::cluster_sync();                          // the peer may still be reading this CTA's shared memory / barriers
-  if (warp == MOE_MMA_WARP) {
+  if (warp == Cfg::MMA_WARP) {
     if constexpr (PAIR) ptx::tmem_dealloc_pair(tmem_base, Cfg::TMEM_COLS);
     else ptx::tmem_dealloc(tmem_base, Cfg::TMEM_COLS);
   }
 }
 
 template <bool INT8, bool GATED>
-__global__ void __launch_bounds__(MOE_THREADS, 1) moe_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmA,
+__global__ void __launch_bounds__(MoeCfg<false>::THREADS, 1) moe_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmA,
                                                                     const __grid_constant__ MoeLinearParams p) {
   moe_linear_body<INT8, GATED, false>(tmW, tmA, p);
 }
 template <bool INT8, bool GATED>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MOE_THREADS, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MoeCfg<true>::THREADS, 1)
 moe_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmA, const __grid_constant__ MoeLinearParams p) {
   moe_linear_body<INT8, GATED, true>(tmW, tmA, p);
 }
@@ -508,11 +576,11 @@ static hero_status launch_moe_linear(hero_handle* h, const CUtensorMap& tmW, con
   if (pair) {
     auto kern = moe_linear_pair_kernel<INT8, GATED>;
     HERO_SMEM_OPT_IN(h, kern, MoeCfg<true>::SMEM_BYTES);
-    HERO_CUDA(launch_dependent(kern, dim3(2 * groups), dim3(MOE_THREADS), MoeCfg<true>::SMEM_BYTES, s, tmW, tmA, p));
+    HERO_CUDA(launch_dependent(kern, dim3(2 * groups), dim3(MoeCfg<true>::THREADS), MoeCfg<true>::SMEM_BYTES, s, tmW, tmA, p));
   } else {
     auto kern = moe_linear_kernel<INT8, GATED>;
     HERO_SMEM_OPT_IN(h, kern, MoeCfg<false>::SMEM_BYTES);
-    HERO_CUDA(launch_dependent(kern, dim3(groups), dim3(MOE_THREADS), MoeCfg<false>::SMEM_BYTES, s, tmW, tmA, p));
+    HERO_CUDA(launch_dependent(kern, dim3(groups), dim3(MoeCfg<false>::THREADS), MoeCfg<false>::SMEM_BYTES, s, tmW, tmA, p));
   }
   return HERO_OK;
 }
@@ -571,15 +639,15 @@ extern "C" hero_status hero_moe_linear(hero_handle* h, const hero_moe_linear_arg
   CUtensorMap tmW;
   st = make_tmap_experts(h, &tmW, a->W, a->A.dtype, a->gated != 0, N, K, E, a->ldw, E == 1 ? N * a->ldw : a->expert_stride);
   if (st != HERO_OK) return st;
-  CUtensorMap tmA;
-  st = make_tmap_2d(h, &tmA, a->A.data, eb, a->A.dtype == HERO_F16, a->A.dtype == HERO_BF16, (uint64_t)a->A.rows, (uint64_t)K, (uint64_t)a->A.ld * eb,
-                    GEMM_BK_BYTES / eb, 1, 128);
-  if (st != HERO_OK) return st;
   // A pair's tile takes up to 256 rows of an expert, a single CTA's 64: few rows an expert leave the pair's column half idle
   const bool pair = R > 32 * E;
   const uint32_t bf = a->A.dtype == HERO_BF16 ? 1 : 0;
   const int m = pair ? 256 : 128;
   p.idesc = int8 ? ptx::make_idesc(2, 1, 1, 0, 0, m, 0) : f8 ? ptx::make_idesc(1, 0, 0, 0, 0, m, 0) : ptx::make_idesc(1, bf, bf, 0, 0, m, 0);
+  CUtensorMap tmA;
+  st = make_tmap_2d(h, &tmA, a->A.data, eb, a->A.dtype == HERO_F16, a->A.dtype == HERO_BF16, (uint64_t)a->A.rows, (uint64_t)K, (uint64_t)a->A.ld * eb,
+                    GEMM_BK_BYTES / eb, a->token ? 1 : pair ? MoeCfg<true>::BOX : MoeCfg<false>::BOX, 128);
+  if (st != HERO_OK) return st;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (int8) return a->gated ? launch_moe_linear<true, true>(h, tmW, tmA, p, pair, s) : launch_moe_linear<true, false>(h, tmW, tmA, p, pair, s);
   return a->gated ? launch_moe_linear<false, true>(h, tmW, tmA, p, pair, s) : launch_moe_linear<false, false>(h, tmW, tmA, p, pair, s);

@@ -107,7 +107,7 @@ def test_observer(h, counts, gated):
 
 
 @pytest.mark.parametrize("M_rows", [5, 40, 300])
-@pytest.mark.parametrize("act", ["none", "gelu_erf", "gelu_tanh"])
+@pytest.mark.parametrize("act", ["none", "gelu_erf"])
 @pytest.mark.parametrize("out", [torch.int8, torch.float16])
 def test_one_expert_is_the_dense_linear_bit_for_bit(h, M_rows, act, out):
     g = np.random.default_rng(18)
