@@ -8,10 +8,14 @@
 //
 // A CTA (or a pair of them, tcgen05 cta_group::2, 128 features each) is persistent over tiles of (expert, rows of the expert, features).  The
 // rows of an expert are dealt evenly to as few tiles as they need.
-//   epilogue warps (8)  tensor memory -> registers -> scales, activation, rounding -> shared memory (turned) -> whole row segments out
+//   epilogue warps (8; pairs with A in order: 16)  tensor memory -> registers -> scales, activation, rounding -> shared memory (turned) -> whole row segments out.  A word holds
+//                       four (two) rows of a feature: shared memory is what the products' operands fill already, and a byte at a time costs it four
+//                       times the cycles
 //   row warps (8; 2)    rows of A picked by token: TMA gathers of four rows.  One warp starts one every 80 cycles or so, a k-block takes 32 in 512
 //                       cycles: two row warps for each four gave 197 us where four gave 231 (8192 tokens, top 8 of 64, 2048 x 2048)
 //   load warp           W tiles, and A where its rows are in order (TMA)
+//   vector warp         row factors, scales, biases and output factors of the next tile, to shared memory (two loads that depend on one another
+//                       and a search for the tile: 2000 cycles that each epilogue warp would spend once a tile)
 //   product warp        products (one elected lane); owns the tensor memory
 // Rows that warps copy themselves (cp.async) need a hand-off from those warps to the tensor core, whose chain is longer than five stages hide: 1850
 // cycles a k-block.  The accumulator is double-buffered.  Every wait is bounded; on expiry the CTA records a code and unwinds.
@@ -23,9 +27,7 @@
 namespace hero {
 
 constexpr int MOE_MAX_E = 512;
-constexpr int MOE_EPI_WARPS = 8;
 constexpr int MOE_CHUNK = 32;                 // rows that an epilogue group turns at a time
-constexpr int MOE_TURN_PITCH = 2 * 128 + 16;  // bytes of a turned row at most (16 more than its values: rows two apart on banks of their own)
 
 struct MoeLinearParams {
   int R, a_rows, E, N, n_out, K;              // K in elements
@@ -40,7 +42,7 @@ struct MoeLinearParams {
   int* err;
 };
 
-template <bool PAIR>
+template <bool PAIR, bool GATHER>
 struct MoeCfg {
   static constexpr int MT = PAIR ? 256 : 64;              // rows of a tile at most
   static constexpr int ROWS = PAIR ? MT / 2 : MT;         // ... that this CTA loads
@@ -48,14 +50,18 @@ struct MoeCfg {
   static constexpr int FEAT = 128;                        // features of this CTA
   static constexpr int W_BYTES = FEAT * GEMM_BK_BYTES, X_BYTES = ROWS * GEMM_BK_BYTES, STAGE_BYTES = W_BYTES + X_BYTES;
   static constexpr int STAGES = PAIR ? 5 : 7;
-  static constexpr int ROW_WARPS = PAIR ? 8 : 2;
-  static constexpr int ROW_WARP = MOE_EPI_WARPS, LOAD_WARP = ROW_WARP + ROW_WARPS, MMA_WARP = LOAD_WARP + 1, THREADS = (MMA_WARP + 1) * 32;
+  static constexpr int EPI_WARPS = PAIR && !GATHER ? 16 : 8, EPI_GROUPS = EPI_WARPS / 4;
+  static constexpr int ROW_WARPS = !GATHER ? 0 : PAIR ? 8 : 2;
+  static constexpr int ROW_WARP = EPI_WARPS, LOAD_WARP = ROW_WARP + ROW_WARPS, MMA_WARP = LOAD_WARP + 1, VEC_WARP = MMA_WARP + 1,
+                       THREADS = (VEC_WARP + 1) * 32;
   static constexpr int BOX = PAIR ? 64 : 16;              // rows of a copy where A is in order
-  static constexpr int TURN_BYTES = 2 * MOE_CHUNK * MOE_TURN_PITCH;       // per epilogue group: two buffers of 32 rows
+  static constexpr int TURN_BUFS = EPI_GROUPS == 2 ? 2 : 1;
+  static constexpr int TURN_BYTES = TURN_BUFS * 16 * 128 * 4;             // per epilogue group: buffers of 32 rows of 16-bit outputs, in words of two rows
   static constexpr int TMEM_COLS = 2 * MT;
   static constexpr int TURN_AT = STAGES * STAGE_BYTES;
-  static constexpr int RS_AT = TURN_AT + 2 * TURN_BYTES;                  // [8 warps][MT / 2] row factors
-  static constexpr int TABLE_AT = RS_AT + 8 * (MT / 2) * 4;               // first row [E + 1] and first tile [E + 1] of each expert
+  static constexpr int VEC_FLOATS = MT + 3 * FEAT + 8;    // of a tile: row factors, scales, biases, output factors, {row0, rows, expert, feature tile}
+  static constexpr int VEC_AT = TURN_AT + EPI_GROUPS * TURN_BYTES;                 // [2]
+  static constexpr int TABLE_AT = VEC_AT + 2 * VEC_FLOATS * 4;            // first row [E + 1] and first tile [E + 1] of each expert
   static constexpr int BARS_AT = TABLE_AT + 2 * (MOE_MAX_E + 4) * 4;
   static constexpr int SMEM_BYTES = 1024 + BARS_AT + 256;
   static_assert(SMEM_BYTES <= 227 * 1024, "shared memory");
@@ -87,21 +93,26 @@ __device__ __forceinline__ MoeTile moe_tile(const MoeLinearParams& p, const int*
 struct MoeShare { int lo, n, fours; };        // first row in the tile, rows (0 or less: none), groups
 template <bool PAIR>
 __device__ __forceinline__ MoeShare moe_share(const MoeTile& w, int rank) {
-  constexpr int STEP = MoeCfg<PAIR>::STEP;
+  constexpr int STEP = MoeCfg<PAIR, true>::STEP;
   const int half = (w.rows + STEP - 1) / STEP * (STEP / (PAIR ? 2 : 1));
   MoeShare s;
   s.lo = rank * half;
   s.n = min(half, w.rows - s.lo);
-  s.fours = max(MoeCfg<PAIR>::ROW_WARPS, (s.n + 3) >> 2);
+  s.fours = max(MoeCfg<PAIR, true>::ROW_WARPS, (s.n + 3) >> 2);
   return s;
 }
 
-// (a denominator beyond 2^126 gives 0, which is what v e^v rounds to there)
-__device__ __forceinline__ float silu_f(float v) { return __fdividef(v, 1.0f + __expf(-v)); }
-
-// 0.5 v (1 + tanh(u)) = v / (1 + e^-2u), u = sqrt(2 / pi) (v + 0.044715 v^3)
+// v / (1 + 2^x).  (A power beyond FP32 makes the quotient 0, a subnormal one changes nothing beside 1.)
+__device__ __forceinline__ float over_one_plus_exp2(float v, float x) {
+  float e, r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
+  return v * r;
+}
+// SiLU: v / (1 + e^-v).  GELU(tanh): 0.5 v (1 + tanh(u)) = v / (1 + e^-2u), u = sqrt(2 / pi) (v + 0.044715 v^3); both with log2 e in the constants
+__device__ __forceinline__ float silu_f(float v) { return over_one_plus_exp2(v, -1.44269504088896340736f * v); }
 __device__ __forceinline__ float gelu_tanh_quotient(float v) {
-  return __fdividef(v, 1.0f + __expf(-1.59576912160573071176f * v * fmaf(0.044715f * v, v, 1.0f)));
+  return over_one_plus_exp2(v, v * fmaf(v * v, -0.10294324f, -2.30220819f));
 }
 template <int ACT>
 __device__ __forceinline__ float moe_act(float v) {
@@ -109,23 +120,6 @@ __device__ __forceinline__ float moe_act(float v) {
   if constexpr (ACT == HERO_ACT_GELU_TANH) return gelu_tanh_quotient(v);
   if constexpr (ACT == HERO_ACT_SILU) return silu_f(v);
   return v;
-}
-
-// y, the value before its rounding, to the turned chunk; 16-bit outputs: the largest magnitude as stored
-template <int OUTK>                           // OUT_I8, OUT_F8, OUT_FP
-__device__ __forceinline__ void moe_put(uint8_t* at, float y, int dt, float& most, bool count) {
-  if constexpr (OUTK == OUT_I8) {
-    const float r = fminf(fmaxf(y + ROUND_MAGIC, ROUND_MAGIC - 127.0f), ROUND_MAGIC + 127.0f);   // RNE in the adder, then clip
-    *at = (uint8_t)(__float_as_uint(r) & 0xff);
-  } else if constexpr (OUTK == OUT_F8) {
-    *at = (uint8_t)(ptx::f32x2_to_e4m3x2(y, 0.0f) & 0xff);
-  } else {
-    unsigned short b;
-    if (dt == HERO_F16) b = __half_as_ushort(__float2half_rn(y));
-    else b = __bfloat16_as_ushort(__float2bfloat16_rn(y));
-    *reinterpret_cast<unsigned short*>(at) = b;
-    if (count) most = fmaxf(most, dt == HERO_F16 ? __half2float(__ushort_as_half(b & 0x7fff)) : __uint_as_float((uint32_t)(b & 0x7fff) << 16));
-  }
 }
 
 template <bool INT8>
@@ -139,39 +133,129 @@ struct MoeFeature {
   float cs[GATED ? 4 : 1], bias[GATED ? 4 : 1], post[GATED ? 2 : 1];      // gated: gate and up of the first, of the second
 };
 
-// A chunk of 32 rows: products, activation, rounding, into the turned chunk.  `rs`: the chunk's row factors; count: rows that exist, or 0 (no observer)
+// Four (8-bit outputs) or two (16-bit) rows of a feature, rounded, in one word.
+template <bool INT8, int OUTK>
+__device__ __forceinline__ uint32_t moe_word4(float2 a, float2 b) {
+  if constexpr (OUTK == OUT_F8) {
+    return ptx::f32x4_to_e4m3x4(a.x, a.y, b.x, b.y);       // saturating, round to nearest even
+  } else {
+    const float2 mg = make_float2(ROUND_MAGIC, ROUND_MAGIC);
+    a = __fadd2_rn(a, mg); b = __fadd2_rn(b, mg);          // the adder rounds, ties to even: 1.5 * 2^23 + k has k in its low byte
+    const float hi = ptx::max3(ptx::max3(a.x, a.y, b.x), b.y, b.y), lo = ptx::min3(ptx::min3(a.x, a.y, b.x), b.y, b.y);
+    // (INT8 operands give no NaN; others are always clipped, which makes a NaN -127)
+    if (!INT8 || hi > ROUND_MAGIC + 127.0f || lo < ROUND_MAGIC - 127.0f) {
+      a.x = fminf(fmaxf(a.x, ROUND_MAGIC - 127.0f), ROUND_MAGIC + 127.0f); a.y = fminf(fmaxf(a.y, ROUND_MAGIC - 127.0f), ROUND_MAGIC + 127.0f);
+      b.x = fminf(fmaxf(b.x, ROUND_MAGIC - 127.0f), ROUND_MAGIC + 127.0f); b.y = fminf(fmaxf(b.y, ROUND_MAGIC - 127.0f), ROUND_MAGIC + 127.0f);
+    }
+    return __byte_perm(__byte_perm(__float_as_uint(a.x), __float_as_uint(a.y), 0x0040), __byte_perm(__float_as_uint(b.x), __float_as_uint(b.y), 0x0040), 0x5410);
+  }
+}
+__device__ __forceinline__ uint32_t moe_word2(float2 a, int dt) {
+  if (dt == HERO_F16) {
+    const __half2 h = __floats2half2_rn(a.x, a.y);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+  const __nv_bfloat162 h = __floats2bfloat162_rn(a.x, a.y);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+// the larger magnitude (16-bit pattern) of the word's rows that exist
+__device__ __forceinline__ uint32_t moe_most(uint32_t most, uint32_t w, bool first, bool second) {
+  return max(most, max(first ? w & 0x7fffu : 0u, second ? (w >> 16) & 0x7fffu : 0u));
+}
+
+template <int ACT>
+__device__ __forceinline__ float2 moe_act2(float2 v) {
+  if constexpr (ACT == HERO_ACT_GELU_ERF) return gelu_erf_f2(v);
+  else return make_float2(moe_act<ACT>(v.x), moe_act<ACT>(v.y));
+}
+
+// A turned chunk is words of four (two) rows of a feature: [groups of rows][features].  Ungated, a group is rows that follow one another; gated, a
+// thread has rows in pairs, eight apart, and a word of four takes two such pairs.  Gated rows of words are 8 longer, so that the four
+// groups of a warp's store lie on banks of their own.
+template <bool GATED>
+constexpr int MOE_WORD_PITCH = GATED ? 64 + 8 : 128;
+
+// A chunk of 32 rows: products, activation, rounding, to the turned chunk.  `rs`: the chunk's row factors; count: rows that exist (observer)
 template <bool INT8, bool GATED, int ACT, int OUTK>
-__device__ __forceinline__ void moe_chunk(const MoeLinearParams& p, const uint32_t (&r)[32], const float* rs, const MoeFeature<GATED>& l, uint8_t* buf, int lane,
-                                          int count, float (&most)[2]) {
-  constexpr int ES = OUTK == OUT_FP ? 2 : 1, PITCH = (GATED ? 64 : 128) * ES + 16;
+__device__ __forceinline__ void moe_chunk(const MoeLinearParams& p, const uint32_t (&r)[32], const float* rs, const MoeFeature<GATED>& l, uint32_t* buf, int lane,
+                                          int count, uint32_t (&most)[2]) {
+  constexpr int PITCH = MOE_WORD_PITCH<GATED>;
   if constexpr (GATED) {
-    uint8_t* at = buf + (2 * (lane & 3)) * PITCH + (lane >> 2) * ES;
+    uint32_t* at = buf + (lane & 3) * PITCH + (lane >> 2);
 #pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      const int row = 8 * b + 2 * (lane & 3);
-      const float2 f = *reinterpret_cast<const float2*>(rs + row);
+    for (int half = 0; half < 2; ++half) {
+      float2 y[4];
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
+      for (int b = 0; b < 4; ++b) {
+        const float2 f = *reinterpret_cast<const float2*>(rs + 8 * b + 2 * (lane & 3));
         const uint32_t* q = &r[half * 16 + b * 4];
         const float2 g = __ffma2_rn(__fmul2_rn(moe_acc2<INT8>(q[0], q[1]), f), make_float2(l.cs[2 * half], l.cs[2 * half]), make_float2(l.bias[2 * half], l.bias[2 * half]));
         const float2 u = __ffma2_rn(__fmul2_rn(moe_acc2<INT8>(q[2], q[3]), f), make_float2(l.cs[2 * half + 1], l.cs[2 * half + 1]), make_float2(l.bias[2 * half + 1], l.bias[2 * half + 1]));
-        moe_put<OUTK>(at + (8 * b) * PITCH + half * 8 * ES, moe_act<ACT>(g.x) * u.x * l.post[half], p.out_dt, most[half], row < count);
-        moe_put<OUTK>(at + (8 * b + 1) * PITCH + half * 8 * ES, moe_act<ACT>(g.y) * u.y * l.post[half], p.out_dt, most[half], row + 1 < count);
+        y[b] = __fmul2_rn(__fmul2_rn(moe_act2<ACT>(g), u), make_float2(l.post[half], l.post[half]));
+      }
+      if constexpr (OUTK == OUT_FP) {
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          const uint32_t w = moe_word2(y[b], p.out_dt);
+          at[4 * b * PITCH + half * 8] = w;
+          if (p.obs) most[half] = moe_most(most[half], w, 8 * b + 2 * (lane & 3) < count, 8 * b + 2 * (lane & 3) + 1 < count);
+        }
+      } else {
+        at[half * 8] = moe_word4<INT8, OUTK>(y[0], y[1]);
+        at[4 * PITCH + half * 8] = moe_word4<INT8, OUTK>(y[2], y[3]);
       }
     }
   } else {
-    uint8_t* at = buf + lane * ES;
+    uint32_t* at = buf + lane;
 #pragma unroll
     for (int j = 0; j < 32; j += 4) {
       const float4 f = *reinterpret_cast<const float4*>(rs + j);
+      float2 y[2];
 #pragma unroll
-      for (int i = 0; i < 4; i += 2) {
+      for (int i = 0; i < 2; ++i) {
         // (without an activation cs and bias carry the output factor)
-        const float2 v = __ffma2_rn(__fmul2_rn(moe_acc2<INT8>(r[j + i], r[j + i + 1]), i ? make_float2(f.z, f.w) : make_float2(f.x, f.y)),
-                                    make_float2(l.cs[0], l.cs[0]), make_float2(l.bias[0], l.bias[0]));
-        moe_put<OUTK>(at + (j + i) * PITCH, ACT == HERO_ACT_NONE ? v.x : moe_act<ACT>(v.x) * l.post[0], p.out_dt, most[0], j + i < count);
-        moe_put<OUTK>(at + (j + i + 1) * PITCH, ACT == HERO_ACT_NONE ? v.y : moe_act<ACT>(v.y) * l.post[0], p.out_dt, most[0], j + i + 1 < count);
+        y[i] = __ffma2_rn(__fmul2_rn(moe_acc2<INT8>(r[j + 2 * i], r[j + 2 * i + 1]), i ? make_float2(f.z, f.w) : make_float2(f.x, f.y)),
+                          make_float2(l.cs[0], l.cs[0]), make_float2(l.bias[0], l.bias[0]));
+        if constexpr (ACT != HERO_ACT_NONE) y[i] = __fmul2_rn(moe_act2<ACT>(y[i]), make_float2(l.post[0], l.post[0]));
       }
+      if constexpr (OUTK == OUT_FP) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const uint32_t w = moe_word2(y[i], p.out_dt);
+          at[(j / 2 + i) * PITCH] = w;
+          if (p.obs) most[0] = moe_most(most[0], w, j + 2 * i < count, j + 2 * i + 1 < count);
+        }
+      } else {
+        at[j / 4 * PITCH] = moe_word4<INT8, OUTK>(y[0], y[1]);
+      }
+    }
+  }
+}
+
+// A turned chunk to the output: a thread takes four features of a group of rows (16 bytes) and writes them row by row; the warps of a group (quarter 0 .. 3)
+// take the groups of rows in turn.  `out`: the chunk's first row at the CTA's first column; left: columns from there to the matrix's end.
+template <bool GATED, int OUTK>
+__device__ __forceinline__ void moe_store(const uint32_t* buf, uint8_t* out, long long pitch, int rows, int left, int quarter, int lane) {
+  constexpr int PITCH = MOE_WORD_PITCH<GATED>, PER = GATED ? 16 : 32, AT_ONCE = 32 / PER;       // threads per group of rows, groups per warp and step
+  constexpr int GROUPS = OUTK == OUT_FP ? 16 : 8, ES = OUTK == OUT_FP ? 2 : 1;
+  const int col = (lane % PER) * 4;
+  if (col >= left) return;
+#pragma unroll
+  for (int s = 0; s < GROUPS / (4 * AT_ONCE); ++s) {
+    const int g = (quarter + 4 * s) * AT_ONCE + lane / PER;
+    const uint4 w = *reinterpret_cast<const uint4*>(buf + g * PITCH + col);
+    if constexpr (OUTK == OUT_FP) {
+      uint8_t* at = out + 2 * g * pitch + col * ES;
+      if (2 * g < rows) *reinterpret_cast<uint2*>(at) = make_uint2(__byte_perm(w.x, w.y, 0x5410), __byte_perm(w.z, w.w, 0x5410));
+      if (2 * g + 1 < rows) *reinterpret_cast<uint2*>(at + pitch) = make_uint2(__byte_perm(w.x, w.y, 0x7632), __byte_perm(w.z, w.w, 0x7632));
+    } else {
+      const int row = GATED ? 16 * (g >> 2) + 2 * (g & 3) : 4 * g, skip = GATED ? 8 : 2;          // rows row, row + 1, row + skip, row + skip + 1
+      const uint32_t a = __byte_perm(w.x, w.y, 0x5140), b = __byte_perm(w.z, w.w, 0x5140), c = __byte_perm(w.x, w.y, 0x7362), d = __byte_perm(w.z, w.w, 0x7362);
+      uint8_t* at = out + row * pitch + col;
+      if (row < rows) *reinterpret_cast<uint32_t*>(at) = __byte_perm(a, b, 0x5410);
+      if (row + 1 < rows) *reinterpret_cast<uint32_t*>(at + pitch) = __byte_perm(a, b, 0x7632);
+      if (row + skip < rows) *reinterpret_cast<uint32_t*>(at + skip * pitch) = __byte_perm(c, d, 0x5410);
+      if (row + skip + 1 < rows) *reinterpret_cast<uint32_t*>(at + (skip + 1) * pitch) = __byte_perm(c, d, 0x7632);
     }
   }
 }
@@ -236,102 +320,141 @@ __device__ __forceinline__ void load_w(uint32_t dst, const CUtensorMap* m, int x
   }
 }
 
-// The epilogue warps' walk over the CTA's tiles.
-template <bool INT8, bool GATED, bool PAIR, int ACT, int OUTK>
-__device__ __forceinline__ void moe_epilogue(const MoeLinearParams& p, uint8_t* smem, const int* first, const int* tiles, uint64_t* acc_full, uint64_t* acc_empty,
-                                             uint32_t tmem_base, int first_tile, int tile_stride, int num_tiles, int rank) {
-  using Cfg = MoeCfg<PAIR>;
-  constexpr int MT = Cfg::MT, COLS = GATED ? 64 : 128, ES = OUTK == OUT_FP ? 2 : 1;    // COLS: output columns of this CTA
-  constexpr int PITCH = COLS * ES + 16, PIECES = COLS * ES / 16;                       // of a turned row: bytes, 16-byte pieces
-  constexpr int SHARE = MT / (2 * MOE_CHUNK);                                          // chunks of a tile that a group of four warps takes, at most
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int quarter = warp & 3, group = warp >> 2;
-  float* rs_mine = reinterpret_cast<float*>(smem + Cfg::RS_AT) + warp * (MT / 2);
-  uint8_t* turn = smem + Cfg::TURN_AT + group * Cfg::TURN_BYTES;
-  const int warp_col = quarter * (GATED ? 16 : 32);                                    // first output column of this warp in the CTA's
-  bool ok = true;
-  int it = 0, turned = 0;
+// The vector warp: what the epilogue needs of each tile, one tile ahead.
+template <bool GATED, bool PAIR, bool GATHER>
+__device__ __forceinline__ void moe_vectors(const MoeLinearParams& p, uint8_t* smem, const int* first, const int* tiles, uint64_t* vec_full, uint64_t* vec_empty,
+                                            int first_tile, int tile_stride, int num_tiles, int rank) {
+  using Cfg = MoeCfg<PAIR, GATHER>;
+  constexpr int MT = Cfg::MT, COLS = GATED ? 64 : 128;
+  const int lane = threadIdx.x & 31;
+  int it = 0;
   for (int t = first_tile; t < num_tiles; t += tile_stride) {
     const MoeTile w = moe_tile<MT, Cfg::STEP>(p, first, tiles, t);
     if (w.rows <= 0) continue;
-    const int c0 = (w.nt * (PAIR ? 2 : 1) + rank) * COLS;
-    MoeFeature<GATED> l;
-    const float* cs = p.cs ? p.cs + (long long)w.e * p.N : nullptr;
-    const float* bias = p.bias ? p.bias + (long long)w.e * p.N : nullptr;
-    const float* post = p.post ? p.post + (long long)w.e * p.n_out : nullptr;
+    float rs[MT / 32], cs[4], bias[4], post[4];
 #pragma unroll
-    for (int i = 0; i < (GATED ? 2 : 1); ++i) {
-      const int col = c0 + warp_col + (GATED ? i * 8 + (lane >> 2) : lane);
-      const bool in = col < p.n_out;
-      l.post[i] = in && post ? __ldg(post + col) : 1.0f;
-#pragma unroll
-      for (int k = 0; k < (GATED ? 2 : 1); ++k) {
-        l.cs[2 * i + k] = in && cs ? __ldg(cs + col + k * p.n_out) : 1.0f;
-        l.bias[2 * i + k] = in && bias ? __ldg(bias + col + k * p.n_out) : 0.0f;
-      }
-      if (!GATED && ACT == HERO_ACT_NONE) { l.cs[0] *= l.post[0]; l.bias[0] *= l.post[0]; }   // (acc rs cs + b) post = acc rs (cs post) + b post
-    }
-    __syncwarp();                                                   // every lane is through with the last tile's row factors
-#pragma unroll
-    for (int k = 0; k < SHARE; ++k) {
-      const int r = (2 * k + group) * MOE_CHUNK + lane;
-      float f = 1.0f;
+    for (int k = 0; k < MT / 32; ++k) {
+      const int r = 32 * k + lane;
+      rs[k] = 1.0f;
       if (p.rs && r < w.rows) {
         int at = w.row0 + r;
-        if (p.token) at = min(max(p.token[at], 0), p.a_rows - 1);
-        f = p.rs[at];
+        if constexpr (GATHER) at = min(max(p.token[at], 0), p.a_rows - 1);
+        rs[k] = p.rs[at];
       }
-      rs_mine[k * MOE_CHUNK + lane] = f;
     }
+    const int c0 = (w.nt * (PAIR ? 2 : 1) + rank) * COLS;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int l = 32 * k + lane;                                  // row of the W tile; gated: eight of the gate, eight of the other
+      const int col = c0 + (GATED ? (l >> 4) * 8 + (l & 7) : l), out = c0 + l;
+      const long long at = (long long)w.e * p.N + col + (GATED && (l & 8) ? p.n_out : 0);
+      cs[k] = col < p.n_out && p.cs ? __ldg(p.cs + at) : 1.0f;
+      bias[k] = col < p.n_out && p.bias ? __ldg(p.bias + at) : 0.0f;
+      post[k] = l < COLS && out < p.n_out && p.post ? __ldg(p.post + (long long)w.e * p.n_out + out) : 1.0f;
+    }
+    if (!ptx::mbar_wait(&vec_empty[it & 1], ((it >> 1) & 1) ^ 1, p.err, 0xF80 | (it & 1))) break;
+    float* v = reinterpret_cast<float*>(smem + Cfg::VEC_AT) + (it & 1) * Cfg::VEC_FLOATS;
+#pragma unroll
+    for (int k = 0; k < MT / 32; ++k) v[32 * k + lane] = rs[k];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      v[MT + 32 * k + lane] = cs[k];
+      v[MT + 128 + 32 * k + lane] = bias[k];
+      v[MT + 256 + 32 * k + lane] = post[k];
+    }
+    if (lane == 0) *reinterpret_cast<int4*>(v + MT + 384) = make_int4(w.row0, w.rows, w.e, w.nt);
     __syncwarp();
+    if (lane == 0) ptx::mbar_arrive(&vec_full[it & 1]);
+    ++it;
+  }
+  // the walk's end: a tile without rows
+  if (ptx::mbar_wait(&vec_empty[it & 1], ((it >> 1) & 1) ^ 1, p.err, 0xF82 | (it & 1)) && lane == 0) {
+    float* v = reinterpret_cast<float*>(smem + Cfg::VEC_AT) + (it & 1) * Cfg::VEC_FLOATS;
+    *reinterpret_cast<int4*>(v + MT + 384) = make_int4(0, 0, 0, 0);
+    ptx::mbar_arrive(&vec_full[it & 1]);
+  }
+}
+
+// The epilogue warps, tile after tile as the vector warp names them.
+template <bool INT8, bool GATED, bool PAIR, bool GATHER, int ACT, int OUTK>
+__device__ __forceinline__ void moe_epilogue(const MoeLinearParams& p, uint8_t* smem, uint64_t* acc_full, uint64_t* acc_empty, uint64_t* vec_full,
+                                             uint64_t* vec_empty, uint32_t tmem_base, int rank) {
+  using Cfg = MoeCfg<PAIR, GATHER>;
+  constexpr int MT = Cfg::MT, COLS = GATED ? 64 : 128, ES = OUTK == OUT_FP ? 2 : 1;    // COLS: output columns of this CTA
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int quarter = warp & 3, group = warp >> 2;
+  uint32_t* turn = reinterpret_cast<uint32_t*>(smem + Cfg::TURN_AT + group * Cfg::TURN_BYTES);
+  const int warp_col = quarter * (GATED ? 16 : 32);                                    // first output column of this warp in the CTA's
+  bool ok = true;
+  int turned = 0;
+  for (int it = 0; ok; ++it) {
     const int as = it & 1;
     const uint32_t aphase = (it >> 1) & 1;
-    ++it;
-    // a wait that gave up has recorded its code; the warp runs on without waiting again so that the kernel ends promptly
-    if (ok && !ptx::mbar_wait(&acc_full[as], aphase, p.err, 0xF00 | as)) ok = false;
+    // (a wait that gives up has recorded its code; the warp leaves after this tile)
+    ok = __all_sync(0xffffffffu, ptx::mbar_wait(&vec_full[as], aphase, p.err, 0xF84 | as));
+    if (!ok) break;
+    const float* vec = reinterpret_cast<const float*>(smem + Cfg::VEC_AT) + as * Cfg::VEC_FLOATS;
+    const int4 tile = *reinterpret_cast<const int4*>(vec + MT + 384);
+    const MoeTile w{tile.z, tile.x, tile.y, tile.w};
+    if (w.rows == 0) break;
+    const int c0 = (w.nt * (PAIR ? 2 : 1) + rank) * COLS;
+    MoeFeature<GATED> l;
+    if constexpr (GATED) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float* at = vec + MT + quarter * 32 + i * 16 + (lane >> 2);
+        l.cs[2 * i] = at[0]; l.cs[2 * i + 1] = at[8];
+        l.bias[2 * i] = at[128]; l.bias[2 * i + 1] = at[128 + 8];
+        l.post[i] = vec[MT + 256 + warp_col + i * 8 + (lane >> 2)];
+      }
+    } else {
+      const float* at = vec + MT + warp_col + lane;
+      l.cs[0] = at[0]; l.bias[0] = at[128]; l.post[0] = at[256];
+      if (ACT == HERO_ACT_NONE) { l.cs[0] *= l.post[0]; l.bias[0] *= l.post[0]; }     // (acc rs cs + b) post = acc rs (cs post) + b post
+    }
+    ok = __all_sync(0xffffffffu, ptx::mbar_wait(&acc_full[as], aphase, p.err, 0xF00 | as));
     ptx::tc_fence_after();
     const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + as * MT;
-    float most[2] = {0.f, 0.f};
+    uint32_t most[2] = {0u, 0u};
     const int chunks = (w.rows + MOE_CHUNK - 1) / MOE_CHUNK;
-    for (int c = group, k = 0; c < chunks; c += 2, ++k) {
-      uint32_t r[32];
-      moe_tmem_ld<GATED>(taddr + c * MOE_CHUNK, r);
+    uint32_t r[32];
+    constexpr int GROUPS = Cfg::EPI_GROUPS;
+    if (group < chunks) moe_tmem_ld<GATED>(taddr + group * MOE_CHUNK, r);
+    for (int c = group; c < chunks; c += GROUPS) {
       ptx::tmem_ld_wait();
-      uint8_t* buf = turn + (turned & 1) * (MOE_CHUNK * MOE_TURN_PITCH);
-      ++turned;
+      uint32_t* buf = turn;
+      if constexpr (Cfg::TURN_BUFS == 2) buf += (turned++ & 1) * (Cfg::TURN_BYTES / 8);
+      else asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory");          // the group is through with the chunk before
       const int rows = min(MOE_CHUNK, w.rows - c * MOE_CHUNK);
-      moe_chunk<INT8, GATED, ACT, OUTK>(p, r, rs_mine + k * MOE_CHUNK, l, buf + warp_col * ES, lane, p.obs ? rows : 0, most);
-      // the group's four warps have written the chunk (the barrier also says that the buffer of two chunks ago is free)
+      moe_chunk<INT8, GATED, ACT, OUTK>(p, r, vec + c * MOE_CHUNK, l, buf + warp_col, lane, rows, most);
+      if (c + GROUPS < chunks) moe_tmem_ld<GATED>(taddr + (c + GROUPS) * MOE_CHUNK, r);       // on its way while this chunk is stored
+      // the group's four warps have written the chunk (of two buffers, the one of two chunks ago is free too)
       asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory");
-      uint8_t* out = static_cast<uint8_t*>(p.out) + ((long long)(w.row0 + c * MOE_CHUNK) * p.out_ld + c0) * ES;
-      const long long pitch = p.out_ld * ES;
-      const int left = (p.n_out - c0) * ES;                         // bytes of a row inside the matrix
-#pragma unroll
-      for (int q0 = 0; q0 < MOE_CHUNK * PIECES; q0 += 128) {
-        const int q = q0 + quarter * 32 + lane, row = q / PIECES, piece = q % PIECES * 16;
-        if (row < rows && piece < left) *reinterpret_cast<uint4*>(out + row * pitch + piece) = *reinterpret_cast<const uint4*>(buf + row * PITCH + piece);
-      }
+      moe_store<GATED, OUTK>(buf, static_cast<uint8_t*>(p.out) + ((long long)(w.row0 + c * MOE_CHUNK) * p.out_ld + c0) * ES, p.out_ld * ES, rows, p.n_out - c0, quarter, lane);
+      __syncwarp();
     }
     if (p.obs) {
 #pragma unroll
       for (int i = 0; i < (GATED ? 2 : 1); ++i) {
         const int col = c0 + warp_col + (GATED ? i * 8 + (lane >> 2) : lane);
-        if (col < p.n_out && most[i] > 0.f) atomicMax(reinterpret_cast<unsigned int*>(p.obs) + (long long)w.e * p.n_out + col, __float_as_uint(most[i]));
+        const float m = p.out_dt == HERO_F16 ? __half2float(__ushort_as_half((unsigned short)most[i])) : __uint_as_float(most[i] << 16);
+        if (col < p.n_out && most[i]) atomicMax(reinterpret_cast<unsigned int*>(p.obs) + (long long)w.e * p.n_out + col, __float_as_uint(m));
       }
     }
-    // hand the accumulator back
+    // hand the accumulator and the vectors back
     ptx::tc_fence_before();
     __syncwarp();
     if (lane == 0) {
+      ptx::mbar_arrive(&vec_empty[as]);
       if constexpr (PAIR) ptx::mbar_arrive_cluster_relaxed(ptx::mapa(ptx::smem_u32(&acc_empty[as]), 0));
       else ptx::mbar_arrive(&acc_empty[as]);
     }
   }
 }
 
-template <bool INT8, bool GATED, bool PAIR>
+template <bool INT8, bool GATED, bool PAIR, bool GATHER>
 __device__ __forceinline__ void moe_linear_body(const CUtensorMap& tmW, const CUtensorMap& tmA, const MoeLinearParams& p) {
-  using Cfg = MoeCfg<PAIR>;
+  using Cfg = MoeCfg<PAIR, GATHER>;
   constexpr int MT = Cfg::MT, STAGES = Cfg::STAGES;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -341,7 +464,9 @@ __device__ __forceinline__ void moe_linear_body(const CUtensorMap& tmW, const CU
   uint64_t* empty = full + STAGES;                                  // [STAGES] operands read
   uint64_t* acc_full = empty + STAGES;                              // [2]
   uint64_t* acc_empty = acc_full + 2;                               // [2] (of a pair: the leader's)
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
+  uint64_t* vec_full = acc_empty + 2;                               // [2] vectors of a tile there
+  uint64_t* vec_empty = vec_full + 2;                               // [2]
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(vec_empty + 2);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = PAIR ? ptx::cluster_ctarank() : 0u;
@@ -349,7 +474,8 @@ __device__ __forceinline__ void moe_linear_body(const CUtensorMap& tmW, const CU
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < STAGES; ++i) { ptx::mbar_init(&full[i], 1); ptx::mbar_init(&empty[i], 1); }
-    for (int i = 0; i < 2; ++i) { ptx::mbar_init(&acc_full[i], 1); ptx::mbar_init(&acc_empty[i], MOE_EPI_WARPS * (PAIR ? 2 : 1)); }
+    for (int i = 0; i < 2; ++i) { ptx::mbar_init(&acc_full[i], 1); ptx::mbar_init(&acc_empty[i], Cfg::EPI_WARPS * (PAIR ? 2 : 1)); }
+    for (int i = 0; i < 2; ++i) { ptx::mbar_init(&vec_full[i], 1); ptx::mbar_init(&vec_empty[i], Cfg::EPI_WARPS); }
     ptx::fence_mbar_init();
   }
   if (warp == Cfg::MMA_WARP) {
@@ -404,9 +530,9 @@ __device__ __forceinline__ void moe_linear_body(const CUtensorMap& tmW, const CU
       const int r0 = (w.nt * (PAIR ? 2 : 1) + (int)rank) * (GATED ? 8 : 128);
       // what both CTAs' copies of a k-block bring: whole groups of four rows, or whole boxes of rows in order
       const MoeShare s0 = moe_share<PAIR>(w, 0), s1 = moe_share<PAIR>(w, 1), sh = rank ? s1 : s0;
-      auto rows_in = [&](const MoeShare& s) { return p.token ? 4 * s.fours : max(0, (s.n + Cfg::BOX - 1) / Cfg::BOX) * Cfg::BOX; };
+      auto rows_in = [&](const MoeShare& s) { return GATHER ? 4 * s.fours : max(0, (s.n + Cfg::BOX - 1) / Cfg::BOX) * Cfg::BOX; };
       const uint32_t bytes = (PAIR ? 2 : 1) * Cfg::W_BYTES + (uint32_t)(rows_in(s0) + (PAIR ? rows_in(s1) : 0)) * GEMM_BK_BYTES;
-      const int in_order = p.token ? 0 : sh.n;
+      const int in_order = GATHER ? 0 : sh.n;
       for (int kb = 0; kb < p.num_kb; ++kb) {
         if (!ptx::mbar_wait(&empty[stage], phase ^ 1, p.err, 0xC00 | stage)) { ok = false; break; }
         if (issue) {
@@ -425,10 +551,11 @@ __device__ __forceinline__ void moe_linear_body(const CUtensorMap& tmW, const CU
       if (++stage == STAGES) { stage = 0; phase ^= 1; }
     }
     __syncwarp();
-  } else if (warp >= Cfg::ROW_WARP && warp < Cfg::LOAD_WARP) {
+  } else if (GATHER && warp >= Cfg::ROW_WARP && warp < Cfg::LOAD_WARP) {
+    if constexpr (GATHER) {
     // ------------------------------------------------------------------ rows of A
     // warp ww has the groups ww, ww + ROW_WARPS, ..
-    constexpr int ROW_WARPS = Cfg::ROW_WARPS, PER = Cfg::ROWS / (4 * ROW_WARPS);
+    constexpr int ROW_WARPS = Cfg::ROW_WARPS, PER = (Cfg::ROWS / 4 + ROW_WARPS - 1) / ROW_WARPS;
     const int ww = warp - Cfg::ROW_WARP;
     const bool issue = ptx::elect_one();
     const uint32_t dst0 = (PAIR ? ptx::mapa(ptx::smem_u32(smem), rank) : ptx::smem_u32(smem)) + Cfg::W_BYTES + ww * (4 * GEMM_BK_BYTES);
@@ -452,14 +579,15 @@ __device__ __forceinline__ void moe_linear_body(const CUtensorMap& tmW, const CU
         }
       }
     };
-    if (p.token && group_id < num_tiles) ask(group_id);
-    for (int t = group_id; p.token && t < num_tiles && ok; t += groups) {
+    if (group_id < num_tiles) ask(group_id);
+    for (int t = group_id; t < num_tiles && ok; t += groups) {
       const int n4 = fours;
+      // (a reduction leaves its result in a uniform register, where a copy's coordinates have to be)
       int r[PER][4];
 #pragma unroll
       for (int s = 0; s < PER; ++s)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) r[s][i] = __shfl_sync(0xffffffffu, mine, 4 * s + i);
+        for (int i = 0; i < 4; ++i) r[s][i] = (int)__reduce_max_sync(0xffffffffu, lane == 4 * s + i ? (uint32_t)mine : 0u);
       if (t + groups < num_tiles) ask(t + groups);                  // the next tile's rows, while this one's are copied
       if (n4 < 0) continue;
       for (int kb = 0; kb < p.num_kb; ++kb) {
@@ -473,6 +601,7 @@ __device__ __forceinline__ void moe_linear_body(const CUtensorMap& tmW, const CU
       }
     }
     __syncwarp();
+    }
   } else if (warp == Cfg::MMA_WARP) {
     // ------------------------------------------------------------------ products (of a pair: the leader's)
     if (rank == 0) {
@@ -523,10 +652,13 @@ __device__ __forceinline__ void moe_linear_body(const CUtensorMap& tmW, const CU
       }
     }
     __syncwarp();
+  } else if (warp == Cfg::VEC_WARP) {
+    moe_vectors<GATED, PAIR, GATHER>(p, smem, first, tiles, vec_full, vec_empty, group_id, groups, num_tiles, (int)rank);
+    __syncwarp();
   } else {
     // ------------------------------------------------------------------ epilogue
 #define MOE_EPILOGUE(ACT, OUTK) \
-  moe_epilogue<INT8, GATED, PAIR, ACT, OUTK>(p, smem, first, tiles, acc_full, acc_empty, tmem_base, group_id, groups, num_tiles, (int)rank)
+  moe_epilogue<INT8, GATED, PAIR, GATHER, ACT, OUTK>(p, smem, acc_full, acc_empty, vec_full, vec_empty, tmem_base, (int)rank)
 #define MOE_EPILOGUE_OUT(ACT)                                        \
   do {                                                               \
     if (p.out_dt == HERO_I8) MOE_EPILOGUE(ACT, OUT_I8);              \
@@ -552,35 +684,36 @@ __device__ __forceinline__ void moe_linear_body(const CUtensorMap& tmW, const CU
   }
 }
 
-template <bool INT8, bool GATED>
-__global__ void __launch_bounds__(MoeCfg<false>::THREADS, 1) moe_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmA,
-                                                                    const __grid_constant__ MoeLinearParams p) {
-  moe_linear_body<INT8, GATED, false>(tmW, tmA, p);
+template <bool INT8, bool GATED, bool GATHER>
+__global__ void __launch_bounds__(MoeCfg<false, GATHER>::THREADS, 1)
+moe_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmA, const __grid_constant__ MoeLinearParams p) {
+  moe_linear_body<INT8, GATED, false, GATHER>(tmW, tmA, p);
 }
-template <bool INT8, bool GATED>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MoeCfg<true>::THREADS, 1)
+template <bool INT8, bool GATED, bool GATHER>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MoeCfg<true, GATHER>::THREADS, 1)
 moe_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmA, const __grid_constant__ MoeLinearParams p) {
-  moe_linear_body<INT8, GATED, true>(tmW, tmA, p);
+  moe_linear_body<INT8, GATED, true, GATHER>(tmW, tmA, p);
 }
 
-template <bool INT8, bool GATED>
+template <bool INT8, bool GATED, bool GATHER>
 static hero_status launch_moe_linear(hero_handle* h, const CUtensorMap& tmW, const CUtensorMap& tmA, MoeLinearParams& p, bool pair, cudaStream_t s) {
+  using One = MoeCfg<false, GATHER>;
+  using Two = MoeCfg<true, GATHER>;
   const int feat = (pair ? 256 : 128) / (GATED ? 2 : 1);
   p.num_nt = (p.n_out + feat - 1) / feat;
   // a launch never needs more CTAs than an even deal of all rows over all experts could make tiles of
-  const int mt = pair ? MoeCfg<true>::MT : MoeCfg<false>::MT;
-  const long long most = ((long long)p.R / mt + (p.E < p.R ? p.E : p.R)) * p.num_nt;
+  const long long most = ((long long)p.R / (pair ? Two::MT : One::MT) + (p.E < p.R ? p.E : p.R)) * p.num_nt;
   const long long room = pair ? h->sm_count / 2 : h->sm_count;
   const unsigned groups = (unsigned)(most < room ? most : room);
   LaunchScope scope(h, s, KERNEL_GEMM);
   if (pair) {
-    auto kern = moe_linear_pair_kernel<INT8, GATED>;
-    HERO_SMEM_OPT_IN(h, kern, MoeCfg<true>::SMEM_BYTES);
-    HERO_CUDA(launch_dependent(kern, dim3(2 * groups), dim3(MoeCfg<true>::THREADS), MoeCfg<true>::SMEM_BYTES, s, tmW, tmA, p));
+    auto kern = moe_linear_pair_kernel<INT8, GATED, GATHER>;
+    HERO_SMEM_OPT_IN(h, kern, Two::SMEM_BYTES);
+    HERO_CUDA(launch_dependent(kern, dim3(2 * groups), dim3(Two::THREADS), Two::SMEM_BYTES, s, tmW, tmA, p));
   } else {
-    auto kern = moe_linear_kernel<INT8, GATED>;
-    HERO_SMEM_OPT_IN(h, kern, MoeCfg<false>::SMEM_BYTES);
-    HERO_CUDA(launch_dependent(kern, dim3(groups), dim3(MoeCfg<false>::THREADS), MoeCfg<false>::SMEM_BYTES, s, tmW, tmA, p));
+    auto kern = moe_linear_kernel<INT8, GATED, GATHER>;
+    HERO_SMEM_OPT_IN(h, kern, One::SMEM_BYTES);
+    HERO_CUDA(launch_dependent(kern, dim3(groups), dim3(One::THREADS), One::SMEM_BYTES, s, tmW, tmA, p));
   }
   return HERO_OK;
 }
@@ -646,9 +779,11 @@ extern "C" hero_status hero_moe_linear(hero_handle* h, const hero_moe_linear_arg
   p.idesc = int8 ? ptx::make_idesc(2, 1, 1, 0, 0, m, 0) : f8 ? ptx::make_idesc(1, 0, 0, 0, 0, m, 0) : ptx::make_idesc(1, bf, bf, 0, 0, m, 0);
   CUtensorMap tmA;
   st = make_tmap_2d(h, &tmA, a->A.data, eb, a->A.dtype == HERO_F16, a->A.dtype == HERO_BF16, (uint64_t)a->A.rows, (uint64_t)K, (uint64_t)a->A.ld * eb,
-                    GEMM_BK_BYTES / eb, a->token ? 1 : pair ? MoeCfg<true>::BOX : MoeCfg<false>::BOX, 128);
+                    GEMM_BK_BYTES / eb, a->token ? 1 : pair ? MoeCfg<true, false>::BOX : MoeCfg<false, false>::BOX, 128);
   if (st != HERO_OK) return st;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (int8) return a->gated ? launch_moe_linear<true, true>(h, tmW, tmA, p, pair, s) : launch_moe_linear<true, false>(h, tmW, tmA, p, pair, s);
-  return a->gated ? launch_moe_linear<false, true>(h, tmW, tmA, p, pair, s) : launch_moe_linear<false, false>(h, tmW, tmA, p, pair, s);
+#define MOE_LAUNCH(INT8, GATED) (a->token ? launch_moe_linear<INT8, GATED, true>(h, tmW, tmA, p, pair, s) : launch_moe_linear<INT8, GATED, false>(h, tmW, tmA, p, pair, s))
+  if (int8) return a->gated ? MOE_LAUNCH(true, true) : MOE_LAUNCH(true, false);
+  return a->gated ? MOE_LAUNCH(false, true) : MOE_LAUNCH(false, false);
+#undef MOE_LAUNCH
 }
