@@ -105,6 +105,12 @@ def test_sizes(h, T, H, k):
     case(h, T + H + k, T, H, k)
 
 
+@pytest.mark.parametrize("T,H,k", [(600, 16, 1), (700, 48, 3), (1000, 1040, 8), (650, 2064, 2), (620, 4096, 8), (601, 4080, 16), (2500, 256, 5)])
+@pytest.mark.parametrize("y,y_gran,out,out_gran", [("bf16", "none", "i8", "twq"), ("f16", "none", "f16", "none"), ("i8", "fwq", "i8", "fwq"), ("i8", "sq", "f8", "twq"), ("f8", "fwq", "bf16", "none")])
+def test_many_tokens(h, T, H, k, y, y_gran, out, out_gran):
+    case(h, T + H, T, H, k, y, y_gran, "f16" if H > 100 else "i8", "none" if H > 100 else "twq", out=out, out_gran=out_gran, drop=0.3, pad=16)
+
+
 @pytest.mark.parametrize("y,y_gran", [("f16", "none"), ("bf16", "none"), ("i8", "fwq"), ("i8", "sq"), ("i8", "none"), ("f8", "fwq"), ("f8", "sq")])
 @pytest.mark.parametrize("res,res_gran", [(None, "none"), ("f16", "none"), ("i8", "twq"), ("i8", "fwq"), ("f8", "twq"), ("bf16", "none")])
 def test_operand_types(h, y, y_gran, res, res_gran):
@@ -120,6 +126,9 @@ def test_outputs(h, out, out_gran, fp):
 
 
 def test_tokens_without_a_row_and_dropped_pairs(h):
+    case(h, 7, 700, 64, 4, drop=1.0)
+    case(h, 8, 700, 64, 4, drop=1.0, res=None, fp=None)
+    case(h, 9, 700, 64, 4, drop=0.9, out=None)
     case(h, 7, 50, 64, 4, drop=1.0)                         # the residual alone
     case(h, 8, 50, 64, 4, drop=1.0, res=None, fp=None)      # nothing at all: zeros, scale of beta alone
     case(h, 9, 50, 64, 4, drop=0.7)
@@ -134,9 +143,10 @@ def test_a_dropped_pair_adds_nothing_whatever_its_weight(h):
     assert torch.all(fp == 0)
 
 
-def test_an_output_may_be_the_residual(h):
+@pytest.mark.parametrize("T", [60, 3000])
+def test_an_output_may_be_the_residual(h, T):
     g = np.random.default_rng(10)
-    T, H, k = 60, 512, 3
+    H, k = 512, 3
     row, expert, weight = (torch.from_numpy(x).cuda() for x in pairs(g, T, k, 4, T * k, 0.1))
     y, res = to(g.standard_normal((T * k, H)), "f16")[0], to(g.standard_normal((T, H)), "f16")[0]
     gamma, beta = f32(np.ones(H))[0], f32(np.zeros(H))[0]
