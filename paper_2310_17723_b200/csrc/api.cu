@@ -128,12 +128,12 @@ hero_status make_tmap_pages(const hero_handle* h, CUtensorMap* out, const void* 
   return HERO_OK;
 }
 
-hero_status make_tmap_experts(const hero_handle* h, CUtensorMap* out, const void* base, int dtype, bool gated, int64_t N, int64_t K, int64_t E,
+hero_status make_tmap_experts(const hero_handle* h, CUtensorMap* out, const void* base, int dtype, bool gated, int box_rows, int64_t N, int64_t K, int64_t E,
                               int64_t ldw, int64_t expert_stride) {
   HERO_REQUIRE(h && h->encode_tiled, HERO_ERR_CUDA, "tensor-map encoder unavailable");
   const int eb = (int)dtype_size(dtype);
   const uint64_t key[6] = {reinterpret_cast<uint64_t>(base), (uint64_t)N | ((uint64_t)E << 32), (uint64_t)K, (uint64_t)ldw, (uint64_t)expert_stride,
-                           5 | ((uint64_t)dtype << 8) | ((uint64_t)(gated ? 1 : 0) << 16)};
+                           5 | ((uint64_t)dtype << 8) | ((uint64_t)(gated ? 1 : 0) << 16) | ((uint64_t)box_rows << 24)};
   hero_handle* hm = const_cast<hero_handle*>(h);
   hero_tmap_slot& slot = tmap_slot(hm, key);
   std::lock_guard<std::mutex> guard(hm->tmap_mu);
@@ -145,7 +145,7 @@ hero_status make_tmap_experts(const hero_handle* h, CUtensorMap* out, const void
   const cuuint32_t inner = (cuuint32_t)(128 / eb), rank = gated ? 5 : 3;
   const cuuint64_t dims3[3] = {(cuuint64_t)K, (cuuint64_t)N, (cuuint64_t)E}, strides3[2] = {row, expert};
   const cuuint64_t dims5[5] = {(cuuint64_t)K, 8, 2, (cuuint64_t)(N / 16), (cuuint64_t)E}, strides5[4] = {row, (cuuint64_t)(N / 2) * row, 8 * row, expert};
-  const cuuint32_t box3[3] = {inner, 128, 1}, box5[5] = {inner, 8, 2, 8, 1}, estr[5] = {1, 1, 1, 1, 1};
+  const cuuint32_t box3[3] = {inner, (cuuint32_t)box_rows, 1}, box5[5] = {inner, 8, 2, (cuuint32_t)box_rows / 16, 1}, estr[5] = {1, 1, 1, 1, 1};
   const CUtensorMapDataType dt = eb == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8
                                          : dtype == HERO_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
   CUresult r = reinterpret_cast<encode_tiled_fn>(h->encode_tiled)(

@@ -185,9 +185,9 @@ hero_status make_tmap_2d(const hero_handle* h, CUtensorMap* out, const void* bas
 // bytes of one page and head, swizzled over rows of dh (64 or 128) bytes.
 hero_status make_tmap_pages(const hero_handle* h, CUtensorMap* out, const void* base, const hero_block_cache* c, uint32_t box_tokens);
 
-// TMA descriptor over weights [E][N][K] of a mixture of experts, 3-D {K, rows, experts}; box = 128 bytes of K x 128 rows of one expert.
-// Gated: 5-D {K, 8 rows, gate / up, groups of 8 rows, experts}; the box's 128 rows are eight of the first half of N and eight of the second in turn.
-hero_status make_tmap_experts(const hero_handle* h, CUtensorMap* out, const void* base, int dtype, bool gated, int64_t N, int64_t K, int64_t E,
+// TMA descriptor over weights [E][N][K] of a mixture of experts, 3-D {K, rows, experts}; box = 128 bytes of K x box_rows rows of one
+// expert.  Gated: 5-D {K, 8 rows, gate / up, groups of 8 rows, experts}; the box's rows are eight of the first half of N and eight of the second in turn.
+hero_status make_tmap_experts(const hero_handle* h, CUtensorMap* out, const void* base, int dtype, bool gated, int box_rows, int64_t N, int64_t K, int64_t E,
                               int64_t ldw, int64_t expert_stride);
 
 }  // namespace hero

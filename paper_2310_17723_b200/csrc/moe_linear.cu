@@ -59,7 +59,7 @@ struct MoeCfg {
   static constexpr int TURN_BYTES = TURN_BUFS * 16 * 128 * 4;             // per epilogue group: buffers of 32 rows of 16-bit outputs, in words of two rows
   static constexpr int TMEM_COLS = 2 * MT;
   static constexpr int TURN_AT = STAGES * STAGE_BYTES;
-  static constexpr int VEC_FLOATS = MT + 3 * FEAT + 8;    // of a tile: row factors, scales, biases, output factors, {row0, rows, expert, feature tile}
+  static constexpr int VEC_FLOATS = MT + 3 * FEAT + 8;    // of a tile: row factors, scales, biases, output factors, {row0, rows + part and split, expert, feature tile}
   static constexpr int VEC_AT = TURN_AT + EPI_GROUPS * TURN_BYTES;                 // [2]
   static constexpr int TABLE_AT = VEC_AT + 2 * VEC_FLOATS * 4;            // first row [E + 1] and first tile [E + 1] of each expert
   static constexpr int BARS_AT = TABLE_AT + 2 * (MOE_MAX_E + 4) * 4;
@@ -67,26 +67,50 @@ struct MoeCfg {
   static_assert(SMEM_BYTES <= 227 * 1024, "shared memory");
 };
 
-struct MoeTile { int e, row0, rows, nt; };    // rows 0: none
+// A piece of work: rows of an expert (0: none) and a tile of features, or a part of it (single CTAs: part `part` of 1 << split parts).
+struct MoeTile { int e, row0, rows, nt, part, split; };
 
-// tile t of the launch; lo[e], tiles[e]: first sorted row of expert e and its first row tile (tables in shared memory)
-template <int MT, int STEP>
-__device__ __forceinline__ MoeTile moe_tile(const MoeLinearParams& p, const int* first, const int* tiles, int t) {
-  MoeTile r;
-  const int rt = t / p.num_nt;
-  r.nt = t - rt * p.num_nt;
-  int lo = 0, hi = p.E;                       // the last expert whose first tile is not behind rt
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (tiles[mid] <= rt) lo = mid; else hi = mid;
+// The launch's tiles are dealt out in rounds, one for each CTA (or pair).  Where the last round has tiles for a half or a quarter of them only, these are cut
+// in two or four, each part for a CTA of its own: single CTAs by features (a part brings its share of the weights, which is what their
+// time goes to), pairs by rows (a product over fewer rows takes less time, one over fewer features does not).
+struct MoeDeal {
+  const int* first; const int* tiles;         // first sorted row, first row tile of each expert (shared memory, [E + 1])
+  int E, num_nt, full, split, units;          // tiles of the full rounds, parts (log2) of the others, units in all
+  __device__ __forceinline__ void init(const MoeLinearParams& p, const int* first_, const int* tiles_, int groups) {
+    first = first_; tiles = tiles_; E = p.E; num_nt = p.num_nt;
+    const int all = tiles[E] * num_nt, rest = all % groups;
+    full = all - rest;
+    split = rest * 4 <= groups ? 2 : rest * 2 <= groups ? 1 : 0;
+    units = full + (rest << split);
   }
-  r.e = lo;
-  const int n = first[lo + 1] - first[lo], k = tiles[lo + 1] - tiles[lo], i = rt - tiles[lo];
-  const int per = ((n + k - 1) / k + STEP - 1) / STEP * STEP;
-  r.row0 = first[lo] + i * per;
-  r.rows = min(per, n - i * per);             // may be 0 or less where an even share rounds up: such a tile is skipped
-  return r;
-}
+  // unit u < units; the whole warp calls
+  template <int MT, int STEP, bool PAIR>
+  __device__ __forceinline__ MoeTile at(int u) const {
+    MoeTile r;
+    r.part = 0; r.split = 0;
+    int t = u;
+    if (u >= full) { r.split = split; t = full + ((u - full) >> split); r.part = (u - full) & ((1 << split) - 1); }
+    const int rt = (int)((unsigned)t / (unsigned)num_nt), lane = threadIdx.x & 31;
+    r.nt = t - rt * num_nt;
+    // the last expert whose first row tile is not behind rt: by sixteens, then among sixteen
+    int base = 0;
+    if (E > 32) base = 16 * (__popc(__ballot_sync(0xffffffffu, 16 * lane < E && tiles[min(16 * lane, E)] <= rt)) - 1);
+    const int e = base + lane;
+    r.e = base + __popc(__ballot_sync(0xffffffffu, (E <= 32 || lane < 16) && e < E && tiles[min(e, E)] <= rt)) - 1;
+    const int lo = first[r.e], n = first[r.e + 1] - lo, k = tiles[r.e + 1] - tiles[r.e], i = rt - tiles[r.e];
+    // an even share of the expert's rows
+    const int per = ((k == 1 ? n : (int)((unsigned)(n + k - 1) / (unsigned)k)) + STEP - 1) / STEP * STEP;
+    r.row0 = lo + i * per;
+    r.rows = min(per, n - i * per);           // may be 0 or less where a share rounds up: such a unit is skipped
+    if (PAIR && r.split) {
+      const int sub = (((r.rows + (1 << r.split) - 1) >> r.split) + STEP - 1) / STEP * STEP;
+      r.row0 += r.part * sub;
+      r.rows = min(sub, r.rows - r.part * sub);
+      r.part = r.split = 0;
+    }
+    return r;
+  }
+};
 
 // Rows of a tile that a CTA loads, in groups of four: of a pair, each has half of the N side.  Every row warp takes part in every stage, with a group
 // that nobody needs if there are too few: a warp without one could fall two uses of a stage behind, where a barrier's parity repeats.
@@ -233,13 +257,14 @@ __device__ __forceinline__ void moe_chunk(const MoeLinearParams& p, const uint32
 }
 
 // A turned chunk to the output: a thread takes four features of a group of rows (16 bytes) and writes them row by row; the warps of a group (quarter 0 .. 3)
-// take the groups of rows in turn.  `out`: the chunk's first row at the CTA's first column; left: columns from there to the matrix's end.
+// take the groups of rows in turn.  `out`: the chunk's first row at the CTA's first column; lo, hi: the columns that are this
+// CTA's to write.
 template <bool GATED, int OUTK>
-__device__ __forceinline__ void moe_store(const uint32_t* buf, uint8_t* out, long long pitch, int rows, int left, int quarter, int lane) {
+__device__ __forceinline__ void moe_store(const uint32_t* buf, uint8_t* out, long long pitch, int rows, int lo, int hi, int quarter, int lane) {
   constexpr int PITCH = MOE_WORD_PITCH<GATED>, PER = GATED ? 16 : 32, AT_ONCE = 32 / PER;       // threads per group of rows, groups per warp and step
   constexpr int GROUPS = OUTK == OUT_FP ? 16 : 8, ES = OUTK == OUT_FP ? 2 : 1;
   const int col = (lane % PER) * 4;
-  if (col >= left) return;
+  if (col < lo || col >= hi) return;
 #pragma unroll
   for (int s = 0; s < GROUPS / (4 * AT_ONCE); ++s) {
     const int g = (quarter + 4 * s) * AT_ONCE + lane / PER;
@@ -299,7 +324,7 @@ __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* m, int
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
                  ::"r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(x), "r"(y), "r"(bar) : "memory");
 }
-// 128 rows of one expert's W: row r0, or (gated) the r0-th group of eight rows of each half
+// a box of one expert's W (pair: 128 rows, else 32): row r0, or (gated) the r0-th group of eight rows of each half
 template <bool GATED, bool PAIR>
 __device__ __forceinline__ void load_w(uint32_t dst, const CUtensorMap* m, int x, int r0, int e, uint32_t bar) {
   const uint64_t map = reinterpret_cast<uint64_t>(m);
@@ -322,14 +347,14 @@ __device__ __forceinline__ void load_w(uint32_t dst, const CUtensorMap* m, int x
 
 // The vector warp: what the epilogue needs of each tile, one tile ahead.
 template <bool GATED, bool PAIR, bool GATHER>
-__device__ __forceinline__ void moe_vectors(const MoeLinearParams& p, uint8_t* smem, const int* first, const int* tiles, uint64_t* vec_full, uint64_t* vec_empty,
-                                            int first_tile, int tile_stride, int num_tiles, int rank) {
+__device__ __forceinline__ void moe_vectors(const MoeLinearParams& p, uint8_t* smem, const MoeDeal& deal, uint64_t* vec_full, uint64_t* vec_empty,
+                                            int first_unit, int stride, int rank) {
   using Cfg = MoeCfg<PAIR, GATHER>;
   constexpr int MT = Cfg::MT, COLS = GATED ? 64 : 128;
   const int lane = threadIdx.x & 31;
   int it = 0;
-  for (int t = first_tile; t < num_tiles; t += tile_stride) {
-    const MoeTile w = moe_tile<MT, Cfg::STEP>(p, first, tiles, t);
+  for (int t = first_unit; t < deal.units; t += stride) {
+    const MoeTile w = deal.at<MT, Cfg::STEP, PAIR>(t);
     if (w.rows <= 0) continue;
     float rs[MT / 32], cs[4], bias[4], post[4];
 #pragma unroll
@@ -362,7 +387,7 @@ __device__ __forceinline__ void moe_vectors(const MoeLinearParams& p, uint8_t* s
       v[MT + 128 + 32 * k + lane] = bias[k];
       v[MT + 256 + 32 * k + lane] = post[k];
     }
-    if (lane == 0) *reinterpret_cast<int4*>(v + MT + 384) = make_int4(w.row0, w.rows, w.e, w.nt);
+    if (lane == 0) *reinterpret_cast<int4*>(v + MT + 384) = make_int4(w.row0, w.rows | (w.part << 16) | (w.split << 24), w.e, w.nt);
     __syncwarp();
     if (lane == 0) ptx::mbar_arrive(&vec_full[it & 1]);
     ++it;
@@ -395,7 +420,7 @@ __device__ __forceinline__ void moe_epilogue(const MoeLinearParams& p, uint8_t* 
     if (!ok) break;
     const float* vec = reinterpret_cast<const float*>(smem + Cfg::VEC_AT) + as * Cfg::VEC_FLOATS;
     const int4 tile = *reinterpret_cast<const int4*>(vec + MT + 384);
-    const MoeTile w{tile.z, tile.x, tile.y, tile.w};
+    const MoeTile w{tile.z, tile.x, tile.y & 0xffff, tile.w, (tile.y >> 16) & 0xff, tile.y >> 24};
     if (w.rows == 0) break;
     const int c0 = (w.nt * (PAIR ? 2 : 1) + rank) * COLS;
     MoeFeature<GATED> l;
@@ -416,6 +441,10 @@ __device__ __forceinline__ void moe_epilogue(const MoeLinearParams& p, uint8_t* 
     ptx::tc_fence_after();
     const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + as * MT;
     uint32_t most[2] = {0u, 0u};
+    // a part of the features is whole quarters of the lanes
+    const int quarters = 4 >> w.split, q0 = w.part * quarters;
+    const bool mine = PAIR || (quarter >= q0 && quarter < q0 + quarters);
+    const int col_lo = PAIR ? 0 : q0 * (COLS / 4), col_hi = PAIR ? p.n_out - c0 : min(p.n_out - c0, (q0 + quarters) * (COLS / 4));
     const int chunks = (w.rows + MOE_CHUNK - 1) / MOE_CHUNK;
     uint32_t r[32];
     constexpr int GROUPS = Cfg::EPI_GROUPS;
@@ -426,11 +455,11 @@ __device__ __forceinline__ void moe_epilogue(const MoeLinearParams& p, uint8_t* 
       if constexpr (Cfg::TURN_BUFS == 2) buf += (turned++ & 1) * (Cfg::TURN_BYTES / 8);
       else asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory");          // the group is through with the chunk before
       const int rows = min(MOE_CHUNK, w.rows - c * MOE_CHUNK);
-      moe_chunk<INT8, GATED, ACT, OUTK>(p, r, vec + c * MOE_CHUNK, l, buf + warp_col, lane, rows, most);
+      if (mine) moe_chunk<INT8, GATED, ACT, OUTK>(p, r, vec + c * MOE_CHUNK, l, buf + warp_col, lane, rows, most);
       if (c + GROUPS < chunks) moe_tmem_ld<GATED>(taddr + (c + GROUPS) * MOE_CHUNK, r);       // on its way while this chunk is stored
       // the group's four warps have written the chunk (of two buffers, the one of two chunks ago is free too)
       asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory");
-      moe_store<GATED, OUTK>(buf, static_cast<uint8_t*>(p.out) + ((long long)(w.row0 + c * MOE_CHUNK) * p.out_ld + c0) * ES, p.out_ld * ES, rows, p.n_out - c0, quarter, lane);
+      moe_store<GATED, OUTK>(buf, static_cast<uint8_t*>(p.out) + ((long long)(w.row0 + c * MOE_CHUNK) * p.out_ld + c0) * ES, p.out_ld * ES, rows, col_lo, col_hi, quarter, lane);
       __syncwarp();
     }
     if (p.obs) {
@@ -487,15 +516,15 @@ __device__ __forceinline__ void moe_linear_body(const CUtensorMap& tmW, const CU
   ptx::pdl_wait();                                                  // the router's offsets (and all else) are there from here on
 
   // ---- the experts' first rows and first tiles
-  for (int e = threadIdx.x; e <= p.E; e += blockDim.x) first[e] = p.offset[e];
-  __syncthreads();
   if (warp == 0) {
     int run = 0;
     for (int e0 = 0; e0 < p.E; e0 += 32) {
       const int e = e0 + lane;
       int k = 0;
       if (e < p.E) {
-        const int lo = first[e], hi = first[e + 1];
+        const int lo = p.offset[e], hi = p.offset[e + 1];
+        first[e] = lo;
+        if (e == p.E - 1) first[p.E] = hi;
         if (lo < 0 || hi < lo || hi > p.R) atomicExch(p.err, ERR_BAD_EXPERT);
         else k = (hi - lo + MT - 1) / MT;
       }
@@ -515,8 +544,10 @@ __device__ __forceinline__ void moe_linear_body(const CUtensorMap& tmW, const CU
   if constexpr (PAIR) ptx::cluster_sync();                          // both CTAs' barriers exist before any remote arrive
   ptx::tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
-  const int num_tiles = tiles[p.E] * p.num_nt;
-  auto tile_at = [&](int t) { return moe_tile<MT, Cfg::STEP>(p, first, tiles, t); };
+  MoeDeal deal;
+  deal.init(p, first, tiles, groups);
+  const int num_tiles = deal.units;
+  auto tile_at = [&](int t) { return deal.at<MT, Cfg::STEP, PAIR>(t); };
 
   if (warp == Cfg::LOAD_WARP) {
     // ------------------------------------------------------------------ weights
@@ -528,16 +559,24 @@ __device__ __forceinline__ void moe_linear_body(const CUtensorMap& tmW, const CU
       const MoeTile w = tile_at(t);
       if (w.rows <= 0) continue;
       const int r0 = (w.nt * (PAIR ? 2 : 1) + (int)rank) * (GATED ? 8 : 128);
+      const int box0 = w.part * (4 >> w.split), box1 = box0 + (4 >> w.split);        // single CTAs: boxes of 32 features
       // what both CTAs' copies of a k-block bring: whole groups of four rows, or whole boxes of rows in order
       const MoeShare s0 = moe_share<PAIR>(w, 0), s1 = moe_share<PAIR>(w, 1), sh = rank ? s1 : s0;
       auto rows_in = [&](const MoeShare& s) { return GATHER ? 4 * s.fours : max(0, (s.n + Cfg::BOX - 1) / Cfg::BOX) * Cfg::BOX; };
-      const uint32_t bytes = (PAIR ? 2 : 1) * Cfg::W_BYTES + (uint32_t)(rows_in(s0) + (PAIR ? rows_in(s1) : 0)) * GEMM_BK_BYTES;
+      const uint32_t bytes = (PAIR ? 2 * Cfg::W_BYTES : Cfg::W_BYTES >> w.split) + (uint32_t)(rows_in(s0) + (PAIR ? rows_in(s1) : 0)) * GEMM_BK_BYTES;
       const int in_order = GATHER ? 0 : sh.n;
       for (int kb = 0; kb < p.num_kb; ++kb) {
         if (!ptx::mbar_wait(&empty[stage], phase ^ 1, p.err, 0xC00 | stage)) { ok = false; break; }
         if (issue) {
           if (rank == 0) ptx::mbar_expect_tx(&full[stage], bytes);
-          load_w<GATED, PAIR>(dst0 + stage * Cfg::STAGE_BYTES, &tmW, kb * p.kelems, r0, w.e, bar0 + 8 * stage);
+          if constexpr (PAIR) {
+            load_w<GATED, PAIR>(dst0 + stage * Cfg::STAGE_BYTES, &tmW, kb * p.kelems, r0, w.e, bar0 + 8 * stage);
+          } else {
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+              if (b >= box0 && b < box1)
+                load_w<GATED, PAIR>(dst0 + stage * Cfg::STAGE_BYTES + b * (Cfg::W_BYTES / 4), &tmW, kb * p.kelems, r0 + b * (GATED ? 2 : 32), w.e, bar0 + 8 * stage);
+          }
 #pragma unroll
           for (int r = 0; r < Cfg::ROWS; r += Cfg::BOX)
             if (r < in_order)
@@ -653,7 +692,7 @@ __device__ __forceinline__ void moe_linear_body(const CUtensorMap& tmW, const CU
     }
     __syncwarp();
   } else if (warp == Cfg::VEC_WARP) {
-    moe_vectors<GATED, PAIR, GATHER>(p, smem, first, tiles, vec_full, vec_empty, group_id, groups, num_tiles, (int)rank);
+    moe_vectors<GATED, PAIR, GATHER>(p, smem, deal, vec_full, vec_empty, group_id, groups, (int)rank);
     __syncwarp();
   } else {
     // ------------------------------------------------------------------ epilogue
@@ -704,7 +743,7 @@ static hero_status launch_moe_linear(hero_handle* h, const CUtensorMap& tmW, con
   // a launch never needs more CTAs than an even deal of all rows over all experts could make tiles of
   const long long most = ((long long)p.R / (pair ? Two::MT : One::MT) + (p.E < p.R ? p.E : p.R)) * p.num_nt;
   const long long room = pair ? h->sm_count / 2 : h->sm_count;
-  const unsigned groups = (unsigned)(most < room ? most : room);
+  const unsigned groups = (unsigned)(4 * most < room ? 4 * most : room);   // (a tile may be cut in four)
   LaunchScope scope(h, s, KERNEL_GEMM);
   if (pair) {
     auto kern = moe_linear_pair_kernel<INT8, GATED, GATHER>;
@@ -769,15 +808,14 @@ extern "C" hero_status hero_moe_linear(hero_handle* h, const hero_moe_linear_arg
   p.kelems = GEMM_BK_BYTES / eb;
   p.obs = a->out_col_absmax;
   p.err = h->d_error;
-  CUtensorMap tmW;
-  st = make_tmap_experts(h, &tmW, a->W, a->A.dtype, a->gated != 0, N, K, E, a->ldw, E == 1 ? N * a->ldw : a->expert_stride);
-  if (st != HERO_OK) return st;
-  // A pair's tile takes up to 256 rows of an expert, a single CTA's 64: few rows an expert leave the pair's column half idle
+    // A pair's tile takes up to 256 rows of an expert, a single CTA's 64: few rows an expert leave the pair's column half idle
   const bool pair = R > 32 * E;
   const uint32_t bf = a->A.dtype == HERO_BF16 ? 1 : 0;
   const int m = pair ? 256 : 128;
   p.idesc = int8 ? ptx::make_idesc(2, 1, 1, 0, 0, m, 0) : f8 ? ptx::make_idesc(1, 0, 0, 0, 0, m, 0) : ptx::make_idesc(1, bf, bf, 0, 0, m, 0);
-  CUtensorMap tmA;
+  CUtensorMap tmW, tmA;
+  st = make_tmap_experts(h, &tmW, a->W, a->A.dtype, a->gated != 0, pair ? 128 : 32, N, K, E, a->ldw, E == 1 ? N * a->ldw : a->expert_stride);
+  if (st != HERO_OK) return st;
   st = make_tmap_2d(h, &tmA, a->A.data, eb, a->A.dtype == HERO_F16, a->A.dtype == HERO_BF16, (uint64_t)a->A.rows, (uint64_t)K, (uint64_t)a->A.ld * eb,
                     GEMM_BK_BYTES / eb, a->token ? 1 : pair ? MoeCfg<true, false>::BOX : MoeCfg<false, false>::BOX, 128);
   if (st != HERO_OK) return st;
