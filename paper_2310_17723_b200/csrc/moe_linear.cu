@@ -8,7 +8,7 @@
 //
 // A CTA (or a pair of them, tcgen05 cta_group::2, 128 features each) is persistent over tiles of (expert, rows of the expert, features).  The
 // rows of an expert are dealt evenly to as few tiles as they need.
-//   epilogue warps (8; pairs with A in order: 16)  tensor memory -> registers -> scales, activation, rounding -> shared memory (turned) -> whole row segments out.  A word holds
+//   epilogue warps (single CTAs 4, pairs 8, pairs with A in order 16)  tensor memory -> registers -> scales, activation, rounding -> shared memory (turned) -> whole row segments out.  A word holds
 //                       four (two) rows of a feature: shared memory is what the products' operands fill already, and a byte at a time costs it four
 //                       times the cycles
 //   row warps (8; 2)    rows of A picked by token: TMA gathers of four rows.  One warp starts one every 80 cycles or so, a k-block takes 32 in 512
@@ -44,18 +44,18 @@ struct MoeLinearParams {
 
 template <bool PAIR, bool GATHER>
 struct MoeCfg {
-  static constexpr int MT = PAIR ? 256 : 64;              // rows of a tile at most
+  static constexpr int MT = PAIR ? 256 : 32;              // rows of a tile at most
   static constexpr int ROWS = PAIR ? MT / 2 : MT;         // ... that this CTA loads
   static constexpr int STEP = PAIR ? 32 : 16;             // granularity of the N side
   static constexpr int FEAT = 128;                        // features of this CTA
   static constexpr int W_BYTES = FEAT * GEMM_BK_BYTES, X_BYTES = ROWS * GEMM_BK_BYTES, STAGE_BYTES = W_BYTES + X_BYTES;
-  static constexpr int STAGES = PAIR ? 5 : 7;
-  static constexpr int EPI_WARPS = PAIR && !GATHER ? 16 : 8, EPI_GROUPS = EPI_WARPS / 4;
+  static constexpr int STAGES = PAIR ? 5 : 4;
+  static constexpr int EPI_WARPS = !PAIR ? 4 : !GATHER ? 16 : 8, EPI_GROUPS = EPI_WARPS / 4;
   static constexpr int ROW_WARPS = !GATHER ? 0 : PAIR ? 8 : 2;
   static constexpr int ROW_WARP = EPI_WARPS, LOAD_WARP = ROW_WARP + ROW_WARPS, MMA_WARP = LOAD_WARP + 1, VEC_WARP = MMA_WARP + 1,
                        THREADS = (VEC_WARP + 1) * 32;
   static constexpr int BOX = PAIR ? 64 : 16;              // rows of a copy where A is in order
-  static constexpr int TURN_BUFS = EPI_GROUPS == 2 ? 2 : 1;
+  static constexpr int TURN_BUFS = EPI_GROUPS <= 2 ? 2 : 1;
   static constexpr int TURN_BYTES = TURN_BUFS * 16 * 128 * 4;             // per epilogue group: buffers of 32 rows of 16-bit outputs, in words of two rows
   static constexpr int TMEM_COLS = 2 * MT;
   static constexpr int TURN_AT = STAGES * STAGE_BYTES;
@@ -64,7 +64,8 @@ struct MoeCfg {
   static constexpr int TABLE_AT = VEC_AT + 2 * VEC_FLOATS * 4;            // first row [E + 1] and first tile [E + 1] of each expert
   static constexpr int BARS_AT = TABLE_AT + 2 * (MOE_MAX_E + 4) * 4;
   static constexpr int SMEM_BYTES = 1024 + BARS_AT + 256;
-  static_assert(SMEM_BYTES <= 227 * 1024, "shared memory");
+  static constexpr int PER_SM = PAIR ? 1 : 2;             // CTAs of an SM
+  static_assert(PER_SM * (SMEM_BYTES + 1024) <= 228 * 1024, "shared memory");
 };
 
 // A piece of work: rows of an expert (0: none) and a tile of features, or a part of it (single CTAs: part `part` of 1 << split parts).
@@ -724,7 +725,7 @@ __device__ __forceinline__ void moe_linear_body(const CUtensorMap& tmW, const CU
 }
 
 template <bool INT8, bool GATED, bool GATHER>
-__global__ void __launch_bounds__(MoeCfg<false, GATHER>::THREADS, 1)
+__global__ void __launch_bounds__(MoeCfg<false, GATHER>::THREADS, MoeCfg<false, GATHER>::PER_SM)
 moe_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmA, const __grid_constant__ MoeLinearParams p) {
   moe_linear_body<INT8, GATED, false, GATHER>(tmW, tmA, p);
 }
@@ -742,7 +743,7 @@ static hero_status launch_moe_linear(hero_handle* h, const CUtensorMap& tmW, con
   p.num_nt = (p.n_out + feat - 1) / feat;
   // a launch never needs more CTAs than an even deal of all rows over all experts could make tiles of
   const long long most = ((long long)p.R / (pair ? Two::MT : One::MT) + (p.E < p.R ? p.E : p.R)) * p.num_nt;
-  const long long room = pair ? h->sm_count / 2 : h->sm_count;
+  const long long room = pair ? h->sm_count / 2 : One::PER_SM * h->sm_count;
   const unsigned groups = (unsigned)(4 * most < room ? 4 * most : room);   // (a tile may be cut in four)
   LaunchScope scope(h, s, KERNEL_GEMM);
   if (pair) {
@@ -808,7 +809,11 @@ extern "C" hero_status hero_moe_linear(hero_handle* h, const hero_moe_linear_arg
   p.kelems = GEMM_BK_BYTES / eb;
   p.obs = a->out_col_absmax;
   p.err = h->d_error;
-    // A pair's tile takes up to 256 rows of an expert, a single CTA's 64: few rows an expert leave the pair's column half idle
+    // Rows of an expert on average decide.  Few: single CTAs with tiles of 32 rows, two on an SM, so that one streams weights while the other starts or
+  // ends (a chain of router, FC1, FC2 and combine, 16 tokens, 64 experts, top 8, 2048 x 1024: 81 us; one CTA an SM, 64 rows: 91).  Many: pairs.
+  // Both sides, us, FC1 / FC2 of 64 experts, 2048 x 1024: 24 rows 50.4 / 26.9 single, 52.4 / 28.7 pairs; 32 rows 54.0 / 28.4 and 53.4 / 29.4;
+  // 16 experts, 4096 x 2048: 24 rows 47.2 / 27.3 and 52.9 / 30.1; 32 rows 52.0 / 29.8 and 53.3 / 30.2.  Beyond, a second tile of an expert costs singles
+  // the weights again.
   const bool pair = R > 32 * E;
   const uint32_t bf = a->A.dtype == HERO_BF16 ? 1 : 0;
   const int m = pair ? 256 : 128;

@@ -480,9 +480,11 @@ class Handle:
     # ---- a mixture of experts (lean for the same reason)
     def _pairs(self, t, dtype, shape, name):
         """Address of a contiguous table of the given type and shape on the handle's device; None -> absent."""
-        if t is not None and tuple(t.shape) != shape:
-            _refuse("%s: shape %s is needed, got %s" % (name, shape, tuple(t.shape)))
-        return self._address(t, dtype, name)
+        if t is None:
+            return None
+        if t.shape != shape or t.dtype is not dtype or not t.is_contiguous() or t.get_device() != self._device:
+            _refuse("%s: a contiguous tensor of %s, shape %s, on CUDA device %d is needed, got %s of %s" % (name, dtype, shape, self._device, tuple(t.shape), t.dtype))
+        return t.data_ptr()
 
     def hero_moe_route_workspace_bytes(self, tokens, n_experts, top_k):
         """Bytes that serve every call with these experts and at most this many tokens."""

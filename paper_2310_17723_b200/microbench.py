@@ -9,6 +9,8 @@
     python -m paper_2310_17723_b200.microbench layer-decode --workload c4 --B 8 --S 2048 --graph   # one decode step of a layer
     python -m paper_2310_17723_b200.microbench block-attn --B 32 --S 4096 --nh 32 --nkv 8 --dh 128 --rows 1   # 8-bit block cache
     python -m paper_2310_17723_b200.microbench block-append | block-read | rope ...   # same shape options
+    python -m paper_2310_17723_b200.microbench moe-fc1 --M 8192 --H 2048 --N 1024 --experts 64 --top-k 8   # M tokens, H features, N hidden
+    python -m paper_2310_17723_b200.microbench moe-route | moe-fc2 | moe-combine ...   # same shape options
     python -m paper_2310_17723_b200.microbench layer --workload c3 [--f8 | --fp]   # one whole layer, us per forward
     ... --sweep runs the standalone-kernel sweep of the benchmark configurations instead of one shape.
 
@@ -287,6 +289,58 @@ def bench_block(h, op, B, S, rows, nh, nkv, dh, page, f8, iters):
     return {"us": t * 1e6, "gbs": byts / t / 1e9}
 
 
+def bench_moe(h, op, T, H, F, E, k, f8, fp, iters):
+    """The operators of a mixture of experts: T tokens of H features, E experts with a hidden width of F, k for each token; fc1 is gated
+    (2 F rows of weights).  Algorithmic bytes: every byte once, weights of the experts that have a row."""
+    dt = torch.bfloat16 if fp else torch.float8_e4m3fn if f8 else torch.int8
+    eb, R = (2 if fp else 1), T * k
+    busy = E * (1 - (1 - 1 / E) ** R)
+    N, K = (2 * F, H) if op == "moe-fc1" else (H, F)
+    byts = {"moe-route": 4 * T * E + 16 * R, "moe-fc1": eb * (busy * N * K + T * H + R * F), "moe-fc2": eb * (busy * N * K + R * F) + 2 * R * H,
+            "moe-combine": 2 * R * H + 5 * T * H}[op]
+    flops = 2.0 * R * N * K if op in ("moe-fc1", "moe-fc2") else 0.0
+    n = max(2, min(16, int(400e6 // byts) + 1))
+
+    def data(*s):
+        return torch.randint(-100, 100, s, device="cuda", dtype=torch.int8) if dt == torch.int8 else torch.randn(*s, device="cuda").to(dt)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    sets = []
+    for _ in range(n):
+        x = torch.randn(T, E, device="cuda")
+        plan = (torch.empty(T, k, **i32), torch.empty(T, k, device="cuda"), torch.empty(E + 1, **i32), torch.empty(R, **i32), torch.empty(T, k, **i32))
+        ws = torch.empty(h.hero_moe_route_workspace_bytes(T, E, k), dtype=torch.uint8, device="cuda")
+        h.hero_moe_route(hero.tensor(x), *plan, workspace=ws)
+        s = dict(x=hero.tensor(x), plan=plan, ws=ws)
+        if op in ("moe-fc1", "moe-fc2"):
+            a, o = data(T if op == "moe-fc1" else R, K), torch.empty(R, F if op == "moe-fc1" else H, device="cuda", dtype=dt if op == "moe-fc1" else torch.bfloat16)
+            s |= dict(a=hero.tensor(a) if fp else hero.tensor(a, "twq", torch.full((a.shape[0],), 0.01, device="cuda")), o=hero.tensor(o), w=data(E, N, K))
+        elif op == "moe-combine":
+            y, r, o = (torch.randn(m, H, device="cuda").to(torch.bfloat16) for m in (R, T, T))
+            s |= dict(y=hero.tensor(y), r=hero.tensor(r), fp=hero.tensor(o),
+                      o=hero.tensor(torch.empty(T, H, dtype=torch.int8, device="cuda"), "twq", torch.empty(T, device="cuda")))
+        sets.append(s)
+    cs, post = torch.full((E, N), 1e-3, device="cuda"), torch.full((E, F), 30.0, device="cuda")
+    g, b = torch.ones(H, device="cuda"), torch.zeros(H, device="cuda")
+
+    def call(i):
+        s = sets[i]
+        expert, weight, offset, token, row = s["plan"]
+        if op == "moe-route":
+            h.hero_moe_route(s["x"], *s["plan"], workspace=s["ws"])
+        elif op == "moe-fc1":
+            h.hero_moe_linear(s["a"], s["w"], s["o"], offset, token=token, w_scale=None if fp else cs, act="silu", gated=True, post_scale=None if fp else post)
+        elif op == "moe-fc2":
+            h.hero_moe_linear(s["a"], s["w"], s["o"], offset, w_scale=None if fp else cs)
+        else:
+            h.hero_moe_combine(s["y"], row, weight, residual=s["r"], fp_out=s["fp"], out=s["o"], gamma=g, beta=b)
+    t = _time(call, n, iters)
+    hbm, peak, src = _peaks()
+    _say("%s tokens=%d H=%d F=%d experts=%d top_k=%d %s: %.1f us, %.0f GB/s, %.2f of %s copy bandwidth%s"
+         % (op, T, H, F, E, k, "bf16" if fp else "e4m3" if f8 else "i8", t * 1e6, byts / t / 1e9, byts / t / 1e9 / hbm, src,
+            ", %.0f TOP/s" % (flops / t / 1e12) if flops else ""))
+    return {"us": t * 1e6, "gbs": byts / t / 1e9, "tops": flops / t / 1e12}
+
+
 def bench_layer(h, workload, payload, fp, iters):
     """One forward of a single layer of a benchmark configuration (INT8, e4m3 or all-FP modules), L2 flushed between
     forwards by a 256 MB write (its time is measured alone and subtracted)."""
@@ -314,14 +368,14 @@ def bench_layer(h, workload, payload, fp, iters):
     h.profile_begin(64)
     st.forward()
     torch.cuda.synchronize()
-    fam = {1: "ln", 2: "gemm", 3: "attention", 4: "block cache"}
+    fam = {1: "ln", 2: "gemm", 3: "attention", 4: "block cache", 5: "routing"}
     print("  launches: " + ", ".join("%s %.1f us" % (fam.get(k, "?"), ms * 1e3) for k, ms in h.profile_end()), flush=True)
 
 
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("kernel", choices=["ln", "gemm", "attn", "absmax", "wquant", "layer", "decode", "layer-decode",
-                                       "block-attn", "block-append", "block-read", "rope"])
+                                       "block-attn", "block-append", "block-read", "rope", "moe-route", "moe-fc1", "moe-fc2", "moe-combine"])
     ap.add_argument("--workload", default="c3", choices=["c1", "c3", "c4"])
     ap.add_argument("--M", type=int, default=65536)
     ap.add_argument("--H", type=int, default=1024)
@@ -334,6 +388,8 @@ def main():
     ap.add_argument("--nkv", type=int, default=8, help="key / value heads of the block cache")
     ap.add_argument("--rows", type=int, default=1, help="new tokens per sequence (block cache)")
     ap.add_argument("--page", type=int, default=64)
+    ap.add_argument("--experts", type=int, default=64)
+    ap.add_argument("--top-k", type=int, default=8)
     ap.add_argument("--kind", default="i8", choices=["i8", "f16"])
     ap.add_argument("--act", default="none")
     ap.add_argument("--mask", default="none")
@@ -372,6 +428,8 @@ def main():
         bench_decode(h, a.B, a.S, a.nh, a.dh, a.iters, a.p_mode)
     elif a.kernel.startswith("block-") or a.kernel == "rope":
         bench_block(h, a.kernel, a.B, a.S, a.rows, a.nh, a.nkv, a.dh, a.page, a.f8, a.iters)
+    elif a.kernel.startswith("moe-"):
+        bench_moe(h, a.kernel, a.M, a.H, a.N, a.experts, a.top_k, a.f8, a.fp, a.iters)
     elif a.kernel == "layer":
         bench_layer(h, a.workload, "f8" if a.f8 else "i8", a.fp, a.iters)
     else:
