@@ -1,18 +1,24 @@
 // The router of a mixture of experts (hero_moe_route): top k of every token's logits, their weights, and the order of the (token, expert)
 // pairs by expert.
 //
-// Choice: one warp per token, expert lane + 32 r in the lane's register r.  Every logit becomes an unsigned key whose order is the logits'
-// (0: does not take part); a round is the lane's own maximum, a warp maximum (redux), and the winner's lane taking it out.  16-bit
-// logits carry the inverted expert in the key's low half, so that one reduction finds the lowest of equal ones; 32-bit keys take a
-// second reduction over the index.  With a selection bias the keys are FP32 scores plus bias: where two neighbours of the k + 1 largest
-// are nearer than FP32 can tell apart, the token is chosen again from FP64 keys.
+// Choice: every logit becomes an unsigned key whose order is the logits' (0: does not take part).
+//   few tokens   one warp per token, expert lane + 32 r in the lane's register r.  A round is the lane's own maximum, a warp maximum (redux), and the
+//                winner's lane taking it out: about 500 instructions a token at 128 experts, 1300 with a bias at 256.
+//   more tokens  eight lanes per token go through an eighth of its keys each, out of shared memory, and keep the largest in a sorted list in
+//                registers (a maximum and a minimum for each place); three exchanges between lanes merge the eight lists.  A key's low bits are the
+//                inverted expert, so that one comparison orders equal logits too: below the 16 bits of a 16-bit logit, in the last 5 to 9 bits of
+//                all other keys, whose k + 1 places are put in order by the whole keys afterwards.  (Whole keys in 64 bits: 36 us against
+//                20 on 5000 tokens of 256 experts.)  Where what the low bits hid could change the choice, the token is chosen again.
+// With a selection bias the keys are FP32 scores plus bias.  Where two neighbours of the k + 1 largest are nearer than FP32 can tell apart, the
+// token is chosen again from FP64 keys: of the experts that are near enough to matter, one a lane, or (more than 32 of them, a softmax) of all.
 //
 // Order: a bit per (expert, token) in shared memory.  The rank of a pair within its expert is the number of bits before its own, whatever
 // the order in which warps set them, so that the result does not depend on timing and no global atomics are needed.  Few tokens: one
 // CTA does everything.  More: each CTA of a first kernel counts its own tokens' experts, and each CTA of a second one adds up the
 // counts of those before it (and of all, for the experts' first rows) and places its pairs.
 //
-// The bytes are few (2 to 4 per logit); what bounds it is the chain of k rounds per token, about 40 instructions each.
+// The bytes are few (2 to 4 per logit); what bounds it is the instructions of the choice and the latency of two launches (measured below the
+// kernels' launch).
 #include "common.cuh"
 #include "ptx.cuh"
 #include <cuda_fp16.h>
@@ -23,6 +29,9 @@ namespace hero {
 constexpr int ROUTE_MAX_E = 512, ROUTE_MAX_K = 16;
 constexpr int ROUTE_THREADS = 1024;
 constexpr int ROUTE_ONE_CTA = 96;        // tokens that one CTA takes alone
+constexpr int ROUTE_LANES = 8, ROUTE_TOKENS = 32 / ROUTE_LANES;   // lanes of a token, tokens of a warp (many tokens)
+constexpr uint32_t ROUTE_TEAM = (1u << ROUTE_LANES) - 1u;
+constexpr int ROUTE_KEY_BYTES = 192 * 1024;   // shared memory for keys
 constexpr int ROUTE_MAX_CHUNK = 1024;    // tokens per CTA of the two-kernel form (bit words: E * chunk / 32)
 
 struct RouteParams {
@@ -33,7 +42,8 @@ struct RouteParams {
   float scale;
   int* expert; float* weight; int* offset; int* token; int* row;
   int* counts;                           // [CTAs][E] (two-kernel form)
-  int chunk, words;                      // tokens per CTA (a multiple of 32), chunk / 32
+  int chunk, words;                      // tokens per CTA, their 32-bit words
+  uint32_t low;                          // bits of a key that hold the expert (more tokens, FP32 keys)
 };
 
 __device__ __forceinline__ uint32_t order32(float x) {     // larger float <=> larger key; -inf and NaN: 0
@@ -104,6 +114,30 @@ __device__ __noinline__ int choose_exactly(const RouteParams& p, const float (&x
       if (e == lane + 32 * r) key[r] = -INFINITY;
   }
   return mine;
+}
+
+// Weights of a token by one warp: lane j < k has place j's expert and logit; m, sum: of the softmax over all experts, where it is needed.
+__device__ __forceinline__ void route_weights(const RouteParams& p, int t, int lane, int mine, float mine_x, float m, float sum) {
+  float w = 0.f;
+  if (p.score == HERO_SCORE_SOFTMAX) {
+    if (p.renorm) {
+      const float top = warp_max(mine_x);
+      w = exp_below(mine_x, top);
+      const float all = warp_sum(w);
+      w = mine >= 0 ? w / all : 0.f;
+    } else if (mine >= 0) {
+      w = exp_below(mine_x, m) / sum;
+    }
+  } else if (p.renorm) {
+    // sigmoid(x) = e^min(x, 0) / (1 + e^-|x|); the first factor relative to its largest, so that logits far below 0 keep their ratios
+    const float low = mine >= 0 ? fminf(mine_x, 0.f) : -INFINITY, top = warp_max(low);
+    w = mine >= 0 ? exp_below(low, top) / (1.f + expf(-fabsf(mine_x))) : 0.f;
+    const float all = warp_sum(w);
+    w = mine >= 0 ? w / all : 0.f;
+  } else if (mine >= 0) {
+    w = 1.f / (1.f + expf(-mine_x));
+  }
+  if (lane < p.k) p.weight[(long long)t * p.k + lane] = w * p.scale;
 }
 
 // One token by one warp: experts and weights written, lane j < k returns the expert of place j (-1: none).
@@ -203,27 +237,7 @@ __device__ __forceinline__ int route_token(const RouteParams& p, int t, int toke
       if (near) mine = choose_exactly<R>(p, x, m, lane);
       if (mine >= 0) mine_x = load_logit<DT>(p.logits, at0 + mine);
     }
-    // ---- weights
-    float w = 0.f;
-    if (p.score == HERO_SCORE_SOFTMAX) {
-      if (p.renorm) {
-        const float top = warp_max(mine_x);
-        w = exp_below(mine_x, top);
-        const float all = warp_sum(w);
-        w = mine >= 0 ? w / all : 0.f;
-      } else if (mine >= 0) {
-        w = exp_below(mine_x, m) / sum;
-      }
-    } else if (p.renorm) {
-      // sigmoid(x) = e^min(x, 0) / (1 + e^-|x|); the first factor relative to its largest, so that logits far below 0 keep their ratios
-      const float low = mine >= 0 ? fminf(mine_x, 0.f) : -INFINITY, top = warp_max(low);
-      w = mine >= 0 ? exp_below(low, top) / (1.f + expf(-fabsf(mine_x))) : 0.f;
-      const float all = warp_sum(w);
-      w = mine >= 0 ? w / all : 0.f;
-    } else if (mine >= 0) {
-      w = 1.f / (1.f + expf(-mine_x));
-    }
-    if (lane < p.k) p.weight[(long long)t * p.k + lane] = w * p.scale;
+    route_weights(p, t, lane, mine, mine_x, m, sum);
   } else if (lane < p.k) {
     p.weight[(long long)t * p.k + lane] = 0.f;
   }
@@ -324,19 +338,291 @@ __global__ void __launch_bounds__(ROUTE_THREADS, 1) route_one_kernel(const __gri
 }
 
 // Two-kernel form, first: choose, and count the chunk's pairs of every expert.
-template <int R, int DT>
+__device__ __forceinline__ float from_order32(uint32_t k) { return __uint_as_float((k & 0x80000000u) ? (k & 0x7fffffffu) : ~k); }
+// list (falling) takes v in, at place `from` or behind
+template <int KM>
+__device__ __forceinline__ void insert(uint32_t (&list)[KM], uint32_t v, int from) {
+#pragma unroll
+  for (int i = 0; i < KM; ++i) {
+    if (i < from) continue;                                // (from is a constant wherever this is unrolled)
+    const uint32_t m = max(list[i], v);
+    v = min(list[i], v);
+    list[i] = m;
+  }
+}
+// How near two FP32 keys with a bias may be and still have their order.  Sigmoid: a score at most 1 with an exponential within 2 + 1.2 |x| units (which
+// score (1 - score) multiplies) and a quotient within 2, half a unit of the sum: below 5e-7 (1 + |v|) each.  Softmax: a sum of up to 512 on top.
+__device__ __forceinline__ float key_error(const RouteParams& p, float v) { return (p.score == HERO_SCORE_SOFTMAX ? 4e-6f : 1e-6f) * (1.f + fabsf(v)); }
+
+// A token without a bias or with sigmoid scores, by one warp: from FP64 keys of the experts whose FP32 keys (row, shared memory) are not clearly below `least`,
+// which the k largest are not below.  list: shared int[64] of the warp.  False: there are more than 32 of them, nothing is written.
+template <int DT>
+__device__ __noinline__ bool route_near(const RouteParams& p, int t, const uint32_t* row, float least, float2 st, int* list, int lane, int& mine) {
+  const uint32_t border = order32(p.bias ? least - 4.f * key_error(p, least) : least);
+  int n = 0;
+  for (int e0 = 0; e0 < p.E; e0 += 32) {
+    const int e = e0 + lane;
+    const bool in = e < p.E && row[e] != 0u && row[e] >= border;
+    const uint32_t some = __ballot_sync(0xffffffffu, in);
+    const int at = n + __popc(some & ((1u << lane) - 1u));
+    if (in && at < 32) list[at] = e;
+    n += __popc(some);
+  }
+  __syncwarp();
+  if (n > 32) return false;
+  const int e = lane < n ? list[lane] : -1;
+  const float x = e >= 0 ? load_logit<DT>(p.logits, (long long)t * p.ld + e) : -INFINITY;
+  const double key = e < 0 ? 0.0 : p.bias ? 1.0 / (1.0 + exp(-(double)x)) + (double)p.bias[e] : (double)x;
+  int rank = 0;
+  for (int c = 0; c < n; ++c) {                            // (experts rise with the lane: of equal keys the lower one is first)
+    const double other = __shfl_sync(0xffffffffu, key, c);
+    rank += other > key || (other == key && c < lane) ? 1 : 0;
+  }
+  if (e >= 0) list[32 + rank] = lane;
+  __syncwarp();
+  const int from = lane < n ? list[32 + lane] : 0;
+  const int place = __shfl_sync(0xffffffffu, e, from);
+  const float place_x = __shfl_sync(0xffffffffu, x, from);
+  mine = lane < n && lane < p.k ? place : -1;
+  route_weights(p, t, lane, mine, mine >= 0 ? place_x : -INFINITY, st.x, st.y);
+  if (lane < p.k) p.expert[(long long)t * p.k + lane] = mine;
+  __syncwarp();
+  return true;
+}
+__device__ __forceinline__ int route_pitch(int E) { return (E + 31) / 32 * 32 + ROUTE_LANES; }    // (tokens on banks of their own)
+
+// KM: places of a lane's list, at least k (PACK16: 16-bit logits without a bias) or k + 1
+template <int KM, int DT, bool PACK16>
 __global__ void __launch_bounds__(ROUTE_THREADS, 1) route_choose_kernel(const __grid_constant__ RouteParams p) {
+  extern __shared__ uint32_t keys_of[];                    // [warps][tokens][pitch]
   __shared__ int count[ROUTE_MAX_E];
+  __shared__ float bias[PACK16 ? 1 : ROUTE_MAX_E];
+  __shared__ int near_list[PACK16 ? 1 : ROUTE_THREADS / 32][64];
+  __shared__ float2 stats[ROUTE_THREADS / 32][ROUTE_TOKENS];          // of a token's softmax over all experts: maximum, sum
   ptx::pdl_launch_dependents();
   for (int e = threadIdx.x; e < p.E; e += blockDim.x) count[e] = 0;
   ptx::pdl_wait();
   const int tokens = token_count(p), lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nw = blockDim.x >> 5;
+  const int pitch = route_pitch(p.E), wide = pitch - ROUTE_LANES;
+  uint32_t* keys = keys_of + warp * ROUTE_TOKENS * pitch;
+  const bool softmax = p.score == HERO_SCORE_SOFTMAX, biased = !PACK16 && p.bias != nullptr, whole = softmax && (biased || !p.renorm);
+  if (biased)
+    for (int e = threadIdx.x; e < wide; e += blockDim.x) bias[e] = e < p.E ? p.bias[e] : -INFINITY;
   __syncthreads();
   const long long t0 = (long long)blockIdx.x * p.chunk;
   const int n = (int)min((long long)p.chunk, p.T - t0);
-  for (int i = warp; i < n; i += nw) {
-    const int e = route_token<R, DT>(p, (int)(t0 + i), tokens, lane);
-    if (e >= 0) atomicAdd(&count[e], 1);                   // (shared memory, whole numbers: any order gives the same)
+  for (int base = warp * ROUTE_TOKENS; base < n; base += nw * ROUTE_TOKENS) {
+    // ---- keys of the warp's tokens, eight loads at a time
+    const int here = (int)min((long long)min(ROUTE_TOKENS, n - base), max(0ll, tokens - (t0 + base)));       // tokens among them
+    {
+      constexpr int AT_ONCE = 8;
+      int i = 0, e0 = 0;                                   // the step's token, its first expert
+      const int steps = here * (wide >> 5);
+      for (int s0 = 0; s0 < steps; s0 += AT_ONCE) {
+        float x[AT_ONCE];
+        int at[AT_ONCE], of[AT_ONCE];                      // place among the keys, expert
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) {                // (indexes kept inside, so that no load waits for a condition)
+          of[u] = e0 + lane;
+          at[u] = i * pitch + of[u];
+          x[u] = load_logit<DT>(p.logits, (t0 + base + min(i, here - 1)) * p.ld + min(of[u], p.E - 1));
+          e0 += 32;
+          if (e0 == wide) { e0 = 0; ++i; }
+        }
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) {
+          if (s0 + u >= steps) break;
+          const int e = of[u];
+          const float b = biased ? bias[e] : 0.f;
+          if (e >= p.E || !(b > -INFINITY)) x[u] = -INFINITY;           // (an expert whose bias is -inf or NaN does not take part at all)
+          uint32_t k;
+          if constexpr (PACK16) {
+            uint32_t o;
+            if constexpr (DT == HERO_BF16) o = order32(x[u]) >> 16;
+            else {
+              const uint32_t h = x[u] == 0.f ? 0u : (uint32_t)__half_as_ushort(__float2half_rn(x[u]));
+              o = !(x[u] > -INFINITY) ? 0u : (h & 0x8000u) ? (~h & 0xffffu) : (h | 0x8000u);
+            }
+            k = o ? (o << 16) | (0xffffu - (uint32_t)e) : 0u;
+          } else {
+            k = order32(biased && !softmax && x[u] > -INFINITY ? __fdividef(1.f, 1.f + __expf(-x[u])) + b : x[u]);
+          }
+          keys[at[u]] = k;
+        }
+      }
+    }
+    if (whole) {
+      for (int i = 0; i < here; ++i) {
+        uint32_t* row = keys + i * pitch;
+        const long long t = t0 + base + i;
+        auto logit = [&](int e) {
+          if constexpr (PACK16) return load_logit<DT>(p.logits, t * p.ld + e);
+          else return row[e] ? from_order32(row[e]) : -INFINITY;
+        };
+        float m = -INFINITY;
+        for (int e = lane; e < p.E; e += 32) m = fmaxf(m, logit(e));
+        m = warp_max(m);
+        float sum = 0.f;
+        for (int e = lane; e < p.E; e += 32) sum += exp_below(logit(e), m);
+        sum = warp_sum(sum);
+        if (lane == 0) stats[warp][i] = make_float2(m, sum);
+        if (biased)
+          for (int e = lane; e < p.E; e += 32)
+            if (row[e]) row[e] = order32(exp_below(from_order32(row[e]), m) / sum + bias[e]);
+      }
+    }
+    __syncwarp();
+    // ---- ROUTE_LANES lanes a token
+    const int i = lane / ROUTE_LANES, q = lane % ROUTE_LANES, t = (int)(t0 + base) + i;
+    const bool live = base + i < n, real = live && t < tokens;
+    const uint32_t* row = keys + i * pitch;
+    uint32_t list[KM];
+#pragma unroll
+    for (int j = 0; j < KM; ++j) list[j] = 0u;
+    if (real) {
+#pragma unroll 4
+      for (int e = q; e < wide; e += ROUTE_LANES) {
+        uint32_t v = row[e];
+        if (!PACK16 && v) v = (v & ~p.low) | (p.low - (uint32_t)e);
+        insert<KM>(list, v, 0);
+      }
+    }
+#pragma unroll
+    for (int o = 1; o < ROUTE_LANES; o <<= 1) {
+      uint32_t other[KM];
+#pragma unroll
+      for (int j = 0; j < KM; ++j) other[j] = __shfl_xor_sync(0xffffffffu, list[j], o);
+#pragma unroll
+      for (int j = 0; j < KM; ++j) insert<KM>(list, other[j], j);      // (what is j-th there has j larger ones before it)
+    }
+    // ---- this lane's entries: q, q + ROUTE_LANES, ..: their places, experts (-1: none, or not among the k largest) and logits
+    constexpr int MINE = (KM + ROUTE_LANES - 1) / ROUTE_LANES;
+    int place[MINE], expert[MINE];
+    float x[MINE];
+    float top = -INFINITY;
+    bool near = false;
+    uint32_t whole_key[PACK16 ? 1 : KM];
+    float least = -INFINITY;                               // the k largest are not below it
+    if constexpr (!PACK16) {
+      uint32_t kth = 0u, behind = 0u;                      // k-th and k + 1-th entry
+#pragma unroll
+      for (int j = 0; j < KM; ++j) {
+        whole_key[j] = list[j] ? row[p.low - (list[j] & p.low)] : 0u;
+        if (j == p.k - 1) kth = list[j];
+        if (j == p.k) behind = list[j];
+      }
+      if (kth) least = from_order32(kth & ~p.low);
+      // an expert outside the list may share the bits of the first that is not chosen
+      if (behind) {
+        const float u = from_order32(behind | p.low);
+        near = ((kth ^ behind) & ~p.low) == 0u || (biased && (least - u < key_error(p, u) || !(least > u)));
+      }
+    }
+#pragma unroll
+    for (int a = 0; a < MINE; ++a) {
+      uint32_t k = 0u, key = 0u;
+#pragma unroll
+      for (int b = 0; b < ROUTE_LANES; ++b) {
+        const int j = ROUTE_LANES * a + b;
+        if (j < KM && b == q) {
+          k = list[j];
+          if constexpr (!PACK16) key = whole_key[j];
+        }
+      }
+      place[a] = ROUTE_LANES * a + q;
+      expert[a] = -1;
+      x[a] = -INFINITY;
+      if (place[a] < KM && k) {
+        if constexpr (PACK16) {
+          if (place[a] < p.k) {
+            expert[a] = (int)(0xffffu - (k & 0xffffu));
+            const uint32_t o = k >> 16, b = (o & 0x8000u) ? (o & 0x7fffu) : (~o & 0xffffu);
+            x[a] = DT == HERO_BF16 ? __uint_as_float(b << 16) : __half2float(__ushort_as_half((unsigned short)b));
+          }
+        } else {
+          // its place among the k + 1 by the whole key; the largest key behind it
+          const int e = (int)(p.low - (k & p.low));
+          int rank = 0;
+          uint32_t next = 0u;
+#pragma unroll
+          for (int c = 0; c < KM; ++c) {
+            const int ec = (int)(p.low - (list[c] & p.low));
+            const bool before = whole_key[c] > key || (whole_key[c] == key && ec < e && list[c] != 0u);
+            if (c <= p.k) {
+              rank += before ? 1 : 0;
+              if (!before && ec != e) next = max(next, whole_key[c]);
+            }
+          }
+          if (place[a] <= p.k && rank < p.k) {
+            place[a] = rank;
+            expert[a] = e;
+            const float v = from_order32(key);
+            x[a] = biased ? load_logit<DT>(p.logits, (long long)t * p.ld + e) : v;
+            if (biased && next) {
+              const float u = from_order32(next);
+              near = near || v - u < key_error(p, u) || v == u;
+            }
+          }
+        }
+      }
+    }
+    const uint32_t slow = PACK16 ? 0u : __ballot_sync(0xffffffffu, near);
+    const bool given = (slow >> (ROUTE_LANES * i) & ROUTE_TEAM) != 0u;       // this token is chosen again
+    // ---- weights
+    float w[MINE], all = 0.f;
+#pragma unroll
+    for (int a = 0; a < MINE; ++a) top = fmaxf(top, softmax ? x[a] : expert[a] >= 0 ? fminf(x[a], 0.f) : -INFINITY);
+#pragma unroll
+    for (int o = 1; o < ROUTE_LANES; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const float2 st = whole ? stats[warp][i] : make_float2(0.f, 1.f);
+#pragma unroll
+    for (int a = 0; a < MINE; ++a) {
+      w[a] = 0.f;
+      if (expert[a] >= 0) {
+        if (p.renorm) {
+          // softmax: the factor of all experts cancels.  sigmoid(x) = e^min(x, 0) / (1 + e^-|x|), the first factor relative to its largest
+          if (softmax) w[a] = exp_below(x[a], top);
+          else w[a] = exp_below(fminf(x[a], 0.f), top) / (1.f + expf(-fabsf(x[a])));
+        } else {
+          w[a] = softmax ? exp_below(x[a], st.x) / st.y : 1.f / (1.f + expf(-x[a]));
+        }
+      }
+      all += w[a];
+    }
+#pragma unroll
+    for (int o = 1; o < ROUTE_LANES; o <<= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
+    // (an empty place is one from the number of experts found on: the list is full up to there)
+    int found = 0;
+#pragma unroll
+    for (int j = 0; j < KM; ++j) found += j < p.k && list[j] ? 1 : 0;
+    if (live && !given) {
+#pragma unroll
+      for (int a = 0; a < MINE; ++a) {
+        if (expert[a] >= 0) {
+          p.expert[(long long)t * p.k + place[a]] = expert[a];
+          p.weight[(long long)t * p.k + place[a]] = (p.renorm ? w[a] / all : w[a]) * p.scale;
+          atomicAdd(&count[expert[a]], 1);                 // (shared memory, whole numbers: any order gives the same)
+        }
+        const int j = ROUTE_LANES * a + q;
+        if (j >= found && j < p.k) {
+          p.expert[(long long)t * p.k + j] = -1;
+          p.weight[(long long)t * p.k + j] = 0.f;
+        }
+      }
+    }
+    if constexpr (!PACK16) {
+      if (slow) {
+        for (int s = 0; s < ROUTE_TOKENS; ++s) {
+          if (!(slow >> (ROUTE_LANES * s) & ROUTE_TEAM)) continue;
+          const float border = __shfl_sync(0xffffffffu, least, ROUTE_LANES * s);
+          int e = -1;
+          if ((softmax && biased) || !route_near<DT>(p, (int)(t0 + base) + s, keys + s * pitch, border, whole ? stats[warp][s] : make_float2(0.f, 1.f), near_list[warp], lane, e))
+            e = route_token<16, DT>(p, (int)(t0 + base) + s, tokens, lane);
+          if (e >= 0) atomicAdd(&count[e], 1);
+        }
+      }
+    }
+    __syncwarp();                                          // the keys are read
   }
   __syncthreads();
   for (int e = threadIdx.x; e < p.E; e += blockDim.x) p.counts[(long long)blockIdx.x * p.E + e] = count[e];
@@ -406,23 +692,32 @@ __global__ void route_none_kernel(int* offset, int E) {    // no tokens at all
 }
 
 static int route_chunk(const hero_handle* h, long long T) {
-  long long c = ((T + h->sm_count - 1) / h->sm_count + 31) / 32 * 32;
+  // as many chunks as SMs, of whole warps' eights
+  long long c = ((T + h->sm_count - 1) / h->sm_count + 7) / 8 * 8;
   return (int)(c > ROUTE_MAX_CHUNK ? ROUTE_MAX_CHUNK : c);
 }
 
 template <int R, int DT>
-static hero_status launch_route(hero_handle* h, RouteParams& p, cudaStream_t s) {
-  if (p.T <= ROUTE_ONE_CTA) {
-    p.words = (p.T + 31) / 32;
-    const int warps = p.T < 32 ? p.T : 32;
-    LaunchScope scope(h, s, KERNEL_ROUTE);
-    HERO_CUDA(launch_dependent(route_one_kernel<R, DT>, dim3(1), dim3(32 * warps), (size_t)p.E * p.words * 4, s, p));
-    return HERO_OK;
-  }
+static hero_status launch_one(hero_handle* h, RouteParams& p, cudaStream_t s) {
+  p.words = (p.T + 31) / 32;
+  const int warps = p.T < 32 ? p.T : 32;
+  LaunchScope scope(h, s, KERNEL_ROUTE);
+  HERO_CUDA(launch_dependent(route_one_kernel<R, DT>, dim3(1), dim3(32 * warps), (size_t)p.E * p.words * 4, s, p));
+  return HERO_OK;
+}
+template <int KM, int DT, bool PACK16>
+static hero_status launch_two(hero_handle* h, RouteParams& p, cudaStream_t s) {
   const unsigned ctas = (unsigned)((p.T + p.chunk - 1) / p.chunk);
+  // a warp for every four tokens of the chunk, as many as the shared memory holds the keys of
+  const size_t warp_bytes = ROUTE_TOKENS * (size_t)((p.E + 31) / 32 * 32 + ROUTE_LANES) * 4;
+  int warps = (p.chunk + ROUTE_TOKENS - 1) / ROUTE_TOKENS;
+  if (warps > ROUTE_THREADS / 32) warps = ROUTE_THREADS / 32;
+  if (warps > (int)(ROUTE_KEY_BYTES / warp_bytes)) warps = (int)(ROUTE_KEY_BYTES / warp_bytes);
+  auto choose = route_choose_kernel<KM, DT, PACK16>;
+  HERO_SMEM_OPT_IN(h, choose, ROUTE_KEY_BYTES);
   {
     LaunchScope scope(h, s, KERNEL_ROUTE);
-    HERO_CUDA(launch_dependent(route_choose_kernel<R, DT>, dim3(ctas), dim3(ROUTE_THREADS), 0, s, p));
+    HERO_CUDA(launch_dependent(choose, dim3(ctas), dim3(32 * warps), warps * warp_bytes, s, p));
   }
   HERO_SMEM_OPT_IN(h, route_place_kernel, ROUTE_MAX_E * (ROUTE_MAX_CHUNK / 32) * 4);
   {
@@ -434,11 +729,27 @@ static hero_status launch_route(hero_handle* h, RouteParams& p, cudaStream_t s) 
 
 template <int DT>
 static hero_status route_for(hero_handle* h, RouteParams& p, cudaStream_t s) {
-  if (p.E <= 32) return launch_route<1, DT>(h, p, s);
-  if (p.E <= 64) return launch_route<2, DT>(h, p, s);
-  if (p.E <= 128) return launch_route<4, DT>(h, p, s);
-  if (p.E <= 256) return launch_route<8, DT>(h, p, s);
-  return launch_route<16, DT>(h, p, s);
+  if (p.T <= ROUTE_ONE_CTA) {
+    if (p.E <= 32) return launch_one<1, DT>(h, p, s);
+    if (p.E <= 64) return launch_one<2, DT>(h, p, s);
+    if (p.E <= 128) return launch_one<4, DT>(h, p, s);
+    if (p.E <= 256) return launch_one<8, DT>(h, p, s);
+    return launch_one<16, DT>(h, p, s);
+  }
+  if constexpr (DT != HERO_F32) {
+    if (p.bias == nullptr) {
+      if (p.k <= 2) return launch_two<2, DT, true>(h, p, s);
+      if (p.k <= 4) return launch_two<4, DT, true>(h, p, s);
+      if (p.k <= 8) return launch_two<8, DT, true>(h, p, s);
+      return launch_two<16, DT, true>(h, p, s);
+    }
+  }
+  p.low = 31u;
+  while (p.low < (uint32_t)p.E - 1) p.low = 2 * p.low + 1;
+  const int places = p.k + 1;
+  if (places <= 4) return launch_two<4, DT, false>(h, p, s);
+  if (places <= 9) return launch_two<9, DT, false>(h, p, s);
+  return launch_two<17, DT, false>(h, p, s);
 }
 
 static hero_status route_sizes(int64_t T, int32_t E, int32_t k) {
@@ -450,7 +761,7 @@ static hero_status route_sizes(int64_t T, int32_t E, int32_t k) {
 static size_t route_workspace(const hero_handle* h, int64_t T, int32_t E) {
   // the most chunks that any smaller number of tokens takes: one per SM, or T / ROUTE_MAX_CHUNK
   const int64_t ctas = (T + ROUTE_MAX_CHUNK - 1) / ROUTE_MAX_CHUNK;
-  const int64_t few = (T + 31) / 32 < h->sm_count ? (T + 31) / 32 : h->sm_count;
+  const int64_t few = (T + 7) / 8 < h->sm_count ? (T + 7) / 8 : h->sm_count;
   return T <= ROUTE_ONE_CTA ? 0 : (size_t)(ctas > few ? ctas : few) * (size_t)E * 4;
 }
 
@@ -500,6 +811,6 @@ extern "C" hero_status hero_moe_route(hero_handle* h, const hero_moe_route_args*
   p.expert = a->expert; p.weight = a->weight; p.offset = a->offset; p.token = a->token; p.row = a->row;
   p.counts = static_cast<int*>(a->workspace);
   p.chunk = route_chunk(h, p.T);
-  p.words = p.chunk / 32;
+  p.words = (p.chunk + 31) / 32;
   return x.dtype == HERO_F32 ? route_for<HERO_F32>(h, p, s) : x.dtype == HERO_F16 ? route_for<HERO_F16>(h, p, s) : route_for<HERO_BF16>(h, p, s);
 }
