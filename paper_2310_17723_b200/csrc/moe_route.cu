@@ -412,27 +412,24 @@ __global__ void __launch_bounds__(ROUTE_THREADS, 1) route_choose_kernel(const __
   const long long t0 = (long long)blockIdx.x * p.chunk;
   const int n = (int)min((long long)p.chunk, p.T - t0);
   for (int base = warp * ROUTE_TOKENS; base < n; base += nw * ROUTE_TOKENS) {
-    // ---- keys of the warp's tokens, eight loads at a time
+    // ---- keys of the warp's tokens, 16 loads at a time
     const int here = (int)min((long long)min(ROUTE_TOKENS, n - base), max(0ll, tokens - (t0 + base)));       // tokens among them
     {
-      constexpr int AT_ONCE = 8;
-      int i = 0, e0 = 0;                                   // the step's token, its first expert
+      constexpr int AT_ONCE = 16;
+      int i = 0, e0 = 0, ci = 0, c0 = 0;                   // token and first expert of the step that is loaded, that is converted
       const int steps = here * (wide >> 5);
       for (int s0 = 0; s0 < steps; s0 += AT_ONCE) {
         float x[AT_ONCE];
-        int at[AT_ONCE], of[AT_ONCE];                      // place among the keys, expert
 #pragma unroll
         for (int u = 0; u < AT_ONCE; ++u) {                // (indexes kept inside, so that no load waits for a condition)
-          of[u] = e0 + lane;
-          at[u] = i * pitch + of[u];
-          x[u] = load_logit<DT>(p.logits, (t0 + base + min(i, here - 1)) * p.ld + min(of[u], p.E - 1));
+          x[u] = load_logit<DT>(p.logits, (t0 + base + min(i, here - 1)) * p.ld + min(e0 + lane, p.E - 1));
           e0 += 32;
           if (e0 == wide) { e0 = 0; ++i; }
         }
 #pragma unroll
         for (int u = 0; u < AT_ONCE; ++u) {
           if (s0 + u >= steps) break;
-          const int e = of[u];
+          const int e = c0 + lane;
           const float b = biased ? bias[e] : 0.f;
           if (e >= p.E || !(b > -INFINITY)) x[u] = -INFINITY;           // (an expert whose bias is -inf or NaN does not take part at all)
           uint32_t k;
@@ -447,7 +444,9 @@ __global__ void __launch_bounds__(ROUTE_THREADS, 1) route_choose_kernel(const __
           } else {
             k = order32(biased && !softmax && x[u] > -INFINITY ? __fdividef(1.f, 1.f + __expf(-x[u])) + b : x[u]);
           }
-          keys[at[u]] = k;
+          keys[ci * pitch + e] = k;
+          c0 += 32;
+          if (c0 == wide) { c0 = 0; ++ci; }
         }
       }
     }
