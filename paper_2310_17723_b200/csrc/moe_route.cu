@@ -23,6 +23,7 @@
 #include "ptx.cuh"
 #include <cuda_fp16.h>
 #include <cuda_bf16.h>
+#include <type_traits>
 
 namespace hero {
 
@@ -391,14 +392,18 @@ __device__ __noinline__ bool route_near(const RouteParams& p, int t, const uint3
 }
 __device__ __forceinline__ int route_pitch(int E) { return (E + 31) / 32 * 32 + ROUTE_LANES; }    // (tokens on banks of their own)
 
+// (keys in 32 bits that are put in order afterwards take more than 64 registers)
+template <bool PACK16>
+constexpr int ROUTE_CHOOSE_THREADS = PACK16 ? 1024 : 512;
+
 // KM: places of a lane's list, at least k (PACK16: 16-bit logits without a bias) or k + 1
 template <int KM, int DT, bool PACK16>
-__global__ void __launch_bounds__(ROUTE_THREADS, 1) route_choose_kernel(const __grid_constant__ RouteParams p) {
+__global__ void __launch_bounds__(ROUTE_CHOOSE_THREADS<PACK16>, 1) route_choose_kernel(const __grid_constant__ RouteParams p) {
   extern __shared__ uint32_t keys_of[];                    // [warps][tokens][pitch]
   __shared__ int count[ROUTE_MAX_E];
   __shared__ float bias[PACK16 ? 1 : ROUTE_MAX_E];
-  __shared__ int near_list[PACK16 ? 1 : ROUTE_THREADS / 32][64];
-  __shared__ float2 stats[ROUTE_THREADS / 32][ROUTE_TOKENS];          // of a token's softmax over all experts: maximum, sum
+  __shared__ int near_list[PACK16 ? 1 : ROUTE_CHOOSE_THREADS<PACK16> / 32][64];
+  __shared__ float2 stats[ROUTE_CHOOSE_THREADS<PACK16> / 32][ROUTE_TOKENS];          // of a token's softmax over all experts: maximum, sum
   ptx::pdl_launch_dependents();
   for (int e = threadIdx.x; e < p.E; e += blockDim.x) count[e] = 0;
   ptx::pdl_wait();
@@ -426,28 +431,38 @@ __global__ void __launch_bounds__(ROUTE_THREADS, 1) route_choose_kernel(const __
           e0 += 32;
           if (e0 == wide) { e0 = 0; ++i; }
         }
+        // (no branch between the steps: their chains overlap)
+        auto convert = [&](auto sigmoid_key) {
 #pragma unroll
-        for (int u = 0; u < AT_ONCE; ++u) {
-          if (s0 + u >= steps) break;
-          const int e = c0 + lane;
-          const float b = biased ? bias[e] : 0.f;
-          if (e >= p.E || !(b > -INFINITY)) x[u] = -INFINITY;           // (an expert whose bias is -inf or NaN does not take part at all)
-          uint32_t k;
-          if constexpr (PACK16) {
-            uint32_t o;
-            if constexpr (DT == HERO_BF16) o = order32(x[u]) >> 16;
-            else {
-              const uint32_t h = x[u] == 0.f ? 0u : (uint32_t)__half_as_ushort(__float2half_rn(x[u]));
-              o = !(x[u] > -INFINITY) ? 0u : (h & 0x8000u) ? (~h & 0xffffu) : (h | 0x8000u);
+          for (int u = 0; u < AT_ONCE; ++u) {
+            const int e = c0 + lane;
+            float v = x[u];
+            if constexpr (!PACK16) {
+              if (biased) {                                // (an expert whose bias is -inf or NaN does not take part at all)
+                const float b = bias[e];
+                if constexpr (decltype(sigmoid_key)::value) v = v > -INFINITY && b > -INFINITY ? __fdividef(1.f, 1.f + __expf(-v)) + b : -INFINITY;
+                else v = b > -INFINITY ? v : -INFINITY;
+              }
             }
-            k = o ? (o << 16) | (0xffffu - (uint32_t)e) : 0u;
-          } else {
-            k = order32(biased && !softmax && x[u] > -INFINITY ? __fdividef(1.f, 1.f + __expf(-x[u])) + b : x[u]);
+            uint32_t k;
+            if constexpr (PACK16) {
+              uint32_t o;
+              if constexpr (DT == HERO_BF16) o = order32(v) >> 16;
+              else {
+                const uint32_t h = v == 0.f ? 0u : (uint32_t)__half_as_ushort(__float2half_rn(v));
+                o = !(v > -INFINITY) ? 0u : (h & 0x8000u) ? (~h & 0xffffu) : (h | 0x8000u);
+              }
+              k = o ? (o << 16) | (0xffffu - (uint32_t)e) : 0u;
+            } else {
+              k = order32(v);
+            }
+            if (s0 + u < steps) keys[ci * pitch + e] = e < p.E ? k : 0u;
+            c0 += 32;
+            if (c0 == wide) { c0 = 0; ++ci; }
           }
-          keys[ci * pitch + e] = k;
-          c0 += 32;
-          if (c0 == wide) { c0 = 0; ++ci; }
-        }
+        };
+        if (biased && !softmax) convert(std::true_type{});
+        else convert(std::false_type{});
       }
     }
     if (whole) {
@@ -710,7 +725,7 @@ static hero_status launch_two(hero_handle* h, RouteParams& p, cudaStream_t s) {
   // a warp for every four tokens of the chunk, as many as the shared memory holds the keys of
   const size_t warp_bytes = ROUTE_TOKENS * (size_t)((p.E + 31) / 32 * 32 + ROUTE_LANES) * 4;
   int warps = (p.chunk + ROUTE_TOKENS - 1) / ROUTE_TOKENS;
-  if (warps > ROUTE_THREADS / 32) warps = ROUTE_THREADS / 32;
+  if (warps > ROUTE_CHOOSE_THREADS<PACK16> / 32) warps = ROUTE_CHOOSE_THREADS<PACK16> / 32;
   if (warps > (int)(ROUTE_KEY_BYTES / warp_bytes)) warps = (int)(ROUTE_KEY_BYTES / warp_bytes);
   auto choose = route_choose_kernel<KM, DT, PACK16>;
   HERO_SMEM_OPT_IN(h, choose, ROUTE_KEY_BYTES);
