@@ -92,20 +92,30 @@ def test_ties_masks_infinities_and_nan(h, T, dt, biased, score):
         check(o, x, k, score=score, renorm=renorm, bias=b)
 
 
+@pytest.mark.parametrize("T", [60, 130])
+@pytest.mark.parametrize("biased", [False, True])
+@pytest.mark.parametrize("few", [False, True])
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
-def test_keys_that_fp32_cannot_tell_apart(h, score):
-    # logits a unit of FP32 apart where a unit of the score is far coarser, in falling order of the expert: rounded keys would tie
-    T, E, k = 130, 96, 7
+def test_keys_that_fp32_cannot_tell_apart(h, score, few, biased, T):
+    # logits a unit of FP32 apart where a unit of the score is far coarser, in falling order of the expert: rounded keys would tie.  All experts, or
+    # (few) nine of them around the border of the choice
+    E, k = 96, 7
     g = np.random.default_rng(6)
     base = g.uniform(2.0, 6.0, (T, 1)).astype(np.float32)
     x = base + np.arange(E, dtype=np.float32)[None] * np.spacing(base)
+    if few:
+        y = (base - 4 + g.standard_normal((T, E)) * 0.5).astype(np.float32)
+        near = np.array([3, 90, 17, 64, 40, 33, 95, 8, 50])
+        y[:, near] = x[:, near]
+        y[:, [1, 2]] = base + 1                            # two that are clearly first
+        x = y
     xt, x = f32(x)
-    bt, b = f32(np.full(E, 0.125))
+    bt, b = f32(np.full(E, 0.125)) if biased else (None, None)
     o = Out(h, T, E, k)
     h.hero_moe_route(hero.tensor(xt), *o.args(), score=score, select_bias=bt, workspace=o.workspace)
     h.check()
     check(o, x.astype(np.float64), k, score=score, bias=b)
-    assert o.expert[0].tolist() == [95, 94, 93, 92, 91, 90, 89]
+    assert o.expert[0].tolist() == ([1, 2, 95, 90, 64, 50, 40] if few else [95, 94, 93, 92, 91, 90, 89])
 
 
 @pytest.mark.parametrize("T", [50, 1000])
