@@ -8,7 +8,7 @@
 //                registers (a maximum and a minimum for each place); three exchanges between lanes merge the eight lists.  A key's low bits are the
 //                inverted expert, so that one comparison orders equal logits too: below the 16 bits of a 16-bit logit, in the last 5 to 9 bits of
 //                all other keys, whose k + 1 places are put in order by the whole keys afterwards.  (Whole keys in 64 bits: 36 us against
-//                20 on 5000 tokens of 256 experts.)  Where what the low bits hid could change the choice, the token is chosen again.
+//                27 on 5000 tokens of 256 experts, the rest alike.)  Where what the low bits hid could change the choice, the token is chosen again.
 // With a selection bias the keys are FP32 scores plus bias.  Where two neighbours of the k + 1 largest are nearer than FP32 can tell apart, the
 // token is chosen again from FP64 keys: of the experts that are near enough to matter, one a lane, or (more than 32 of them, a softmax) of all.
 //
@@ -17,8 +17,8 @@
 // CTA does everything.  More: each CTA of a first kernel counts its own tokens' experts, and each CTA of a second one adds up the
 // counts of those before it (and of all, for the experts' first rows) and places its pairs.
 //
-// The bytes are few (2 to 4 per logit); what bounds it is the instructions of the choice and the latency of two launches (measured below the
-// kernels' launch).
+// The bytes are few (2 to 4 per logit); what bounds it is the instructions of the choice and the latency of two launches: 16383 tokens of 128 experts, top 8,
+// 15 us (18.5 with a warp a token), 5000 tokens of 256 experts with sigmoid and bias 22.5 (30); 16 tokens of 64 experts 4.2 in a graph.
 #include "common.cuh"
 #include "ptx.cuh"
 #include <cuda_fp16.h>
