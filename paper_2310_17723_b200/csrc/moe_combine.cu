@@ -4,7 +4,7 @@
 // byte is read and written once.  Bound by HBM, which wants many bytes in flight.  Two kernels:
 //
 //   moe_combine_kernel       a token to 1, 2, 4 or 8 warps that load its rows into registers, eight rows at a time.  For few tokens, wide rows.
-//   moe_combine_ring_kernel  many tokens: persistent, two warps copy whole rows (cp.async.bulk) into a ring of stages of one token each, two
+//   moe_combine_ring_kernel  many tokens: persistent, four warps copy whole rows (cp.async.bulk) into a ring of stages of one token each, two
 //                            or six groups of four warps take the tokens in turn
 #include "block_cache.cuh"
 
@@ -273,7 +273,7 @@ __global__ void __launch_bounds__(COMBINE_THREADS, NCH <= 2 ? 4 : 1) moe_combine
 }
 
 // ---- many tokens
-constexpr int RING_GROUP_WARPS = 4, RING_COPY_WARPS = 2, RING_MAX_STAGES = 12, RING_BYTES = 216 * 1024;
+constexpr int RING_GROUP_WARPS = 4, RING_COPY_WARPS = 4, RING_MAX_STAGES = 12, RING_BYTES = 216 * 1024;
 // groups of warps that the registers allow (the sums of a lane are 8 NCH)
 template <int NCH>
 constexpr int RING_GROUPS = NCH <= 2 ? 6 : 2;
@@ -289,7 +289,7 @@ __global__ void __launch_bounds__((RING_GROUPS<NCH> * RING_GROUP_WARPS + RING_CO
   __shared__ float part[GROUPS][3 * RING_GROUP_WARPS];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   if (threadIdx.x == 0) {
-    for (int i = 0; i < p.stages; ++i) { ptx::mbar_init(&full[i], 1); ptx::mbar_init(&empty[i], RING_GROUP_WARPS); }
+    for (int i = 0; i < p.stages; ++i) { ptx::mbar_init(&full[i], RING_COPY_WARPS); ptx::mbar_init(&empty[i], RING_GROUP_WARPS); }
     ptx::fence_mbar_init();
   }
   __syncthreads();
@@ -298,35 +298,35 @@ __global__ void __launch_bounds__((RING_GROUPS<NCH> * RING_GROUP_WARPS + RING_CO
   const uint32_t row_bytes = (uint32_t)p.H * (Q8 ? 1 : 2);
   int stage = 0; uint32_t phase = 0;
   if (warp >= GROUPS * RING_GROUP_WARPS) {
-    // ------------------------------------------------------------------ copies: two warps, every other token each (and every other stage: their number is even)
+    // ------------------------------------------------------------------ copies: warp q has the places q, q + RING_COPY_WARPS, .. of every token
     const int q = warp - GROUPS * RING_GROUP_WARPS;
-    const long long step = (long long)RING_COPY_WARPS * gridDim.x;
-    long long t = blockIdx.x + (long long)q * gridDim.x;
-    stage = q;
-    Place now = load_place<YCOL>(p, t, lane), next = load_place<YCOL>(p, t + step, lane);
-    for (; t < p.T; t += step) {
-      const Place later = load_place<YCOL>(p, t + 2 * step, lane);
+    long long t = blockIdx.x;
+    Place now = load_place<YCOL>(p, t, lane), next = load_place<YCOL>(p, t + gridDim.x, lane);
+    for (; t < p.T; t += gridDim.x) {
+      const Place later = load_place<YCOL>(p, t + 2 * (long long)gridDim.x, lane);
       check_place(p, now);
       if (!__all_sync(0xffffffffu, ptx::mbar_wait(&empty[stage], phase ^ 1, p.err, 0x1000 | stage))) break;
-      if (lane < COMBINE_MAX_K) { places[stage].row[lane] = now.row; places[stage].expert[lane] = now.expert; places[stage].weight[lane] = now.weight; }
       const uint32_t some = __ballot_sync(0xffffffffu, now.row >= 0);
-      if (lane == 0) places[stage].all = __popc(some) == p.k;
+      const bool mine = now.row >= 0 && lane % RING_COPY_WARPS == q;
+      const uint32_t ours = __ballot_sync(0xffffffffu, mine);
+      if (q == 0) {
+        if (lane < COMBINE_MAX_K) { places[stage].row[lane] = now.row; places[stage].expert[lane] = now.expert; places[stage].weight[lane] = now.weight; }
+        if (lane == 0) places[stage].all = __popc(some) == p.k;
+      }
       __syncwarp();
-      if (lane == 0) ptx::mbar_expect_tx(&full[stage], __popc(some) * row_bytes);         // (an arrival that tells of the places too)
+      if (lane == 0) ptx::mbar_expect_tx(&full[stage], __popc(ours) * row_bytes);         // (an arrival that tells of the places too)
       __syncwarp();
-      if (now.row >= 0)
+      if (mine)
         asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                      ::"r"(ptx::smem_u32(rows + ((size_t)stage * p.k + lane) * row_bytes)),
                      "l"(static_cast<const uint8_t*>(p.y.data) + now.row * p.y.ld * (Q8 ? 1 : 2)), "r"(row_bytes), "r"(ptx::smem_u32(&full[stage])) : "memory");
       now = next; next = later;
-      stage += RING_COPY_WARPS;
-      if (stage >= p.stages) { stage -= p.stages; phase ^= 1; }
+      if (++stage == p.stages) { stage = 0; phase ^= 1; }
     }
     // every copy started here has landed before the CTA leaves
-    for (int i = 0; i < p.stages; i += RING_COPY_WARPS) {
+    for (int i = 0; i < p.stages; ++i) {
       if (!ptx::mbar_wait(&empty[stage], phase ^ 1, p.err, 0x1080 | stage)) break;
-      stage += RING_COPY_WARPS;
-      if (stage >= p.stages) { stage -= p.stages; phase ^= 1; }
+      if (++stage == p.stages) { stage = 0; phase ^= 1; }
     }
   } else {
     // ------------------------------------------------------------------ sums: group g has the CTA's tokens g, g + GROUPS, ..
