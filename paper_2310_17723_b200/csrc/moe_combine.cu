@@ -6,6 +6,9 @@
 //   moe_combine_kernel       a token to 1, 2, 4 or 8 warps that load its rows into registers, eight rows at a time.  For few tokens, wide rows.
 //   moe_combine_ring_kernel  many tokens: persistent, four warps copy whole rows (cp.async.bulk) into a ring of stages of one token each, two
 //                            or six groups of four warps take the tokens in turn
+//
+// 8192 tokens, top 8, 2048 features of BF16, LN^quant: the ring 69 us (0.78 of copy bandwidth; two copying warps 76, three groups 94), registers 87, a CTA a token
+// 147.  INT8 rows with a scale for each expert and feature: 92 us (4 bytes of scale for each code, through L2: the ring leaves the first-level cache nothing).
 #include "block_cache.cuh"
 
 namespace hero {
