@@ -341,6 +341,7 @@ __global__ void __launch_bounds__((RING_GROUPS<NCH> * RING_GROUP_WARPS + RING_CO
     const float one = !YCOL && p.y.col_scale ? __ldg(p.y.col_scale) : 1.f;
     auto forward = [&]() { if (++stage == p.stages) { stage = 0; phase ^= 1; } };
     for (int i = 0; i < g; ++i) forward();
+    bool ok = true;
     for (long long t = blockIdx.x + (long long)g * gridDim.x; t < p.T; t += (long long)GROUPS * gridDim.x) {
       float2 v[NCH][4];
 #pragma unroll
@@ -352,7 +353,8 @@ __global__ void __launch_bounds__((RING_GROUPS<NCH> * RING_GROUP_WARPS + RING_CO
           add_side(p.shared, t, first + c * STRIDE, v[c]);
         }
       }
-      if (!__all_sync(0xffffffffu, ptx::mbar_wait(&full[stage], phase, p.err, 0x1100 | stage))) break;
+      // (a wait that gave up has recorded its code: the warp runs on without waiting, so that none is left at a barrier, and its tokens become NaN)
+      ok = ok && __all_sync(0xffffffffu, ptx::mbar_wait(&full[stage], phase, p.err, 0x1100 | stage));
       const RingPlace& at = places[stage];
       const uint8_t* base = rows + (size_t)stage * p.k * row_bytes;
       auto add = [&](int j) {
@@ -363,12 +365,18 @@ __global__ void __launch_bounds__((RING_GROUPS<NCH> * RING_GROUP_WARPS + RING_CO
           if (first + c * STRIDE < p.H)
             add_row<KIND, YCOL>(load8<Q8>(base + j * row_bytes, first + c * STRIDE), scale + c * STRIDE, one, wj, v[c]);
       };
-      int j = 0;
+      int j = ok ? 0 : p.k;
       for (; at.all && j + 4 <= p.k; j += 4) {             // no place is empty: four rows at a time, without a question between their loads
         add(j); add(j + 1); add(j + 2); add(j + 3);
       }
       for (; j < p.k; ++j)
         if (at.row[j] >= 0) add(j);
+      if (!ok) {
+#pragma unroll
+        for (int c = 0; c < NCH; ++c)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[c][i] = make_float2(NAN, NAN);
+      }
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(&empty[stage]);
       finish_token<NCH>(p, t, first, STRIDE, v, team);

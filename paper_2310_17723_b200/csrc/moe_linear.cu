@@ -8,10 +8,10 @@
 //
 // A CTA (or a pair of them, tcgen05 cta_group::2, 128 features each) is persistent over tiles of (expert, rows of the expert, features).  The
 // rows of an expert are dealt evenly to as few tiles as they need.
-//   epilogue warps (single CTAs 4, pairs 8, pairs with A in order 16)  tensor memory -> registers -> scales, activation, rounding -> shared memory (turned) -> whole row segments out.  A word holds
-//                       four (two) rows of a feature: shared memory is what the products' operands fill already, and a byte at a time costs it four
-//                       times the cycles
-//   row warps (8; 2)    rows of A picked by token: TMA gathers of four rows.  One warp starts one every 80 cycles or so, a k-block takes 32 in 512
+//   epilogue warps      (single CTAs 4, pairs 8, pairs with A in order 16)  tensor memory -> registers -> scales, activation, rounding -> shared memory
+//                       (turned) -> whole row segments out.  A word holds four (two) rows of a feature: shared memory is what the products' operands
+//                       fill already, and a byte at a time costs it four times the cycles
+//   row warps           (pairs 8, single CTAs 2)  rows of A picked by token: TMA gathers of four rows.  One warp starts one every 80 cycles or so, a k-block takes 32 in 512
 //                       cycles: two row warps for each four gave 197 us where four gave 231 (8192 tokens, top 8 of 64, 2048 x 2048)
 //   load warp           W tiles, and A where its rows are in order (TMA)
 //   vector warp         row factors, scales, biases and output factors of the next tile, to shared memory (two loads that depend on one another
@@ -401,6 +401,21 @@ __device__ __forceinline__ void moe_vectors(const MoeLinearParams& p, uint8_t* s
   }
 }
 
+// Whether all four warps of an epilogue group say so (they meet on the group's barrier): what one warp's wait did not bring ends the walk of all, none of
+// them is left at a barrier.
+__device__ __forceinline__ bool group_all(bool ok, int id) {
+  uint32_t r;
+  __syncwarp();
+  asm volatile(
+      "{\n"
+      ".reg .pred p, q;\n"
+      "setp.ne.u32 p, %1, 0;\n"
+      "bar.red.and.pred q, %2, 128, p;\n"
+      "selp.u32 %0, 1, 0, q;\n"
+      "}\n" : "=r"(r) : "r"(ok ? 1u : 0u), "r"(id) : "memory");
+  return r != 0;
+}
+
 // The epilogue warps, tile after tile as the vector warp names them.
 template <bool INT8, bool GATED, bool PAIR, bool GATHER, int ACT, int OUTK>
 __device__ __forceinline__ void moe_epilogue(const MoeLinearParams& p, uint8_t* smem, uint64_t* acc_full, uint64_t* acc_empty, uint64_t* vec_full,
@@ -413,12 +428,11 @@ __device__ __forceinline__ void moe_epilogue(const MoeLinearParams& p, uint8_t* 
   const int warp_col = quarter * (GATED ? 16 : 32);                                    // first output column of this warp in the CTA's
   bool ok = true;
   int turned = 0;
-  for (int it = 0; ok; ++it) {
+  for (int it = 0;; ++it) {
     const int as = it & 1;
     const uint32_t aphase = (it >> 1) & 1;
-    // (a wait that gives up has recorded its code; the warp leaves after this tile)
-    ok = __all_sync(0xffffffffu, ptx::mbar_wait(&vec_full[as], aphase, p.err, 0xF84 | as));
-    if (!ok) break;
+    // (a wait that gives up has recorded its code; the group leaves before the next tile)
+    if (!group_all(ok && ptx::mbar_wait(&vec_full[as], aphase, p.err, 0xF84 | as), 1 + group)) break;
     const float* vec = reinterpret_cast<const float*>(smem + Cfg::VEC_AT) + as * Cfg::VEC_FLOATS;
     const int4 tile = *reinterpret_cast<const int4*>(vec + MT + 384);
     const MoeTile w{tile.z, tile.x, tile.y & 0xffff, tile.w, (tile.y >> 16) & 0xff, tile.y >> 24};
@@ -456,7 +470,7 @@ __device__ __forceinline__ void moe_epilogue(const MoeLinearParams& p, uint8_t* 
       if constexpr (Cfg::TURN_BUFS == 2) buf += (turned++ & 1) * (Cfg::TURN_BYTES / 8);
       else asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory");          // the group is through with the chunk before
       const int rows = min(MOE_CHUNK, w.rows - c * MOE_CHUNK);
-      if (mine) moe_chunk<INT8, GATED, ACT, OUTK>(p, r, vec + c * MOE_CHUNK, l, buf + warp_col, lane, rows, most);
+      if (mine && ok) moe_chunk<INT8, GATED, ACT, OUTK>(p, r, vec + c * MOE_CHUNK, l, buf + warp_col, lane, rows, most);
       if (c + GROUPS < chunks) moe_tmem_ld<GATED>(taddr + (c + GROUPS) * MOE_CHUNK, r);       // on its way while this chunk is stored
       // the group's four warps have written the chunk (of two buffers, the one of two chunks ago is free too)
       asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory");
