@@ -23,6 +23,7 @@
 // Gated products (act(gate) * up): a tile's 128 rows of W are eight rows of the gate's half and eight of the other in turn (one tensor map does
 // that).  Read in the shape of 16 lanes x 256 bits, tensor memory then gives a thread both products of a feature for the same two rows.
 #include "gemm_common.cuh"
+#include "moe_deal.cuh"
 
 namespace hero {
 
@@ -44,17 +45,15 @@ struct MoeLinearParams {
 
 template <bool PAIR, bool GATHER>
 struct MoeCfg {
-  static constexpr int MT = PAIR ? 256 : 32;              // rows of a tile at most
-  static constexpr int ROWS = PAIR ? MT / 2 : MT;         // ... that this CTA loads
-  static constexpr int STEP = PAIR ? 32 : 16;             // granularity of the N side
+  static constexpr int MT = MoeRows<PAIR>::MT, ROWS = MoeRows<PAIR>::ROWS, STEP = MoeRows<PAIR>::STEP;
   static constexpr int FEAT = 128;                        // features of this CTA
   static constexpr int W_BYTES = FEAT * GEMM_BK_BYTES, X_BYTES = ROWS * GEMM_BK_BYTES, STAGE_BYTES = W_BYTES + X_BYTES;
   static constexpr int STAGES = PAIR ? 5 : 4;
   static constexpr int EPI_WARPS = !PAIR ? 4 : !GATHER ? 16 : 8, EPI_GROUPS = EPI_WARPS / 4;
-  static constexpr int ROW_WARPS = !GATHER ? 0 : PAIR ? 8 : 2;
+  static constexpr int ROW_WARPS = GATHER ? MoeRows<PAIR>::WARPS : 0;
   static constexpr int ROW_WARP = EPI_WARPS, LOAD_WARP = ROW_WARP + ROW_WARPS, MMA_WARP = LOAD_WARP + 1, VEC_WARP = MMA_WARP + 1,
                        THREADS = (VEC_WARP + 1) * 32;
-  static constexpr int BOX = PAIR ? 64 : 16;              // rows of a copy where A is in order
+  static constexpr int BOX = MoeRows<PAIR>::BOX;
   static constexpr int TURN_BUFS = EPI_GROUPS <= 2 ? 2 : 1;
   static constexpr int TURN_BYTES = TURN_BUFS * 16 * 128 * 4;             // per epilogue group: buffers of 32 rows of 16-bit outputs, in words of two rows
   static constexpr int TMEM_COLS = 2 * MT;
@@ -67,65 +66,6 @@ struct MoeCfg {
   static constexpr int PER_SM = PAIR ? 1 : 2;             // CTAs of an SM
   static_assert(PER_SM * (SMEM_BYTES + 1024) <= 228 * 1024, "shared memory");
 };
-
-// A piece of work: rows of an expert (0: none) and a tile of features, or a part of it (single CTAs: part `part` of 1 << split parts).
-struct MoeTile { int e, row0, rows, nt, part, split; };
-
-// The launch's tiles are dealt out in rounds, one for each CTA (or pair).  Where the last round has tiles for a half or a quarter of them only, these are cut
-// in two or four, each part for a CTA of its own: single CTAs by features (a part brings its share of the weights, which is what their
-// time goes to), pairs by rows (a product over fewer rows takes less time, one over fewer features does not).
-struct MoeDeal {
-  const int* first; const int* tiles;         // first sorted row, first row tile of each expert (shared memory, [E + 1])
-  int E, num_nt, full, split, units;          // tiles of the full rounds, parts (log2) of the others, units in all
-  __device__ __forceinline__ void init(const MoeLinearParams& p, const int* first_, const int* tiles_, int groups) {
-    first = first_; tiles = tiles_; E = p.E; num_nt = p.num_nt;
-    const int all = tiles[E] * num_nt, rest = all % groups;
-    full = all - rest;
-    split = rest * 4 <= groups ? 2 : rest * 2 <= groups ? 1 : 0;
-    units = full + (rest << split);
-  }
-  // unit u < units; the whole warp calls
-  template <int MT, int STEP, bool PAIR>
-  __device__ __forceinline__ MoeTile at(int u) const {
-    MoeTile r;
-    r.part = 0; r.split = 0;
-    int t = u;
-    if (u >= full) { r.split = split; t = full + ((u - full) >> split); r.part = (u - full) & ((1 << split) - 1); }
-    const int rt = (int)((unsigned)t / (unsigned)num_nt), lane = threadIdx.x & 31;
-    r.nt = t - rt * num_nt;
-    // the last expert whose first row tile is not behind rt: by sixteens, then among sixteen
-    int base = 0;
-    if (E > 32) base = 16 * (__popc(__ballot_sync(0xffffffffu, 16 * lane < E && tiles[min(16 * lane, E)] <= rt)) - 1);
-    const int e = base + lane;
-    r.e = base + __popc(__ballot_sync(0xffffffffu, (E <= 32 || lane < 16) && e < E && tiles[min(e, E)] <= rt)) - 1;
-    const int lo = first[r.e], n = first[r.e + 1] - lo, k = tiles[r.e + 1] - tiles[r.e], i = rt - tiles[r.e];
-    // an even share of the expert's rows
-    const int per = ((k == 1 ? n : (int)((unsigned)(n + k - 1) / (unsigned)k)) + STEP - 1) / STEP * STEP;
-    r.row0 = lo + i * per;
-    r.rows = min(per, n - i * per);           // may be 0 or less where a share rounds up: such a unit is skipped
-    if (PAIR && r.split) {
-      const int sub = (((r.rows + (1 << r.split) - 1) >> r.split) + STEP - 1) / STEP * STEP;
-      r.row0 += r.part * sub;
-      r.rows = min(sub, r.rows - r.part * sub);
-      r.part = r.split = 0;
-    }
-    return r;
-  }
-};
-
-// Rows of a tile that a CTA loads, in groups of four: of a pair, each has half of the N side.  Every row warp takes part in every stage, with a group
-// that nobody needs if there are too few: a warp without one could fall two uses of a stage behind, where a barrier's parity repeats.
-struct MoeShare { int lo, n, fours; };        // first row in the tile, rows (0 or less: none), groups
-template <bool PAIR>
-__device__ __forceinline__ MoeShare moe_share(const MoeTile& w, int rank) {
-  constexpr int STEP = MoeCfg<PAIR, true>::STEP;
-  const int half = (w.rows + STEP - 1) / STEP * (STEP / (PAIR ? 2 : 1));
-  MoeShare s;
-  s.lo = rank * half;
-  s.n = min(half, w.rows - s.lo);
-  s.fours = max(MoeCfg<PAIR, true>::ROW_WARPS, (s.n + 3) >> 2);
-  return s;
-}
 
 // v / (1 + 2^x).  (A power beyond FP32 makes the quotient 0, a subnormal one changes nothing beside 1.)
 __device__ __forceinline__ float over_one_plus_exp2(float v, float x) {
@@ -355,7 +295,7 @@ __device__ __forceinline__ void moe_vectors(const MoeLinearParams& p, uint8_t* s
   const int lane = threadIdx.x & 31;
   int it = 0;
   for (int t = first_unit; t < deal.units; t += stride) {
-    const MoeTile w = deal.at<MT, Cfg::STEP, PAIR>(t);
+    const MoeTile w = deal.at<PAIR>(t, lane);
     if (w.rows <= 0) continue;
     float rs[MT / 32], cs[4], bias[4], post[4];
 #pragma unroll
@@ -540,8 +480,8 @@ __device__ __forceinline__ void moe_linear_body(const CUtensorMap& tmW, const CU
         const int lo = p.offset[e], hi = p.offset[e + 1];
         first[e] = lo;
         if (e == p.E - 1) first[p.E] = hi;
-        if (lo < 0 || hi < lo || hi > p.R) atomicExch(p.err, ERR_BAD_EXPERT);
-        else k = (hi - lo + MT - 1) / MT;
+        k = moe_tiles<PAIR>(lo, hi, p.R);
+        if (k < 0) { atomicExch(p.err, ERR_BAD_EXPERT); k = 0; }
       }
       int s = k;
 #pragma unroll
@@ -560,9 +500,9 @@ __device__ __forceinline__ void moe_linear_body(const CUtensorMap& tmW, const CU
   ptx::tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
   MoeDeal deal;
-  deal.init(p, first, tiles, groups);
+  deal.init(p.E, p.num_nt, first, tiles, groups);
   const int num_tiles = deal.units;
-  auto tile_at = [&](int t) { return deal.at<MT, Cfg::STEP, PAIR>(t); };
+  auto tile_at = [&](int t) { return deal.at<PAIR>(t, lane); };
 
   if (warp == Cfg::LOAD_WARP) {
     // ------------------------------------------------------------------ weights
