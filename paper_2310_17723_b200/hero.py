@@ -302,6 +302,13 @@ def _current_raw_stream(device):
 _ABSENT = tensor(None)
 
 
+def _scaled_rows(t, name):
+    """A token-wise scale has to reach the tensor's last row (the kernels read one entry per row)."""
+    scale = getattr(t, "_keep", (None, None))[1]
+    if t.gran == GRAN_TWQ and scale is not None and scale.numel() < t.rows:
+        _refuse("%s: a token-wise scale of %d entries for %d rows" % (name, scale.numel(), t.rows))
+
+
 class Handle:
     """Owns a hero_handle on the current CUDA device."""
 
@@ -515,6 +522,7 @@ class Handle:
         """A, out: hero.Tensor; W: [experts, N, K] of A's type (K contiguous); offset: int32 [experts + 1]; token: int32 [rows of out] (None: A is in
         sorted order); w_scale, bias: float32 [experts, N]; post_scale, out_col_absmax: float32 [experts, columns of out]."""
         self._here(A, out)
+        _scaled_rows(A, "A")
         if W.dim() != 3 or W.stride(2) != 1 or W.shape[2] != A.cols or W.get_device() != self._device or _DT.get(W.dtype) != A.dtype:
             _refuse("W: [experts, N, K = %d] of A's type on the handle's device, K contiguous" % A.cols)
         E, N, K = W.shape
