@@ -352,6 +352,7 @@ class Handle:
         """A, out: hero.Tensor; W: torch tensor [N, K] (K contiguous); out_col_absmax: float32 [N] running per-column
         absolute maximum of an FP16 / BF16 output (calibration observer fused into the epilogue)."""
         assert W.dim() == 2 and W.stride(1) == 1
+        _scaled_rows(A, "A")
         a = LinearArgs(A, W.data_ptr(), W.shape[0], W.stride(0), _ptr(w_scale), _ptr(bias),
                        ACT[act] if isinstance(act, str) else act, _ptr(post_scale), out, _ptr(out_col_absmax))
         _check(lib().hero_w8a8_linear(self._h, C.byref(a), _stream(stream)))

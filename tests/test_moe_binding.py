@@ -42,3 +42,17 @@ def test_a_token_wise_scale_reaches_the_last_row_of_the_grouped_products(h, gath
     else:
         call()
     assert h._lib.calls == ([] if refused else ["hero_moe_linear"])
+
+
+@pytest.mark.parametrize("entries,refused", [(7, True), (8, False), (9, False)])
+def test_a_token_wise_scale_reaches_the_last_row_of_the_dense_products(h, monkeypatch, entries, refused):
+    monkeypatch.setattr(hero, "lib", lambda: h._lib)
+    monkeypatch.setattr(hero, "_stream", lambda s: None)
+    A, out, W = torch.zeros(8, 64, dtype=torch.int8), torch.zeros(8, 96, dtype=torch.float16), torch.zeros(96, 64, dtype=torch.int8)
+    call = lambda: h.hero_w8a8_linear(on_nowhere(A, "twq", torch.ones(entries)), W, on_nowhere(out), w_scale=torch.ones(96))  # noqa: E731
+    if refused:
+        with pytest.raises(hero.HeroError, match="scale"):
+            call()
+    else:
+        call()
+    assert h._lib.calls == ([] if refused else ["hero_w8a8_linear"])
