@@ -670,7 +670,7 @@ hero_status hero_moe_route(hero_handle* h, const hero_moe_route_args* a, void* s
  *   out    : [T k][N, gated N/2]; I8 from I8 or 16-bit operands, F8 from F8 or 16-bit operands, F16 / BF16 from any
  *   out_col_absmax : device float[E][columns of out] or NULL: running per-expert column maxima of |out| as stored (F16 / BF16 outputs), from
  *            which calibration takes the static scale of an expert's hidden features (zero it before the first batch)
- *   act    : hero_act, HERO_ACT_SILU included;  E <= 512.  out overlaps neither A nor W.
+ *   act    : hero_act, HERO_ACT_SILU included (SiLU and GELU(tanh) of less than 2^-134 in magnitude are 0);  E <= 512.  out overlaps neither A nor W.
  * The kernel is chosen by out.rows over E, the most rows an expert can have on average: up to 32 one that is bound by the weights' bytes, above that one
  * for the tensor cores (tiles of up to 256 rows).  A captured graph for far more tokens than it is replayed with has the second one's price. */
 typedef struct {

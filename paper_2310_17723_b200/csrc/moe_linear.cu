@@ -67,17 +67,20 @@ struct MoeCfg {
   static_assert(PER_SM * (SMEM_BYTES + 1024) <= 228 * 1024, "shared memory");
 };
 
-// v / (1 + 2^x).  (A power beyond FP32 makes the quotient 0, a subnormal one changes nothing beside 1.)
-__device__ __forceinline__ float over_one_plus_exp2(float v, float x) {
+// v / (1 + 2^x), given x - 15 (ACT_SHIFT): v 2^-15 / (2^-15 + 2^(x - 15)).  Neither the power nor the quotient, whose instructions know no subnormal numbers,
+// leaves FP32's normal range up to x = 141, where the result (|v| < 100 there) is below half of the smallest BF16; from there on it is 0.  (Without the shift
+// every result below 2^-119 or so was.)  The shift rounds the exponent to 2^-21 for 0 < x < 31, 3e-7 of the result.
+constexpr float ACT_SHIFT = 15.0f, ACT_ONE = 1.0f / 32768.0f;
+__device__ __forceinline__ float over_one_plus_exp2(float v, float x15) {
   float e, r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x));
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
-  return v * r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x15));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(ACT_ONE + e));
+  return v * (r * ACT_ONE);
 }
 // SiLU: v / (1 + e^-v).  GELU(tanh): 0.5 v (1 + tanh(u)) = v / (1 + e^-2u), u = sqrt(2 / pi) (v + 0.044715 v^3); both with log2 e in the constants
-__device__ __forceinline__ float silu_f(float v) { return over_one_plus_exp2(v, -1.44269504088896340736f * v); }
+__device__ __forceinline__ float silu_f(float v) { return over_one_plus_exp2(v, fmaf(v, -1.44269504088896340736f, -ACT_SHIFT)); }
 __device__ __forceinline__ float gelu_tanh_quotient(float v) {
-  return over_one_plus_exp2(v, v * fmaf(v * v, -0.10294324f, -2.30220819f));
+  return over_one_plus_exp2(v, fmaf(v, fmaf(v * v, -0.10294324f, -2.30220819f), -ACT_SHIFT));
 }
 template <int ACT>
 __device__ __forceinline__ float moe_act(float v) {
