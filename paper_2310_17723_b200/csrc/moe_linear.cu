@@ -137,12 +137,6 @@ __device__ __forceinline__ float2 moe_act2(float2 v) {
   else return make_float2(moe_act<ACT>(v.x), moe_act<ACT>(v.y));
 }
 
-// A turned chunk is words of four (two) rows of a feature: [groups of rows][features].  Ungated, a group is rows that follow one another; gated, a
-// thread has rows in pairs, eight apart, and a word of four takes two such pairs.  Gated rows of words are 8 longer, so that the four
-// groups of a warp's store lie on banks of their own.
-template <bool GATED>
-constexpr int MOE_WORD_PITCH = GATED ? 64 + 8 : 128;
-
 // A chunk of 32 rows: products, activation, rounding, to the turned chunk.  `rs`: the chunk's row factors; count: rows that exist (observer)
 template <bool INT8, bool GATED, int ACT, int OUTK>
 __device__ __forceinline__ void moe_chunk(const MoeLinearParams& p, const uint32_t (&r)[32], const float* rs, const MoeFeature<GATED>& l, uint32_t* buf, int lane,
@@ -413,7 +407,8 @@ __device__ __forceinline__ void moe_epilogue(const MoeLinearParams& p, uint8_t* 
       if constexpr (Cfg::TURN_BUFS == 2) buf += (turned++ & 1) * (Cfg::TURN_BYTES / 8);
       else asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory");          // the group is through with the chunk before
       const int rows = min(MOE_CHUNK, w.rows - c * MOE_CHUNK);
-      if (mine && ok) moe_chunk<INT8, GATED, ACT, OUTK>(p, r, vec + c * MOE_CHUNK, l, buf + warp_col, lane, rows, most);
+      if (!ok) moe_blank<GATED, OUTK == OUT_FP, OUTK == OUT_F8>(buf + warp_col, lane);
+      else if (mine) moe_chunk<INT8, GATED, ACT, OUTK>(p, r, vec + c * MOE_CHUNK, l, buf + warp_col, lane, rows, most);
       if (c + GROUPS < chunks) moe_tmem_ld<GATED>(taddr + (c + GROUPS) * MOE_CHUNK, r);       // on its way while this chunk is stored
       // the group's four warps have written the chunk (of two buffers, the one of two chunks ago is free too)
       asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory");
