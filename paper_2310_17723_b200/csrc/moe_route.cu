@@ -15,7 +15,9 @@
 // Order: a bit per (expert, token) in shared memory.  The rank of a pair within its expert is the number of bits before its own, whatever
 // the order in which warps set them, so that the result does not depend on timing and no global atomics are needed.  Few tokens: one
 // CTA does everything.  More: each CTA of a first kernel counts its own tokens' experts, and each CTA of a second one adds up the
-// counts of those before it (and of all, for the experts' first rows) and places its pairs.
+// counts of those before it (and of all, for the experts' first rows) and places its pairs.  Where there are more CTAs than SMs (each has the most
+// tokens that it can have then), a kernel between the two adds the counts up, one CTA for each expert: for every CTA to add up all of them
+// would grow with the square of the tokens (8 experts, top 1: 24.5 ms instead of 8.6 for 2^25 tokens, a minute for 2^31).
 //
 // The bytes are few (2 to 4 per logit); what bounds it is the instructions of the choice and the latency of two launches: 16383 tokens of 128 experts, top 8,
 // 15 us (18.5 with a warp a token), 5000 tokens of 256 experts with sigmoid and bias 22.5 (30); 16 tokens of 64 experts 4.2 in a graph.
@@ -42,7 +44,8 @@ struct RouteParams {
   int T, E, k, score, renorm;
   float scale;
   int* expert; float* weight; int* offset; int* token; int* row;
-  int* counts;                           // [CTAs][E] (two-kernel form)
+  int* counts;                           // [CTAs][E] (two-kernel form); summed: of the CTAs before, and [E] of all behind them
+  int summed;
   int chunk, words;                      // tokens per CTA, their 32-bit words
   uint32_t low;                          // bits of a key that hold the expert (more tokens, FP32 keys)
 };
@@ -642,6 +645,23 @@ __global__ void __launch_bounds__(ROUTE_CHOOSE_THREADS<PACK16>, 1) route_choose_
   for (int e = threadIdx.x; e < p.E; e += blockDim.x) p.counts[(long long)blockIdx.x * p.E + e] = count[e];
 }
 
+// More CTAs than SMs, between the two kernels: CTA e turns the counts of expert e into sums over the CTAs before, and puts that of all behind them.
+__global__ void __launch_bounds__(ROUTE_THREADS, 1) route_sum_kernel(const __grid_constant__ RouteParams p, int ctas) {
+  __shared__ int warps[32];
+  ptx::pdl_launch_dependents();
+  ptx::pdl_wait();
+  int run = 0;
+  for (int c0 = 0; c0 < ctas; c0 += ROUTE_THREADS) {
+    const int c = c0 + threadIdx.x;
+    int* at = p.counts + (long long)c * p.E + blockIdx.x;
+    const int v = c < ctas ? *at : 0, before = exclusive_sum(v, warps);
+    if (c < ctas) *at = run + before;
+    for (int w = 0; w < ROUTE_THREADS / 32; ++w) run += warps[w];
+    __syncthreads();                                       // the sums of the warps are read
+  }
+  if (threadIdx.x == 0) p.counts[(long long)ctas * p.E + blockIdx.x] = run;
+}
+
 // Two-kernel form, second: the first row of every expert for this chunk, and the place of each of its pairs.
 __global__ void __launch_bounds__(ROUTE_THREADS, 1) route_place_kernel(const __grid_constant__ RouteParams p) {
   extern __shared__ uint32_t bits[];                       // [E][words]
@@ -651,10 +671,15 @@ __global__ void __launch_bounds__(ROUTE_THREADS, 1) route_place_kernel(const __g
   for (int e = threadIdx.x; e < p.E; e += blockDim.x) before[e] = total[e] = 0;
   ptx::pdl_wait();
   __syncthreads();
-  // counts of all chunks: as many threads of an expert as fit, each a share of the chunks
-  int pe = 32;
-  while (pe < p.E) pe <<= 1;
-  {
+  if (p.summed) {
+    for (int e = threadIdx.x; e < p.E; e += blockDim.x) {
+      before[e] = p.counts[(long long)blockIdx.x * p.E + e];
+      total[e] = p.counts[(long long)gridDim.x * p.E + e];
+    }
+  } else {
+    // counts of all chunks: as many threads of an expert as fit, each a share of the chunks
+    int pe = 32;
+    while (pe < p.E) pe <<= 1;
     const int e = threadIdx.x & (pe - 1), g = threadIdx.x / pe, groups = blockDim.x / pe;
     if (e < p.E) {
       int b = 0, a = 0;
@@ -710,6 +735,7 @@ static int route_chunk(const hero_handle* h, long long T) {
   long long c = ((T + h->sm_count - 1) / h->sm_count + 7) / 8 * 8;
   return (int)(c > ROUTE_MAX_CHUNK ? ROUTE_MAX_CHUNK : c);
 }
+static long long route_ctas(long long T, int chunk) { return (T + chunk - 1) / chunk; }    // (in 64 bits: T may be 2^31 - 1)
 
 template <int R, int DT>
 static hero_status launch_one(hero_handle* h, RouteParams& p, cudaStream_t s) {
@@ -721,7 +747,8 @@ static hero_status launch_one(hero_handle* h, RouteParams& p, cudaStream_t s) {
 }
 template <int KM, int DT, bool PACK16>
 static hero_status launch_two(hero_handle* h, RouteParams& p, cudaStream_t s) {
-  const unsigned ctas = (unsigned)((p.T + p.chunk - 1) / p.chunk);
+  const unsigned ctas = (unsigned)route_ctas(p.T, p.chunk);
+  p.summed = ctas > (unsigned)h->sm_count;
   // a warp for every four tokens of the chunk, as many as the shared memory holds the keys of
   const size_t warp_bytes = ROUTE_TOKENS * (size_t)((p.E + 31) / 32 * 32 + ROUTE_LANES) * 4;
   int warps = (p.chunk + ROUTE_TOKENS - 1) / ROUTE_TOKENS;
@@ -732,6 +759,10 @@ static hero_status launch_two(hero_handle* h, RouteParams& p, cudaStream_t s) {
   {
     LaunchScope scope(h, s, KERNEL_ROUTE);
     HERO_CUDA(launch_dependent(choose, dim3(ctas), dim3(32 * warps), warps * warp_bytes, s, p));
+  }
+  if (p.summed) {
+    LaunchScope scope(h, s, KERNEL_ROUTE);
+    HERO_CUDA(launch_dependent(route_sum_kernel, dim3((unsigned)p.E), dim3(ROUTE_THREADS), 0, s, p, (int)ctas));
   }
   HERO_SMEM_OPT_IN(h, route_place_kernel, ROUTE_MAX_E * (ROUTE_MAX_CHUNK / 32) * 4);
   {
@@ -773,8 +804,8 @@ static hero_status route_sizes(int64_t T, int32_t E, int32_t k) {
   return HERO_OK;
 }
 static size_t route_workspace(const hero_handle* h, int64_t T, int32_t E) {
-  // the most chunks that any smaller number of tokens takes: one per SM, or T / ROUTE_MAX_CHUNK
-  const int64_t ctas = (T + ROUTE_MAX_CHUNK - 1) / ROUTE_MAX_CHUNK;
+  // the most chunks that any smaller number of tokens takes: one per SM, or T / ROUTE_MAX_CHUNK and a place for the sums of all
+  const int64_t ctas = route_ctas(T, ROUTE_MAX_CHUNK) + 1;
   const int64_t few = (T + 7) / 8 < h->sm_count ? (T + 7) / 8 : h->sm_count;
   return T <= ROUTE_ONE_CTA ? 0 : (size_t)(ctas > few ? ctas : few) * (size_t)E * 4;
 }
