@@ -101,20 +101,4 @@ HERO_MOE_FN MoeShare moe_share(const MoeTile& w, int rank) {
   return s;
 }
 
-// A turned chunk (32 rows on their way out) is words of four rows of a feature (8-bit outputs) or two (16-bit): [groups of rows][features].  Ungated, a group
-// is rows that follow one another; gated, a thread has rows in pairs, eight apart, and a word of four takes two such pairs.  Gated rows of words are 8
-// longer, so that the four groups of a warp's store lie on banks of their own.
-template <bool GATED>
-constexpr int MOE_WORD_PITCH = GATED ? 64 + 8 : 128;
-
-// What a warp whose products did not arrive in time (the error word says so) leaves in its features of a chunk, in place of what the chunk held before: NaN,
-// in INT8, which has none, the one code that no product gives.  at: the warp's first feature.
-template <bool GATED, bool FP, bool F8>
-HERO_MOE_FN void moe_blank(unsigned* at, int lane) {
-  constexpr unsigned word = FP ? 0x7fff7fffu : F8 ? 0x7f7f7f7fu : 0x80808080u;
-  constexpr int GROUPS = FP ? 16 : 8, COLS = GATED ? 16 : 32;
-  if (lane < COLS)
-    for (int g = 0; g < GROUPS; ++g) at[g * MOE_WORD_PITCH<GATED> + lane] = word;
-}
-
 }  // namespace hero

@@ -137,6 +137,12 @@ __device__ __forceinline__ float2 moe_act2(float2 v) {
   else return make_float2(moe_act<ACT>(v.x), moe_act<ACT>(v.y));
 }
 
+// A turned chunk is words of four (two) rows of a feature: [groups of rows][features].  Ungated, a group is rows that follow one another; gated, a
+// thread has rows in pairs, eight apart, and a word of four takes two such pairs.  Gated rows of words are 8 longer, so that the four
+// groups of a warp's store lie on banks of their own.
+template <bool GATED>
+constexpr int MOE_WORD_PITCH = GATED ? 64 + 8 : 128;
+
 // A chunk of 32 rows: products, activation, rounding, to the turned chunk.  `rs`: the chunk's row factors; count: rows that exist (observer)
 template <bool INT8, bool GATED, int ACT, int OUTK>
 __device__ __forceinline__ void moe_chunk(const MoeLinearParams& p, const uint32_t (&r)[32], const float* rs, const MoeFeature<GATED>& l, uint32_t* buf, int lane,
@@ -363,17 +369,14 @@ __device__ __forceinline__ void moe_epilogue(const MoeLinearParams& p, uint8_t* 
   const int quarter = warp & 3, group = warp >> 2;
   uint32_t* turn = reinterpret_cast<uint32_t*>(smem + Cfg::TURN_AT + group * Cfg::TURN_BYTES);
   const int warp_col = quarter * (GATED ? 16 : 32);                                    // first output column of this warp in the CTA's
-  bool ok = true;
   int turned = 0;
   for (int it = 0;; ++it) {
     const int as = it & 1;
     const uint32_t aphase = (it >> 1) & 1;
-    // (a wait that gives up has recorded its code; the group leaves before the next tile)
-    if (!group_all(ok && ptx::mbar_wait(&vec_full[as], aphase, p.err, 0xF84 | as), 1 + group)) break;
+    bool ok = ptx::mbar_wait(&vec_full[as], aphase, p.err, 0xF84 | as);
     const float* vec = reinterpret_cast<const float*>(smem + Cfg::VEC_AT) + as * Cfg::VEC_FLOATS;
     const int4 tile = *reinterpret_cast<const int4*>(vec + MT + 384);
     const MoeTile w{tile.z, tile.x, tile.y & 0xffff, tile.w, (tile.y >> 16) & 0xff, tile.y >> 24};
-    if (w.rows == 0) break;
     const int c0 = (w.nt * (PAIR ? 2 : 1) + rank) * COLS;
     MoeFeature<GATED> l;
     if constexpr (GATED) {
@@ -389,7 +392,9 @@ __device__ __forceinline__ void moe_epilogue(const MoeLinearParams& p, uint8_t* 
       l.cs[0] = at[0]; l.bias[0] = at[128]; l.post[0] = at[256];
       if (ACT == HERO_ACT_NONE) { l.cs[0] *= l.post[0]; l.bias[0] *= l.post[0]; }     // (acc rs cs + b) post = acc rs (cs post) + b post
     }
-    ok = __all_sync(0xffffffffu, ptx::mbar_wait(&acc_full[as], aphase, p.err, 0xF00 | as));
+    if (ok && w.rows != 0) ok = ptx::mbar_wait(&acc_full[as], aphase, p.err, 0xF00 | as);
+    // (a wait that gave up has recorded its code: the group leaves together, and writes nothing of a tile of which any of it is missing)
+    if (!group_all(ok, 1 + group) || w.rows == 0) break;
     ptx::tc_fence_after();
     const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + as * MT;
     uint32_t most[2] = {0u, 0u};
@@ -407,8 +412,7 @@ __device__ __forceinline__ void moe_epilogue(const MoeLinearParams& p, uint8_t* 
       if constexpr (Cfg::TURN_BUFS == 2) buf += (turned++ & 1) * (Cfg::TURN_BYTES / 8);
       else asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory");          // the group is through with the chunk before
       const int rows = min(MOE_CHUNK, w.rows - c * MOE_CHUNK);
-      if (!ok) moe_blank<GATED, OUTK == OUT_FP, OUTK == OUT_F8>(buf + warp_col, lane);
-      else if (mine) moe_chunk<INT8, GATED, ACT, OUTK>(p, r, vec + c * MOE_CHUNK, l, buf + warp_col, lane, rows, most);
+      if (mine) moe_chunk<INT8, GATED, ACT, OUTK>(p, r, vec + c * MOE_CHUNK, l, buf + warp_col, lane, rows, most);
       if (c + GROUPS < chunks) moe_tmem_ld<GATED>(taddr + (c + GROUPS) * MOE_CHUNK, r);       // on its way while this chunk is stored
       // the group's four warps have written the chunk (of two buffers, the one of two chunks ago is free too)
       asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory");

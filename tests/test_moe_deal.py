@@ -5,9 +5,7 @@ import random
 import shutil
 import subprocess
 
-import numpy as np
 import pytest
-import torch
 
 from paper_2310_17723_b200 import build as B
 
@@ -55,22 +53,7 @@ template <bool PAIR> static int go(int R, int num_nt, int groups, bool list, int
   if (!list) printf("%lld pieces up to row %d\n", pieces, next);
   return 0;
 }
-// the chunk that four warps leave behind after a wait that ran out, with the bytes of an earlier chunk in it
-template <bool GATED, bool FP, bool F8> static int blank() {
-  constexpr int PITCH = MOE_WORD_PITCH<GATED>, COLS = GATED ? 64 : 128, GROUPS = FP ? 16 : 8;
-  std::vector<unsigned> buf(16 * 128, 0x3c003c00u);
-  for (int warp = 0; warp < 4; ++warp)
-    for (int lane = 0; lane < 32; ++lane) moe_blank<GATED, FP, F8>(buf.data() + warp * COLS / 4, lane);
-  for (int g = 0; g < GROUPS; ++g)
-    for (int c = 0; c < COLS; ++c) printf("%u\n", buf[g * PITCH + c]);
-  return 0;
-}
 int main(int argc, char** argv) {
-  if (argc == 3) {
-    const int what = atoi(argv[2]);                          // 0: 16-bit, 1: e4m3, 2: INT8
-    if (atoi(argv[1])) return what == 0 ? blank<true, true, false>() : what == 1 ? blank<true, false, true>() : blank<true, false, false>();
-    return what == 0 ? blank<false, true, false>() : what == 1 ? blank<false, false, true>() : blank<false, false, false>();
-  }
   const bool list = argv[5][0] == 'l';
   auto f = atoi(argv[1]) ? go<true> : go<false>;
   return f(atoi(argv[2]), atoi(argv[3]), atoi(argv[4]), list, argc - 7, argv + 6);
@@ -87,9 +70,7 @@ def deal(tmp_path_factory):
     subprocess.run([compiler, "-std=c++17", "-O2", "-Wall", "-Werror", "-ftrapv", "-I", B.CSRC, "-o", str(d / "deal"),
                     str(d / "deal.cpp")], check=True)
 
-    def run(pair, R, num_nt=None, groups=None, how=None, offset=()):
-        if num_nt is None:
-            return subprocess.run([str(d / "deal"), str(int(pair)), str(R)], check=True, capture_output=True, text=True).stdout.split()
+    def run(pair, R, num_nt, groups, how, offset):
         out = subprocess.run([str(d / "deal"), *map(str, (int(pair), R, num_nt, groups, how, *offset))], capture_output=True, text=True)
         assert out.returncode == 0, out.stdout + out.stderr
         return out.stdout.splitlines()
@@ -138,14 +119,3 @@ def test_rows_outside_the_tensor_are_no_work(deal, pair):
     assert deal(pair, 100, 1, 4, "list", [50, 20, 20])[0] == "bad 0"
     assert len(deal(pair, 100, 1, 4, "list", [50, 20, 20])) == 1
     assert len(deal(pair, 100, 1, 1, "list", [0, 0])) == 0
-
-
-@pytest.mark.parametrize("gated", [False, True])
-@pytest.mark.parametrize("what", ["16 bits", "e4m3", "int8"])
-def test_products_that_did_not_arrive_leave_nothing_of_an_earlier_chunk(deal, gated, what):
-    words = torch.from_numpy(np.array(deal(gated, ["16 bits", "e4m3", "int8"].index(what)), dtype=np.uint32).view(np.int32))
-    assert words.numel() == 32 * (64 if gated else 128) * (2 if what == "16 bits" else 1) // 4
-    if what == "int8":
-        assert bool((words.view(torch.int8) == -128).all())
-    for dt in {"16 bits": [torch.float16, torch.bfloat16], "e4m3": [torch.float8_e4m3fn], "int8": []}[what]:
-        assert bool(words.view(dt).float().isnan().all())
