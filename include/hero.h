@@ -613,8 +613,8 @@ hero_status hero_qk_norm_rope(hero_handle* h, const hero_qk_norm_rope_args* a, v
  *     hero_moe_combine  residual + weighted sum of each token's rows, LN^quant of the result
  *
  * "Sorted rows" are the pairs ordered by expert, then by token.  offset (device int32 [E + 1]): expert e has the sorted rows
- * offset[e] .. offset[e + 1] - 1.  A tensor of sorted rows has T k rows, of which offset[E] are in use; the others are neither read nor
- * written.  How many rows an expert gets is known on the device alone, so that the calls can be captured in a CUDA graph
+ * offset[e] .. offset[e + 1] - 1.  A tensor of sorted rows has T k rows, of which offset[E] are in use; the others are not written, and what they
+ * hold changes no result (a copy of whole boxes of rows may read some of them).  How many rows an expert gets is known on the device alone, so that the calls can be captured in a CUDA graph
  * and replayed with other tokens.
  *
  * What the host cannot see is bounded on the device and reported by the next hero_check() as HERO_ERR_INVALID_ARG: an expert whose rows are
@@ -672,7 +672,8 @@ hero_status hero_moe_route(hero_handle* h, const hero_moe_route_args* a, void* s
  *            which calibration takes the static scale of an expert's hidden features (zero it before the first batch)
  *   act    : hero_act, HERO_ACT_SILU included (SiLU and GELU(tanh) of less than 2^-134 in magnitude are 0);  E <= 512.  out overlaps neither A nor W.
  * The kernel is chosen by out.rows over E, the most rows an expert can have on average: up to 32 one that is bound by the weights' bytes, above that one
- * for the tensor cores (tiles of up to 256 rows).  A captured graph for far more tokens than it is replayed with has the second one's price. */
+ * for the tensor cores (tiles of up to 256 rows).  A captured graph for far more tokens than it is replayed with has the second one's price, and an expert that
+ * gets many of few rows has the first one's: its weights once for each 32 rows.  INT8 products are summed in 32-bit integers: exact for K up to 131071. */
 typedef struct {
   hero_tensor A;
   const int32_t* token;

@@ -11,8 +11,9 @@
 //   epilogue warps      (single CTAs 4, pairs 8, pairs with A in order 16)  tensor memory -> registers -> scales, activation, rounding -> shared memory
 //                       (turned) -> whole row segments out.  A word holds four (two) rows of a feature: shared memory is what the products' operands
 //                       fill already, and a byte at a time costs it four times the cycles
-//   row warps           (pairs 8, single CTAs 2)  rows of A picked by token: TMA gathers of four rows.  One warp starts one every 80 cycles or so, a k-block takes 32 in 512
-//                       cycles: two row warps for each four gave 197 us where four gave 231 (8192 tokens, top 8 of 64, 2048 x 2048)
+//   row warps           (pairs 8, single CTAs 2)  rows of A picked by token: TMA gathers of four rows.  One warp starts one every 80 cycles or so, a k-block of a pair takes
+//                       64, 32 in each CTA, in 512 cycles: eight warps, with the gated products no longer exchanged between lanes, took the gated prompt (8192 tokens,
+//                       top 8 of 64, 2048 x 2048) from 259 us to 227
 //   load warp           W tiles, and A where its rows are in order (TMA)
 //   vector warp         row factors, scales, biases and output factors of the next tile, to shared memory (two loads that depend on one another
 //                       and a search for the tile: 2000 cycles that each epilogue warp would spend once a tile)
@@ -31,7 +32,7 @@ constexpr int MOE_MAX_E = 512;
 constexpr int MOE_CHUNK = 32;                 // rows that an epilogue group turns at a time
 
 struct MoeLinearParams {
-  int R, a_rows, E, N, n_out, K;              // K in elements
+  int R, a_rows, E, N, n_out;
   int num_kb, num_nt;                         // 128-byte steps of K, feature tiles of an expert
   const int* offset; const int* token;
   const float* rs; const float* cs; const float* bias; const float* post;
@@ -754,7 +755,7 @@ extern "C" hero_status hero_moe_linear(hero_handle* h, const hero_moe_linear_arg
 
   MoeLinearParams p;
   memset(&p, 0, sizeof(p));
-  p.R = (int)R; p.a_rows = (int)a->A.rows; p.E = (int)E; p.N = (int)N; p.n_out = (int)n_out; p.K = (int)K;
+  p.R = (int)R; p.a_rows = (int)a->A.rows; p.E = (int)E; p.N = (int)N; p.n_out = (int)n_out;
   p.num_kb = (int)((K * eb + GEMM_BK_BYTES - 1) / GEMM_BK_BYTES);
   p.offset = a->offset; p.token = a->token;
   p.rs = q8 && a->A.gran == HERO_GRAN_TWQ ? a->A.scale : nullptr;
@@ -765,7 +766,7 @@ extern "C" hero_status hero_moe_linear(hero_handle* h, const hero_moe_linear_arg
   p.kelems = GEMM_BK_BYTES / eb;
   p.obs = a->out_col_absmax;
   p.err = h->d_error;
-    // Rows of an expert on average decide.  Few: single CTAs with tiles of 32 rows, two on an SM, so that one streams weights while the other starts or
+  // Rows of an expert on average decide.  Few: single CTAs with tiles of 32 rows, two on an SM, so that one streams weights while the other starts or
   // ends (a chain of router, FC1, FC2 and combine, 16 tokens, 64 experts, top 8, 2048 x 1024: 81 us; one CTA an SM, 64 rows: 91).  Many: pairs.
   // Both sides, us, FC1 / FC2 of 64 experts, 2048 x 1024: 24 rows 50.4 / 26.9 single, 52.4 / 28.7 pairs; 32 rows 54.0 / 28.4 and 53.4 / 29.4;
   // 16 experts, 4096 x 2048: 24 rows 47.2 / 27.3 and 52.9 / 30.1; 32 rows 52.0 / 29.8 and 53.3 / 30.2.  Beyond, a second tile of an expert costs singles

@@ -20,7 +20,8 @@
 // would grow with the square of the tokens (8 experts, top 1: 24.5 ms instead of 8.6 for 2^25 tokens, a minute for 2^31).
 //
 // The bytes are few (2 to 4 per logit); what bounds it is the instructions of the choice and the latency of two launches: 16383 tokens of 128 experts, top 8,
-// 15 us (18.5 with a warp a token), 5000 tokens of 256 experts with sigmoid and bias 22.5 (30); 16 tokens of 64 experts 4.2 in a graph.
+// 15 us with BF16 logits (18.5 with a warp a token) and 24 with FP32 ones, 5000 tokens of 256 experts with sigmoid and bias 22.4 (29.6); 16 tokens of 64
+// experts 4.2 in a graph.
 #include "common.cuh"
 #include "ptx.cuh"
 #include <cuda_fp16.h>
